@@ -1,0 +1,134 @@
+// Shared between the kernels of the serving operators (lc_w4.hip, lc_kv.hip): element types, packing, matrix instructions.  gfx950 only.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "../../include/lc_serve.h"
+
+namespace lc {
+namespace serve {
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+
+constexpr float kSmallest = 1.17549435e-38f;      // 2^-126: scales below it are stored as zero, so that 1/s stays finite
+
+inline bool served_type(int dtype) { return dtype == LC_F32 || dtype == LC_BF16 || dtype == LC_F16; }
+inline bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+inline uintptr_t size_of(int dtype) { return dtype == LC_F32 ? 4 : 2; }
+
+// n / d for 32-bit n by a product with what the host worked out once (round-up method: exact for every n).
+struct FastDiv {
+    uint32_t d, m, s;
+    explicit FastDiv(uint32_t d_ = 1) : d(d_), m(0), s(0) {
+        while (s < 32 && (1ull << s) < d) ++s;
+        m = (uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        const uint32_t t = __umulhi(m, n);
+        return s == 0 ? n : (t + ((n - t) >> 1)) >> (s - 1);
+    }
+};
+
+// 16 bytes from anywhere that suits the element (global loads need no more than that here).
+template <typename V> __device__ __forceinline__ V load_any(const void* p) { V v; __builtin_memcpy(&v, p, sizeof(V)); return v; }
+template <typename V> __device__ __forceinline__ void store_any(void* p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
+
+__device__ __forceinline__ uint32_t bits_of(float f) { return __float_as_uint(f); }
+__device__ __forceinline__ float float_of(uint32_t b) { return __uint_as_float(b); }
+
+// To nearest even; a NaN stays one.
+__device__ __forceinline__ uint32_t bf16_of(float f) {
+    const uint32_t b = bits_of(f);
+    const uint32_t r = (b + 0x7fffu + ((b >> 16) & 1u)) >> 16;
+    return (b & 0x7fffffffu) > 0x7f800000u ? 0x7fc0u : r;
+}
+__device__ __forceinline__ float of_bf16(uint32_t b) { return float_of(b << 16); }
+__device__ __forceinline__ uint32_t f16_of(float f) { const _Float16 h = (_Float16)f; uint16_t u; __builtin_memcpy(&u, &h, 2); return u; }
+__device__ __forceinline__ float of_f16(uint32_t b) { const uint16_t u = (uint16_t)b; _Float16 h; __builtin_memcpy(&h, &u, 2); return (float)h; }
+
+// One element of an array of type T (LC_F32, LC_BF16, LC_F16).
+template <int T> __device__ __forceinline__ float load_one(const void* p, uint64_t i) {
+    if (T == LC_F32) return static_cast<const float*>(p)[i];
+    const uint32_t u = static_cast<const uint16_t*>(p)[i];
+    return T == LC_BF16 ? of_bf16(u) : of_f16(u);
+}
+template <int T> __device__ __forceinline__ void store_one(void* p, uint64_t i, float v) {
+    if (T == LC_F32) static_cast<float*>(p)[i] = v;
+    else static_cast<uint16_t*>(p)[i] = (uint16_t)(T == LC_BF16 ? bf16_of(v) : f16_of(v));
+}
+// Eight elements in a row, the first `valid` of them (the others read as zero, or are not written).
+template <int T> __device__ __forceinline__ void load_eight(const void* p, uint64_t i, int valid, float v[8]) {
+    if (valid >= 8) {
+        if (T == LC_F32) {
+            const f32x4 a = load_any<f32x4>(static_cast<const float*>(p) + i), b = load_any<f32x4>(static_cast<const float*>(p) + i + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+        } else {
+            const u32x4 a = load_any<u32x4>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t u = a[e / 2];
+                v[e] = T == LC_BF16 ? float_of(e % 2 ? u & 0xffff0000u : u << 16) : of_f16(e % 2 ? u >> 16 : u & 0xffffu);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < valid ? load_one<T>(p, i + e) : 0.0f;
+    }
+}
+template <int T> __device__ __forceinline__ void store_eight(void* p, uint64_t i, int valid, const float v[8]) {
+    if (valid >= 8) {
+        if (T == LC_F32) {
+            store_any(static_cast<float*>(p) + i, f32x4{v[0], v[1], v[2], v[3]});
+            store_any(static_cast<float*>(p) + i + 4, f32x4{v[4], v[5], v[6], v[7]});
+        } else {
+            u32x4 a;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                a[e] = T == LC_BF16 ? bf16_of(v[2 * e]) | bf16_of(v[2 * e + 1]) << 16 : f16_of(v[2 * e]) | f16_of(v[2 * e + 1]) << 16;
+            store_any(static_cast<uint16_t*>(p) + i, a);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < valid) store_one<T>(p, i + e, v[e]);
+    }
+}
+
+// The largest of `lanes` neighbouring lanes' values in every one of them (lanes: 4, 8 or 16, aligned).
+template <int LANES> __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
+#define LC_DPP_MAX(ctrl) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false); v = v > o ? v : o; }
+    if (LANES >= 2) LC_DPP_MAX(0xB1)      // the other of each two
+    if (LANES >= 4) LC_DPP_MAX(0x4E)      // the other two of each four
+    if (LANES >= 8) LC_DPP_MAX(0x141)     // the other four of each eight
+    if (LANES >= 16) LC_DPP_MAX(0x140)    // the other eight of each sixteen
+#undef LC_DPP_MAX
+    return v;
+}
+
+// rint(t) + bias for |t| <= 127 in the low bits: added to 1.5 * 2^23 the sum has no room for a fraction, and its rounding is the
+// one to nearest even.
+__device__ __forceinline__ uint32_t rounded(float t, float bias) { return bits_of(t + (12582912.0f + bias)); }
+
+// D = A B + C, 16 x 16 x 32: lane l gives row l % 16 of A and column l % 16 of B, eight places of the inner dimension of its
+// own (the same ones for A and B) per quarter l / 16, and receives column l % 16, rows 4 (l / 16) + 0..3 of D.
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+    bf16x8 x, y; __builtin_memcpy(&x, &a, 16); __builtin_memcpy(&y, &b, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+    f16x8 x, y; __builtin_memcpy(&x, &a, 16); __builtin_memcpy(&y, &b, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+}
+
+// The low (0x05040100) or high (0x07060302) halves of a and b, a's below b's.
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+}  // namespace serve
+}  // namespace lc

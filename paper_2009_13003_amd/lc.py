@@ -1,4 +1,4 @@
-"""Thin ctypes binding of liblc.so: argument marshalling only, same names as include/lc.h.
+"""Thin ctypes binding of liblc.so: argument marshalling only, same names as include/lc.h and include/lc_serve.h.
 
 Device buffers are torch CUDA tensors (torch is used for device memory and streams,
 nothing else).  There is no CPU fallback: if the library is missing, importing fails.
@@ -88,6 +88,20 @@ _lib.lc_profile_read.restype = _int
 _lib.lc_profile_read.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_u64), _int]
 _lib.lc_profile_name.restype = ctypes.c_char_p
 _lib.lc_profile_name.argtypes = [_int]
+
+
+class _W4(ctypes.Structure):            # struct lc_w4
+    _fields_ = [("codes", _vp), ("scales", _vp), ("n", _u64), ("k", _u64), ("codes_pitch", _u64), ("scales_pitch", _u64), ("group", _int)]
+
+
+_lib.lc_w4_row_bytes.restype = _sz
+_lib.lc_w4_row_bytes.argtypes = [_u64]
+_lib.lc_w4_quantize.restype = _int
+_lib.lc_w4_quantize.argtypes = [_vp, _u64, _int, _vp, _vp]
+_lib.lc_w4_dequantize.restype = _int
+_lib.lc_w4_dequantize.argtypes = [_vp, _vp, _u64, _int, _vp]
+_lib.lc_w4_matmul.restype = _int
+_lib.lc_w4_matmul.argtypes = [_vp, _u64, _u64, _vp, _vp, _vp, _u64, _int, _vp]
 
 
 class LcError(RuntimeError):
@@ -473,3 +487,97 @@ def lc_profile_read():
 def alloc_out(n, nbits, device="cuda"):
     """A device buffer large enough for any blob of (n, nbits)."""
     return torch.empty(lc_encode_bound(n, nbits), dtype=torch.uint8, device=device)
+
+
+# ---------------------------------------------------------------- serving a restored checkpoint (include/lc_serve.h)
+SERVED = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def lc_w4_row_bytes(k):
+    """Bytes of a row of k 4-bit codes (a multiple of 16)."""
+    return int(_lib.lc_w4_row_bytes(k))
+
+
+class W4:
+    """A matrix [n][k] in 4 bits with group scales: codes uint8 [n][at least lc_w4_row_bytes(k)], scales bfloat16
+    [n][at least ceil(k / group)], rows of any pitch (codes: a multiple of 16 bytes).  Keeps the two tensors and the
+    marshalled description of them for the calls that take it; they must stay in place."""
+
+    def __init__(self, codes, scales, k, group):
+        if group not in (32, 64, 128):
+            raise LcError(ERR_BADARG)
+        assert codes.is_cuda and codes.dtype == torch.uint8 and codes.dim() == 2 and (codes.stride(1) == 1 or codes.shape[1] <= 1)
+        assert scales.is_cuda and scales.dtype == torch.bfloat16 and scales.dim() == 2 and (scales.stride(1) == 1 or scales.shape[1] <= 1)
+        assert codes.shape[0] == scales.shape[0] and codes.shape[1] >= lc_w4_row_bytes(k) and scales.shape[1] >= -(-k // group)
+        self.codes, self.scales, self.n, self.k, self.group = codes, scales, codes.shape[0], k, group
+        one = self.n == 1                                    # (the pitch of a single row says nothing)
+        self._c = _W4(codes.data_ptr() or None, scales.data_ptr() or None, self.n, k, lc_w4_row_bytes(k) if one else codes.stride(0),
+                      scales.shape[1] if one else scales.stride(0), group)
+        self._p = ctypes.addressof(self._c)
+
+
+def _matrix(t):
+    """Pointer and pitch of a two-dimensional CUDA tensor whose rows are contiguous."""
+    assert t.is_cuda and t.dtype in SERVED and t.dim() == 2, "need a CUDA float32 / bfloat16 / float16 matrix"
+    n, k = t.shape
+    assert t.stride(1) == 1 or k <= 1, "need contiguous rows"
+    return t.data_ptr(), (t.stride(0) if n > 1 else k)
+
+
+def _own(t, stream):
+    """An output allocated here is used on `stream`, whose work the allocator has to know of where it is not the current one."""
+    if stream is not None:
+        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        if s != torch.cuda.current_stream():
+            t.record_stream(s)
+    return t
+
+
+def lc_w4_quantize(w, group, out=None, stream=None):
+    """w [n][k] (float32, bfloat16 or float16, contiguous rows) in 4 bits; returns a W4 (`out`, if one is given)."""
+    p, ld = _matrix(w)
+    n, k = w.shape
+    if out is None:
+        codes = _own(torch.empty(n, lc_w4_row_bytes(k), dtype=torch.uint8, device=w.device), stream)
+        scales = _own(torch.empty(n, -(-k // max(group, 1)), dtype=torch.bfloat16, device=w.device), stream)
+        out = W4(codes, scales, k, group)
+    assert out.n == n and out.k == k and out.group == group
+    st = _lib.lc_w4_quantize(p, ld, SERVED[w.dtype], out._p, _stream(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def lc_w4_dequantize(w4, dtype=None, out=None, stream=None):
+    """The values that w4 stands for, as a matrix of `dtype` (or in `out`)."""
+    if out is None:
+        out = _own(torch.empty(w4.n, w4.k, dtype=dtype if dtype is not None else torch.float32, device=w4.codes.device), stream)
+    p, ld = _matrix(out)
+    assert out.shape == (w4.n, w4.k) and (dtype is None or out.dtype == dtype)
+    st = _lib.lc_w4_dequantize(w4._p, p, ld, SERVED[out.dtype], _stream(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
+    """x [m][k] times w4 [n][k] transposed, plus bias [n]: a matrix [m][n] of x's dtype (or in `out`)."""
+    p, ld = _matrix(x)
+    m, k = x.shape
+    dtype = x.dtype
+    assert k == w4.k
+    if bias is not None:
+        assert bias.is_cuda and bias.dtype == dtype and bias.shape == (w4.n,) and (bias.stride(0) == 1 or w4.n <= 1)
+        bias = bias.data_ptr()
+    if out is None:
+        out = torch.empty(m, w4.n, dtype=dtype, device=x.device)
+        if stream is not None:
+            _own(out, stream)
+        q, ldq = out.data_ptr(), w4.n
+    else:
+        q, ldq = _matrix(out)
+        assert out.shape == (m, w4.n) and out.dtype == dtype
+    st = _lib.lc_w4_matmul(p, ld, m, w4._p, bias, q, ldq, SERVED[dtype], _stream(stream))
+    if st != OK:
+        raise LcError(st)
+    return out

@@ -1,0 +1,244 @@
+"""Weights in 4 bits with group scales (include/lc_serve.h): quantising against the definition's own arithmetic, bit for bit; the
+product against 64 bits, with bounds that follow from the roundings the kernels are allowed."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+HALF_ULP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}     # of a value rounded to nearest: significands of 24, 8 and 11 bits
+LEAST = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}
+
+
+@pytest.fixture(scope="module")
+def lc():
+    from paper_2009_13003_amd import lc as mod
+    return mod
+
+
+def bf16_bits(f):
+    b = f.view(np.uint32).astype(np.uint64)
+    r = ((b + 0x7FFF + ((b >> 16) & 1)) >> 16).astype(np.uint32)
+    return np.where(np.isnan(f), np.uint32(0x7FC0), r)
+
+
+def by_definition(w, group):
+    """codes (nibbles [n][k]) and scale bits of a float32 matrix, in numpy's IEEE arithmetic."""
+    n, k = w.shape
+    groups = -(-k // group)
+    q, sb = np.full((n, k), 8, np.uint8), np.zeros((n, groups), np.uint32)
+    with np.errstate(all="ignore"):
+        for g in range(groups):
+            part = w[:, g * group:(g + 1) * group]
+            most = np.abs(part).max(1)
+            bits = bf16_bits((most * np.float32(1.0 / 7.0)).astype(np.float32))
+            s = (bits << 16).astype(np.uint32).view(np.float32)
+            dead = ~np.isfinite(most)
+            zero = ~dead & (s < np.float32(2.0 ** -126))
+            bits = np.where(dead, 0x7FC0, np.where(zero, 0, bits))
+            live = ~dead & ~zero
+            inv = np.where(live, np.float32(1) / np.where(live, s, np.float32(1)), np.float32(0)).astype(np.float32)
+            t = np.rint((part * inv[:, None]).astype(np.float32))
+            t = np.where(live[:, None], np.clip(t, -7, 7), 0)
+            q[:, g * group:(g + 1) * group] = (t + 8).astype(np.uint8)
+            sb[:, g] = bits
+    return q, sb
+
+
+def nibbles_of(codes, k):
+    c = codes.cpu().numpy()
+    out = np.empty((c.shape[0], 2 * c.shape[1]), np.uint8)
+    out[:, 0::2], out[:, 1::2] = c & 15, c >> 4
+    return out[:, :k], out[:, k:]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("n,k", [(1, 1), (3, 2), (2, 31), (5, 33), (4, 64), (7, 129), (3, 255), (2, 1000), (33, 1025), (1000, 96)])
+def test_quantize_is_the_definition(lc, dtype, group, n, k):
+    g = torch.Generator(device=DEV); g.manual_seed(n * 1000 + k)
+    wide = torch.full((n, k + 5), 7e4, device=DEV)
+    wide[:, :k] = torch.randn(n, k, generator=g, device=DEV) * torch.exp(3 * torch.randn(n, 1, generator=g, device=DEV))
+    wide[0, :k] *= 0
+    w = wide.to(dtype)[:, :k]                               # a pitch that no vector load is aligned to
+    w4 = lc.lc_w4_quantize(w, group)
+    q, sb = by_definition(w.float().cpu().numpy(), group)
+    got, behind = nibbles_of(w4.codes, k)
+    assert np.array_equal(got, q)
+    assert (behind == 8).all()
+    assert np.array_equal(w4.scales.view(torch.int16).cpu().numpy().astype(np.uint32) & 0xFFFF, sb)
+    values = lc.lc_w4_dequantize(w4, torch.float32)
+    s = (sb << 16).astype(np.uint32).view(np.float32)
+    want = (q.astype(np.float32) - 8) * np.repeat(s, group, 1)[:, :k]
+    assert np.array_equal(values.cpu().numpy(), want, equal_nan=True)          # (rows beyond the range of fp16 hold infinities)
+    # off by at most half a step, and by what the scale's own rounding cuts off the largest (7 steps by 2^-8, limited to 7)
+    kept = np.isfinite(want)
+    with np.errstate(invalid="ignore"):
+        miss = np.abs(want.astype(np.float64) - w.float().cpu().numpy())
+    assert (miss <= np.repeat(s, group, 1)[:, :k] * (0.5 + 2.0 ** -15) + 1e-45)[kept].all()
+    back = torch.full((n, k + 3), 5.0, dtype=dtype, device=DEV)
+    lc.lc_w4_dequantize(w4, out=back[:, :k])
+    assert np.array_equal(back[:, :k].float().cpu().numpy(), torch.from_numpy(want).to(dtype).float().numpy(), equal_nan=True) and (back[:, k:] == 5).all()
+
+
+def test_quantize_extremes(lc):
+    top = float(np.finfo(np.float32).max)
+    w = torch.zeros(12, 64, device=DEV)
+    w[0, 3] = top
+    w[1, :] = -top
+    w[2, 5] = float("inf")
+    w[3, 40] = float("nan")
+    w[4, 1] = 1e-45
+    w[5, 1] = 7 * 2.0 ** -126
+    w[6, 1] = 6.9 * 2.0 ** -126
+    w[7, :7] = torch.tensor([7.0, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5])      # ties
+    w[8, 1] = -float("inf")
+    w[9, :] = -0.0
+    w[10, :32], w[10, 32:] = 3.0, float("nan")
+    w[11, 0] = 8 * 2.0 ** -126
+    for group in (32, 64):
+        w4 = lc.lc_w4_quantize(w, group)
+        q, sb = by_definition(w.cpu().numpy(), group)
+        got, _ = nibbles_of(w4.codes, 64)
+        assert np.array_equal(got, q)
+        assert np.array_equal(w4.scales.view(torch.int16).cpu().numpy().astype(np.uint32) & 0xFFFF, sb)
+        v = lc.lc_w4_dequantize(w4)
+        assert v[2].isnan().sum() == group and v[3].isnan().sum() == group and v[8].isnan().sum() == group
+        assert (v[4] == 0).all() and (v[9] == 0).all() and v[5, 1] != 0 and v[11, 0] != 0
+        assert v[10, :32].isnan().all() == (group == 64) and v[10, 32:].isnan().all()
+
+
+def random_w4(lc, n, k, group, seed, spare=0, low=0):
+    """Every nibble from `low`; garbage behind the rows' ends, NaN behind the scales."""
+    g = torch.Generator(device=DEV); g.manual_seed(seed)
+    codes = torch.randint(0, 256, (n, lc.lc_w4_row_bytes(k) + 16 * spare), generator=g, device=DEV, dtype=torch.uint8)
+    if low:
+        codes = codes.clamp(min=low) | (low << 4)
+    scales = torch.full((n, -(-k // group) + spare), float("nan"), dtype=torch.bfloat16, device=DEV)
+    scales[:, :-(-k // group)] = torch.exp(torch.randn(n, -(-k // group), generator=g, device=DEV)).to(torch.bfloat16)
+    return lc.W4(codes, scales, k, group)
+
+
+def product64(x, w4, bias):
+    """y and the sum of |x| s over the width, both in 64 bits."""
+    nib, _ = nibbles_of(w4.codes, w4.k)
+    q = torch.from_numpy(nib.astype(np.float64) - 8).to(DEV)
+    s = w4.scales.double().repeat_interleave(w4.group, 1)[:, :w4.k]
+    y = x.double() @ (q * s).t().contiguous()
+    return (y if bias is None else y + bias.double()), x.double().abs() @ s.t().contiguous()
+
+
+def check(x, w4, bias, y):
+    want, size = product64(x, w4, bias)
+    groups = -(-w4.k // w4.group)
+    # In a group: at most 2 * group sums, each rounded once, of what stays below (31 + 24) sum |x|; then a product and a sum a
+    # group and one a wavefront (16 at most), on at most 8 sum |x| s; the bias; and the result's own rounding.
+    bound = 2.0 ** -24 * (2 * w4.group * 55 + 8 * (2 * groups + 17)) * size + 2.0 ** -24 * (want.abs() + (0 if bias is None else bias.double().abs()))
+    bound = bound * (1 + HALF_ULP[y.dtype]) + HALF_ULP[y.dtype] * want.abs() + LEAST[y.dtype] + 1e-44
+    off = ((y.double() - want).abs() - bound).max().item()
+    assert off <= 0, off
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 128), (1, 17, 31), (2, 5, 33), (3, 100, 64), (15, 33, 127), (16, 16, 129), (17, 40, 200), (1, 1000, 1024),
+                                   (33, 7, 255), (5, 50, 1000), (1, 48, 4096), (9, 31, 2047), (40, 70, 513), (64, 64, 256), (70, 130, 300), (130, 257, 384),
+                                   (128, 128, 1024), (200, 96, 31), (257, 300, 640)])
+def test_product(lc, dtype, group, m, n, k):
+    g = torch.Generator(device=DEV); g.manual_seed(m * 7 + n * 5 + k * 3 + group)
+    w4 = random_w4(lc, n, k, group, m + n + k)
+    x = torch.randn(m, k, generator=g, device=DEV).to(dtype)
+    bias = torch.randn(n, generator=g, device=DEV).to(dtype) if (m + n) % 2 else None
+    check(x, w4, bias, lc.lc_w4_matmul(x, w4, bias))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,group", [(1, 33, 200, 64), (6, 20, 511, 32), (18, 40, 130, 128), (150, 140, 258, 64)])
+def test_product_of_views(lc, dtype, m, n, k, group):
+    """Pitches and first elements off every alignment; nothing beside the output is written."""
+    g = torch.Generator(device=DEV); g.manual_seed(k)
+    w4 = random_w4(lc, n, k, group, k, spare=3)
+    store = torch.full((m * (k + 3) + 1,), float("nan"), dtype=dtype, device=DEV)
+    x = store[1:].view(m, k + 3)[:, 1:k + 1]
+    x.copy_(torch.randn(m, k, generator=g, device=DEV).to(dtype))
+    bias = torch.randn(n + 1, generator=g, device=DEV).to(dtype)[1:]
+    held = torch.full((m + 2, n + 7), 3.0, dtype=dtype, device=DEV)
+    y = held[1:-1, 3:3 + n]
+    assert lc.lc_w4_matmul(x, w4, bias, out=y) is y
+    check(x, w4, bias, y)
+    held[1:-1, 3:3 + n] = 3.0
+    assert (held == 3).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [3, 150])
+def test_product_of_what_is_not_finite(lc, dtype, m):
+    n, k, group = 40, 300, 64
+    w4 = random_w4(lc, n, k, group, 5, low=9)                # q from 1 to 7: an infinity in x keeps its sign
+    g = torch.Generator(device=DEV); g.manual_seed(9)
+    x = torch.randn(m, k, generator=g, device=DEV).to(dtype)
+    x[0, 7], x[1, 299] = float("inf"), float("-inf")
+    x[2, 64] = float("nan")
+    y = lc.lc_w4_matmul(x, w4)
+    assert (y[0] == float("inf")).all() and (y[1] == float("-inf")).all() and y[2].isnan().all()
+    check(x[3:], w4, None, y[3:]) if m > 3 else None
+    w4.scales[4, 1] = float("nan")                           # a group that held one when it was quantised
+    x = torch.randn(m, k, generator=g, device=DEV).to(dtype)
+    y = lc.lc_w4_matmul(x, w4)
+    assert y[:, 4].isnan().all() and not y[:, :4].isnan().any() and not y[:, 5:].isnan().any()
+
+
+def test_product_of_large_and_small_numbers(lc):
+    """fp32 over its whole range: parts of x below the range of 16 bits, sums that only the plain formula can hold."""
+    w4 = random_w4(lc, 20, 128, 32, 3)
+    w4.scales.fill_(2.0 ** -10)
+    g = torch.Generator(device=DEV); g.manual_seed(1)
+    for power in (-100, -60, 0, 60, 115):
+        x = torch.randn(4, 128, generator=g, device=DEV) * 2.0 ** power
+        check(x, w4, None, lc.lc_w4_matmul(x, w4))
+    x = torch.full((1, 128), 2.0 ** 123, device=DEV)         # 24 times a group's sum of these is beyond the range
+    x[0, ::2] *= -1
+    check(x, w4, None, lc.lc_w4_matmul(x, w4))
+
+
+def test_empty_sizes_and_refusals(lc):
+    w4 = random_w4(lc, 8, 64, 32, 1)
+    assert lc.lc_w4_matmul(torch.zeros(0, 64, device=DEV), w4).shape == (0, 8)
+    none = lc.lc_w4_quantize(torch.zeros(0, 64, device=DEV), 32)
+    assert lc.lc_w4_matmul(torch.zeros(3, 64, device=DEV), none).shape == (3, 0)
+    flat = lc.lc_w4_quantize(torch.zeros(5, 0, device=DEV), 32)
+    bias = torch.arange(5.0, device=DEV)
+    assert torch.equal(lc.lc_w4_matmul(torch.zeros(3, 0, device=DEV), flat, bias), bias.expand(3, 5))
+    assert torch.equal(lc.lc_w4_matmul(torch.zeros(3, 0, device=DEV), flat), torch.zeros(3, 5, device=DEV))
+    with pytest.raises(lc.LcError):
+        lc.lc_w4_quantize(torch.zeros(5, 64, device=DEV), 48)
+    with pytest.raises(AssertionError):
+        lc.lc_w4_matmul(torch.zeros(3, 65, device=DEV), w4)
+    with pytest.raises(AssertionError):
+        lc.lc_w4_matmul(torch.zeros(3, 64, device=DEV, dtype=torch.float64), w4)
+    with pytest.raises(AssertionError):
+        lc.lc_w4_matmul(torch.zeros(3, 64, device=DEV), w4, torch.zeros(8, device=DEV, dtype=torch.bfloat16))
+
+
+def test_on_another_stream_and_in_a_graph(lc):
+    g = torch.Generator(device=DEV); g.manual_seed(2)
+    w = torch.randn(64, 512, generator=g, device=DEV)
+    x = torch.randn(3, 512, generator=g, device=DEV)
+    want = lc.lc_w4_matmul(x, lc.lc_w4_quantize(w, 64))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = lc.lc_w4_matmul(x, lc.lc_w4_quantize(w, 64, stream=side), stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    w4, out = lc.lc_w4_quantize(w, 64), torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lc.lc_w4_quantize(w, 64, out=w4)
+        lc.lc_w4_matmul(x, w4, out=out)
+    for seed in range(3):
+        x.copy_(torch.randn(3, 512, generator=g, device=DEV))
+        w.copy_(torch.randn(64, 512, generator=g, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, lc.lc_w4_matmul(x, lc.lc_w4_quantize(w, 64)))
