@@ -1,6 +1,7 @@
 /*
  * lc_serve.h -- what a program that answers with a restored checkpoint needs next to lc.h: weights held in 4 bits with
- * group scales and their products with activations.  Hand-written HIP kernels for MI355X (gfx950) behind the same C ABI as lc.h.
+ * group scales and their products with activations, and a paged cache of keys and values in 8 or 4 bits, written, read
+ * back and attended to.  Hand-written HIP kernels for MI355X (gfx950) behind the same C ABI as lc.h.
  *
  * As in lc.h: every pointer is a DEVICE pointer unless a parameter says "host"; `stream` is a hipStream_t passed as
  * void* (NULL = the null stream).  Every call here enqueues on `stream` and returns at once with an lc_status; it
@@ -55,6 +56,57 @@ int lc_w4_dequantize(const lc_w4* w4, void* w, uint64_t ldw, int dtype, void* st
  */
 int lc_w4_matmul(const void* x, uint64_t ldx, uint64_t m, const lc_w4* w4, const void* bias, void* y, uint64_t ldy,
                  int dtype, void* stream);
+
+/*
+ * A paged cache of keys and values.  A slot is page * page_tokens + token.  Codes lie as [page][head][token][dim],
+ * dim elements in dim * bits / 8 bytes; scales as [page][head][token], one fp32 for the dim elements of a key or value:
+ *     s = max |v| * fl32(1/most),  q = rint(v * fl32(1/s)) limited to [-most, most],  the value meant is q * s,
+ * with most = 127 and q a two's complement byte (bits = 8), or most = 7 and q + 8 a nibble, the even element in the
+ * low half (bits = 4).  Scales below 2^-126 and vectors that are not finite as for lc_w4.
+ */
+typedef struct lc_kv_cache {
+    void *k, *v;                /* codes, 16-byte aligned */
+    float *k_scale, *v_scale;   /* 16-byte aligned */
+    uint64_t pages;             /* pages * page_tokens at most 2^31 */
+    int page_tokens;            /* a power of two, 8 to 1024 */
+    int heads;                  /* at most 1024 */
+    int dim;                    /* a multiple of 32, at most 256 */
+    int bits;                   /* 8 or 4 */
+} lc_kv_cache;
+
+/*
+ * Quantises the keys and values of `tokens` tokens into the cache: k and v are [tokens][heads][dim] of type dtype, token i at
+ * element i * ld_token, head h at h * ld_head behind that (both may be any multiple of 1 that keeps vectors apart).
+ * slots: int64 [tokens], the slot of each token; a slot outside [0, pages * page_tokens) is passed over.  If a slot
+ * occurs twice, which of its tokens it holds afterwards is not defined.
+ */
+int lc_kv_write(const lc_kv_cache* cache, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots,
+                uint64_t tokens, int dtype, void* stream);
+
+/* Reads back the tokens at `slots` (int64 [tokens]) into k and v (laid out as for lc_kv_write), each value fl32(q * s)
+ * rounded once to dtype; a slot outside the cache reads as zeros. */
+int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, void* k, void* v, uint64_t ld_token, uint64_t ld_head,
+               int dtype, void* stream);
+
+/*
+ * Attention of nq drafted tokens a sequence over its cached tokens, the drafted ones already written among them:
+ *   q, out  [batch][nq][heads][dim] of type dtype, contiguous, 16-byte aligned; heads a multiple of cache->heads, at most 4096, and head h
+ *           reads the cache's head h / (heads / cache->heads)
+ *   table   int32 [batch][ld_table]: the pages of a sequence, in order; lens int32 [batch]: its cached tokens, of which
+ *           the newest nq are the drafted ones (fewer than nq: the drafted tokens that would lie before the first do not exist).
+ *           A length is held to what the table has room for (table_pages pages); a page outside the cache counts as not seen.
+ *   mask    NULL, or uint64 [batch][nq]: drafted token i sees drafted token j iff bit j of mask[i] is set (a tree's ancestors and
+ *           itself).  NULL: j <= i.  Everything before the drafted tokens is seen by all of them.  nq is at most 64; nq = 1 is
+ *           the step of one token.
+ *   out     softmax over the seen tokens of (scale * q . k), times v; zeros where a token sees nothing.  Sums, maxima and
+ *           products with the probabilities are held in 32 bits.  Keys and values that are not seen do not matter, whatever they hold.
+ *   ws      scratch, 256-byte aligned, lc_kv_workspace_bytes; its content need not be anything.  Calls that may run at the same
+ *           time (on different streams) need areas of their own.
+ */
+size_t lc_kv_workspace_bytes(uint64_t batch, int nq, int heads, int kv_heads, int dim);
+int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq, int heads, const int32_t* table, uint64_t ld_table,
+                 uint64_t table_pages, const int32_t* lens, const uint64_t* mask, float scale, void* out, int dtype, void* ws,
+                 size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

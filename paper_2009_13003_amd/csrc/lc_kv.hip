@@ -1,0 +1,512 @@
+// A paged cache of keys and values in 8 or 4 bits: writing, reading back, and the attention over it (include/lc_serve.h).
+#include "lc_serve.h"
+
+namespace lc {
+namespace serve {
+namespace {
+
+struct Cache {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    uint64_t slots;             // pages * page_tokens
+    uint32_t page_shift, heads, dim, row_bytes;
+};
+
+// Where a head's token lies: the row of codes and the scale, counted in rows.
+__device__ __forceinline__ uint64_t row_of(const Cache& c, uint64_t page, uint32_t head, uint32_t token) {
+    return ((page * c.heads + head) << c.page_shift) + token;
+}
+
+// ---------------------------------------------------------------- writing and reading back
+// A lane takes eight elements of a token's head, a power of two of lanes (those behind the last element idle) the whole head; the
+// keys are the first half of the grid, the values the second.
+template <int T, int BITS, int LANES>
+__global__ __launch_bounds__(256) void k_kv_write(Cache c, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots,
+                                                  uint32_t items, FastDiv by_heads) {
+    const uint32_t item = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, at = 8 * (threadIdx.x % LANES);
+    const bool in = item < items;
+    const uint32_t token = by_heads(in ? item : 0), head = (in ? item : 0) - token * c.heads;
+    const void* from = blockIdx.y ? v : k;
+    float x[8];
+    load_eight<T>(from, token * ld_token + head * ld_head + at, in && at < c.dim ? 8 : 0, x);
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { const uint32_t a = bits_of(x[e]) & 0x7fffffffu; most = a > most ? a : most; }
+    most = max_of_lanes<LANES>(most);
+    constexpr float kMost = BITS == 8 ? 127.0f : 7.0f;
+    float s = float_of(most) * (1.0f / kMost), inv = 0.0f;
+    if (most >= 0x7f800000u) s = __builtin_nanf("");
+    else if (s < kSmallest) s = 0.0f;
+    else inv = 1.0f / s;
+    if (!in || at >= c.dim) return;
+    const int64_t slot = slots[token];
+    if (slot < 0 || (uint64_t)slot >= c.slots) return;
+    uint32_t q[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = rounded(fminf(fmaxf(inv == 0.0f ? 0.0f : x[e] * inv, -kMost), kMost), BITS == 8 ? 0.0f : 8.0f);
+    const uint64_t row = row_of(c, (uint64_t)slot >> c.page_shift, head, (uint32_t)slot & ((1u << c.page_shift) - 1));
+    uint8_t* to = (blockIdx.y ? c.v : c.k) + row * c.row_bytes + at * BITS / 8;
+    if (BITS == 8) {
+        u32x2 w = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= (q[e] & 255u) << (8 * (e % 4));
+        *reinterpret_cast<u32x2*>(to) = w;
+    } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w |= (q[e] & 15u) << (4 * e);
+        *reinterpret_cast<uint32_t*>(to) = w;
+    }
+    if (at == 0) (blockIdx.y ? c.v_scale : c.k_scale)[row] = s;
+}
+
+template <int T, int BITS>
+__global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, void* k, void* v, uint64_t ld_token, uint64_t ld_head, uint32_t lanes,
+                                                 FastDiv by_row, FastDiv by_heads) {
+    const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
+    if (lane >= lanes) return;
+    const uint32_t item = by_row(lane), at = 8 * (lane - item * by_row.d);
+    const uint32_t token = by_heads(item), head = item - token * c.heads;
+    const int64_t slot = slots[token];
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (slot >= 0 && (uint64_t)slot < c.slots) {
+        const uint64_t row = row_of(c, (uint64_t)slot >> c.page_shift, head, (uint32_t)slot & ((1u << c.page_shift) - 1));
+        const uint8_t* from = (blockIdx.y ? c.v : c.k) + row * c.row_bytes + at * BITS / 8;
+        const float s = (blockIdx.y ? c.v_scale : c.k_scale)[row];
+        if (BITS == 8) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(from);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)(w[e / 4] >> (8 * (e % 4))) * s;
+        } else {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(from);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)((int)(w >> (4 * e) & 15u) - 8) * s;
+        }
+    }
+    store_eight<T>(blockIdx.y ? v : k, token * ld_token + head * ld_head + at, 8, x);
+}
+
+// ---------------------------------------------------------------- attention
+// The rows that share a head of the cache are the nq * (heads / kv heads) queries of a sequence; a wavefront holds 16 of them (or 32, 64)
+// and walks over its part of the sequence 32 tokens at a time, everything in registers:
+//   S^T = K Q^T   rows of the matrix instruction are tokens, columns the queries: lane l gets query l % 16, tokens 4 (l / 16) + 0..3
+//   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens
+//                    in the order 4 h + 0..3, 16 + 4 h + 0..3, in which the values are then loaded too
+// so the running maximum, the sum and the factors of the rescaling are one number a lane, and nothing passes through LDS.
+// Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly.
+constexpr int kTile = 32, kWaves = 4;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr uint32_t kMostSplits = 64, kWantBlocks = 1024, kLeastTokens = 128;
+
+struct Attend {
+    Cache c;
+    const void* q;
+    const int32_t* table; uint64_t ld_table; uint64_t table_pages;
+    const int32_t* lens;
+    const uint64_t* mask;
+    void* out;
+    float* part;                // [row][split][dim], then the maximum and the sum of each [row][split]
+    float* stats;
+    float scale;                // times log2(e)
+    uint32_t batch, nq, heads, group, rows;     // rows = nq * group of a head of the cache
+    uint32_t splits, tiles;                     // 32-token tiles a split
+    int32_t pages;
+};
+
+template <int T> struct Kind;       // how many 16-bit parts an element of q, and a probability, are given
+template <> struct Kind<LC_F32> { static constexpr int kQ = 3, kP = 3; static constexpr bool kHalf = false; };
+template <> struct Kind<LC_BF16> { static constexpr int kQ = 1, kP = 2; static constexpr bool kHalf = false; };
+template <> struct Kind<LC_F16> { static constexpr int kQ = 1, kP = 2; static constexpr bool kHalf = true; };
+
+template <bool HALF> __device__ __forceinline__ f32x4 mfma_16(u32x4 a, u32x4 b, f32x4 c) { return HALF ? mfma_f16(a, b, c) : mfma_bf16(a, b, c); }
+
+// Two whole numbers of at most 8 bits as an operand's pair: exact in either type.
+template <bool HALF> __device__ __forceinline__ uint32_t pair_of(float a, float b) {
+    if (HALF) { const auto h = __builtin_amdgcn_cvt_pkrtz(a, b); uint32_t u; __builtin_memcpy(&u, &h, 4); return u; }
+    return high_halves(bits_of(a), bits_of(b));
+}
+// Nibble j of a word of 4-bit codes as a sixteenth of what it stands for: the instruction reads four bits as a two's complement number
+// of sixteenths, which the code with its top bit turned round is.
+__device__ __forceinline__ uint32_t turned(uint32_t w) { return w ^ 0x88888888u; }
+__device__ __forceinline__ float nibble_of(uint32_t w, int j) { return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * j))); }
+template <int BYTE> __device__ __forceinline__ float byte_of(uint32_t w) { return (float)(int8_t)(w >> (8 * BYTE)); }
+
+// A bf16 operand of the values of eight tokens at element j of each token's `w` (4 bits: turned words, and sixteenths).
+template <int BITS> __device__ __forceinline__ u32x4 values_at(const uint32_t (&w)[8], int j) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a, b;
+        if (BITS == 8) { a = (float)(int8_t)(w[2 * e] >> (8 * j)); b = (float)(int8_t)(w[2 * e + 1] >> (8 * j)); }
+        else { a = nibble_of(w[2 * e], j); b = nibble_of(w[2 * e + 1], j); }
+        r[e] = high_halves(bits_of(a), bits_of(b));
+    }
+    return r;
+}
+
+__device__ __forceinline__ float max_over_quarters(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ __forceinline__ float sum_over_quarters(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+
+template <int T, int BITS, int DP>
+__global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
+    constexpr bool HALF = Kind<T>::kHalf;
+    constexpr int NQ = Kind<T>::kQ, NP = Kind<T>::kP;
+    // Keys in 4 bits for 16-bit queries: 16 + c, a nibble put into the mantissa of 16 (two operations for two codes), and 24 times the
+    // query's sum taken away, which moves scores by some 2^-24 of 24 sum |q|; for fp32 exact codes instead.
+    constexpr bool LIFTED = BITS == 4 && T != LC_F32;
+    constexpr int KOPS = DP / 32;                           // operands of a token's key
+    constexpr int LANE_K = DP * BITS / 8 / 4 < 16 ? DP * BITS / 8 / 4 : 16;     // bytes of a key a lane loads at once
+    constexpr int LOADS_K = DP * BITS / 8 / 4 / LANE_K, WORDS_K = LANE_K / 4;
+    constexpr int VD = DP / 16;                             // elements of a value a lane holds
+    constexpr int LANE_V = VD * BITS / 8, WORDS_V = (LANE_V + 3) / 4, PER_WORD = 32 / BITS < VD ? 32 / BITS : VD;
+    __shared__ float so[kWaves][16][DP + 4];
+    __shared__ float sm[kWaves][16], sl[kWaves][16];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
+    const uint32_t split = blockIdx.x, row_groups = (a.rows + 15) / 16;
+    const uint32_t head = blockIdx.y / row_groups, row0 = (blockIdx.y - head * row_groups) * 16, b = blockIdx.z;
+    const uint32_t row = row0 + c;                          // this lane's query
+    const bool has_row = row < a.rows;
+    const uint32_t qi = (has_row ? row : 0) / a.group, qg = (has_row ? row : 0) - qi * a.group;
+    const uint64_t q_at = (((uint64_t)b * a.nq + qi) * a.heads + head * a.group + qg) * a.c.dim;
+    const int64_t room = (int64_t)(a.table_pages << a.c.page_shift);
+    const int64_t len = a.lens[b] < 0 ? 0 : a.lens[b] < room ? a.lens[b] : room;
+    const int64_t base = len - (int64_t)a.nq;               // the first drafted token
+    const uint64_t mask = a.mask ? a.mask[(uint64_t)b * a.nq + qi] : qi >= 63 ? ~0ull : (2ull << qi) - 1;
+    const int32_t* table = a.table + b * a.ld_table;
+
+    // the queries, eight elements an operand at the places at which the keys' codes lie
+    u32x4 q[KOPS][NQ];
+    f32x4 less = {0, 0, 0, 0};                              // -24 times each query's sum
+#pragma unroll
+    for (int o = 0; o < KOPS; ++o) {
+        uint32_t d;
+        if (BITS == 8) d = 16 * h * (LANE_K / 16) + 64 * (o / 2) + 8 * (o % 2);
+        else d = 2 * LANE_K * h + 8 * LANE_K * (o / WORDS_K) + 8 * (o % WORDS_K);
+        float v[8];
+        load_eight<T>(a.q, q_at + d, has_row && d < a.c.dim ? 8 : 0, v);
+#pragma unroll
+        for (int p = 0; p < NQ; ++p) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = BITS == 8 ? v[2 * j] : v[j], y = BITS == 8 ? v[2 * j + 1] : v[j + 4];
+                q[o][p][j] = HALF ? f16_of(x) | f16_of(y) << 16 : high_halves(bits_of(x), bits_of(y));
+            }
+            if (NQ > 1)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);
+        }
+        if (LIFTED) {
+            const uint32_t m24 = HALF ? 0xCE00CE00u : 0xC1C0C1C0u;
+#pragma unroll
+            for (int p = NQ - 1; p >= 0; --p) less = mfma_16<HALF>(u32x4{m24, m24, m24, m24}, q[o][p], less);
+        }
+    }
+
+    f32x4 acc[VD];
+#pragma unroll
+    for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    float top = -__builtin_inff(), sum = 0;
+    const int64_t first = (int64_t)split * a.tiles * kTile;
+    const int64_t end = first + (int64_t)a.tiles * kTile < len ? first + (int64_t)a.tiles * kTile : len;
+    for (int64_t tb = first + wave * kTile; tb < end; tb += kWaves * kTile) {
+        // keys: token 16 s + c of the tile
+        u32x4 key[2][KOPS];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int64_t t = tb + 16 * s + c < len ? tb + 16 * s + c : len - 1;
+            int32_t page = table[t >> a.c.page_shift];
+            page = (uint32_t)page < (uint32_t)a.pages ? page : 0;
+            const uint8_t* from = a.c.k + row_of(a.c, page, head, (uint32_t)t & ((1u << a.c.page_shift) - 1)) * a.c.row_bytes + h * LANE_K;
+#pragma unroll
+            for (int l = 0; l < LOADS_K; ++l) {
+                uint32_t w[WORDS_K];
+                const bool in = l * 4 * LANE_K + h * LANE_K < a.c.row_bytes;
+#pragma unroll
+                for (int i = 0; i < WORDS_K; ++i) w[i] = 0;
+                if (in) __builtin_memcpy(w, __builtin_assume_aligned(from + l * 4 * LANE_K, LANE_K), LANE_K);
+                if (BITS == 8) {
+#pragma unroll
+                    for (int i = 0; i < WORDS_K; ++i) {
+                        key[s][l * WORDS_K / 2 + i / 2][2 * (i % 2)] = pair_of<HALF>(byte_of<0>(w[i]), byte_of<1>(w[i]));
+                        key[s][l * WORDS_K / 2 + i / 2][2 * (i % 2) + 1] = pair_of<HALF>(byte_of<2>(w[i]), byte_of<3>(w[i]));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < WORDS_K; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (!LIFTED) { key[s][l * WORDS_K + i][j] = high_halves(bits_of(nibble_of(turned(w[i]), j)), bits_of(nibble_of(turned(w[i]), j + 4))); continue; }
+                            const int up = (HALF ? 6 : 3) - 4 * j;
+                            const uint32_t m = up >= 0 ? w[i] << (up & 31) : w[i] >> (-up & 31);
+                            key[s][l * WORDS_K + i][j] = HALF ? (m & 0x03C003C0u) | 0x4C004C00u : (m & 0x00780078u) | 0x41804180u;
+                        }
+                }
+            }
+        }
+        // values and scales: tokens 16 s + 4 h + 0..3
+        uint32_t val[WORDS_V][8];
+        float ks[8], vs[8];
+        uint32_t seen = 0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int64_t t0 = tb + 16 * s + 4 * h;
+            const int64_t tc = t0 < len ? t0 : (len - 1) & ~(int64_t)3;
+            int32_t page = table[tc >> a.c.page_shift];
+            const bool there = (uint32_t)page < (uint32_t)a.pages;
+            page = there ? page : 0;
+            const uint64_t at = row_of(a.c, page, head, (uint32_t)tc & ((1u << a.c.page_shift) - 1));
+            const f32x4 k4 = *reinterpret_cast<const f32x4*>(a.c.k_scale + at), v4 = *reinterpret_cast<const f32x4*>(a.c.v_scale + at);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                ks[4 * s + r] = k4[r] * (BITS == 4 && !LIFTED ? 16.0f * a.scale : a.scale);
+                vs[4 * s + r] = v4[r];
+                const int64_t t = t0 + r, j = t - base;
+                if (there && t < end && (j < 0 || (mask >> (j & 63) & 1))) seen |= 1u << (4 * s + r);
+                uint32_t w[WORDS_V];
+#pragma unroll
+                for (int i = 0; i < WORDS_V; ++i) w[i] = 0;
+                if (c * LANE_V < a.c.row_bytes) __builtin_memcpy(w, __builtin_assume_aligned(a.c.v + (at + r) * a.c.row_bytes + c * LANE_V, LANE_V < 16 ? LANE_V : 16), LANE_V);
+#pragma unroll
+                for (int i = 0; i < WORDS_V; ++i) val[i][4 * s + r] = BITS == 4 ? turned(w[i]) : w[i];
+            }
+        }
+        f32x4 score[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            score[s] = LIFTED ? less : f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int o = 0; o < KOPS; ++o)
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p) score[s] = mfma_16<HALF>(key[s][o], q[o][p], score[s]);
+        }
+        float x[8], most = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = seen >> e & 1 ? score[e / 4][e % 4] * ks[e] : -__builtin_inff();
+            most = fmaxf(most, x[e]);
+        }
+        most = fmaxf(max_over_quarters(most), top);
+        const float from = most == -__builtin_inff() ? 0.0f : most;
+        const float shrink = __builtin_amdgcn_exp2f(top - from);
+        top = most;
+        sum *= shrink;
+#pragma unroll
+        for (int j = 0; j < VD; ++j) acc[j] *= shrink;
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float w = __builtin_amdgcn_exp2f(x[e] - from);
+            sum += w;
+            p[e] = seen >> e & 1 ? w * vs[e] : 0.0f;            // (what is not seen may have any scale)
+        }
+        u32x4 pp[NP];
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pp[n][e] = high_halves(bits_of(p[2 * e]), bits_of(p[2 * e + 1]));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
+        }
+#pragma unroll
+        for (int j = 0; j < VD; ++j) {
+            const u32x4 v = values_at<BITS>(val[j / PER_WORD], j % PER_WORD);
+#pragma unroll
+            for (int n = NP - 1; n >= 0; --n) acc[j] = mfma_bf16(v, pp[n], acc[j]);
+        }
+    }
+    sum = sum_over_quarters(sum);
+
+    // the wavefronts' parts, joined: lane (c, h) holds elements VD (4 h + r) + j of query c
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < VD; ++j) so[wave][c][VD * (4 * h + r) + j] = BITS == 4 ? 16.0f * acc[j][r] : acc[j][r];
+    if (h == 0) { sm[wave][c] = top; sl[wave][c] = sum; }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < 16 * a.c.dim; e += kWaves * 64) {
+        const uint32_t r = e / a.c.dim, d = e - r * a.c.dim;
+        if (row0 + r >= a.rows) break;
+        float m = sm[0][r];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][r]);
+        const float from = m == -__builtin_inff() ? 0.0f : m;
+        float l = 0, o = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(sm[w][r] - from);
+            l += sl[w][r] == 0.0f ? 0.0f : f * sl[w][r];
+            o += sl[w][r] == 0.0f ? 0.0f : f * so[w][r][d];
+        }
+        const uint32_t i = (row0 + r) / a.group, g = (row0 + r) - i * a.group;
+        const uint64_t out_row = ((uint64_t)b * a.nq + i) * a.heads + head * a.group + g;
+        if (a.splits == 1) store_one<T>(a.out, out_row * a.c.dim + d, l == 0.0f ? 0.0f : o / l);
+        else {
+            a.part[(out_row * a.splits + split) * a.c.dim + d] = o;
+            if (d == 0) { a.stats[2 * (out_row * a.splits + split)] = m; a.stats[2 * (out_row * a.splits + split) + 1] = l; }
+        }
+    }
+}
+
+// The splits of each row, joined: a wavefront a row.
+template <int T>
+__global__ __launch_bounds__(256) void k_kv_join(const float* part, const float* stats, void* out, uint64_t rows, uint32_t splits, uint32_t dim) {
+    const uint64_t row = blockIdx.x * 4ull + threadIdx.x / 64;
+    if (row >= rows) return;
+    const uint32_t lane = threadIdx.x % 64;
+    const bool has = lane < splits;
+    const float m = has ? stats[2 * (row * splits + lane)] : -__builtin_inff(), l = has ? stats[2 * (row * splits + lane) + 1] : 0.0f;
+    float top = m;
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float f = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
+    float total = l == 0.0f ? 0.0f : f * l;
+    for (int x = 1; x < 64; x *= 2) total += __shfl_xor(total, x);
+    float o[4] = {0, 0, 0, 0};
+    for (uint32_t s = 0; s < splits; ++s) {
+        if (__shfl(l, s) == 0.0f) continue;
+        const float w = __shfl(f, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 64 * i < dim) o[i] = fmaf(w, part[(row * splits + s) * dim + lane + 64 * i], o[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (lane + 64 * i < dim) store_one<T>(out, row * dim + lane + 64 * i, total == 0.0f ? 0.0f : o[i] / total);
+}
+
+// Splits of a sequence: as many as give the chip enough workgroups, whatever its length.
+uint32_t most_splits(uint64_t batch, uint32_t nq, uint32_t heads, uint32_t kv_heads) {
+    const uint64_t rows = (uint64_t)nq * (heads / kv_heads), blocks = batch * kv_heads * ((rows + 15) / 16);
+    const uint64_t s = blocks ? (kWantBlocks + blocks - 1) / blocks : 1;
+    return (uint32_t)(s < kMostSplits ? s : kMostSplits);
+}
+
+bool bad(const lc_kv_cache* c) {
+    if (!c || c->heads < 1 || c->heads > 1024 || c->dim < 32 || c->dim > 256 || c->dim % 32 || (c->bits != 8 && c->bits != 4)) return true;
+    if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) || c->pages > (1ull << 31) / c->page_tokens) return true;
+    if (c->pages == 0) return false;
+    return !c->k || !c->v || !c->k_scale || !c->v_scale || off(c->k, 16) || off(c->v, 16) || off(c->k_scale, 16) || off(c->v_scale, 16);
+}
+Cache described(const lc_kv_cache& c) {
+    return {static_cast<uint8_t*>(c.k), static_cast<uint8_t*>(c.v), c.k_scale, c.v_scale, c.pages * c.page_tokens,
+            (uint32_t)__builtin_ctz((unsigned)c.page_tokens), (uint32_t)c.heads, (uint32_t)c.dim, (uint32_t)(c.dim * c.bits / 8)};
+}
+int launched() { return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP; }
+
+bool bad_vectors(const lc_kv_cache* c, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots, uint64_t tokens, int dtype) {
+    const uintptr_t size = size_of(dtype);
+    return !k || !v || !slots || off(k, size) || off(v, size) || off(slots, 8) || tokens > (1ull << 31) || ld_token > (1ull << 40) || ld_head > (1ull << 40) ||
+           (c->heads > 1 && ld_head < (uint64_t)c->dim) || (tokens > 1 && ld_token < (uint64_t)c->dim);
+}
+
+template <int T, int BITS>
+void write(const Cache& c, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots, uint64_t tokens, hipStream_t s) {
+    const uint32_t lanes = c.dim <= 32 ? 4 : c.dim <= 64 ? 8 : c.dim <= 128 ? 16 : 32;
+    const uint64_t step = (1ull << 25) / c.heads;                  // items are counted in 25 bits, a launch's lanes in 31
+    for (uint64_t t = 0; t < tokens; t += step) {
+        const uint32_t items = (uint32_t)((tokens - t < step ? tokens - t : step) * c.heads);
+        const uint64_t by = t * ld_token * (T == LC_F32 ? 4 : 2);
+        const void *from_k = static_cast<const uint8_t*>(k) + by, *from_v = static_cast<const uint8_t*>(v) + by;
+        const dim3 grid((items + 256 / lanes - 1) / (256 / lanes), 2);
+        const FastDiv div(c.heads);
+        if (lanes == 4) k_kv_write<T, BITS, 4><<<grid, 256, 0, s>>>(c, from_k, from_v, ld_token, ld_head, slots + t, items, div);
+        else if (lanes == 8) k_kv_write<T, BITS, 8><<<grid, 256, 0, s>>>(c, from_k, from_v, ld_token, ld_head, slots + t, items, div);
+        else if (lanes == 16) k_kv_write<T, BITS, 16><<<grid, 256, 0, s>>>(c, from_k, from_v, ld_token, ld_head, slots + t, items, div);
+        else k_kv_write<T, BITS, 32><<<grid, 256, 0, s>>>(c, from_k, from_v, ld_token, ld_head, slots + t, items, div);
+    }
+}
+template <int T, int BITS>
+void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* v, uint64_t ld_token, uint64_t ld_head, hipStream_t s) {
+    const uint64_t step = (1ull << 25) / c.heads;
+    for (uint64_t t = 0; t < tokens; t += step) {
+        const uint32_t lanes = (uint32_t)((tokens - t < step ? tokens - t : step) * c.heads * (c.dim / 8));
+        const uint64_t by = t * ld_token * (T == LC_F32 ? 4 : 2);
+        k_kv_read<T, BITS><<<dim3((lanes + 255) / 256, 2), 256, 0, s>>>(c, slots + t, static_cast<uint8_t*>(k) + by, static_cast<uint8_t*>(v) + by, ld_token,
+                                                                        ld_head, lanes, FastDiv(c.dim / 8), FastDiv(c.heads));
+    }
+}
+template <int T, int BITS>
+void attend(const Attend& a, hipStream_t s) {
+    const dim3 grid(a.splits, a.c.heads * ((a.rows + 15) / 16), a.batch);
+    if (a.c.dim <= 64) k_kv_attend<T, BITS, 64><<<grid, kWaves * 64, 0, s>>>(a);
+    else if (a.c.dim <= 128) k_kv_attend<T, BITS, 128><<<grid, kWaves * 64, 0, s>>>(a);
+    else k_kv_attend<T, BITS, 256><<<grid, kWaves * 64, 0, s>>>(a);
+    const uint64_t rows = (uint64_t)a.batch * a.nq * a.heads;
+    if (a.splits > 1) k_kv_join<T><<<(uint32_t)((rows + 3) / 4), 256, 0, s>>>(a.part, a.stats, a.out, rows, a.splits, a.c.dim);
+}
+
+}  // namespace
+}  // namespace serve
+}  // namespace lc
+
+using namespace lc::serve;
+
+#define LC_BY_BITS(call, T, bits) do { if ((bits) == 8) call(T, 8); else call(T, 4); } while (0)
+#define LC_BY_TYPE(call, dtype, bits) \
+    do { if ((dtype) == LC_F32) LC_BY_BITS(call, LC_F32, bits); else if ((dtype) == LC_BF16) LC_BY_BITS(call, LC_BF16, bits); \
+         else LC_BY_BITS(call, LC_F16, bits); } while (0)
+
+extern "C" {
+
+int lc_kv_write(const lc_kv_cache* cache, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots, uint64_t tokens, int dtype,
+                void* stream) {
+    if (!served_type(dtype) || bad(cache)) return LC_ERR_BADARG;
+    if (tokens == 0) return LC_OK;
+    if (bad_vectors(cache, k, v, ld_token, ld_head, slots, tokens, dtype)) return LC_ERR_BADARG;
+    const Cache c = described(*cache);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define CALL(T, B) write<T, B>(c, k, v, ld_token, ld_head, slots, tokens, s)
+    LC_BY_TYPE(CALL, dtype, cache->bits);
+#undef CALL
+    return launched();
+}
+
+int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, void* k, void* v, uint64_t ld_token, uint64_t ld_head, int dtype, void* stream) {
+    if (!served_type(dtype) || bad(cache)) return LC_ERR_BADARG;
+    if (tokens == 0) return LC_OK;
+    if (bad_vectors(cache, k, v, ld_token, ld_head, slots, tokens, dtype)) return LC_ERR_BADARG;
+    const Cache c = described(*cache);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define CALL(T, B) read<T, B>(c, slots, tokens, k, v, ld_token, ld_head, s)
+    LC_BY_TYPE(CALL, dtype, cache->bits);
+#undef CALL
+    return launched();
+}
+
+size_t lc_kv_workspace_bytes(uint64_t batch, int nq, int heads, int kv_heads, int dim) {
+    if (batch > 65535 || nq < 1 || nq > 64 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 ||
+        dim > 256 || dim % 32) return 0;
+    const uint64_t splits = most_splits(batch, (uint32_t)nq, (uint32_t)heads, (uint32_t)kv_heads);
+    return splits == 1 ? 256 : (size_t)((batch * nq * heads * splits * (dim + 2) * 4 + 255) / 256 * 256);
+}
+
+int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq, int heads, const int32_t* table, uint64_t ld_table, uint64_t table_pages,
+                 const int32_t* lens, const uint64_t* mask, float scale, void* out, int dtype, void* ws, size_t ws_bytes, void* stream) {
+    if (!served_type(dtype) || bad(cache) || batch > 65535) return LC_ERR_BADARG;
+    const size_t need = lc_kv_workspace_bytes(batch, nq, heads, cache->heads, cache->dim);
+    if (!need) return LC_ERR_BADARG;
+    if (batch == 0) return LC_OK;
+    if (!q || !out || !lens || off(q, 16) || off(out, 16) || off(lens, 4) || off(mask, 8) || (table_pages && (!table || off(table, 4))) ||
+        ld_table > (1ull << 31) || table_pages > (1ull << 31) / cache->page_tokens || (batch > 1 && ld_table < table_pages)) return LC_ERR_BADARG;
+    if (!ws || off(ws, 256) || ws_bytes < need) return LC_ERR_WORKSPACE;
+    Attend a = {};
+    a.c = described(*cache);
+    a.q = q; a.table = table; a.ld_table = ld_table; a.table_pages = cache->pages ? table_pages : 0; a.lens = lens; a.mask = mask; a.out = out;
+    a.scale = scale * kLog2e;
+    a.batch = (uint32_t)batch; a.nq = (uint32_t)nq; a.heads = (uint32_t)heads; a.group = (uint32_t)(heads / cache->heads); a.rows = a.nq * a.group;
+    a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
+    // (splits by what the table has room for: the lengths are known on the device only)
+    const uint64_t room = a.table_pages << a.c.page_shift, by_room = (room + kLeastTokens - 1) / kLeastTokens;
+    uint64_t splits = most_splits(batch, a.nq, a.heads, a.c.heads);
+    splits = by_room < splits ? (by_room ? by_room : 1) : splits;
+    a.tiles = (uint32_t)((room + splits * kTile - 1) / (splits * kTile));
+    a.splits = (uint32_t)splits;
+    a.part = static_cast<float*>(ws);
+    a.stats = a.part + batch * nq * heads * splits * a.c.dim;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define CALL(T, B) attend<T, B>(a, s)
+    LC_BY_TYPE(CALL, dtype, cache->bits);
+#undef CALL
+    return launched();
+}
+
+}  // extern "C"

@@ -100,7 +100,7 @@ template <int T> __device__ __forceinline__ void store_eight(void* p, uint64_t i
     }
 }
 
-// The largest of `lanes` neighbouring lanes' values in every one of them (lanes: 4, 8 or 16, aligned).
+// The largest of `lanes` neighbouring lanes' values in every one of them (lanes: 4, 8, 16 or 32, aligned).
 template <int LANES> __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
 #define LC_DPP_MAX(ctrl) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false); v = v > o ? v : o; }
     if (LANES >= 2) LC_DPP_MAX(0xB1)      // the other of each two
@@ -108,6 +108,7 @@ template <int LANES> __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v
     if (LANES >= 8) LC_DPP_MAX(0x141)     // the other four of each eight
     if (LANES >= 16) LC_DPP_MAX(0x140)    // the other eight of each sixteen
 #undef LC_DPP_MAX
+    if (LANES >= 32) { const uint32_t o = (uint32_t)__shfl_xor((int)v, 16); v = v > o ? v : o; }
     return v;
 }
 

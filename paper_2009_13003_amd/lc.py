@@ -94,6 +94,11 @@ class _W4(ctypes.Structure):            # struct lc_w4
     _fields_ = [("codes", _vp), ("scales", _vp), ("n", _u64), ("k", _u64), ("codes_pitch", _u64), ("scales_pitch", _u64), ("group", _int)]
 
 
+class _KvCache(ctypes.Structure):       # struct lc_kv_cache
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _u64), ("page_tokens", _int), ("heads", _int),
+                ("dim", _int), ("bits", _int)]
+
+
 _lib.lc_w4_row_bytes.restype = _sz
 _lib.lc_w4_row_bytes.argtypes = [_u64]
 _lib.lc_w4_quantize.restype = _int
@@ -102,6 +107,15 @@ _lib.lc_w4_dequantize.restype = _int
 _lib.lc_w4_dequantize.argtypes = [_vp, _vp, _u64, _int, _vp]
 _lib.lc_w4_matmul.restype = _int
 _lib.lc_w4_matmul.argtypes = [_vp, _u64, _u64, _vp, _vp, _vp, _u64, _int, _vp]
+
+_lib.lc_kv_write.restype = _int
+_lib.lc_kv_write.argtypes = [_vp, _vp, _vp, _u64, _u64, _vp, _u64, _int, _vp]
+_lib.lc_kv_read.restype = _int
+_lib.lc_kv_read.argtypes = [_vp, _vp, _u64, _vp, _vp, _u64, _u64, _int, _vp]
+_lib.lc_kv_workspace_bytes.restype = _sz
+_lib.lc_kv_workspace_bytes.argtypes = [_u64, _int, _int, _int, _int]
+_lib.lc_kv_attend.restype = _int
+_lib.lc_kv_attend.argtypes = [_vp, _vp, _u64, _int, _int, _vp, _u64, _u64, _vp, _vp, ctypes.c_float, _vp, _int, _vp, _sz, _vp]
 
 
 class LcError(RuntimeError):
@@ -578,6 +592,111 @@ def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
         q, ldq = _matrix(out)
         assert out.shape == (m, w4.n) and out.dtype == dtype
     st = _lib.lc_w4_matmul(p, ld, m, w4._p, bias, q, ldq, SERVED[dtype], _stream(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+class KvCache:
+    """A paged cache of keys and values: k and v uint8 [pages][heads][page_tokens][dim * bits / 8], k_scale and v_scale float32
+    [pages][heads][page_tokens], all contiguous.  Keeps the tensors and their marshalled description; they must stay in place."""
+
+    def __init__(self, k, v, k_scale, v_scale, bits):
+        if bits not in (8, 4):
+            raise LcError(ERR_BADARG)
+        for t in (k, v):
+            assert t.is_cuda and t.dtype == torch.uint8 and t.dim() == 4 and t.is_contiguous() and t.shape == k.shape
+        for t in (k_scale, v_scale):
+            assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == k.shape[:3]
+        self.k, self.v, self.k_scale, self.v_scale, self.bits = k, v, k_scale, v_scale, bits
+        self.pages, self.heads, self.page_tokens, row = k.shape
+        self.dim = row * 8 // bits
+        self._c = _KvCache(k.data_ptr() or None, v.data_ptr() or None, k_scale.data_ptr() or None, v_scale.data_ptr() or None, self.pages,
+                           self.page_tokens, self.heads, self.dim, bits)
+        self._p = ctypes.addressof(self._c)
+
+
+def new_kv_cache(pages, heads, page_tokens, dim, bits, device="cuda"):
+    """An empty cache (every key and value zero)."""
+    k, v = (torch.full((pages, heads, page_tokens, dim * bits // 8), 0 if bits == 8 else 0x88, dtype=torch.uint8, device=device) for _ in range(2))
+    ks, vs = (torch.zeros(pages, heads, page_tokens, dtype=torch.float32, device=device) for _ in range(2))
+    return KvCache(k, v, ks, vs, bits)
+
+
+def _vectors(cache, k, v):
+    """Pitches of two tensors [tokens][heads][dim] that are laid out alike, each head's elements contiguous."""
+    assert k.is_cuda and v.is_cuda and k.dtype in SERVED and v.dtype == k.dtype and k.dim() == 3 and v.shape == k.shape
+    tokens, heads, dim = k.shape
+    assert heads == cache.heads and dim == cache.dim
+    st, sh, s1 = k.stride()
+    assert s1 == 1 and (v.stride() == k.stride() or tokens == 0), "keys and values need contiguous heads and the same pitches"
+    return (st if tokens > 1 else heads * dim), (sh if heads > 1 else dim)
+
+
+def _slots(slots, tokens):
+    assert slots.is_cuda and slots.dtype == torch.int64 and slots.shape == (tokens,) and slots.is_contiguous()
+    return slots.data_ptr()
+
+
+def lc_kv_write(cache, k, v, slots, stream=None):
+    """Quantises k and v [tokens][heads][dim] into the cache at `slots` (int64 [tokens]; a negative one is passed over)."""
+    ldt, ldh = _vectors(cache, k, v)
+    st = _lib.lc_kv_write(cache._p, k.data_ptr(), v.data_ptr(), ldt, ldh, _slots(slots, k.shape[0]), k.shape[0], SERVED[k.dtype], _stream(stream))
+    if st != OK:
+        raise LcError(st)
+
+
+def lc_kv_read(cache, slots, dtype=None, out=None, stream=None):
+    """The keys and values [tokens][heads][dim] that the cache holds at `slots` (zeros for a slot outside), of `dtype` or in out = (k, v)."""
+    tokens = slots.shape[0]
+    if out is None:
+        k, v = torch.empty(2, tokens, cache.heads, cache.dim, dtype=dtype if dtype is not None else torch.float32, device=slots.device).unbind(0)
+        if stream is not None:
+            _own(k, stream)
+    else:
+        k, v = out
+        assert k.shape[0] == tokens and (dtype is None or k.dtype == dtype)
+    ldt, ldh = _vectors(cache, k, v)
+    st = _lib.lc_kv_read(cache._p, _slots(slots, tokens), tokens, k.data_ptr(), v.data_ptr(), ldt, ldh, SERVED[k.dtype], _stream(stream))
+    if st != OK:
+        raise LcError(st)
+    return k, v
+
+
+def lc_kv_workspace_bytes(batch, nq, heads, kv_heads, dim):
+    return int(_lib.lc_kv_workspace_bytes(batch, nq, heads, kv_heads, dim))
+
+
+def new_kv_workspace(cache, batch, nq, heads):
+    """Scratch for lc_kv_attend with these sizes; calls that may run at the same time need one each."""
+    return torch.empty(lc_kv_workspace_bytes(batch, nq, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device)
+
+
+def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None, stream=None):
+    """Attention of q [batch][nq][heads][dim] over the cache: table int32 [batch][pages a sequence], lens int32 [batch] (the nq
+    newest tokens are the drafted ones), mask int64 [batch][nq] of the bits that each drafted token sees (None: itself and
+    those before it).  scale: 1 / sqrt(dim) if None.  ws: a tensor from new_kv_workspace (None: allocated for this call)."""
+    batch, nq, heads, dim = q.shape
+    assert q.is_cuda and q.dtype in SERVED and q.is_contiguous() and dim == cache.dim
+    assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == batch and (table.stride(1) == 1 or table.shape[1] <= 1)
+    assert lens.is_cuda and lens.dtype == torch.int32 and lens.shape == (batch,) and lens.is_contiguous()
+    if mask is not None:
+        assert mask.is_cuda and mask.dtype == torch.int64 and mask.shape == (batch, nq) and mask.is_contiguous()
+        mask = mask.data_ptr()
+    if out is None:
+        out = torch.empty_like(q)
+        if stream is not None:
+            _own(out, stream)
+    else:
+        assert out.is_cuda and out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
+    if ws is None:
+        ws = new_kv_workspace(cache, batch, nq, heads)
+        if stream is not None:
+            _own(ws, stream)
+    assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
+    st = _lib.lc_kv_attend(cache._p, q.data_ptr(), batch, nq, heads, table.data_ptr(), table.stride(0) if batch > 1 else table.shape[1], table.shape[1],
+                           lens.data_ptr(), mask, dim ** -0.5 if scale is None else scale, out.data_ptr(), SERVED[q.dtype], ws.data_ptr(), ws.numel(),
+                           _stream(stream))
     if st != OK:
         raise LcError(st)
     return out
