@@ -80,62 +80,80 @@ void dequantize(const lc_w4& q, void* w, uint64_t ldw, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- the product
-// Codes enter the matrix instructions as whole numbers: a nibble c put into the mantissa of 16 makes 16 + c = q + 24 in two
-// operations for two codes, and -24 times the sum of x, which the same instruction works out with a constant for B, takes the 24
-// away again.  All of that is exact but for the sums' own rounding in 32 bits.
+// Codes enter the matrix instructions as whole numbers: a nibble c put into the lowest bits of the mantissa of 2^7 (bf16) or 2^10
+// (fp16) makes 128 + c = q + 136, or 1024 + c = q + 1032, in little more than two operations for two codes, and the same instruction with
+// a constant for B takes 136 (1032) times the sum of x away first.  All of that is exact but for the sums' own rounding in 32 bits, which
+// this makes some 136 / 4 (1032 / 4) times that of the sum of q x: 2e-6 (2e-5) of it, nothing beside the result's rounding to 16 bits.  fp32
+// takes 16 + c = q + 24 and a shift for each two codes more, and three bf16 parts of x that add up to it exactly.
 template <int T> struct Num;
 template <> struct Num<LC_BF16> {
-    static constexpr int kParts = 1;
-    static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u, kMinus24 = 0xC1C0C1C0u;
-    static constexpr int kAt = 3;           // where a nibble lies in the mantissa
+    static constexpr int kParts = 1, kUp = 0;               // how far a nibble is moved up into the mantissa
+    static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x43004300u, kLess = 0xC308C308u;        // 128, -136
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
-template <> struct Num<LC_F32> : Num<LC_BF16> { static constexpr int kParts = 3; };
+template <> struct Num<LC_F32> {
+    static constexpr int kParts = 3, kUp = 3;
+    static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u, kLess = 0xC1C0C1C0u;        // 16, -24
+    static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
+};
 template <> struct Num<LC_F16> {
-    static constexpr int kParts = 1;
-    static constexpr uint32_t kMask = 0x03C003C0u, kBase = 0x4C004C00u, kMinus24 = 0xCE00CE00u;
-    static constexpr int kAt = 6;
+    static constexpr int kParts = 1, kUp = 0;
+    static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x64006400u, kLess = 0xE408E408u;        // 1024, -1032
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16(a, b, c); }
 };
+template <int T> __device__ __forceinline__ f32x4 less_of(u32x4 x, f32x4 c) { return Num<T>::mfma(x, u32x4{Num<T>::kLess, Num<T>::kLess, Num<T>::kLess, Num<T>::kLess}, c); }
 
-// Eight codes as operand: elements 0 4 1 5 2 6 3 7 in this order.
+// Eight codes as operand, in their order.  (The mask is kept in a register that the compiler does not see through: as constants, mask and
+// base would take an instruction each.)
 template <int T> __device__ __forceinline__ u32x4 codes_as_operand(uint32_t w) {
     u32x4 r;
+    const uint32_t odd = w >> 4;
+    uint32_t mask = Num<T>::kMask;
+    asm("" : "+v"(mask));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int up = Num<T>::kAt - 4 * j;
-        r[j] = ((up >= 0 ? w << (up & 31) : w >> (-up & 31)) & Num<T>::kMask) | Num<T>::kBase;
+        const uint32_t pair = __builtin_amdgcn_perm(odd, w, 0x0C000C00u | (uint32_t)j | (uint32_t)(4 + j) << 16);      // byte j of w, byte j of odd
+        r[j] = (pair << Num<T>::kUp & mask) | Num<T>::kBase;
     }
     return r;
 }
 
-// Eight elements of x from place i, the first `valid` of them, as the operand that goes with codes_as_operand (fp32: its three parts).
+// Eight elements of x from place i, the first `valid` of them (the others zero), as they lie in memory.
+template <int T> struct Raw { u32x4 w[T == LC_F32 ? 2 : 1]; };
+template <int T> __device__ __forceinline__ Raw<T> x_as_it_is(const void* x, uint64_t i, int valid) {
+    Raw<T> r;
+    if (valid >= 8) {
+#pragma unroll
+        for (int j = 0; j < (T == LC_F32 ? 2 : 1); ++j) r.w[j] = load_any<u32x4>(static_cast<const uint8_t*>(x) + i * (T == LC_F32 ? 4 : 2) + 16 * j);
+    } else if (T == LC_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w[e / 4][e % 4] = e < valid ? static_cast<const uint32_t*>(x)[i + e] : 0u;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = 2 * j < valid ? static_cast<const uint16_t*>(x)[i + 2 * j] : 0u;
+            const uint32_t hi = 2 * j + 1 < valid ? static_cast<const uint16_t*>(x)[i + 2 * j + 1] : 0u;
+            r.w[0][j] = lo | hi << 16;
+        }
+    }
+    return r;
+}
+// ... and as operand: fp32 as three bf16 parts that add up to it.
 template <int T> struct Operand { u32x4 part[Num<T>::kParts]; };
-template <int T> __device__ __forceinline__ Operand<T> x_as_operand(const void* x, uint64_t i, int valid) {
+template <int T> __device__ __forceinline__ Operand<T> x_as_operand(const Raw<T>& x) {
     Operand<T> r;
     if (T == LC_F32) {
         float v[8];
-        load_eight<T>(x, i, valid, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = float_of(x.w[e / 4][e % 4]);
 #pragma unroll
         for (int p = 0; p < Num<T>::kParts; ++p) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r.part[p][j] = high_halves(bits_of(v[j]), bits_of(v[j + 4]));
+            for (int j = 0; j < 4; ++j) r.part[p][j] = high_halves(bits_of(v[2 * j]), bits_of(v[2 * j + 1]));
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);     // what the part leaves: at most 16, then 8 bits
         }
-    } else {
-        u32x4 a;
-        if (valid >= 8) a = load_any<u32x4>(static_cast<const uint16_t*>(x) + i);
-        else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t lo = 2 * j < valid ? static_cast<const uint16_t*>(x)[i + 2 * j] : 0u;
-                const uint32_t hi = 2 * j + 1 < valid ? static_cast<const uint16_t*>(x)[i + 2 * j + 1] : 0u;
-                a[j] = lo | hi << 16;
-            }
-        }
-        r.part[0] = u32x4{low_halves(a[0], a[2]), high_halves(a[0], a[2]), low_halves(a[1], a[3]), high_halves(a[1], a[3])};
-    }
+    } else r.part[0] = x.w[0];
     return r;
 }
 
@@ -167,66 +185,304 @@ __device__ __forceinline__ void finish(const Product& p, uint32_t i, uint32_t j,
     store_one<T>(p.y, i * p.ldy + j, v);
 }
 
-// Up to 16 rows of x by 16 rows of w a workgroup; its wavefronts take the width in turn, 128 elements (64 bytes of a row of codes)
+// Sixteen bytes of codes a lane, 64 to each of 16 rows, as the words that four matrix instructions take.  A lane holds row l % 16,
+// quarter l / 16 of the 64 bytes.  With groups of 128 its four words go to four instructions as they are (instruction i and quarter h: the
+// eight elements from 32 h + 8 i); with shorter groups they change places between the quarters first, so that every instruction stays
+// inside a group (from 32 i + 8 h): word (a, b) of quarter (h1, h0) is the 8 codes from (h1 h0 a b); a and h1, then b and h0 change places.
+template <int G> __device__ __forceinline__ u32x4 words_in_order(u32x4 w) {
+    if (G == 128) return w;
+    const auto p02 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto p13 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto q01 = __builtin_amdgcn_permlane16_swap(p02[0], p13[0], false, false);
+    const auto q23 = __builtin_amdgcn_permlane16_swap(p02[1], p13[1], false, false);
+    return u32x4{q01[0], q01[1], q23[0], q23[1]};
+}
+template <int G> __device__ __forceinline__ uint32_t place(uint32_t h, uint32_t i) { return G == 128 ? 32 * h + 8 * i : 32 * i + 8 * h; }
+
+// Up to 16 MT rows of x by 16 NT rows of w a workgroup; its wavefronts take the width in turn, 128 elements (64 bytes of a row of codes)
 // at a time, and their sums meet in LDS.  Columns of the matrix instruction are rows of w, so a lane's four results share a scale.
-// Lane l loads 16 bytes of row l % 16, quarter l / 16 of the 64: with groups of 128 its four words go to four instructions as they
-// are; with shorter groups they change places between the quarters first, so that every instruction stays inside a group.
-template <int T, int G, int WAVES>
+// x comes straight from memory into the operands, by every wavefront the part of the width that it works on.
+template <int T, int G, int MT, int NT, int WAVES, int AHEAD>
 __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
+    constexpr int PARTS = Num<T>::kParts, PER = G / 32, GROUPS = 128 / G;
     __shared__ float sums[WAVES][4][64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
-    const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-    const uint32_t row = n0 + c < p.n ? n0 + c : p.n - 1;
-    const uint8_t* codes = p.codes + row * p.codes_pitch;
-    const uint16_t* scales = p.scales + row * p.scales_pitch;
-    const bool has_x = m0 + c < p.m;
-    const uint64_t x_row = (m0 + (has_x ? c : 0)) * p.ldx;
+    const uint32_t n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
     const uint32_t steps = (p.k + 127) / 128;
-    constexpr int PER = G / 32, GROUPS = 128 / G;
-    f32x4 total = {0, 0, 0, 0};
-    for (uint32_t step = wave; step < steps; step += WAVES) {
-        u32x4 w = {0, 0, 0, 0};
-        if (step * 64 + h * 16 < p.row_bytes) w = *reinterpret_cast<const u32x4*>(codes + step * 64 + h * 16);
-        float s[GROUPS];
+    const uint8_t* codes[NT];
+    const uint16_t* scales[NT];
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) s[g] = step * GROUPS + g < p.groups ? of_bf16(scales[step * GROUPS + g]) : 0.0f;
-        if (G < 128) {      // word (a, b) of quarter (h1, h0) holds the 8 codes from (h1 h0 a b): a and h1 change places, then b and h0
-            const auto p02 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-            const auto p13 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-            const auto q01 = __builtin_amdgcn_permlane16_swap(p02[0], p13[0], false, false);
-            const auto q23 = __builtin_amdgcn_permlane16_swap(p02[1], p13[1], false, false);
-            w = u32x4{q01[0], q01[1], q23[0], q23[1]};
-        }
-        f32x4 acc;
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t row = n0 + 16 * n + c < p.n ? n0 + 16 * n + c : p.n - 1;
+        codes[n] = p.codes + row * p.codes_pitch + 16 * h;
+        scales[n] = p.scales + row * p.scales_pitch;
+    }
+    uint64_t x_row[MT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t at = step * 128 + (G == 128 ? 32 * h + 8 * i : 32 * i + 8 * h);
-            const int valid = has_x && at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0;
-            const Operand<T> x = x_as_operand<T>(p.x, x_row + at, valid);
-            const u32x4 b = codes_as_operand<T>(w[i]);
-            if (i % PER == 0) acc = f32x4{0, 0, 0, 0};
+    for (int m = 0; m < MT; ++m) x_row[m] = (m0 + 16 * m + c < p.m ? m0 + 16 * m + c : p.m - 1) * p.ldx;      // (a row beyond the last: any, its results go nowhere)
+    struct Step { u32x4 w[NT]; uint16_t s[NT][GROUPS]; Raw<T> x[MT][4]; };
+    Step ring[AHEAD];
+    auto fetch = [&](Step& f, uint32_t step) {
+        if ((step + 1) * 128 <= p.k) {
 #pragma unroll
-            for (int q = Num<T>::kParts - 1; q >= 0; --q) {
-                acc = Num<T>::mfma(x.part[q], u32x4{Num<T>::kMinus24, Num<T>::kMinus24, Num<T>::kMinus24, Num<T>::kMinus24}, acc);
-                acc = Num<T>::mfma(x.part[q], b, acc);
+            for (int n = 0; n < NT; ++n) {
+                f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
             }
-            if (i % PER == PER - 1) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) total[r] = fmaf(acc[r], s[i / PER], total[r]);
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + step * 128 + place<G>(h, i), 8);
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f.w[n] = u32x4{0, 0, 0, 0};
+            if (step * 64 + h * 16 < p.row_bytes) f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = step * GROUPS + g < p.groups ? scales[n][step * GROUPS + g] : 0;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = step * 128 + place<G>(h, i);
+                f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + at, at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
+            }
+    };
+    f32x4 total[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) total[m][n] = f32x4{0, 0, 0, 0};
+    auto use = [&](const Step& f) {
+        u32x4 w[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w[n] = words_in_order<G>(f.w[n]);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            f32x4 less[MT];
+            Operand<T> x[MT][PER];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                less[m] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    x[m][i] = x_as_operand<T>(f.x[m][g * PER + i]);
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q) less[m] = less_of<T>(x[m][i].part[q], less[m]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4 acc[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[m] = less[m];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const u32x4 b = codes_as_operand<T>(w[n][g * PER + i]);
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) acc[m] = Num<T>::mfma(x[m][i].part[q], b, acc[m]);
+                }
+                const float s = of_bf16(f.s[n][g]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) total[m][n][r] = fmaf(acc[m][r], s, total[m][n][r]);
+            }
+        }
+    };
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+        if (wave + a * WAVES < steps) fetch(ring[a], wave + a * WAVES);
+    for (uint32_t step = wave; step < steps; step += AHEAD * WAVES) {
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {                    // (each step's registers stay its own: moved on, they would have to be waited for)
+            const uint32_t now = step + a * WAVES;
+            if (now < steps) {
+                use(ring[a]);
+                if (now + AHEAD * WAVES < steps) fetch(ring[a], now + AHEAD * WAVES);
             }
         }
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sums[wave][r][lane] = total[r];
+    for (int t = 0; t < MT * NT; ++t) {
+        if (t) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][r][lane] = total[t / NT][t % NT][r];
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < 256; e += WAVES * 64) {
+            const uint32_t i = m0 + 16 * (t / NT) + 4 * (e / 64) + e % 64 / 16, j = n0 + 16 * (t % NT) + e % 16;      // neighbours write neighbours
+            const uint32_t from = (e / 64) * 16 + e % 16, r = e % 64 / 16;
+            if (i >= p.m || j >= p.n) continue;
+            float v = 0;
+#pragma unroll
+            for (int q = 0; q < WAVES; ++q) v += sums[q][r][from];
+            finish<T, G>(p, i, j, v);
+        }
+    }
+}
+
+// More rows: a tile of 16 MT WM rows of x by 16 NT WN rows of w a workgroup of WM x WN x WK wavefronts, WK of them on different parts of the
+// width.  x passes through LDS, 128 WK elements of the width at a time, twice buffered: the next piece is under way in registers while this
+// one is worked on.  Codes come straight into registers and are unpacked by the wavefront that needs them.
+template <int T, int MT, int NT, int WM, int WN, int WK> struct Tile {
+    static constexpr int kThreads = 64 * WM * WN * WK, kRows = 16 * MT * WM, kCols = 16 * NT * WN, kParts = Num<T>::kParts;
+    static constexpr uint32_t kPitch = WK * 256 + 16, kPart = kRows * kPitch, kBuffer = kParts * kPart;     // 16 bytes beside a multiple of 256: sixteen rows in sixteen bank groups
+    static constexpr uint32_t kSums = WK * kRows * (kCols + 4) * 4;
+    static constexpr uint32_t kLds = 2 * kBuffer > kSums ? 2 * kBuffer : kSums;
+    static constexpr int kItems = kRows * WK * 16 / kThreads;            // eights of x a thread brings in at a time
+    static_assert(kRows * WK * 16 % kThreads == 0, "whole items");
+};
+template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD, bool WHOLE>
+__global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product p) {
+    using L = Tile<T, MT, NT, WM, WN, WK>;
+    constexpr int PARTS = L::kParts, PER = G / 32, GROUPS = 128 / G;
+    extern __shared__ __align__(16) uint8_t held[];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
+    const uint32_t wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
+    const uint32_t n0 = blockIdx.x * L::kCols, m0 = blockIdx.y * L::kRows;
+    const uint32_t steps = (p.k + 127) / 128, rounds = (steps + WK - 1) / WK;
+    const uint8_t* codes[NT];
+    const uint16_t* scales[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t j = n0 + 16 * (wn * NT + n) + c, row = j < p.n ? j : p.n - 1;
+        codes[n] = p.codes + row * p.codes_pitch + 16 * h;
+        scales[n] = p.scales + row * p.scales_pitch;
+    }
+    struct Step { u32x4 w[NT]; uint16_t s[NT][GROUPS]; };
+    auto fetch = [&](Step& f, uint32_t step) {
+        if (WHOLE || (step + 1) * 128 <= p.k) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
+            }
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f.w[n] = u32x4{0, 0, 0, 0};
+            if (step < steps && step * 64 + h * 16 < p.row_bytes) f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = step * GROUPS + g < p.groups ? scales[n][step * GROUPS + g] : 0;
+        }
+    };
+    struct Piece { Raw<T> x[L::kItems]; };
+    const uint8_t* x_from[L::kItems];
+#pragma unroll
+    for (int i = 0; i < L::kItems; ++i) {
+        const uint32_t item = threadIdx.x + i * L::kThreads, r = item / (WK * 16);
+        x_from[i] = static_cast<const uint8_t*>(p.x) + ((m0 + r < p.m ? m0 + r : p.m - 1) * p.ldx + 8 * (item % (WK * 16))) * (T == LC_F32 ? 4 : 2);      // (a row beyond the last: any, its results go nowhere)
+    }
+    auto bring = [&](Piece& next, uint32_t round) {
+        const uint32_t from = round * WK * 128;
+        const bool whole = WHOLE || from + WK * 128 <= p.k;
+#pragma unroll
+        for (int i = 0; i < L::kItems; ++i) {
+            const uint32_t at = from + 8 * ((threadIdx.x + i * L::kThreads) % (WK * 16));
+            next.x[i] = x_as_it_is<T>(x_from[i], from, whole ? 8 : at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
+        }
+    };
+    auto keep = [&](const Piece& next, uint32_t buffer) {
+#pragma unroll
+        for (int i = 0; i < L::kItems; ++i) {
+            const uint32_t item = threadIdx.x + i * L::kThreads, r = item / (WK * 16), at = item % (WK * 16);
+            const Operand<T> x = x_as_operand<T>(next.x[i]);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4*>(held + buffer * L::kBuffer + q * L::kPart + r * L::kPitch + at * 16) = x.part[q];
+        }
+    };
+    f32x4 total[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) total[m][n] = f32x4{0, 0, 0, 0};
+    auto use = [&](const Step& f, const uint8_t* x_at) {
+        u32x4 w[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w[n] = words_in_order<G>(f.w[n]);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            f32x4 less[MT];
+            u32x4 x[MT][PER][PARTS];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                less[m] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q) {
+                        x[m][i][q] = *reinterpret_cast<const u32x4*>(x_at + 16 * m * L::kPitch + q * L::kPart + 2 * place<G>(h, g * PER + i));
+                        less[m] = less_of<T>(x[m][i][q], less[m]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4 acc[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[m] = less[m];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const u32x4 b = codes_as_operand<T>(w[n][g * PER + i]);
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) acc[m] = Num<T>::mfma(x[m][i][q], b, acc[m]);
+                }
+                const float s = of_bf16(f.s[n][g]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) total[m][n][r] = fmaf(acc[m][r], s, total[m][n][r]);
+            }
+        }
+    };
+    // Round r works on buffer r % 2 and on the codes that were asked for two rounds before; x of round r + 1 is put into the other buffer
+    // behind it.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on.
+    Piece next[DEEP];
+    Step codes_of[2];
+    bring(next[0], 0);
+    fetch(codes_of[0], wk);
+    keep(next[0], 0);
+    if (1 < rounds) { fetch(codes_of[1], WK + wk); bring(next[DEEP - 1], 1); }
+    if (DEEP == 2 && 2 < rounds) bring(next[0], 2);
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < 256; e += WAVES * 64) {
-        const uint32_t i = m0 + 4 * (e / 64) + e % 64 / 16, j = n0 + e % 16;      // neighbours write neighbours
-        const uint32_t from = (e / 64) * 16 + e % 16, r = e % 64 / 16;
-        if (i >= p.m || j >= p.n) continue;
+    const uint8_t* x_at = held + (16 * MT * wm + c) * L::kPitch + wk * 256;
+    for (uint32_t first = 0; first < rounds; first += 2) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const uint32_t round = first + b;
+            if (round >= rounds) break;
+            Piece& after = next[DEEP == 2 ? 1 - b : 0];
+            if (WHOLE || round * WK + wk < steps) use(codes_of[b], x_at + b * L::kBuffer);
+            if (round + 2 < rounds) fetch(codes_of[b], (round + 2) * WK + wk);
+            if (round + 1 < rounds) keep(after, 1 - b);
+            if (round + 1 + DEEP < rounds) bring(after, round + 1 + DEEP);
+            __syncthreads();
+        }
+    }
+    float* sums = reinterpret_cast<float*>(held);
+    constexpr uint32_t kSumPitch = L::kCols + 4;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[(wk * L::kRows + 16 * (wm * MT + m) + 4 * h + r) * kSumPitch + 16 * (wn * NT + n) + c] = total[m][n][r];
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < L::kRows * L::kCols; e += L::kThreads) {
+        const uint32_t r = e / L::kCols, j = e % L::kCols;
+        if (m0 + r >= p.m || n0 + j >= p.n) continue;
         float v = 0;
 #pragma unroll
-        for (int q = 0; q < WAVES; ++q) v += sums[q][r][from];
-        finish<T, G>(p, i, j, v);
+        for (int q = 0; q < WK; ++q) v += sums[(q * L::kRows + r) * kSumPitch + j];
+        finish<T, G>(p, m0 + r, n0 + j, v);
     }
 }
 
@@ -238,13 +494,33 @@ __global__ __launch_bounds__(256) void k_w4_bias_only(Product p) {      // k = 0
     store_one<T>(p.y, i * p.ldy + j, p.bias ? load_one<T>(p.bias, j) : 0.0f);
 }
 
+template <int T, int G, int MT, int NT, int WAVES, int AHEAD>
+void product_of_rows(const Product& p, hipStream_t s) {
+    k_w4_rows<T, G, MT, NT, WAVES, AHEAD><<<dim3((p.n + 16 * NT - 1) / (16 * NT), (p.m + 16 * MT - 1) / (16 * MT)), WAVES * 64, 0, s>>>(p);
+}
+
+template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD>
+void product_of_tiles(const Product& p, hipStream_t s) {
+    using L = Tile<T, MT, NT, WM, WN, WK>;
+    static_assert(L::kLds <= 160 * 1024, "LDS of a compute unit");
+    const dim3 grid((p.n + L::kCols - 1) / L::kCols, (p.m + L::kRows - 1) / L::kRows);
+    if (p.k % (128 * WK) == 0) k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD, true><<<grid, L::kThreads, L::kLds, s>>>(p);
+    else k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD, false><<<grid, L::kThreads, L::kLds, s>>>(p);
+}
+
 template <int T, int G>
 void product(const Product& p, hipStream_t s) {
     const uint32_t steps = (p.k + 127) / 128;
-    const dim3 grid((p.n + 15) / 16, (p.m + 15) / 16);
-    if (steps <= 1) k_w4_rows<T, G, 1><<<grid, 64, 0, s>>>(p);
-    else if (steps <= 4) k_w4_rows<T, G, 4><<<grid, 256, 0, s>>>(p);
-    else k_w4_rows<T, G, 8><<<grid, 512, 0, s>>>(p);
+    if (p.m > 16) {
+        if constexpr (T == LC_F32) product_of_tiles<T, G, 2, 2, 2, 2, 1, 1, 1>(p, s);
+        else {
+            if (p.m <= 64) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
+            else product_of_tiles<T, G, 4, 2, 1, 4, 1, 1, 2>(p, s);
+        }
+        return;
+    }
+    if (steps <= 4) product_of_rows<T, G, 1, 1, 4, 1>(p, s);
+    else product_of_rows<T, G, 1, 1, 8, 1>(p, s);
 }
 
 // Whether a matrix in 4 bits is one the kernels can take.
