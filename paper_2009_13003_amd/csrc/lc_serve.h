@@ -112,6 +112,17 @@ template <int LANES> __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v
     return v;
 }
 
+// The sum over 4, 8 or 16 neighbouring lanes in every one of them.
+template <int LANES> __device__ __forceinline__ float sum_of_lanes(float v) {
+#define LC_DPP_SUM(ctrl) v += float_of((uint32_t)__builtin_amdgcn_update_dpp(0, (int)bits_of(v), ctrl, 0xf, 0xf, false))
+    LC_DPP_SUM(0xB1);
+    LC_DPP_SUM(0x4E);
+    if (LANES >= 8) LC_DPP_SUM(0x141);
+    if (LANES >= 16) LC_DPP_SUM(0x140);
+#undef LC_DPP_SUM
+    return v;
+}
+
 // rint(t) + bias for |t| <= 127 in the low bits: added to 1.5 * 2^23 the sum has no room for a fraction, and its rounding is the
 // one to nearest even.
 __device__ __forceinline__ uint32_t rounded(float t, float bias) { return bits_of(t + (12582912.0f + bias)); }
@@ -125,6 +136,18 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
     f16x8 x, y; __builtin_memcpy(&x, &a, 16); __builtin_memcpy(&y, &b, 16);
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+}
+
+// c plus the two products of a pair, in 32 bits.
+template <bool HALF> __device__ __forceinline__ float dot_16(uint32_t a, uint32_t b, float c) {
+    if (HALF) {
+        typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+        f16x2 x, y; __builtin_memcpy(&x, &a, 4); __builtin_memcpy(&y, &b, 4);
+        return __builtin_amdgcn_fdot2(x, y, c, false);
+    }
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    bf16x2 x, y; __builtin_memcpy(&x, &a, 4); __builtin_memcpy(&y, &b, 4);
+    return __builtin_amdgcn_fdot2_f32_bf16(x, y, c, false);
 }
 
 // The low (0x05040100) or high (0x07060302) halves of a and b, a's below b's.

@@ -82,21 +82,24 @@ void dequantize(const lc_w4& q, void* w, uint64_t ldw, hipStream_t s) {
 // ---------------------------------------------------------------- the product
 // Codes enter the matrix instructions as whole numbers: a nibble c put into the lowest bits of the mantissa of 2^7 (bf16) or 2^10
 // (fp16) makes 128 + c = q + 136, or 1024 + c = q + 1032, in little more than two operations for two codes, and the same instruction with
-// a constant for B takes 136 (1032) times the sum of x away first.  All of that is exact but for the sums' own rounding in 32 bits, which
+// a constant for B takes 136 (1032) times the sum of x away first (or those who bring x into LDS add it up).  All of that is exact but for the sums' own rounding in 32 bits, which
 // this makes some 136 / 4 (1032 / 4) times that of the sum of q x: 2e-6 (2e-5) of it, nothing beside the result's rounding to 16 bits.  fp32
 // takes 16 + c = q + 24 and a shift for each two codes more, and three bf16 parts of x that add up to it exactly.
 template <int T> struct Num;
 template <> struct Num<LC_BF16> {
+    static constexpr float kTaken = -136.0f;
     static constexpr int kParts = 1, kUp = 0;               // how far a nibble is moved up into the mantissa
     static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x43004300u, kLess = 0xC308C308u;        // 128, -136
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F32> {
+    static constexpr float kTaken = -24.0f;
     static constexpr int kParts = 3, kUp = 3;
     static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u, kLess = 0xC1C0C1C0u;        // 16, -24
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F16> {
+    static constexpr float kTaken = -1032.0f;
     static constexpr int kParts = 1, kUp = 0;
     static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x64006400u, kLess = 0xE408E408u;        // 1024, -1032
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16(a, b, c); }
@@ -155,6 +158,19 @@ template <int T> __device__ __forceinline__ Operand<T> x_as_operand(const Raw<T>
         }
     } else r.part[0] = x.w[0];
     return r;
+}
+
+// The sum of an operand's eight elements (fp32: of the elements themselves), in 32 bits.
+template <int T> __device__ __forceinline__ float sum_of(const Raw<T>& x) {
+    float s = 0;
+    if (T == LC_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += float_of(x.w[e / 4][e % 4]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = dot_16<T == LC_F16>(x.w[0][j], T == LC_F16 ? 0x3C003C00u : 0x3F803F80u, s);
+    }
+    return s;
 }
 
 struct Product {
@@ -331,7 +347,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
 // one is worked on.  Codes come straight into registers and are unpacked by the wavefront that needs them.
 template <int T, int MT, int NT, int WM, int WN, int WK> struct Tile {
     static constexpr int kThreads = 64 * WM * WN * WK, kRows = 16 * MT * WM, kCols = 16 * NT * WN, kParts = Num<T>::kParts;
-    static constexpr uint32_t kPitch = WK * 256 + 16, kPart = kRows * kPitch, kBuffer = kParts * kPart;     // 16 bytes beside a multiple of 256: sixteen rows in sixteen bank groups
+    static constexpr uint32_t kPitch = WK * 256 + 16, kPart = kRows * kPitch;       // 16 bytes beside a multiple of 256: sixteen rows in sixteen bank groups
+    // What is taken away: where several wavefronts work on the same rows of x, added up once by those who bring x in; else by each for itself, by
+    // the matrix instruction.  (2048 rows by 4096x11008 in tiles of 64 x 128: 233 us instead of 250; 32 rows in tiles of 32 x 16: 24.4 instead of 20.3.)
+    static constexpr bool kAdded = WN > 1;
+    static constexpr uint32_t kLess = kParts * kPart, kBuffer = kLess + WK * 4 * kRows * 4;      // behind x what is taken away for each of (at most four) groups and rows
     static constexpr uint32_t kSums = WK * kRows * (kCols + 4) * 4;
     static constexpr uint32_t kLds = 2 * kBuffer > kSums ? 2 * kBuffer : kSums;
     static constexpr int kItems = kRows * WK * 16 / kThreads;            // eights of x a thread brings in at a time
@@ -396,6 +416,9 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
             const Operand<T> x = x_as_operand<T>(next.x[i]);
 #pragma unroll
             for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4*>(held + buffer * L::kBuffer + q * L::kPart + r * L::kPitch + at * 16) = x.part[q];
+            if (!L::kAdded) continue;
+            const float taken = Num<T>::kTaken * sum_of_lanes<G / 8>(sum_of<T>(next.x[i]));
+            *reinterpret_cast<float*>(held + buffer * L::kBuffer + L::kLess + (at / (G / 8) * L::kRows + r) * 4) = taken;     // (a group's lanes all write it: no branch)
         }
     };
     f32x4 total[MT][NT];
@@ -403,7 +426,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) total[m][n] = f32x4{0, 0, 0, 0};
-    auto use = [&](const Step& f, const uint8_t* x_at) {
+    auto use = [&](const Step& f, const uint8_t* x_at, const uint8_t* less_at) {
         u32x4 w[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) w[n] = words_in_order<G>(f.w[n]);
@@ -413,13 +436,13 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
             u32x4 x[MT][PER][PARTS];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                less[m] = f32x4{0, 0, 0, 0};
+                less[m] = L::kAdded ? *reinterpret_cast<const f32x4*>(less_at + (g * L::kRows + 16 * m) * 4) : f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
 #pragma unroll
                     for (int q = PARTS - 1; q >= 0; --q) {
                         x[m][i][q] = *reinterpret_cast<const u32x4*>(x_at + 16 * m * L::kPitch + q * L::kPart + 2 * place<G>(h, g * PER + i));
-                        less[m] = less_of<T>(x[m][i][q], less[m]);
+                        if (!L::kAdded) less[m] = less_of<T>(x[m][i][q], less[m]);
                     }
             }
 #pragma unroll
@@ -444,29 +467,34 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
         }
     };
     // Round r works on buffer r % 2 and on the codes that were asked for two rounds before; x of round r + 1 is put into the other buffer
-    // behind it.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on.
+    // behind it.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on, and the
+    // last rounds ask for the last piece again instead of asking whether there is one: a branch there costs more than the loads.
+    const uint32_t last = rounds - 1;
     Piece next[DEEP];
     Step codes_of[2];
     bring(next[0], 0);
     fetch(codes_of[0], wk);
     keep(next[0], 0);
-    if (1 < rounds) { fetch(codes_of[1], WK + wk); bring(next[DEEP - 1], 1); }
-    if (DEEP == 2 && 2 < rounds) bring(next[0], 2);
+    fetch(codes_of[1], (last < 1 ? last : 1) * WK + wk);
+    bring(next[DEEP - 1], last < 1 ? last : 1);
+    if (DEEP == 2) bring(next[0], last < 2 ? last : 2);
     __syncthreads();
     const uint8_t* x_at = held + (16 * MT * wm + c) * L::kPitch + wk * 256;
-    for (uint32_t first = 0; first < rounds; first += 2) {
+    const uint8_t* less_at = held + L::kLess + (wk * GROUPS * L::kRows + 16 * MT * wm + 4 * h) * 4;
+    uint32_t round = 0;
+    for (; round < last; round += 2) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const uint32_t round = first + b;
-            if (round >= rounds) break;
             Piece& after = next[DEEP == 2 ? 1 - b : 0];
-            if (WHOLE || round * WK + wk < steps) use(codes_of[b], x_at + b * L::kBuffer);
-            if (round + 2 < rounds) fetch(codes_of[b], (round + 2) * WK + wk);
-            if (round + 1 < rounds) keep(after, 1 - b);
-            if (round + 1 + DEEP < rounds) bring(after, round + 1 + DEEP);
+            use(codes_of[b], x_at + b * L::kBuffer, less_at + b * L::kBuffer);
+            fetch(codes_of[b], (round + b + 2 < last ? round + b + 2 : last) * WK + wk);
+            keep(after, 1 - b);
+            bring(after, round + b + 1 + DEEP < last ? round + b + 1 + DEEP : last);
             __syncthreads();
         }
     }
+    if (round == last) use(codes_of[0], x_at, less_at);
+    __syncthreads();
     float* sums = reinterpret_cast<float*>(held);
     constexpr uint32_t kSumPitch = L::kCols + 4;
 #pragma unroll
@@ -505,16 +533,21 @@ void product_of_tiles(const Product& p, hipStream_t s) {
     static_assert(L::kLds <= 160 * 1024, "LDS of a compute unit");
     const dim3 grid((p.n + L::kCols - 1) / L::kCols, (p.m + L::kRows - 1) / L::kRows);
     if (p.k % (128 * WK) == 0) k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD, true><<<grid, L::kThreads, L::kLds, s>>>(p);
-    else k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD, false><<<grid, L::kThreads, L::kLds, s>>>(p);
+    else k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, 1, false><<<grid, L::kThreads, L::kLds, s>>>(p);
 }
 
 template <int T, int G>
 void product(const Product& p, hipStream_t s) {
     const uint32_t steps = (p.k + 127) / 128;
     if (p.m > 16) {
+        // Tiles as large as still give every compute unit two workgroups (2048 rows by 4096x11008, us: 64 x 128 233, 64 x 64 338; 256 by
+        // 4096x4096: 37 and 30); few rows split the width over the wavefronts instead (32 rows by 4096x11008: 20).
         if constexpr (T == LC_F32) product_of_tiles<T, G, 2, 2, 2, 2, 1, 1, 1>(p, s);
         else {
-            if (p.m <= 64) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
+            const uint64_t blocks = (uint64_t)((p.m + 63) / 64) * ((p.n + 127) / 128);
+            if (p.m <= 32) product_of_tiles<T, G, 2, 1, 1, 1, 8, 1, 1>(p, s);
+            else if (p.m <= 64) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
+            else if (blocks < 512) product_of_tiles<T, G, 2, 2, 2, 2, 1, 1, 2>(p, s);
             else product_of_tiles<T, G, 4, 2, 1, 4, 1, 1, 2>(p, s);
         }
         return;
