@@ -94,7 +94,7 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
  *           reads the cache's head h / (heads / cache->heads)
  *   table   int32 [batch][ld_table]: the pages of a sequence, in order; lens int32 [batch]: its cached tokens, of which
  *           the newest nq are the drafted ones (fewer than nq: the drafted tokens that would lie before the first do not exist).
- *           A length is held to what the table has room for (table_pages pages); a page outside the cache counts as not seen.
+ *           A length is held to what the table has room for (table_pages pages, at most 2^30 tokens); a page outside the cache counts as not seen.
  *   mask    NULL, or uint64 [batch][nq]: drafted token i sees drafted token j iff bit j of mask[i] is set (a tree's ancestors and
  *           itself).  NULL: j <= i.  Everything before the drafted tokens is seen by all of them.  nq is at most 64; nq = 1 is
  *           the step of one token.

@@ -147,202 +147,284 @@ template <int BITS> __device__ __forceinline__ u32x4 values_at(const uint32_t (&
 __device__ __forceinline__ float max_over_quarters(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float sum_over_quarters(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
-template <int T, int BITS, int DP>
+// A tile of 32 tokens as it lies in the cache.
+template <int BITS, int DP> struct InCache {
+    static constexpr int kKey = DP * BITS / 32 < 16 ? DP * BITS / 32 : 16;      // bytes of a key a lane loads at once
+    static constexpr int kKeyLoads = DP * BITS / 32 / kKey, kKeyWords = kKey / 4;
+    static constexpr int kDims = DP / 16;                                       // elements of a value a lane holds
+    static constexpr int kValue = kDims * BITS / 8, kValueWords = (kValue + 3) / 4, kPerWord = 32 / BITS < kDims ? 32 / BITS : kDims;
+    uint32_t key[2][kKeyLoads][kKeyWords];      // of token 16 s + l % 16
+    uint32_t value[8][kValueWords];             // of tokens 16 s + 4 (l / 16) + r, at 4 s + r
+    f32x4 key_scale[2], value_scale[2];
+};
+
+// Sequences lie in pages of a power of two of tokens, at least 8, so eight tokens that begin at a multiple of eight lie together: where
+// each eight of a tile lie is the same for all lanes.
+struct Eights { uint64_t row[4]; uint32_t there; };
+
+template <int T, int BITS, int DP, int NT>
 __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
+    using Raw = InCache<BITS, DP>;
     constexpr bool HALF = Kind<T>::kHalf;
     constexpr int NQ = Kind<T>::kQ, NP = Kind<T>::kP;
     // Keys in 4 bits for 16-bit queries: 16 + c, a nibble put into the mantissa of 16 (two operations for two codes), and 24 times the
     // query's sum taken away, which moves scores by some 2^-24 of 24 sum |q|; for fp32 exact codes instead.
     constexpr bool LIFTED = BITS == 4 && T != LC_F32;
-    constexpr int KOPS = DP / 32;                           // operands of a token's key
-    constexpr int LANE_K = DP * BITS / 8 / 4 < 16 ? DP * BITS / 8 / 4 : 16;     // bytes of a key a lane loads at once
-    constexpr int LOADS_K = DP * BITS / 8 / 4 / LANE_K, WORDS_K = LANE_K / 4;
-    constexpr int VD = DP / 16;                             // elements of a value a lane holds
-    constexpr int LANE_V = VD * BITS / 8, WORDS_V = (LANE_V + 3) / 4, PER_WORD = 32 / BITS < VD ? 32 / BITS : VD;
+    constexpr int KOPS = DP / 32, VD = Raw::kDims;
     __shared__ float so[kWaves][16][DP + 4];
     __shared__ float sm[kWaves][16], sl[kWaves][16];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
-    const uint32_t split = blockIdx.x, row_groups = (a.rows + 15) / 16;
-    const uint32_t head = blockIdx.y / row_groups, row0 = (blockIdx.y - head * row_groups) * 16, b = blockIdx.z;
-    const uint32_t row = row0 + c;                          // this lane's query
-    const bool has_row = row < a.rows;
-    const uint32_t qi = (has_row ? row : 0) / a.group, qg = (has_row ? row : 0) - qi * a.group;
-    const uint64_t q_at = (((uint64_t)b * a.nq + qi) * a.heads + head * a.group + qg) * a.c.dim;
-    const int64_t room = (int64_t)(a.table_pages << a.c.page_shift);
-    const int64_t len = a.lens[b] < 0 ? 0 : a.lens[b] < room ? a.lens[b] : room;
-    const int64_t base = len - (int64_t)a.nq;               // the first drafted token
-    const uint64_t mask = a.mask ? a.mask[(uint64_t)b * a.nq + qi] : qi >= 63 ? ~0ull : (2ull << qi) - 1;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 16, h = lane / 16;
+    const uint32_t split = blockIdx.x, row_groups = (a.rows + 16 * NT - 1) / (16 * NT);
+    const uint32_t head = blockIdx.y / row_groups, row0 = (blockIdx.y - head * row_groups) * 16 * NT, b = blockIdx.z;
+    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    const int32_t given = __builtin_amdgcn_readfirstlane(a.lens[b]);
+    const int32_t len = given < 0 ? 0 : given < room ? given : room;
+    const int32_t base = len - (int32_t)a.nq;               // the first drafted token
     const int32_t* table = a.table + b * a.ld_table;
+    const int32_t first = (int32_t)(split * a.tiles * kTile);
+    const int32_t end = first + (int32_t)a.tiles * kTile < len ? first + (int32_t)a.tiles * kTile : len;
+    const int32_t own = first + (int32_t)wave * kTile;      // this wavefront's first tile; every kWaves-th is its own
+    const int32_t tiles = own < end ? (end - own + kWaves * kTile - 1) / (kWaves * kTile) : 0;
 
-    // the queries, eight elements an operand at the places at which the keys' codes lie
-    u32x4 q[KOPS][NQ];
-    f32x4 less = {0, 0, 0, 0};                              // -24 times each query's sum
+    // this lane's queries, eight elements an operand at the places at which the keys' codes lie
+    u32x4 q[NT][KOPS][NQ];
+    f32x4 less[NT];                                         // -24 times each query's sum
+    uint64_t mask[NT];
 #pragma unroll
-    for (int o = 0; o < KOPS; ++o) {
-        uint32_t d;
-        if (BITS == 8) d = 16 * h * (LANE_K / 16) + 64 * (o / 2) + 8 * (o % 2);
-        else d = 2 * LANE_K * h + 8 * LANE_K * (o / WORDS_K) + 8 * (o % WORDS_K);
-        float v[8];
-        load_eight<T>(a.q, q_at + d, has_row && d < a.c.dim ? 8 : 0, v);
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t row = row0 + 16 * n + c;
+        const bool has_row = row < a.rows;
+        const uint32_t qi = (has_row ? row : 0) / a.group, qg = (has_row ? row : 0) - qi * a.group;
+        const uint64_t q_at = (((uint64_t)b * a.nq + qi) * a.heads + head * a.group + qg) * a.c.dim;
+        mask[n] = a.mask ? a.mask[(uint64_t)b * a.nq + qi] : qi >= 63 ? ~0ull : (2ull << qi) - 1;
+        less[n] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int p = 0; p < NQ; ++p) {
+        for (int o = 0; o < KOPS; ++o) {
+            uint32_t d;
+            if (BITS == 8) d = 16 * h + 64 * (o / 2) + 8 * (o % 2);
+            else d = 2 * Raw::kKey * h + 8 * Raw::kKey * (o / Raw::kKeyWords) + 8 * (o % Raw::kKeyWords);
+            float v[8];
+            load_eight<T>(a.q, q_at + d, has_row && d < a.c.dim ? 8 : 0, v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = BITS == 8 ? v[2 * j] : v[j], y = BITS == 8 ? v[2 * j + 1] : v[j + 4];
-                q[o][p][j] = HALF ? f16_of(x) | f16_of(y) << 16 : high_halves(bits_of(x), bits_of(y));
+            for (int p = 0; p < NQ; ++p) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = BITS == 8 ? v[2 * j] : v[j], y = BITS == 8 ? v[2 * j + 1] : v[j + 4];
+                    q[n][o][p][j] = HALF ? f16_of(x) | f16_of(y) << 16 : high_halves(bits_of(x), bits_of(y));
+                }
+                if (NQ > 1)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);
             }
-            if (NQ > 1)
+            if (LIFTED) {
+                const uint32_t m24 = HALF ? 0xCE00CE00u : 0xC1C0C1C0u;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);
-        }
-        if (LIFTED) {
-            const uint32_t m24 = HALF ? 0xCE00CE00u : 0xC1C0C1C0u;
-#pragma unroll
-            for (int p = NQ - 1; p >= 0; --p) less = mfma_16<HALF>(u32x4{m24, m24, m24, m24}, q[o][p], less);
+                for (int p = NQ - 1; p >= 0; --p) less[n] = mfma_16<HALF>(u32x4{m24, m24, m24, m24}, q[n][o][p], less[n]);
+            }
         }
     }
 
-    f32x4 acc[VD];
+    auto find = [&](int32_t i) {                            // where this wavefront's tile i lies (beyond the last: the last again)
+        Eights e;
+        e.there = 0;
+        const int32_t tb = own + (i < tiles ? i : tiles - 1) * kWaves * kTile;
 #pragma unroll
-    for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
-    float top = -__builtin_inff(), sum = 0;
-    const int64_t first = (int64_t)split * a.tiles * kTile;
-    const int64_t end = first + (int64_t)a.tiles * kTile < len ? first + (int64_t)a.tiles * kTile : len;
-    for (int64_t tb = first + wave * kTile; tb < end; tb += kWaves * kTile) {
-        // keys: token 16 s + c of the tile
-        u32x4 key[2][KOPS];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int64_t t = tb + 16 * s + c < len ? tb + 16 * s + c : len - 1;
-            int32_t page = table[t >> a.c.page_shift];
-            page = (uint32_t)page < (uint32_t)a.pages ? page : 0;
-            const uint8_t* from = a.c.k + row_of(a.c, page, head, (uint32_t)t & ((1u << a.c.page_shift) - 1)) * a.c.row_bytes + h * LANE_K;
-#pragma unroll
-            for (int l = 0; l < LOADS_K; ++l) {
-                uint32_t w[WORDS_K];
-                const bool in = l * 4 * LANE_K + h * LANE_K < a.c.row_bytes;
-#pragma unroll
-                for (int i = 0; i < WORDS_K; ++i) w[i] = 0;
-                if (in) __builtin_memcpy(w, __builtin_assume_aligned(from + l * 4 * LANE_K, LANE_K), LANE_K);
-                if (BITS == 8) {
-#pragma unroll
-                    for (int i = 0; i < WORDS_K; ++i) {
-                        key[s][l * WORDS_K / 2 + i / 2][2 * (i % 2)] = pair_of<HALF>(byte_of<0>(w[i]), byte_of<1>(w[i]));
-                        key[s][l * WORDS_K / 2 + i / 2][2 * (i % 2) + 1] = pair_of<HALF>(byte_of<2>(w[i]), byte_of<3>(w[i]));
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < WORDS_K; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (!LIFTED) { key[s][l * WORDS_K + i][j] = high_halves(bits_of(nibble_of(turned(w[i]), j)), bits_of(nibble_of(turned(w[i]), j + 4))); continue; }
-                            const int up = (HALF ? 6 : 3) - 4 * j;
-                            const uint32_t m = up >= 0 ? w[i] << (up & 31) : w[i] >> (-up & 31);
-                            key[s][l * WORDS_K + i][j] = HALF ? (m & 0x03C003C0u) | 0x4C004C00u : (m & 0x00780078u) | 0x41804180u;
-                        }
-                }
-            }
-        }
-        // values and scales: tokens 16 s + 4 h + 0..3
-        uint32_t val[WORDS_V][8];
-        float ks[8], vs[8];
-        uint32_t seen = 0;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int64_t t0 = tb + 16 * s + 4 * h;
-            const int64_t tc = t0 < len ? t0 : (len - 1) & ~(int64_t)3;
-            int32_t page = table[tc >> a.c.page_shift];
+        for (int g = 0; g < 4; ++g) {
+            const int32_t t = tb + 8 * g < len ? tb + 8 * g : (len - 1) & ~7;
+            const int32_t page = __builtin_amdgcn_readfirstlane(table[t >> a.c.page_shift]);
             const bool there = (uint32_t)page < (uint32_t)a.pages;
-            page = there ? page : 0;
-            const uint64_t at = row_of(a.c, page, head, (uint32_t)tc & ((1u << a.c.page_shift) - 1));
-            const f32x4 k4 = *reinterpret_cast<const f32x4*>(a.c.k_scale + at), v4 = *reinterpret_cast<const f32x4*>(a.c.v_scale + at);
+            e.row[g] = row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
+            e.there |= there ? 1u << g : 0;
+        }
+        return e;
+    };
+    const uint32_t key_off = (c % 8) * a.c.row_bytes + h * Raw::kKey, value_off = (4 * h % 8) * a.c.row_bytes + c * Raw::kValue;
+    auto load = [&](Raw& f, const Eights& e) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint64_t key_row = c < 8 ? e.row[2 * s] : e.row[2 * s + 1], value_row = h < 2 ? e.row[2 * s] : e.row[2 * s + 1];
+            const uint8_t* from = a.c.k + key_row * a.c.row_bytes + key_off;
+#pragma unroll
+            for (int l = 0; l < Raw::kKeyLoads; ++l) {
+#pragma unroll
+                for (int i = 0; i < Raw::kKeyWords; ++i) f.key[s][l][i] = 0;
+                if (l * 4 * Raw::kKey + h * Raw::kKey < a.c.row_bytes)
+                    __builtin_memcpy(f.key[s][l], __builtin_assume_aligned(from + l * 4 * Raw::kKey, Raw::kKey), Raw::kKey);
+            }
+            f.key_scale[s] = *reinterpret_cast<const f32x4*>(a.c.k_scale + value_row + 4 * h % 8);
+            f.value_scale[s] = *reinterpret_cast<const f32x4*>(a.c.v_scale + value_row + 4 * h % 8);
+            const uint8_t* values = a.c.v + value_row * a.c.row_bytes + value_off;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                ks[4 * s + r] = k4[r] * (BITS == 4 && !LIFTED ? 16.0f * a.scale : a.scale);
-                vs[4 * s + r] = v4[r];
-                const int64_t t = t0 + r, j = t - base;
-                if (there && t < end && (j < 0 || (mask >> (j & 63) & 1))) seen |= 1u << (4 * s + r);
-                uint32_t w[WORDS_V];
 #pragma unroll
-                for (int i = 0; i < WORDS_V; ++i) w[i] = 0;
-                if (c * LANE_V < a.c.row_bytes) __builtin_memcpy(w, __builtin_assume_aligned(a.c.v + (at + r) * a.c.row_bytes + c * LANE_V, LANE_V < 16 ? LANE_V : 16), LANE_V);
-#pragma unroll
-                for (int i = 0; i < WORDS_V; ++i) val[i][4 * s + r] = BITS == 4 ? turned(w[i]) : w[i];
+                for (int i = 0; i < Raw::kValueWords; ++i) f.value[4 * s + r][i] = 0;
+                if (c * Raw::kValue < a.c.row_bytes)
+                    __builtin_memcpy(f.value[4 * s + r], __builtin_assume_aligned(values + r * a.c.row_bytes, Raw::kValue < 16 ? Raw::kValue : 16), Raw::kValue);
             }
         }
-        f32x4 score[2];
+    };
+
+    f32x4 acc[NT][VD];
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        top[n] = -__builtin_inff();
+        sum[n] = 0;
+#pragma unroll
+        for (int j = 0; j < VD; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
+    }
+    auto use = [&](const Raw& f, const Eights& e, int32_t tb) {
+        f32x4 score[NT][2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            score[s] = LIFTED ? less : f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int o = 0; o < KOPS; ++o)
+            for (int n = 0; n < NT; ++n) score[n][s] = LIFTED ? less[n] : f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int p = NQ - 1; p >= 0; --p) score[s] = mfma_16<HALF>(key[s][o], q[o][p], score[s]);
+            for (int o = 0; o < KOPS; ++o) {
+                u32x4 key;
+                if (BITS == 8) {
+                    const uint32_t *w = &f.key[s][o / 2][2 * (o % 2)];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        key[2 * i] = pair_of<HALF>(byte_of<0>(w[i]), byte_of<1>(w[i]));
+                        key[2 * i + 1] = pair_of<HALF>(byte_of<2>(w[i]), byte_of<3>(w[i]));
+                    }
+                } else {
+                    const uint32_t w = f.key[s][o / Raw::kKeyWords][o % Raw::kKeyWords];
+                    uint32_t into = HALF ? 0x03C003C0u : 0x00780078u;
+                    asm("" : "+v"(into));                   // (see codes_as_operand of the products)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int up = (HALF ? 6 : 3) - 4 * j;
+                        const uint32_t m = up >= 0 ? w << (up & 31) : w >> (-up & 31);
+                        key[j] = LIFTED ? (m & into) | (HALF ? 0x4C004C00u : 0x41804180u)
+                                        : high_halves(bits_of(nibble_of(turned(w), j)), bits_of(nibble_of(turned(w), j + 4)));
+                    }
+                }
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) score[n][s] = mfma_16<HALF>(key, q[n][o][p], score[n][s]);
+            }
         }
-        float x[8], most = -__builtin_inff();
+        float ks[8], vs[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = seen >> e & 1 ? score[e / 4][e % 4] * ks[e] : -__builtin_inff();
-            most = fmaxf(most, x[e]);
+        for (int i = 0; i < 8; ++i) {
+            ks[i] = f.key_scale[i / 4][i % 4] * (BITS == 4 && !LIFTED ? 16.0f * a.scale : a.scale);
+            vs[i] = f.value_scale[i / 4][i % 4];
         }
-        most = fmaxf(max_over_quarters(most), top);
-        const float from = most == -__builtin_inff() ? 0.0f : most;
-        const float shrink = __builtin_amdgcn_exp2f(top - from);
-        top = most;
-        sum *= shrink;
+        const bool whole = tb + kTile <= base && tb + kTile <= end && e.there == 15;      // all of the tile is seen by all
+        u32x4 pp[NT][NP];
 #pragma unroll
-        for (int j = 0; j < VD; ++j) acc[j] *= shrink;
-        float p[8];
+        for (int n = 0; n < NT; ++n) {
+            float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float w = __builtin_amdgcn_exp2f(x[e] - from);
-            sum += w;
-            p[e] = seen >> e & 1 ? w * vs[e] : 0.0f;            // (what is not seen may have any scale)
-        }
-        u32x4 pp[NP];
+            for (int i = 0; i < 8; ++i) x[i] = score[n][i / 4][i % 4] * ks[i];
+            uint32_t seen = 0xff;
+            if (!whole) {
+                seen = 0;
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t t = tb + 16 * (i / 4) + 4 * h + i % 4, j = t - base;
+                    const bool there = e.there >> (2 * (i / 4) + h / 2) & 1;
+                    if (there && t < end && (j < 0 || (mask[n] >> (j & 63) & 1))) seen |= 1u << i;
+                    if (!(seen >> i & 1)) x[i] = -__builtin_inff();
+                }
+            }
+            float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            most = fmaxf(max_over_quarters(most), top[n]);
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+            if (__any(most > top[n])) {
+                const float shrink = __builtin_amdgcn_exp2f(top[n] - from);
+                sum[n] *= shrink;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pp[n][e] = high_halves(bits_of(p[2 * e]), bits_of(p[2 * e + 1]));
+                for (int j = 0; j < VD; ++j) acc[n][j] *= shrink;
+            }
+            top[n] = most;
+            float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(x[i] - from);
+                sum[n] += p[i];
+                p[i] *= vs[i];
+            }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = seen >> i & 1 ? p[i] : 0.0f;          // (what is not seen may have any scale)
+            }
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pp[n][k][i] = high_halves(bits_of(p[2 * i]), bits_of(p[2 * i + 1]));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] -= float_of(bits_of(p[i]) & 0xffff0000u);
+            }
         }
 #pragma unroll
         for (int j = 0; j < VD; ++j) {
-            const u32x4 v = values_at<BITS>(val[j / PER_WORD], j % PER_WORD);
+            uint32_t w[8];
 #pragma unroll
-            for (int n = NP - 1; n >= 0; --n) acc[j] = mfma_bf16(v, pp[n], acc[j]);
+            for (int i = 0; i < 8; ++i) w[i] = BITS == 4 ? turned(f.value[i][j / Raw::kPerWord]) : f.value[i][j / Raw::kPerWord];
+            const u32x4 v = values_at<BITS>(w, j % Raw::kPerWord);
+#pragma unroll
+            for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[n][j] = mfma_bf16(v, pp[n][k], acc[n][j]);
+        }
+    };
+
+    // While a tile is worked on, the next one is on its way into registers of its own, and the places of the one after that are looked up.
+    if (tiles > 0) {
+        Raw raw[2];
+        Eights at[2];
+        at[0] = find(0);
+        load(raw[0], at[0]);
+        at[1] = find(1);
+        for (int32_t i = 0; i < tiles; i += 2) {
+            load(raw[1], at[1]);
+            const Eights two = find(i + 2);
+            use(raw[0], at[0], own + i * kWaves * kTile);
+            if (i + 1 >= tiles) break;
+            load(raw[0], two);
+            const Eights three = find(i + 3);
+            use(raw[1], at[1], own + (i + 1) * kWaves * kTile);
+            at[0] = two;
+            at[1] = three;
         }
     }
-    sum = sum_over_quarters(sum);
 
     // the wavefronts' parts, joined: lane (c, h) holds elements VD (4 h + r) + j of query c
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int n = 0; n < NT; ++n) {
+        if (n) __syncthreads();
+        const float total = sum_over_quarters(sum[n]);
 #pragma unroll
-        for (int j = 0; j < VD; ++j) so[wave][c][VD * (4 * h + r) + j] = BITS == 4 ? 16.0f * acc[j][r] : acc[j][r];
-    if (h == 0) { sm[wave][c] = top; sl[wave][c] = sum; }
-    __syncthreads();
-    for (uint32_t e = threadIdx.x; e < 16 * a.c.dim; e += kWaves * 64) {
-        const uint32_t r = e / a.c.dim, d = e - r * a.c.dim;
-        if (row0 + r >= a.rows) break;
-        float m = sm[0][r];
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][r]);
-        const float from = m == -__builtin_inff() ? 0.0f : m;
-        float l = 0, o = 0;
+            for (int j = 0; j < VD; ++j) so[wave][c][VD * (4 * h + r) + j] = BITS == 4 ? 16.0f * acc[n][j][r] : acc[n][j][r];
+        if (h == 0) { sm[wave][c] = top[n]; sl[wave][c] = total; }
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < 16 * a.c.dim; e += kWaves * 64) {
+            const uint32_t r = e / a.c.dim, d = e - r * a.c.dim, row = row0 + 16 * n + r;
+            if (row >= a.rows) break;
+            float m = sm[0][r];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm[w][r] - from);
-            l += sl[w][r] == 0.0f ? 0.0f : f * sl[w][r];
-            o += sl[w][r] == 0.0f ? 0.0f : f * so[w][r][d];
-        }
-        const uint32_t i = (row0 + r) / a.group, g = (row0 + r) - i * a.group;
-        const uint64_t out_row = ((uint64_t)b * a.nq + i) * a.heads + head * a.group + g;
-        if (a.splits == 1) store_one<T>(a.out, out_row * a.c.dim + d, l == 0.0f ? 0.0f : o / l);
-        else {
-            a.part[(out_row * a.splits + split) * a.c.dim + d] = o;
-            if (d == 0) { a.stats[2 * (out_row * a.splits + split)] = m; a.stats[2 * (out_row * a.splits + split) + 1] = l; }
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][r]);
+            const float from = m == -__builtin_inff() ? 0.0f : m;
+            float l = 0, o = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(sm[w][r] - from);
+                l += sl[w][r] == 0.0f ? 0.0f : f * sl[w][r];
+                o += sl[w][r] == 0.0f ? 0.0f : f * so[w][r][d];
+            }
+            const uint32_t i = row / a.group, g = row - i * a.group;
+            const uint64_t out_row = ((uint64_t)b * a.nq + i) * a.heads + head * a.group + g;
+            if (a.splits == 1) store_one<T>(a.out, out_row * a.c.dim + d, l == 0.0f ? 0.0f : o / l);
+            else {
+                a.part[(out_row * a.splits + split) * a.c.dim + d] = o;
+                if (d == 0) { a.stats[2 * (out_row * a.splits + split)] = m; a.stats[2 * (out_row * a.splits + split) + 1] = l; }
+            }
         }
     }
 }
@@ -424,12 +506,16 @@ void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* 
                                                                         ld_head, lanes, FastDiv(c.dim / 8), FastDiv(c.heads));
     }
 }
+template <int T, int BITS, int DP, int NT>
+void attend_of(const Attend& a, hipStream_t s) {
+    k_kv_attend<T, BITS, DP, NT><<<dim3(a.splits, a.c.heads * ((a.rows + 16 * NT - 1) / (16 * NT)), a.batch), kWaves * 64, 0, s>>>(a);
+}
 template <int T, int BITS>
 void attend(const Attend& a, hipStream_t s) {
-    const dim3 grid(a.splits, a.c.heads * ((a.rows + 15) / 16), a.batch);
-    if (a.c.dim <= 64) k_kv_attend<T, BITS, 64><<<grid, kWaves * 64, 0, s>>>(a);
-    else if (a.c.dim <= 128) k_kv_attend<T, BITS, 128><<<grid, kWaves * 64, 0, s>>>(a);
-    else k_kv_attend<T, BITS, 256><<<grid, kWaves * 64, 0, s>>>(a);
+    const bool two = a.rows > 16 && T != LC_F32;
+    if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2>(a, s) : attend_of<T, BITS, 64, 1>(a, s);
+    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2>(a, s) : attend_of<T, BITS, 128, 1>(a, s);
+    else attend_of<T, BITS, 256, 1>(a, s);
     const uint64_t rows = (uint64_t)a.batch * a.nq * a.heads;
     if (a.splits > 1) k_kv_join<T><<<(uint32_t)((rows + 3) / 4), 256, 0, s>>>(a.part, a.stats, a.out, rows, a.splits, a.c.dim);
 }
@@ -486,7 +572,7 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
     if (!need) return LC_ERR_BADARG;
     if (batch == 0) return LC_OK;
     if (!q || !out || !lens || off(q, 16) || off(out, 16) || off(lens, 4) || off(mask, 8) || (table_pages && (!table || off(table, 4))) ||
-        ld_table > (1ull << 31) || table_pages > (1ull << 31) / cache->page_tokens || (batch > 1 && ld_table < table_pages)) return LC_ERR_BADARG;
+        ld_table > (1ull << 31) || table_pages > (1ull << 30) / cache->page_tokens || (batch > 1 && ld_table < table_pages)) return LC_ERR_BADARG;
     if (!ws || off(ws, 256) || ws_bytes < need) return LC_ERR_WORKSPACE;
     Attend a = {};
     a.c = described(*cache);

@@ -101,7 +101,7 @@ def test_attention_arguments(lib):
     ok = dict(q=P, batch=2, nq=3, heads=4, table=P, ld_table=4, table_pages=4, lens=P, mask=P, scale=1.0, out=P, dtype=F32, ws=P, ws_bytes=1 << 30)
     for name, value, want in (("q", None, BADARG), ("q", P + 8, BADARG), ("out", None, BADARG), ("out", P + 8, BADARG), ("lens", None, BADARG),
                               ("lens", P + 2, BADARG), ("table", None, BADARG), ("table", P + 2, BADARG), ("mask", P + 4, BADARG), ("ld_table", 3, BADARG),
-                              ("table_pages", (1 << 27) + 1, BADARG), ("nq", 0, BADARG), ("nq", 65, BADARG), ("heads", 3, BADARG), ("heads", 0, BADARG),
+                              ("table_pages", (1 << 26) + 1, BADARG), ("nq", 0, BADARG), ("nq", 65, BADARG), ("heads", 3, BADARG), ("heads", 0, BADARG),
                               ("heads", 4098, BADARG), ("batch", 65536, BADARG), ("dtype", F64, BADARG), ("ws", None, WORKSPACE), ("ws", P + 128, WORKSPACE),
                               ("ws_bytes", 255, WORKSPACE)):
         a = dict(ok)
