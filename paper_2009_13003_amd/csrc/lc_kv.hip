@@ -177,10 +177,13 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
     const uint32_t split = blockIdx.x, row_groups = (a.rows + 16 * NT - 1) / (16 * NT);
     const uint32_t head = blockIdx.y / row_groups, row0 = (blockIdx.y - head * row_groups) * 16 * NT, b = blockIdx.z;
     const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
-    const int32_t given = __builtin_amdgcn_readfirstlane(a.lens[b]);
+    // (What all lanes read alike is read by the scalar unit, which counts its loads apart: a vector load of it, waited for, would wait for
+    // the keys and values asked for before it as well.)
+    typedef const __attribute__((address_space(4))) int32_t* Uniform;
+    const int32_t given = ((Uniform)(uintptr_t)a.lens)[b];
     const int32_t len = given < 0 ? 0 : given < room ? given : room;
     const int32_t base = len - (int32_t)a.nq;               // the first drafted token
-    const int32_t* table = a.table + b * a.ld_table;
+    const Uniform table = (Uniform)(uintptr_t)(a.table + b * a.ld_table);
     const int32_t first = (int32_t)(split * a.tiles * kTile);
     const int32_t end = first + (int32_t)a.tiles * kTile < len ? first + (int32_t)a.tiles * kTile : len;
     const int32_t own = first + (int32_t)wave * kTile;      // this wavefront's first tile; every kWaves-th is its own
@@ -231,35 +234,36 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int32_t t = tb + 8 * g < len ? tb + 8 * g : (len - 1) & ~7;
-            const int32_t page = __builtin_amdgcn_readfirstlane(table[t >> a.c.page_shift]);
+            const int32_t page = table[t >> a.c.page_shift];
             const bool there = (uint32_t)page < (uint32_t)a.pages;
             e.row[g] = row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
             e.there |= there ? 1u << g : 0;
         }
         return e;
     };
-    const uint32_t key_off = (c % 8) * a.c.row_bytes + h * Raw::kKey, value_off = (4 * h % 8) * a.c.row_bytes + c * Raw::kValue;
+    // (Lanes whose elements lie beyond dim read the row's first: their queries are zero there, or their results go nowhere.)
+    uint32_t key_off[Raw::kKeyLoads];
+#pragma unroll
+    for (int l = 0; l < Raw::kKeyLoads; ++l) {
+        const uint32_t at = (4 * l + h) * Raw::kKey;
+        key_off[l] = (c % 8) * a.c.row_bytes + (at < a.c.row_bytes ? at : 0);
+    }
+    const uint32_t value_off = (4 * h % 8) * a.c.row_bytes + (c * Raw::kValue < a.c.row_bytes ? c * Raw::kValue : 0);
     auto load = [&](Raw& f, const Eights& e) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const uint64_t key_row = c < 8 ? e.row[2 * s] : e.row[2 * s + 1], value_row = h < 2 ? e.row[2 * s] : e.row[2 * s + 1];
-            const uint8_t* from = a.c.k + key_row * a.c.row_bytes + key_off;
+            const uint64_t k0 = e.row[2 * s] * a.c.row_bytes, k1 = e.row[2 * s + 1] * a.c.row_bytes;
+            const uint8_t* keys = a.c.k + (c < 8 ? k0 : k1);
 #pragma unroll
-            for (int l = 0; l < Raw::kKeyLoads; ++l) {
-#pragma unroll
-                for (int i = 0; i < Raw::kKeyWords; ++i) f.key[s][l][i] = 0;
-                if (l * 4 * Raw::kKey + h * Raw::kKey < a.c.row_bytes)
-                    __builtin_memcpy(f.key[s][l], __builtin_assume_aligned(from + l * 4 * Raw::kKey, Raw::kKey), Raw::kKey);
-            }
+            for (int l = 0; l < Raw::kKeyLoads; ++l) __builtin_memcpy(f.key[s][l], __builtin_assume_aligned(keys + key_off[l], Raw::kKey), Raw::kKey);
+            const uint64_t value_row = h < 2 ? e.row[2 * s] : e.row[2 * s + 1];
             f.key_scale[s] = *reinterpret_cast<const f32x4*>(a.c.k_scale + value_row + 4 * h % 8);
             f.value_scale[s] = *reinterpret_cast<const f32x4*>(a.c.v_scale + value_row + 4 * h % 8);
-            const uint8_t* values = a.c.v + value_row * a.c.row_bytes + value_off;
+            const uint8_t* values = a.c.v + (h < 2 ? k0 : k1) + value_off;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-#pragma unroll
-                for (int i = 0; i < Raw::kValueWords; ++i) f.value[4 * s + r][i] = 0;
-                if (c * Raw::kValue < a.c.row_bytes)
-                    __builtin_memcpy(f.value[4 * s + r], __builtin_assume_aligned(values + r * a.c.row_bytes, Raw::kValue < 16 ? Raw::kValue : 16), Raw::kValue);
+                if (Raw::kValue < 4) f.value[4 * s + r][0] = 0;
+                __builtin_memcpy(f.value[4 * s + r], __builtin_assume_aligned(values + r * a.c.row_bytes, Raw::kValue < 16 ? Raw::kValue : 16), Raw::kValue);
             }
         }
     };
@@ -332,15 +336,17 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
                 }
             }
             float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            most = fmaxf(max_over_quarters(most), top[n]);
-            const float from = most == -__builtin_inff() ? 0.0f : most;
-            if (__any(most > top[n])) {
-                const float shrink = __builtin_amdgcn_exp2f(top[n] - from);
+            // What probabilities are measured from moves only when one would pass 2^8, so that the sums are seldom rescaled.
+            most = max_over_quarters(most);
+            if (__any(most > top[n] + 8.0f)) {
+                most = fmaxf(most, top[n]);
+                const float shrink = __builtin_amdgcn_exp2f(top[n] - (most == -__builtin_inff() ? 0.0f : most));
                 sum[n] *= shrink;
 #pragma unroll
                 for (int j = 0; j < VD; ++j) acc[n][j] *= shrink;
+                top[n] = most;
             }
-            top[n] = most;
+            const float from = top[n] == -__builtin_inff() ? 0.0f : top[n];
             float p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -361,15 +367,21 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
             }
         }
 #pragma unroll
-        for (int j = 0; j < VD; ++j) {
+        for (int o = 0; o < Raw::kValueWords; ++o) {
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = BITS == 4 ? turned(f.value[i][j / Raw::kPerWord]) : f.value[i][j / Raw::kPerWord];
-            const u32x4 v = values_at<BITS>(w, j % Raw::kPerWord);
+            for (int i = 0; i < 8; ++i) {
+                w[i] = BITS == 4 ? turned(f.value[i][o]) : f.value[i][o];
+                if (BITS == 4) asm("" : "+v"(w[i]));         // (turned once, not again for every element)
+            }
 #pragma unroll
-            for (int k = NP - 1; k >= 0; --k)
+            for (int j = 0; j < Raw::kPerWord; ++j) {
+                const u32x4 v = values_at<BITS>(w, j);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[n][j] = mfma_bf16(v, pp[n][k], acc[n][j]);
+                for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][o * Raw::kPerWord + j] = mfma_bf16(v, pp[n][k], acc[n][o * Raw::kPerWord + j]);
+            }
         }
     };
 
