@@ -9,6 +9,9 @@ SOURCES = ["lc_encode.hip", "lc_decode.hip", "lc_decode_one.hip", "lc_api.hip", 
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC", "-ffp-contract=off",
          # packed fp32 instructions stay off: some of their forms have given wrong results on this hardware
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# the attention's sums live in vector registers from end to end; left to itself the compiler moves them to the accumulation
+# registers and back for every tile
+MORE_FLAGS = {"lc_kv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _run(cmd, verbose):
@@ -26,7 +29,7 @@ def build_library(verbose=False):
     os.makedirs(objdir, exist_ok=True)
     compile_flags = [f for f in FLAGS if f != "-shared"]
     objs = [os.path.join(objdir, s.replace(".hip", ".o")) for s in SOURCES]
-    cmds = [["hipcc"] + compile_flags + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objs)]
+    cmds = [["hipcc"] + compile_flags + MORE_FLAGS.get(s, []) + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objs)]
     with ThreadPoolExecutor(len(cmds)) as pool:
         list(pool.map(lambda c: _run(c, verbose), cmds))
     _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs, verbose)

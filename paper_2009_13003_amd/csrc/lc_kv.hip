@@ -1,6 +1,8 @@
 // A paged cache of keys and values in 8 or 4 bits: writing, reading back, and the attention over it (include/lc_serve.h).
 #include "lc_serve.h"
 
+#include <atomic>
+
 namespace lc {
 namespace serve {
 namespace {
@@ -96,7 +98,8 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 // Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly.
 constexpr int kTile = 32, kWaves = 4;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr uint32_t kMostSplits = 64, kWantBlocks = 1024, kLeastTokens = 128;
+// A sequence whose heads and queries alone do not give the chip kWantBlocks workgroups (two a compute unit) is split along its tokens.
+constexpr uint32_t kMostSplits = 60, kWantBlocks = 512, kLeastTokens = kWaves * kTile;
 
 struct Attend {
     Cache c;
@@ -105,12 +108,15 @@ struct Attend {
     const int32_t* lens;
     const uint64_t* mask;
     void* out;
-    float* part;                // [row][split][dim], then the maximum and the sum of each [row][split]
-    float* stats;
+    unsigned long long* marks;  // [head and group of rows][slot]: the call's number where that part is done
+    float* stats;               // the maximum and the sum of each [slot][query][head]
+    float* part;                // [slot][query][head][dim]
+    unsigned long long call;
     float scale;                // times log2(e)
     uint32_t batch, nq, heads, group, rows;     // rows = nq * group of a head of the cache
-    uint32_t splits, tiles;                     // 32-token tiles a split
+    uint32_t slots;             // parts of all sequences together: batch of them if none is split
     int32_t pages;
+    FastDiv by_group;
 };
 
 template <int T> struct Kind;       // how many 16-bit parts an element of q, and a probability, are given
@@ -162,8 +168,86 @@ template <int BITS, int DP> struct InCache {
 // each eight of a tile lie is the same for all lanes.
 struct Eights { uint64_t row[4]; uint32_t there; };
 
-template <int T, int BITS, int DP, int NT>
-__global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
+// What passes between workgroups goes through agent-scope atomic operations, whose completion each waits for before it arrives: a fence
+// would write back the L2 of a die from every workgroup (1000 tokens of 16 heads in 8 parts: 37 us with fences).
+__device__ __forceinline__ void put_shared(float* p, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)bits_of(y) << 32 | bits_of(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 get_shared(const float* p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return f32x2{float_of((uint32_t)v), float_of((uint32_t)(v >> 32))};
+}
+
+// Which part of which sequence a workgroup has: its slot, counted over the parts of all sequences.
+struct Part { uint32_t b, index, count; int32_t len, first, end; };
+
+// With as many slots as sequences each has one.  With more, all parts are of one length (the last of a sequence may be shorter): the
+// least that the slots suffice for, so that long sequences have more parts than short ones.  The lengths are known on the
+// device only; each wavefront works the division out for itself.
+__device__ __forceinline__ int32_t length_of(const Attend& a, uint32_t b, int32_t room) {
+    typedef const __attribute__((address_space(4))) int32_t* Uniform;
+    const int32_t n = ((Uniform)(uintptr_t)a.lens)[b];
+    return n < 0 ? 0 : n < room ? n : room;
+}
+__device__ __forceinline__ Part part_of(const Attend& a, uint32_t slot, uint32_t lane) {
+    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    Part p = {slot, 0, 1, 0, 0, 0};
+    if (a.slots == a.batch) {
+        p.len = p.end = length_of(a, slot, room);
+        return p;
+    }
+    // In units of kLeastTokens; lengths add up to less than 2^32 of them.
+    auto units_of = [&](uint32_t i) {
+        int32_t n = i < a.batch ? a.lens[i] : 0;
+        n = n < 0 ? 0 : n < room ? n : room;
+        return (uint32_t)(n + (int32_t)kLeastTokens - 1) / kLeastTokens;
+    };
+    uint32_t total = 0, longest = 0;
+    for (uint32_t i = lane; i < a.batch; i += 64) {
+        const uint32_t n = units_of(i);
+        total += n;
+        longest = n > longest ? n : longest;
+    }
+    if (a.batch > 1)
+        for (int x = 1; x < 64; x *= 2) {
+            total += __shfl_xor(total, x);
+            const uint32_t o = __shfl_xor(longest, x);
+            longest = o > longest ? o : longest;
+        }
+    total = __builtin_amdgcn_readfirstlane(total);
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    const uint32_t more = a.slots - a.batch;                // (sum of ceil(n / length) <= batch + sum of n / length)
+    uint32_t length = (total + more - 1) / more, least = (longest + kMostSplits - 1) / kMostSplits;
+    length = length > least ? length : least;
+    length = length ? length : 1;
+    uint32_t before = 0;
+    p.count = 0;                                            // (none: a slot beyond the last part)
+    for (uint32_t i0 = 0; i0 < a.batch; i0 += 64) {
+        const uint32_t i = i0 + lane, n = units_of(i), own = i < a.batch ? (n ? (n + length - 1) / length : 1) : 0;
+        uint32_t upto = own;
+        if (a.batch > 1)
+            for (int x = 1; x < 64; x *= 2) { const uint32_t o = __shfl_up(upto, x); if (lane >= (uint32_t)x) upto += o; }
+        const unsigned long long mine = __ballot(before + upto > slot && before + upto - own <= slot);
+        if (mine) {
+            const int from = __builtin_ctzll(mine);
+            p.b = i0 + from;
+            p.count = __builtin_amdgcn_readfirstlane(__shfl(own, from));
+            p.index = slot - (before + __builtin_amdgcn_readfirstlane(__shfl(upto, from)) - p.count);
+            p.len = length_of(a, p.b, room);
+            p.first = (int32_t)(p.index * length * kLeastTokens);
+            const uint64_t end = (uint64_t)(p.index + 1) * length * kLeastTokens;
+            p.end = end < (uint64_t)p.len ? (int32_t)end : p.len;
+            break;
+        }
+        before += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+    }
+    p.first = __builtin_amdgcn_readfirstlane(p.first);
+    p.end = __builtin_amdgcn_readfirstlane(p.end);
+    return p;
+}
+
+template <int T, int BITS, int DP, int NT, int PERSIMD>
+__global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
     using Raw = InCache<BITS, DP>;
     constexpr bool HALF = Kind<T>::kHalf;
     constexpr int NQ = Kind<T>::kQ, NP = Kind<T>::kP;
@@ -174,20 +258,72 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
     __shared__ float so[kWaves][16][DP + 4];
     __shared__ float sm[kWaves][16], sl[kWaves][16];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 16, h = lane / 16;
-    const uint32_t split = blockIdx.x, row_groups = (a.rows + 16 * NT - 1) / (16 * NT);
-    const uint32_t head = blockIdx.y / row_groups, row0 = (blockIdx.y - head * row_groups) * 16 * NT, b = blockIdx.z;
-    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    const uint32_t row_groups = (a.rows + 16 * NT - 1) / (16 * NT), head = blockIdx.x / row_groups, row0 = (blockIdx.x - head * row_groups) * 16 * NT;
+    const uint32_t slot = blockIdx.y;
+    const Part part = part_of(a, slot, lane);
+    if (part.count == 0) return;
+    const uint32_t b = part.b;
+    const int32_t len = part.len, first = part.first, end = part.end, base = len - (int32_t)a.nq;      // base: the first drafted token
     // (What all lanes read alike is read by the scalar unit, which counts its loads apart: a vector load of it, waited for, would wait for
     // the keys and values asked for before it as well.)
     typedef const __attribute__((address_space(4))) int32_t* Uniform;
-    const int32_t given = ((Uniform)(uintptr_t)a.lens)[b];
-    const int32_t len = given < 0 ? 0 : given < room ? given : room;
-    const int32_t base = len - (int32_t)a.nq;               // the first drafted token
     const Uniform table = (Uniform)(uintptr_t)(a.table + b * a.ld_table);
-    const int32_t first = (int32_t)(split * a.tiles * kTile);
-    const int32_t end = first + (int32_t)a.tiles * kTile < len ? first + (int32_t)a.tiles * kTile : len;
     const int32_t own = first + (int32_t)wave * kTile;      // this wavefront's first tile; every kWaves-th is its own
     const int32_t tiles = own < end ? (end - own + kWaves * kTile - 1) / (kWaves * kTile) : 0;
+
+    auto find = [&](int32_t i) {                            // where this wavefront's tile i lies (beyond the last: the last again)
+        Eights e;
+        e.there = 0;
+        const int32_t tb = own + (i < tiles ? i : tiles - 1) * kWaves * kTile;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int32_t t = tb + 8 * g < len ? tb + 8 * g : (len - 1) & ~7;
+            const int32_t page = table[t >> a.c.page_shift];
+            const bool there = (uint32_t)page < (uint32_t)a.pages;
+            e.row[g] = row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
+            e.there |= there ? 1u << g : 0;
+        }
+        return e;
+    };
+    // (Lanes whose elements lie beyond dim read the row's first: their queries are zero there, or their results go nowhere.)
+    uint32_t key_off[Raw::kKeyLoads];
+#pragma unroll
+    for (int l = 0; l < Raw::kKeyLoads; ++l) {
+        const uint32_t at = (4 * l + h) * Raw::kKey;
+        key_off[l] = (c % 8) * a.c.row_bytes + (at < a.c.row_bytes ? at : 0);
+    }
+    const uint32_t value_off = (4 * h % 8) * a.c.row_bytes + (c * Raw::kValue < a.c.row_bytes ? c * Raw::kValue : 0);
+    auto load_keys = [&](Raw& f, const Eights& e) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint64_t k0 = e.row[2 * s] * a.c.row_bytes, k1 = e.row[2 * s + 1] * a.c.row_bytes;
+            const uint8_t* keys = a.c.k + (c < 8 ? k0 : k1);
+#pragma unroll
+            for (int l = 0; l < Raw::kKeyLoads; ++l) __builtin_memcpy(f.key[s][l], __builtin_assume_aligned(keys + key_off[l], Raw::kKey), Raw::kKey);
+        }
+    };
+    auto load_values = [&](Raw& f, const Eights& e) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint64_t k0 = e.row[2 * s] * a.c.row_bytes, k1 = e.row[2 * s + 1] * a.c.row_bytes;
+            const uint64_t value_row = h < 2 ? e.row[2 * s] : e.row[2 * s + 1];
+            f.key_scale[s] = *reinterpret_cast<const f32x4*>(a.c.k_scale + value_row + 4 * h % 8);
+            f.value_scale[s] = *reinterpret_cast<const f32x4*>(a.c.v_scale + value_row + 4 * h % 8);
+            const uint8_t* values = a.c.v + (h < 2 ? k0 : k1) + value_off;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (Raw::kValue < 4) f.value[4 * s + r][0] = 0;
+                __builtin_memcpy(f.value[4 * s + r], __builtin_assume_aligned(values + r * a.c.row_bytes, Raw::kValue < 16 ? Raw::kValue : 16), Raw::kValue);
+            }
+        }
+    };
+    Raw raw;
+    Eights at = {};
+    if (tiles > 0) {
+        at = find(0);
+        load_keys(raw, at);
+        load_values(raw, at);
+    }
 
     // this lane's queries, eight elements an operand at the places at which the keys' codes lie
     u32x4 q[NT][KOPS][NQ];
@@ -197,7 +333,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
     for (int n = 0; n < NT; ++n) {
         const uint32_t row = row0 + 16 * n + c;
         const bool has_row = row < a.rows;
-        const uint32_t qi = (has_row ? row : 0) / a.group, qg = (has_row ? row : 0) - qi * a.group;
+        const uint32_t qi = a.by_group(has_row ? row : 0), qg = (has_row ? row : 0) - qi * a.group;
         const uint64_t q_at = (((uint64_t)b * a.nq + qi) * a.heads + head * a.group + qg) * a.c.dim;
         mask[n] = a.mask ? a.mask[(uint64_t)b * a.nq + qi] : qi >= 63 ? ~0ull : (2ull << qi) - 1;
         less[n] = f32x4{0, 0, 0, 0};
@@ -227,47 +363,6 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
         }
     }
 
-    auto find = [&](int32_t i) {                            // where this wavefront's tile i lies (beyond the last: the last again)
-        Eights e;
-        e.there = 0;
-        const int32_t tb = own + (i < tiles ? i : tiles - 1) * kWaves * kTile;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int32_t t = tb + 8 * g < len ? tb + 8 * g : (len - 1) & ~7;
-            const int32_t page = table[t >> a.c.page_shift];
-            const bool there = (uint32_t)page < (uint32_t)a.pages;
-            e.row[g] = row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
-            e.there |= there ? 1u << g : 0;
-        }
-        return e;
-    };
-    // (Lanes whose elements lie beyond dim read the row's first: their queries are zero there, or their results go nowhere.)
-    uint32_t key_off[Raw::kKeyLoads];
-#pragma unroll
-    for (int l = 0; l < Raw::kKeyLoads; ++l) {
-        const uint32_t at = (4 * l + h) * Raw::kKey;
-        key_off[l] = (c % 8) * a.c.row_bytes + (at < a.c.row_bytes ? at : 0);
-    }
-    const uint32_t value_off = (4 * h % 8) * a.c.row_bytes + (c * Raw::kValue < a.c.row_bytes ? c * Raw::kValue : 0);
-    auto load = [&](Raw& f, const Eights& e) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint64_t k0 = e.row[2 * s] * a.c.row_bytes, k1 = e.row[2 * s + 1] * a.c.row_bytes;
-            const uint8_t* keys = a.c.k + (c < 8 ? k0 : k1);
-#pragma unroll
-            for (int l = 0; l < Raw::kKeyLoads; ++l) __builtin_memcpy(f.key[s][l], __builtin_assume_aligned(keys + key_off[l], Raw::kKey), Raw::kKey);
-            const uint64_t value_row = h < 2 ? e.row[2 * s] : e.row[2 * s + 1];
-            f.key_scale[s] = *reinterpret_cast<const f32x4*>(a.c.k_scale + value_row + 4 * h % 8);
-            f.value_scale[s] = *reinterpret_cast<const f32x4*>(a.c.v_scale + value_row + 4 * h % 8);
-            const uint8_t* values = a.c.v + (h < 2 ? k0 : k1) + value_off;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (Raw::kValue < 4) f.value[4 * s + r][0] = 0;
-                __builtin_memcpy(f.value[4 * s + r], __builtin_assume_aligned(values + r * a.c.row_bytes, Raw::kValue < 16 ? Raw::kValue : 16), Raw::kValue);
-            }
-        }
-    };
-
     f32x4 acc[NT][VD];
     float top[NT], sum[NT];
 #pragma unroll
@@ -277,7 +372,11 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
 #pragma unroll
         for (int j = 0; j < VD; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
     }
-    auto use = [&](const Raw& f, const Eights& e, int32_t tb) {
+    // Keys are spent once the scores are there, values once they are added up: then the next tile's are asked for, into the same registers.
+    for (int32_t i = 0; i < tiles; ++i) {
+        const Raw& f = raw;
+        const int32_t tb = own + i * kWaves * kTile;
+        const Eights next = find(i + 1);
         f32x4 score[NT][2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -311,13 +410,14 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
                     for (int n = 0; n < NT; ++n) score[n][s] = mfma_16<HALF>(key, q[n][o][p], score[n][s]);
             }
         }
+        load_keys(raw, next);
         float ks[8], vs[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             ks[i] = f.key_scale[i / 4][i % 4] * (BITS == 4 && !LIFTED ? 16.0f * a.scale : a.scale);
             vs[i] = f.value_scale[i / 4][i % 4];
         }
-        const bool whole = tb + kTile <= base && tb + kTile <= end && e.there == 15;      // all of the tile is seen by all
+        const bool whole = tb + kTile <= base && tb + kTile <= end && at.there == 15;      // all of the tile is seen by all
         u32x4 pp[NT][NP];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -330,7 +430,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int32_t t = tb + 16 * (i / 4) + 4 * h + i % 4, j = t - base;
-                    const bool there = e.there >> (2 * (i / 4) + h / 2) & 1;
+                    const bool there = at.there >> (2 * (i / 4) + h / 2) & 1;
                     if (there && t < end && (j < 0 || (mask[n] >> (j & 63) & 1))) seen |= 1u << i;
                     if (!(seen >> i & 1)) x[i] = -__builtin_inff();
                 }
@@ -383,29 +483,17 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
                     for (int n = 0; n < NT; ++n) acc[n][o * Raw::kPerWord + j] = mfma_bf16(v, pp[n][k], acc[n][o * Raw::kPerWord + j]);
             }
         }
-    };
-
-    // While a tile is worked on, the next one is on its way into registers of its own, and the places of the one after that are looked up.
-    if (tiles > 0) {
-        Raw raw[2];
-        Eights at[2];
-        at[0] = find(0);
-        load(raw[0], at[0]);
-        at[1] = find(1);
-        for (int32_t i = 0; i < tiles; i += 2) {
-            load(raw[1], at[1]);
-            const Eights two = find(i + 2);
-            use(raw[0], at[0], own + i * kWaves * kTile);
-            if (i + 1 >= tiles) break;
-            load(raw[0], two);
-            const Eights three = find(i + 3);
-            use(raw[1], at[1], own + (i + 1) * kWaves * kTile);
-            at[0] = two;
-            at[1] = three;
-        }
+        load_values(raw, next);
+        at = next;
     }
 
-    // the wavefronts' parts, joined: lane (c, h) holds elements VD (4 h + r) + j of query c
+    // The wavefronts' parts, joined: lane (c, h) holds elements VD (4 h + r) + j of query c.
+    const uint64_t heads_of = (uint64_t)a.nq * a.heads;
+    auto place = [&](uint32_t row) {                        // of a row of this head, among a sequence's queries and heads
+        const uint32_t i = a.by_group(row), g = row - i * a.group;
+        return (uint64_t)i * a.heads + head * a.group + g;
+    };
+    const uint32_t quads = a.c.dim / 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (n) __syncthreads();
@@ -413,66 +501,132 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(Attend a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int j = 0; j < VD; ++j) so[wave][c][VD * (4 * h + r) + j] = BITS == 4 ? 16.0f * acc[n][j][r] : acc[n][j][r];
+            for (int j = 0; j < VD; j += 4) {
+                f32x4 v = {acc[n][j][r], acc[n][j + 1][r], acc[n][j + 2][r], acc[n][j + 3][r]};
+                if (BITS == 4) v *= 16.0f;
+                *reinterpret_cast<f32x4*>(&so[wave][c][VD * (4 * h + r) + j]) = v;
+            }
         if (h == 0) { sm[wave][c] = top[n]; sl[wave][c] = total; }
         __syncthreads();
-        for (uint32_t e = threadIdx.x; e < 16 * a.c.dim; e += kWaves * 64) {
-            const uint32_t r = e / a.c.dim, d = e - r * a.c.dim, row = row0 + 16 * n + r;
-            if (row >= a.rows) break;
-            float m = sm[0][r];
+        if (threadIdx.x < 16) {
+            const uint32_t r = threadIdx.x;
+            float m = sm[0][r], l = 0, f[kWaves];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][r]);
-            const float from = m == -__builtin_inff() ? 0.0f : m;
-            float l = 0, o = 0;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(sm[w][r] - from);
-                l += sl[w][r] == 0.0f ? 0.0f : f * sl[w][r];
-                o += sl[w][r] == 0.0f ? 0.0f : f * so[w][r][d];
+                f[w] = sl[w][r] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(sm[w][r] - m);      // (where a sum is not zero the maximum is a number, or all is NaN)
+                l += sl[w][r] == 0.0f ? 0.0f : f[w] * sl[w][r];
             }
-            const uint32_t i = row / a.group, g = row - i * a.group;
-            const uint64_t out_row = ((uint64_t)b * a.nq + i) * a.heads + head * a.group + g;
-            if (a.splits == 1) store_one<T>(a.out, out_row * a.c.dim + d, l == 0.0f ? 0.0f : o / l);
+            if (part.count > 1 && row0 + 16 * n + r < a.rows) {
+                put_shared(a.stats + 2 * (slot * heads_of + place(row0 + 16 * n + r)), m, l);
+            }
+            const float whole = part.count > 1 || l == 0.0f ? 1.0f : 1.0f / l;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sm[w][r] = f[w] * whole;
+        }
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < 16 * quads; e += kWaves * 64) {
+            const uint32_t r = e / quads, d = 4 * (e - r * quads), row = row0 + 16 * n + r;
+            if (row >= a.rows) break;
+            f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = sm[w][r];
+                const f32x4 v = *reinterpret_cast<const f32x4*>(&so[w][r][d]);
+                if (f != 0.0f)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[k] = fmaf(f, v[k], o[k]);
+            }
+            if (part.count == 1) store_four<T>(a.out, (b * heads_of + place(row)) * a.c.dim + d, o);
             else {
-                a.part[(out_row * a.splits + split) * a.c.dim + d] = o;
-                if (d == 0) { a.stats[2 * (out_row * a.splits + split)] = m; a.stats[2 * (out_row * a.splits + split) + 1] = l; }
+                float* to = a.part + (slot * heads_of + place(row)) * a.c.dim + d;
+                put_shared(to, o[0], o[1]);
+                put_shared(to + 2, o[2], o[3]);
             }
         }
     }
-}
+    if (part.count == 1) return;
 
-// The splits of each row, joined: a wavefront a row.
-template <int T>
-__global__ __launch_bounds__(256) void k_kv_join(const float* part, const float* stats, void* out, uint64_t rows, uint32_t splits, uint32_t dim) {
-    const uint64_t row = blockIdx.x * 4ull + threadIdx.x / 64;
-    if (row >= rows) return;
-    const uint32_t lane = threadIdx.x % 64;
-    const bool has = lane < splits;
-    const float m = has ? stats[2 * (row * splits + lane)] : -__builtin_inff(), l = has ? stats[2 * (row * splits + lane) + 1] : 0.0f;
-    float top = m;
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float f = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
-    float total = l == 0.0f ? 0.0f : f * l;
-    for (int x = 1; x < 64; x *= 2) total += __shfl_xor(total, x);
-    float o[4] = {0, 0, 0, 0};
-    for (uint32_t s = 0; s < splits; ++s) {
-        if (__shfl(l, s) == 0.0f) continue;
-        const float w = __shfl(f, s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < dim) o[i] = fmaf(w, part[(row * splits + s) * dim + lane + 64 * i], o[i]);
+    // The last workgroup of a sequence's parts to get here joins them: each marks its part done with the call's number, once what it has
+    // written has arrived, and then looks at the marks of all.  Whoever marks last finds them all there; should two find that, both
+    // write the same.  Marks are taken back, so that the same call replayed from a graph begins without them; what was there before the
+    // call does not matter.
+    __shared__ uint32_t is_last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (wave == 0) {
+        unsigned long long* marks = a.marks + (uint64_t)blockIdx.x * a.slots + slot - part.index;
+        if (lane == 0) __hip_atomic_store(marks + part.index, a.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const bool done = lane >= part.count || __hip_atomic_load(marks + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.call;
+        const bool all = __all(done);
+        if (lane == 0) is_last = all;
+        if (all && lane < part.count) __hip_atomic_store(marks + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    __syncthreads();
+    if (!is_last) return;
+    f32x2 (*stat)[kMostSplits] = reinterpret_cast<f32x2 (*)[kMostSplits]>(&so[0][0][0]);
+    static_assert(sizeof(so) >= 16 * NT * kMostSplits * sizeof(f32x2), "room for every row and part");
+    static_assert(kMostSplits <= 64, "a lane a part");
+    const uint64_t slot0 = slot - part.index;
+    const uint32_t rows_here = a.rows - row0 < 16 * NT ? a.rows - row0 : 16 * NT;
+    for (uint32_t e = threadIdx.x; e < rows_here * part.count; e += kWaves * 64) {
+        const uint32_t k = e / rows_here, r = e - k * rows_here;
+        stat[r][k] = get_shared(a.stats + 2 * ((slot0 + k) * heads_of + place(row0 + r)));
+    }
+    __syncthreads();
+    if (threadIdx.x < rows_here) {
+        const uint32_t r = threadIdx.x;
+        float m = -__builtin_inff(), l = 0;
+        for (uint32_t k = 0; k < part.count; ++k) m = fmaxf(m, stat[r][k][0]);
+        for (uint32_t k = 0; k < part.count; ++k) {
+            const float sum_k = stat[r][k][1], f = sum_k == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(stat[r][k][0] - m);
+            stat[r][k][0] = f;
+            l += sum_k == 0.0f ? 0.0f : f * sum_k;
+        }
+        const float whole = l == 0.0f ? 1.0f : 1.0f / l;
+        for (uint32_t k = 0; k < part.count; ++k) stat[r][k][0] *= whole;
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < rows_here * quads; e += kWaves * 64) {
+        const uint32_t r = e / quads, d = 4 * (e - r * quads);
+        const float* from = a.part + (slot0 * heads_of + place(row0 + r)) * a.c.dim + d;
+        f32x4 o = {0, 0, 0, 0};
+        for (uint32_t k0 = 0; k0 < part.count; k0 += 8) {                // (the last part again beyond the last: eight loads under way at once)
+            f32x2 v[8][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < dim) store_one<T>(out, row * dim + lane + 64 * i, total == 0.0f ? 0.0f : o[i] / total);
+            for (int k = 0; k < 8; ++k) {
+                const float* at = from + (k0 + k < part.count ? k0 + k : part.count - 1) * heads_of * a.c.dim;
+                v[k][0] = get_shared(at);
+                v[k][1] = get_shared(at + 2);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = k0 + k < part.count ? stat[r][k0 + k][0] : 0.0f;
+                if (f != 0.0f) o = f32x4{fmaf(f, v[k][0][0], o[0]), fmaf(f, v[k][0][1], o[1]), fmaf(f, v[k][1][0], o[2]), fmaf(f, v[k][1][1], o[3])};
+            }
+        }
+        store_four<T>(a.out, (b * heads_of + place(row0 + r)) * a.c.dim + d, o);
+    }
 }
 
-// Splits of a sequence: as many as give the chip enough workgroups, whatever its length.
-uint32_t most_splits(uint64_t batch, uint32_t nq, uint32_t heads, uint32_t kv_heads) {
-    const uint64_t rows = (uint64_t)nq * (heads / kv_heads), blocks = batch * kv_heads * ((rows + 15) / 16);
-    const uint64_t s = blocks ? (kWantBlocks + blocks - 1) / blocks : 1;
-    return (uint32_t)(s < kMostSplits ? s : kMostSplits);
+// Slots for the parts of all sequences: a slot a sequence, and as many more as give the chip its workgroups.
+uint64_t slots_of(uint64_t batch, uint32_t kv_heads, uint64_t row_groups) {
+    const uint64_t blocks = kv_heads * row_groups;
+    const uint64_t slots = batch * blocks >= kWantBlocks ? batch : batch + (kWantBlocks + blocks - 1) / blocks;
+    return slots < batch * kMostSplits ? slots : batch * kMostSplits;
 }
+struct Scratch { uint64_t stats, part, bytes; };            // where the parts of the scratch memory begin
+Scratch scratch_of(uint64_t batch, uint64_t slots, uint64_t groups, uint64_t nq, uint64_t heads, uint64_t dim) {
+    if (slots == batch) return {0, 0, 256};
+    Scratch s;
+    s.stats = (slots * groups * 8 + 255) / 256 * 256;
+    s.part = s.stats + (slots * nq * heads * 8 + 255) / 256 * 256;
+    s.bytes = (s.part + slots * nq * heads * dim * 4 + 255) / 256 * 256;
+    return s;
+}
+int tiles_of_rows(uint64_t rows, int dim, int dtype) { return rows > 16 && dtype != LC_F32 && dim <= 128 ? 2 : 1; }
 
 bool bad(const lc_kv_cache* c) {
     if (!c || c->heads < 1 || c->heads > 1024 || c->dim < 32 || c->dim > 256 || c->dim % 32 || (c->bits != 8 && c->bits != 4)) return true;
@@ -518,18 +672,16 @@ void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* 
                                                                         ld_head, lanes, FastDiv(c.dim / 8), FastDiv(c.heads));
     }
 }
-template <int T, int BITS, int DP, int NT>
+template <int T, int BITS, int DP, int NT, int PERSIMD>
 void attend_of(const Attend& a, hipStream_t s) {
-    k_kv_attend<T, BITS, DP, NT><<<dim3(a.splits, a.c.heads * ((a.rows + 16 * NT - 1) / (16 * NT)), a.batch), kWaves * 64, 0, s>>>(a);
+    k_kv_attend<T, BITS, DP, NT, PERSIMD><<<dim3(a.c.heads * ((a.rows + 16 * NT - 1) / (16 * NT)), a.slots), kWaves * 64, 0, s>>>(a);
 }
 template <int T, int BITS>
 void attend(const Attend& a, hipStream_t s) {
-    const bool two = a.rows > 16 && T != LC_F32;
-    if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2>(a, s) : attend_of<T, BITS, 64, 1>(a, s);
-    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2>(a, s) : attend_of<T, BITS, 128, 1>(a, s);
-    else attend_of<T, BITS, 256, 1>(a, s);
-    const uint64_t rows = (uint64_t)a.batch * a.nq * a.heads;
-    if (a.splits > 1) k_kv_join<T><<<(uint32_t)((rows + 3) / 4), 256, 0, s>>>(a.part, a.stats, a.out, rows, a.splits, a.c.dim);
+    const bool two = tiles_of_rows(a.rows, (int)a.c.dim, T) == 2;
+    if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2, 2>(a, s) : attend_of<T, BITS, 64, 1, 3>(a, s);
+    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2, 2>(a, s) : attend_of<T, BITS, 128, 1, 2>(a, s);
+    else attend_of<T, BITS, 256, 1, 1>(a, s);
 }
 
 }  // namespace
@@ -573,8 +725,13 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
 size_t lc_kv_workspace_bytes(uint64_t batch, int nq, int heads, int kv_heads, int dim) {
     if (batch > 65535 || nq < 1 || nq > 64 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 ||
         dim > 256 || dim % 32) return 0;
-    const uint64_t splits = most_splits(batch, (uint32_t)nq, (uint32_t)heads, (uint32_t)kv_heads);
-    return splits == 1 ? 256 : (size_t)((batch * nq * heads * splits * (dim + 2) * 4 + 255) / 256 * 256);
+    uint64_t most = 0;                                      // (of the ways the rows may be grouped, whatever the type)
+    for (int tiles = 1; tiles <= 2; ++tiles) {
+        const uint64_t rows = (uint64_t)nq * (heads / kv_heads), groups = (rows + 16 * tiles - 1) / (16 * tiles);
+        const uint64_t bytes = scratch_of(batch, slots_of(batch, (uint32_t)kv_heads, groups), kv_heads * groups, nq, heads, dim).bytes;
+        most = bytes > most ? bytes : most;
+    }
+    return (size_t)most;
 }
 
 int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq, int heads, const int32_t* table, uint64_t ld_table, uint64_t table_pages,
@@ -591,15 +748,18 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
     a.q = q; a.table = table; a.ld_table = ld_table; a.table_pages = cache->pages ? table_pages : 0; a.lens = lens; a.mask = mask; a.out = out;
     a.scale = scale * kLog2e;
     a.batch = (uint32_t)batch; a.nq = (uint32_t)nq; a.heads = (uint32_t)heads; a.group = (uint32_t)(heads / cache->heads); a.rows = a.nq * a.group;
+    a.by_group = FastDiv(a.group);
     a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
-    // (splits by what the table has room for: the lengths are known on the device only)
-    const uint64_t room = a.table_pages << a.c.page_shift, by_room = (room + kLeastTokens - 1) / kLeastTokens;
-    uint64_t splits = most_splits(batch, a.nq, a.heads, a.c.heads);
-    splits = by_room < splits ? (by_room ? by_room : 1) : splits;
-    a.tiles = (uint32_t)((room + splits * kTile - 1) / (splits * kTile));
-    a.splits = (uint32_t)splits;
-    a.part = static_cast<float*>(ws);
-    a.stats = a.part + batch * nq * heads * splits * a.c.dim;
+    const int tiles = tiles_of_rows(a.rows, cache->dim, dtype);
+    const uint64_t groups = (a.rows + 16 * tiles - 1) / (16 * tiles);
+    a.slots = (uint32_t)slots_of(batch, a.c.heads, groups);
+    if ((a.table_pages << a.c.page_shift) <= kLeastTokens) a.slots = a.batch;      // (nothing to split)
+    const Scratch at = scratch_of(batch, a.slots, a.c.heads * groups, nq, heads, a.c.dim);
+    a.marks = static_cast<unsigned long long*>(ws);
+    a.stats = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.stats);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.part);
+    static std::atomic<unsigned long long> calls{0x5bd1e995};
+    a.call = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull | 1;      // (one to one on 63 bits, and never zero)
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define CALL(T, B) attend<T, B>(a, s)
     LC_BY_TYPE(CALL, dtype, cache->bits);

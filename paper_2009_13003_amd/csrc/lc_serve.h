@@ -11,6 +11,7 @@ namespace serve {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -24,7 +25,7 @@ inline uintptr_t size_of(int dtype) { return dtype == LC_F32 ? 4 : 2; }
 // n / d for 32-bit n by a product with what the host worked out once (round-up method: exact for every n).
 struct FastDiv {
     uint32_t d, m, s;
-    explicit FastDiv(uint32_t d_ = 1) : d(d_), m(0), s(0) {
+    FastDiv(uint32_t d_ = 1) : d(d_), m(0), s(0) {
         while (s < 32 && (1ull << s) < d) ++s;
         m = (uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
     }
@@ -98,6 +99,14 @@ template <int T> __device__ __forceinline__ void store_eight(void* p, uint64_t i
         for (int e = 0; e < 8; ++e)
             if (e < valid) store_one<T>(p, i + e, v[e]);
     }
+}
+
+// Four elements in a row, aligned to their size together.
+template <int T> __device__ __forceinline__ void store_four(void* p, uint64_t i, f32x4 v) {
+    if (T == LC_F32) { *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = v; return; }
+    const u32x2 w = T == LC_BF16 ? u32x2{bf16_of(v[0]) | bf16_of(v[1]) << 16, bf16_of(v[2]) | bf16_of(v[3]) << 16}
+                                 : u32x2{f16_of(v[0]) | f16_of(v[1]) << 16, f16_of(v[2]) | f16_of(v[3]) << 16};
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + i) = w;
 }
 
 // The largest of `lanes` neighbouring lanes' values in every one of them (lanes: 4, 8, 16 or 32, aligned).
