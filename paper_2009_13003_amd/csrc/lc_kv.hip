@@ -150,8 +150,30 @@ template <int BITS> __device__ __forceinline__ u32x4 values_at(const uint32_t (&
     return r;
 }
 
-__device__ __forceinline__ float max_over_quarters(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float sum_over_quarters(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+// Over the four lanes of a column (c, c + 16, c + 32, c + 48), in each of them: rows of sixteen lanes change places, without LDS.
+__device__ __forceinline__ float max_over_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(bits_of(v), bits_of(v), false, false);
+    v = fmaxf(float_of(a[0]), float_of(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(bits_of(v), bits_of(v), false, false);
+    return fmaxf(float_of(b[0]), float_of(b[1]));
+}
+__device__ __forceinline__ float sum_over_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(bits_of(v), bits_of(v), false, false);
+    v = float_of(a[0]) + float_of(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(bits_of(v), bits_of(v), false, false);
+    return float_of(b[0]) + float_of(b[1]);
+}
+// Over all lanes, as a number that all of them share.
+template <bool MAX> __device__ __forceinline__ uint32_t over_wave(uint32_t v) {
+#define LC_DPP(ctrl) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false); v = MAX ? (v > o ? v : o) : v + o; }
+    LC_DPP(0xB1) LC_DPP(0x4E) LC_DPP(0x141) LC_DPP(0x140)
+#undef LC_DPP
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = MAX ? (a[0] > a[1] ? a[0] : a[1]) : a[0] + a[1];
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = MAX ? (b[0] > b[1] ? b[0] : b[1]) : b[0] + b[1];
+    return __builtin_amdgcn_readfirstlane(v);
+}
 
 // A tile of 32 tokens as it lies in the cache.
 template <int BITS, int DP> struct InCache {
@@ -181,9 +203,9 @@ __device__ __forceinline__ f32x2 get_shared(const float* p) {
 // Which part of which sequence a workgroup has: its slot, counted over the parts of all sequences.
 struct Part { uint32_t b, index, count; int32_t len, first, end; };
 
-// With as many slots as sequences each has one.  With more, all parts are of one length (the last of a sequence may be shorter): the
-// least that the slots suffice for, so that long sequences have more parts than short ones.  The lengths are known on the
-// device only; each wavefront works the division out for itself.
+// With as many slots as sequences each has one.  With more, all parts are of one length (the last of a sequence may be shorter): about the
+// least that the slots suffice for, so that long sequences have more parts than short ones and no part waits for another to
+// leave the chip.  The lengths are known on the device only; each wavefront works the division out for itself.
 __device__ __forceinline__ int32_t length_of(const Attend& a, uint32_t b, int32_t room) {
     typedef const __attribute__((address_space(4))) int32_t* Uniform;
     const int32_t n = ((Uniform)(uintptr_t)a.lens)[b];
@@ -208,18 +230,16 @@ __device__ __forceinline__ Part part_of(const Attend& a, uint32_t slot, uint32_t
         total += n;
         longest = n > longest ? n : longest;
     }
-    if (a.batch > 1)
-        for (int x = 1; x < 64; x *= 2) {
-            total += __shfl_xor(total, x);
-            const uint32_t o = __shfl_xor(longest, x);
-            longest = o > longest ? o : longest;
-        }
-    total = __builtin_amdgcn_readfirstlane(total);
-    longest = __builtin_amdgcn_readfirstlane(longest);
-    const uint32_t more = a.slots - a.batch;                // (sum of ceil(n / length) <= batch + sum of n / length)
-    uint32_t length = (total + more - 1) / more, least = (longest + kMostSplits - 1) / kMostSplits;
+    total = over_wave<false>(total);
+    longest = over_wave<true>(longest);
+    uint32_t length = (total + a.slots - 1) / a.slots, least = (longest + kMostSplits - 1) / kMostSplits;
     length = length > least ? length : least;
     length = length ? length : 1;
+    for (; length < longest; length += 1 + length / 16) {   // (at the longest, if not before, each sequence has one part)
+        uint32_t parts = 0;
+        for (uint32_t i = lane; i < a.batch; i += 64) { const uint32_t n = units_of(i); parts += n ? (n + length - 1) / length : 1; }
+        if (over_wave<false>(parts) <= a.slots) break;
+    }
     uint32_t before = 0;
     p.count = 0;                                            // (none: a slot beyond the last part)
     for (uint32_t i0 = 0; i0 < a.batch; i0 += 64) {
@@ -611,10 +631,10 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
     }
 }
 
-// Slots for the parts of all sequences: a slot a sequence, and as many more as give the chip its workgroups.
+// Slots for the parts of all sequences: one a sequence, or as many more as all fit the chip together.
 uint64_t slots_of(uint64_t batch, uint32_t kv_heads, uint64_t row_groups) {
     const uint64_t blocks = kv_heads * row_groups;
-    const uint64_t slots = batch * blocks >= kWantBlocks ? batch : batch + (kWantBlocks + blocks - 1) / blocks;
+    const uint64_t slots = batch * blocks >= kWantBlocks ? batch : kWantBlocks / blocks;
     return slots < batch * kMostSplits ? slots : batch * kMostSplits;
 }
 struct Scratch { uint64_t stats, part, bytes; };            // where the parts of the scratch memory begin
