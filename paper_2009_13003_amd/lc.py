@@ -523,11 +523,20 @@ class W4:
         assert codes.is_cuda and codes.dtype == torch.uint8 and codes.dim() == 2 and (codes.stride(1) == 1 or codes.shape[1] <= 1)
         assert scales.is_cuda and scales.dtype == torch.bfloat16 and scales.dim() == 2 and (scales.stride(1) == 1 or scales.shape[1] <= 1)
         assert codes.shape[0] == scales.shape[0] and codes.shape[1] >= lc_w4_row_bytes(k) and scales.shape[1] >= -(-k // group)
-        self.codes, self.scales, self.n, self.k, self.group = codes, scales, codes.shape[0], k, group
-        one = self.n == 1                                    # (the pitch of a single row says nothing)
-        self._c = _W4(codes.data_ptr() or None, scales.data_ptr() or None, self.n, k, lc_w4_row_bytes(k) if one else codes.stride(0),
-                      scales.shape[1] if one else scales.stride(0), group)
+        one = codes.shape[0] == 1                            # (the pitch of a single row says nothing)
+        self._describe(codes, scales, codes.shape[0], k, group, lc_w4_row_bytes(k) if one else codes.stride(0), scales.shape[1] if one else scales.stride(0))
+
+    def _describe(self, codes, scales, n, k, group, codes_pitch, scales_pitch):
+        self.codes, self.scales, self.n, self.k, self.group = codes, scales, n, k, group
+        self._c = _W4(codes.data_ptr() or None, scales.data_ptr() or None, n, k, codes_pitch, scales_pitch, group)
         self._p = ctypes.addressof(self._c)
+
+
+def _handle(stream):
+    """_stream for the calls below, which are made once a token: a plain number."""
+    if stream is None and _raw_current_stream is not None:
+        return _raw_current_stream(_current_device())
+    return _stream(stream).value
 
 
 def _matrix(t):
@@ -552,11 +561,19 @@ def lc_w4_quantize(w, group, out=None, stream=None):
     p, ld = _matrix(w)
     n, k = w.shape
     if out is None:
-        codes = _own(torch.empty(n, lc_w4_row_bytes(k), dtype=torch.uint8, device=w.device), stream)
-        scales = _own(torch.empty(n, -(-k // max(group, 1)), dtype=torch.bfloat16, device=w.device), stream)
-        out = W4(codes, scales, k, group)
-    assert out.n == n and out.k == k and out.group == group
-    st = _lib.lc_w4_quantize(p, ld, SERVED[w.dtype], out._p, _stream(stream))
+        if group not in (32, 64, 128):
+            raise LcError(ERR_BADARG)
+        row, groups, device = (k + 31) // 32 * 16, -(-k // group), w.device
+        codes = torch.empty(n, row, dtype=torch.uint8, device=device)
+        scales = torch.empty(n, groups, dtype=torch.bfloat16, device=device)
+        if stream is not None:
+            _own(codes, stream)
+            _own(scales, stream)
+        out = W4.__new__(W4)
+        out._describe(codes, scales, n, k, group, row, groups)
+    else:
+        assert out.n == n and out.k == k and out.group == group
+    st = _lib.lc_w4_quantize(p, ld, SERVED[w.dtype], out._p, _handle(stream))
     if st != OK:
         raise LcError(st)
     return out
@@ -565,10 +582,16 @@ def lc_w4_quantize(w, group, out=None, stream=None):
 def lc_w4_dequantize(w4, dtype=None, out=None, stream=None):
     """The values that w4 stands for, as a matrix of `dtype` (or in `out`)."""
     if out is None:
-        out = _own(torch.empty(w4.n, w4.k, dtype=dtype if dtype is not None else torch.float32, device=w4.codes.device), stream)
-    p, ld = _matrix(out)
-    assert out.shape == (w4.n, w4.k) and (dtype is None or out.dtype == dtype)
-    st = _lib.lc_w4_dequantize(w4._p, p, ld, SERVED[out.dtype], _stream(stream))
+        dtype = torch.float32 if dtype is None else dtype
+        out = torch.empty(w4.n, w4.k, dtype=dtype, device=w4.codes.device)
+        if stream is not None:
+            _own(out, stream)
+        p, ld = out.data_ptr(), w4.k
+    else:
+        p, ld = _matrix(out)
+        assert out.shape == (w4.n, w4.k) and (dtype is None or out.dtype == dtype)
+        dtype = out.dtype
+    st = _lib.lc_w4_dequantize(w4._p, p, ld, SERVED.get(dtype, -1), _handle(stream))
     if st != OK:
         raise LcError(st)
     return out
@@ -578,20 +601,20 @@ def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
     """x [m][k] times w4 [n][k] transposed, plus bias [n]: a matrix [m][n] of x's dtype (or in `out`)."""
     p, ld = _matrix(x)
     m, k = x.shape
-    dtype = x.dtype
+    dtype, n = x.dtype, w4.n
     assert k == w4.k
     if bias is not None:
-        assert bias.is_cuda and bias.dtype == dtype and bias.shape == (w4.n,) and (bias.stride(0) == 1 or w4.n <= 1)
+        assert bias.is_cuda and bias.dtype == dtype and bias.shape == (n,) and (bias.stride(0) == 1 or n <= 1)
         bias = bias.data_ptr()
     if out is None:
-        out = torch.empty(m, w4.n, dtype=dtype, device=x.device)
+        out = x.new_empty(m, n)
         if stream is not None:
             _own(out, stream)
-        q, ldq = out.data_ptr(), w4.n
+        q, ldq = out.data_ptr(), n
     else:
         q, ldq = _matrix(out)
-        assert out.shape == (m, w4.n) and out.dtype == dtype
-    st = _lib.lc_w4_matmul(p, ld, m, w4._p, bias, q, ldq, SERVED[dtype], _stream(stream))
+        assert out.shape == (m, n) and out.dtype == dtype
+    st = _lib.lc_w4_matmul(p, ld, m, w4._p, bias, q, ldq, SERVED[dtype], _handle(stream))
     if st != OK:
         raise LcError(st)
     return out
@@ -641,7 +664,8 @@ def _slots(slots, tokens):
 def lc_kv_write(cache, k, v, slots, stream=None):
     """Quantises k and v [tokens][heads][dim] into the cache at `slots` (int64 [tokens]; a negative one is passed over)."""
     ldt, ldh = _vectors(cache, k, v)
-    st = _lib.lc_kv_write(cache._p, k.data_ptr(), v.data_ptr(), ldt, ldh, _slots(slots, k.shape[0]), k.shape[0], SERVED[k.dtype], _stream(stream))
+    tokens = k.shape[0]
+    st = _lib.lc_kv_write(cache._p, k.data_ptr(), v.data_ptr(), ldt, ldh, _slots(slots, tokens), tokens, SERVED[k.dtype], _handle(stream))
     if st != OK:
         raise LcError(st)
 
@@ -650,14 +674,19 @@ def lc_kv_read(cache, slots, dtype=None, out=None, stream=None):
     """The keys and values [tokens][heads][dim] that the cache holds at `slots` (zeros for a slot outside), of `dtype` or in out = (k, v)."""
     tokens = slots.shape[0]
     if out is None:
-        k, v = torch.empty(2, tokens, cache.heads, cache.dim, dtype=dtype if dtype is not None else torch.float32, device=slots.device).unbind(0)
+        heads, dim, dtype = cache.heads, cache.dim, torch.float32 if dtype is None else dtype
+        k = torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device)
+        v = torch.empty_like(k)
         if stream is not None:
             _own(k, stream)
+            _own(v, stream)
+        ldt, ldh = heads * dim, dim
     else:
         k, v = out
         assert k.shape[0] == tokens and (dtype is None or k.dtype == dtype)
-    ldt, ldh = _vectors(cache, k, v)
-    st = _lib.lc_kv_read(cache._p, _slots(slots, tokens), tokens, k.data_ptr(), v.data_ptr(), ldt, ldh, SERVED[k.dtype], _stream(stream))
+        ldt, ldh = _vectors(cache, k, v)
+        dtype = k.dtype
+    st = _lib.lc_kv_read(cache._p, _slots(slots, tokens), tokens, k.data_ptr(), v.data_ptr(), ldt, ldh, SERVED.get(dtype, -1), _handle(stream))
     if st != OK:
         raise LcError(st)
     return k, v
@@ -696,7 +725,7 @@ def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None
     assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
     st = _lib.lc_kv_attend(cache._p, q.data_ptr(), batch, nq, heads, table.data_ptr(), table.stride(0) if batch > 1 else table.shape[1], table.shape[1],
                            lens.data_ptr(), mask, dim ** -0.5 if scale is None else scale, out.data_ptr(), SERVED[q.dtype], ws.data_ptr(), ws.numel(),
-                           _stream(stream))
+                           _handle(stream))
     if st != OK:
         raise LcError(st)
     return out
