@@ -62,6 +62,7 @@ __global__ __launch_bounds__(256) void k_kv_write(Cache c, const void* k, const 
     if (at == 0) (blockIdx.y ? c.v_scale : c.k_scale)[row] = s;
 }
 
+// A lane takes eight elements of a token's head, keys and values alike.
 template <int T, int BITS>
 __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, void* k, void* v, uint64_t ld_token, uint64_t ld_head, uint32_t lanes,
                                                  FastDiv by_row, FastDiv by_heads) {
@@ -70,22 +71,20 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
     const uint32_t item = by_row(lane), at = 8 * (lane - item * by_row.d);
     const uint32_t token = by_heads(item), head = item - token * c.heads;
     const int64_t slot = slots[token];
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float x[2][8] = {};
     if (slot >= 0 && (uint64_t)slot < c.slots) {
-        const uint64_t row = row_of(c, (uint64_t)slot >> c.page_shift, head, (uint32_t)slot & ((1u << c.page_shift) - 1));
-        const uint8_t* from = (blockIdx.y ? c.v : c.k) + row * c.row_bytes + at * BITS / 8;
-        const float s = (blockIdx.y ? c.v_scale : c.k_scale)[row];
-        if (BITS == 8) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(from);
+        const uint64_t row = row_of(c, (uint64_t)slot >> c.page_shift, head, (uint32_t)slot & ((1u << c.page_shift) - 1)), from = row * c.row_bytes + at * BITS / 8;
+        const float s[2] = {c.k_scale[row], c.v_scale[row]};
+        u32x2 w[2];
+        if (BITS == 8) { w[0] = *reinterpret_cast<const u32x2*>(c.k + from); w[1] = *reinterpret_cast<const u32x2*>(c.v + from); }
+        else { w[0][0] = *reinterpret_cast<const uint32_t*>(c.k + from); w[1][0] = *reinterpret_cast<const uint32_t*>(c.v + from); }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)(w[e / 4] >> (8 * (e % 4))) * s;
-        } else {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(from);
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)((int)(w >> (4 * e) & 15u) - 8) * s;
-        }
+            for (int e = 0; e < 8; ++e) x[n][e] = (BITS == 8 ? (float)(int8_t)(w[n][e / 4] >> (8 * (e % 4))) : (float)((int)(w[n][0] >> (4 * e) & 15u) - 8)) * s[n];
     }
-    store_eight<T>(blockIdx.y ? v : k, token * ld_token + head * ld_head + at, 8, x);
+    store_eight<T>(k, token * ld_token + head * ld_head + at, 8, x[0]);
+    store_eight<T>(v, token * ld_token + head * ld_head + at, 8, x[1]);
 }
 
 // ---------------------------------------------------------------- attention
@@ -688,7 +687,7 @@ void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* 
     for (uint64_t t = 0; t < tokens; t += step) {
         const uint32_t lanes = (uint32_t)((tokens - t < step ? tokens - t : step) * c.heads * (c.dim / 8));
         const uint64_t by = t * ld_token * (T == LC_F32 ? 4 : 2);
-        k_kv_read<T, BITS><<<dim3((lanes + 255) / 256, 2), 256, 0, s>>>(c, slots + t, static_cast<uint8_t*>(k) + by, static_cast<uint8_t*>(v) + by, ld_token,
+        k_kv_read<T, BITS><<<(lanes + 255) / 256, 256, 0, s>>>(c, slots + t, static_cast<uint8_t*>(k) + by, static_cast<uint8_t*>(v) + by, ld_token,
                                                                         ld_head, lanes, FastDiv(c.dim / 8), FastDiv(c.heads));
     }
 }
