@@ -62,29 +62,33 @@ __global__ __launch_bounds__(256) void k_kv_write(Cache c, const void* k, const 
     if (at == 0) (blockIdx.y ? c.v_scale : c.k_scale)[row] = s;
 }
 
-// A lane takes eight elements of a token's head, keys and values alike.
+template <int N> struct Bits;
+template <> struct Bits<16> { typedef uint16_t Type; };
+template <> struct Bits<32> { typedef uint32_t Type; };
+template <> struct Bits<64> { typedef uint64_t Type; };
+// A lane takes 16 bytes' worth of a token's head, keys and values alike.
 template <int T, int BITS>
 __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, void* k, void* v, uint64_t ld_token, uint64_t ld_head, uint32_t lanes,
                                                  FastDiv by_row, FastDiv by_heads) {
     const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
     if (lane >= lanes) return;
-    const uint32_t item = by_row(lane), at = 8 * (lane - item * by_row.d);
+    constexpr int N = kAtOnce<T>;
+    const uint32_t item = by_row(lane), at = N * (lane - item * by_row.d);
     const uint32_t token = by_heads(item), head = item - token * c.heads;
     const int64_t slot = slots[token];
-    float x[2][8] = {};
+    float x[2][N] = {};
     if (slot >= 0 && (uint64_t)slot < c.slots) {
+        typedef typename Bits<N * BITS>::Type Word;
         const uint64_t row = row_of(c, (uint64_t)slot >> c.page_shift, head, (uint32_t)slot & ((1u << c.page_shift) - 1)), from = row * c.row_bytes + at * BITS / 8;
         const float s[2] = {c.k_scale[row], c.v_scale[row]};
-        u32x2 w[2];
-        if (BITS == 8) { w[0] = *reinterpret_cast<const u32x2*>(c.k + from); w[1] = *reinterpret_cast<const u32x2*>(c.v + from); }
-        else { w[0][0] = *reinterpret_cast<const uint32_t*>(c.k + from); w[1][0] = *reinterpret_cast<const uint32_t*>(c.v + from); }
+        const uint64_t w[2] = {*reinterpret_cast<const Word*>(c.k + from), *reinterpret_cast<const Word*>(c.v + from)};
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[n][e] = (BITS == 8 ? (float)(int8_t)(w[n][e / 4] >> (8 * (e % 4))) : (float)((int)(w[n][0] >> (4 * e) & 15u) - 8)) * s[n];
+            for (int e = 0; e < N; ++e) x[n][e] = (BITS == 8 ? (float)(int8_t)(w[n] >> (8 * e)) : (float)((int)(w[n] >> (4 * e) & 15u) - 8)) * s[n];
     }
-    store_eight<T>(k, token * ld_token + head * ld_head + at, 8, x[0]);
-    store_eight<T>(v, token * ld_token + head * ld_head + at, 8, x[1]);
+    store_some<T>(k, token * ld_token + head * ld_head + at, N, x[0]);
+    store_some<T>(v, token * ld_token + head * ld_head + at, N, x[1]);
 }
 
 // ---------------------------------------------------------------- attention
@@ -683,12 +687,12 @@ void write(const Cache& c, const void* k, const void* v, uint64_t ld_token, uint
 }
 template <int T, int BITS>
 void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* v, uint64_t ld_token, uint64_t ld_head, hipStream_t s) {
-    const uint64_t step = (1ull << 25) / c.heads;
+    const uint64_t step = (1ull << 24) / c.heads;
     for (uint64_t t = 0; t < tokens; t += step) {
-        const uint32_t lanes = (uint32_t)((tokens - t < step ? tokens - t : step) * c.heads * (c.dim / 8));
+        const uint32_t lanes = (uint32_t)((tokens - t < step ? tokens - t : step) * c.heads * (c.dim / kAtOnce<T>));
         const uint64_t by = t * ld_token * (T == LC_F32 ? 4 : 2);
         k_kv_read<T, BITS><<<(lanes + 255) / 256, 256, 0, s>>>(c, slots + t, static_cast<uint8_t*>(k) + by, static_cast<uint8_t*>(v) + by, ld_token,
-                                                                        ld_head, lanes, FastDiv(c.dim / 8), FastDiv(c.heads));
+                                                                        ld_head, lanes, FastDiv(c.dim / kAtOnce<T>), FastDiv(c.heads));
     }
 }
 template <int T, int BITS, int DP, int NT, int PERSIMD>

@@ -38,19 +38,21 @@ __global__ __launch_bounds__(256) void k_w4_quantize(const void* w, uint64_t ldw
     if (at % LANES == 0) scales[row * scales_pitch + at / LANES] = (uint16_t)sb;
 }
 
-template <int T, int LANES>
+template <int T, int G>
 __global__ __launch_bounds__(256) void k_w4_dequantize(const uint8_t* codes, uint64_t codes_pitch, const uint16_t* scales, uint64_t scales_pitch,
                                                        void* w, uint64_t ldw, uint32_t rows, uint32_t k, uint32_t row_lanes, FastDiv div) {
+    constexpr int N = kAtOnce<T>;
     const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
     const uint32_t row = div(lane), at = lane - row * row_lanes;
-    const uint64_t col = 8ull * at;
+    const uint64_t col = (uint64_t)N * at;
     if (row >= rows || col >= k) return;
-    const uint32_t word = *reinterpret_cast<const uint32_t*>(codes + row * codes_pitch + 4ull * at);
-    const float s = of_bf16(scales[row * scales_pitch + at / LANES]);
-    float v[8];
+    const uint8_t* from = codes + row * codes_pitch + col / 2;
+    const uint32_t word = N == 8 ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from);
+    const float s = of_bf16(scales[row * scales_pitch + col / G]);
+    float v[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)((int)(word >> (4 * e) & 15u) - 8) * s;
-    store_eight<T>(w, row * ldw + col, (int)(k - col < 8 ? k - col : 8), v);
+    for (int e = 0; e < N; ++e) v[e] = (float)((int)(word >> (4 * e) & 15u) - 8) * s;
+    store_some<T>(w, row * ldw + col, (int)(k - col < N ? k - col : N), v);
 }
 
 // Launches over at most this many rows of `row_lanes` lanes at once, so that lanes are counted in 31 bits.
@@ -67,13 +69,13 @@ void quantize(const void* w, uint64_t ldw, const lc_w4& q, hipStream_t s) {
             static_cast<uint16_t*>(q.scales) + r * q.scales_pitch, q.scales_pitch, rows, (uint32_t)q.k, (uint32_t)lc_w4_row_bytes(q.k), lanes, FastDiv(lanes));
     }
 }
-template <int T, int LANES>
+template <int T, int G>
 void dequantize(const lc_w4& q, void* w, uint64_t ldw, hipStream_t s) {
-    const uint32_t lanes = (uint32_t)((q.k + 7) / 8);
+    const uint32_t lanes = (uint32_t)((q.k + kAtOnce<T> - 1) / kAtOnce<T>);
     const uint64_t step = rows_at_once(lanes);
     for (uint64_t r = 0; r < q.n; r += step) {
         const uint32_t rows = (uint32_t)(q.n - r < step ? q.n - r : step);
-        k_w4_dequantize<T, LANES><<<(uint32_t)(((uint64_t)rows * lanes + 255) / 256), 256, 0, s>>>(
+        k_w4_dequantize<T, G><<<(uint32_t)(((uint64_t)rows * lanes + 255) / 256), 256, 0, s>>>(
             static_cast<const uint8_t*>(q.codes) + r * q.codes_pitch, q.codes_pitch, static_cast<const uint16_t*>(q.scales) + r * q.scales_pitch,
             q.scales_pitch, static_cast<uint8_t*>(w) + r * ldw * (T == LC_F32 ? 4 : 2), ldw, rows, (uint32_t)q.k, lanes, FastDiv(lanes));
     }
@@ -600,7 +602,7 @@ int lc_w4_dequantize(const lc_w4* w4, void* w, uint64_t ldw, int dtype, void* st
     if (!w || off(w, size_of(dtype)) || ldw < w4->k || ldw > (1ull << 40)) return LC_ERR_BADARG;
     const lc_w4 q = *w4;
     hipStream_t s = static_cast<hipStream_t>(stream);
-#define CALL(T, G) dequantize<T, G / 8>(q, w, ldw, s)
+#define CALL(T, G) dequantize<T, G>(q, w, ldw, s)
     LC_BY_TYPE(CALL, dtype, q);
 #undef CALL
     return launched();
