@@ -269,7 +269,7 @@ __device__ __forceinline__ Part part_of(const Attend& a, uint32_t slot, uint32_t
     return p;
 }
 
-template <int T, int BITS, int DP, int NT, int PERSIMD>
+template <int T, int BITS, int DP, int NT, int DEEP, int PERSIMD>
 __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
     using Raw = InCache<BITS, DP>;
     constexpr bool HALF = Kind<T>::kHalf;
@@ -340,12 +340,15 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
             }
         }
     };
-    Raw raw;
-    Eights at = {};
+    Raw raw[DEEP];                                          // the tiles under way
+    Eights places[DEEP] = {};
     if (tiles > 0) {
-        at = find(0);
-        load_keys(raw, at);
-        load_values(raw, at);
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            places[d] = find(d);
+            load_keys(raw[d], places[d]);
+            load_values(raw[d], places[d]);
+        }
     }
 
     // this lane's queries, eight elements an operand at the places at which the keys' codes lie
@@ -395,11 +398,11 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
 #pragma unroll
         for (int j = 0; j < VD; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
     }
-    // Keys are spent once the scores are there, values once they are added up: then the next tile's are asked for, into the same registers.
-    for (int32_t i = 0; i < tiles; ++i) {
-        const Raw& f = raw;
+    // Keys are spent once the scores are there, values once they are added up: then those of the DEEP-th tile behind are asked for, into the
+    // same registers.
+    auto use = [&](Raw& f, Eights& at, int32_t i) {
         const int32_t tb = own + i * kWaves * kTile;
-        const Eights next = find(i + 1);
+        const Eights next = find(i + DEEP);
         f32x4 score[NT][2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
                     for (int n = 0; n < NT; ++n) score[n][s] = mfma_16<HALF>(key, q[n][o][p], score[n][s]);
             }
         }
-        load_keys(raw, next);
+        load_keys(f, next);
         float ks[8], vs[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -444,18 +447,16 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
         u32x4 pp[NT][NP];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float x[8];
+            float x[8], weight[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = score[n][i / 4][i % 4] * ks[i];
-            uint32_t seen = 0xff;
-            if (!whole) {
-                seen = 0;
+            for (int i = 0; i < 8; ++i) { x[i] = score[n][i / 4][i % 4] * ks[i]; weight[i] = vs[i]; }
+            if (!whole) {                                    // (what is not seen may have any scale)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int32_t t = tb + 16 * (i / 4) + 4 * h + i % 4, j = t - base;
-                    const bool there = at.there >> (2 * (i / 4) + h / 2) & 1;
-                    if (there && t < end && (j < 0 || (mask[n] >> (j & 63) & 1))) seen |= 1u << i;
-                    if (!(seen >> i & 1)) x[i] = -__builtin_inff();
+                    const bool there = at.there >> (2 * (i / 4) + h / 2) & 1, seen = there && t < end && (j < 0 || (mask[n] >> (j & 63) & 1));
+                    x[i] = seen ? x[i] : -__builtin_inff();
+                    weight[i] = seen ? weight[i] : 0.0f;
                 }
             }
             float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -475,11 +476,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
             for (int i = 0; i < 8; ++i) {
                 p[i] = __builtin_amdgcn_exp2f(x[i] - from);
                 sum[n] += p[i];
-                p[i] *= vs[i];
-            }
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = seen >> i & 1 ? p[i] : 0.0f;          // (what is not seen may have any scale)
+                p[i] *= weight[i];
             }
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
@@ -506,9 +503,13 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
                     for (int n = 0; n < NT; ++n) acc[n][o * Raw::kPerWord + j] = mfma_bf16(v, pp[n][k], acc[n][o * Raw::kPerWord + j]);
             }
         }
-        load_values(raw, next);
+        load_values(f, next);
         at = next;
-    }
+    };
+    for (int32_t i = 0; i < tiles; i += DEEP)
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d)
+            if (i + d < tiles) use(raw[d], places[d], i + d);
 
     // The wavefronts' parts, joined: lane (c, h) holds elements VD (4 h + r) + j of query c.
     const uint64_t heads_of = (uint64_t)a.nq * a.heads;
@@ -695,16 +696,16 @@ void read(const Cache& c, const int64_t* slots, uint64_t tokens, void* k, void* 
                                                                         ld_head, lanes, FastDiv(c.dim / kAtOnce<T>), FastDiv(c.heads));
     }
 }
-template <int T, int BITS, int DP, int NT, int PERSIMD>
+template <int T, int BITS, int DP, int NT, int DEEP, int PERSIMD>
 void attend_of(const Attend& a, hipStream_t s) {
-    k_kv_attend<T, BITS, DP, NT, PERSIMD><<<dim3(a.c.heads * ((a.rows + 16 * NT - 1) / (16 * NT)), a.slots), kWaves * 64, 0, s>>>(a);
+    k_kv_attend<T, BITS, DP, NT, DEEP, PERSIMD><<<dim3(a.c.heads * ((a.rows + 16 * NT - 1) / (16 * NT)), a.slots), kWaves * 64, 0, s>>>(a);
 }
 template <int T, int BITS>
 void attend(const Attend& a, hipStream_t s) {
     const bool two = tiles_of_rows(a.rows, (int)a.c.dim, T) == 2;
-    if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2, 2>(a, s) : attend_of<T, BITS, 64, 1, 3>(a, s);
-    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2, 2>(a, s) : attend_of<T, BITS, 128, 1, 2>(a, s);
-    else attend_of<T, BITS, 256, 1, 1>(a, s);
+    if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2, 2, 2>(a, s) : attend_of<T, BITS, 64, 1, 2, 3>(a, s);
+    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2, 2, 2>(a, s) : attend_of<T, BITS, 128, 1, 2, 2>(a, s);
+    else attend_of<T, BITS, 256, 1, 1, 1>(a, s);
 }
 
 }  // namespace

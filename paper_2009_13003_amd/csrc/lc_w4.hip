@@ -226,7 +226,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
     __shared__ float sums[WAVES][4][64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
     const uint32_t n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
-    const uint32_t steps = (p.k + 127) / 128;
+    const uint32_t steps = p.k / 128;                       // whole ones
     const uint8_t* codes[NT];
     const uint16_t* scales[NT];
 #pragma unroll
@@ -240,20 +240,19 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
     for (int m = 0; m < MT; ++m) x_row[m] = (m0 + 16 * m + c < p.m ? m0 + 16 * m + c : p.m - 1) * p.ldx;      // (a row beyond the last: any, its results go nowhere)
     struct Step { u32x4 w[NT]; uint16_t s[NT][GROUPS]; Raw<T> x[MT][4]; };
     Step ring[AHEAD];
-    auto fetch = [&](Step& f, uint32_t step) {
-        if ((step + 1) * 128 <= p.k) {
+    auto fetch = [&](Step& f, uint32_t step) {              // a whole step
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+        for (int n = 0; n < NT; ++n) {
+            f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + step * 128 + place<G>(h, i), 8);
-            return;
+            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
         }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + step * 128 + place<G>(h, i), 8);
+    };
+    auto fetch_rest = [&](Step& f, uint32_t step) {         // what is left behind the last whole one
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             f.w[n] = u32x4{0, 0, 0, 0};
@@ -326,6 +325,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
             }
         }
     }
+    if (p.k % 128 && wave == steps % WAVES) {
+        fetch_rest(ring[0], steps);
+        use(ring[0]);
+    }
 #pragma unroll
     for (int t = 0; t < MT * NT; ++t) {
         if (t) __syncthreads();
@@ -359,7 +362,7 @@ template <int T, int MT, int NT, int WM, int WN, int WK> struct Tile {
     static constexpr int kItems = kRows * WK * 16 / kThreads;            // eights of x a thread brings in at a time
     static_assert(kRows * WK * 16 % kThreads == 0, "whole items");
 };
-template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD, bool WHOLE>
+template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD>
 __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product p) {
     using L = Tile<T, MT, NT, WM, WN, WK>;
     constexpr int PARTS = L::kParts, PER = G / 32, GROUPS = 128 / G;
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
     const uint32_t wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
     const uint32_t n0 = blockIdx.x * L::kCols, m0 = blockIdx.y * L::kRows;
-    const uint32_t steps = (p.k + 127) / 128, rounds = (steps + WK - 1) / WK;
+    const uint32_t rounds = p.k / (128 * WK);               // whole ones
     const uint8_t* codes[NT];
     const uint16_t* scales[NT];
 #pragma unroll
@@ -377,20 +380,19 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
         scales[n] = p.scales + row * p.scales_pitch;
     }
     struct Step { u32x4 w[NT]; uint16_t s[NT][GROUPS]; };
-    auto fetch = [&](Step& f, uint32_t step) {
-        if (WHOLE || (step + 1) * 128 <= p.k) {
+    auto fetch = [&](Step& f, uint32_t step) {              // a whole step
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+        for (int n = 0; n < NT; ++n) {
+            f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
-            }
-            return;
+            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
         }
+    };
+    auto fetch_rest = [&](Step& f, uint32_t step) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             f.w[n] = u32x4{0, 0, 0, 0};
-            if (step < steps && step * 64 + h * 16 < p.row_bytes) f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
+            if (step * 64 + h * 16 < p.row_bytes) f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) f.s[n][g] = step * GROUPS + g < p.groups ? scales[n][step * GROUPS + g] : 0;
         }
@@ -402,9 +404,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
         const uint32_t item = threadIdx.x + i * L::kThreads, r = item / (WK * 16);
         x_from[i] = static_cast<const uint8_t*>(p.x) + ((m0 + r < p.m ? m0 + r : p.m - 1) * p.ldx + 8 * (item % (WK * 16))) * (T == LC_F32 ? 4 : 2);      // (a row beyond the last: any, its results go nowhere)
     }
-    auto bring = [&](Piece& next, uint32_t round) {
+    auto bring = [&](Piece& next, uint32_t round, bool whole) {
         const uint32_t from = round * WK * 128;
-        const bool whole = WHOLE || from + WK * 128 <= p.k;
 #pragma unroll
         for (int i = 0; i < L::kItems; ++i) {
             const uint32_t at = from + 8 * ((threadIdx.x + i * L::kThreads) % (WK * 16));
@@ -471,32 +472,42 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
     // Round r works on buffer r % 2 and on the codes that were asked for two rounds before; x of round r + 1 is put into the other buffer
     // behind it.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on, and the
     // last rounds ask for the last piece again instead of asking whether there is one: a branch there costs more than the loads.
-    const uint32_t last = rounds - 1;
     Piece next[DEEP];
     Step codes_of[2];
-    bring(next[0], 0);
-    fetch(codes_of[0], wk);
-    keep(next[0], 0);
-    fetch(codes_of[1], (last < 1 ? last : 1) * WK + wk);
-    bring(next[DEEP - 1], last < 1 ? last : 1);
-    if (DEEP == 2) bring(next[0], last < 2 ? last : 2);
-    __syncthreads();
     const uint8_t* x_at = held + (16 * MT * wm + c) * L::kPitch + wk * 256;
     const uint8_t* less_at = held + L::kLess + (wk * GROUPS * L::kRows + 16 * MT * wm + 4 * h) * 4;
-    uint32_t round = 0;
-    for (; round < last; round += 2) {
+    if (rounds) {
+        const uint32_t last = rounds - 1;
+        bring(next[0], 0, true);
+        fetch(codes_of[0], wk);
+        keep(next[0], 0);
+        fetch(codes_of[1], (last < 1 ? last : 1) * WK + wk);
+        bring(next[DEEP - 1], last < 1 ? last : 1, true);
+        if (DEEP == 2) bring(next[0], last < 2 ? last : 2, true);
+        __syncthreads();
+        uint32_t round = 0;
+        for (; round < last; round += 2) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            Piece& after = next[DEEP == 2 ? 1 - b : 0];
-            use(codes_of[b], x_at + b * L::kBuffer, less_at + b * L::kBuffer);
-            fetch(codes_of[b], (round + b + 2 < last ? round + b + 2 : last) * WK + wk);
-            keep(after, 1 - b);
-            bring(after, round + b + 1 + DEEP < last ? round + b + 1 + DEEP : last);
-            __syncthreads();
+            for (int b = 0; b < 2; ++b) {
+                Piece& after = next[DEEP == 2 ? 1 - b : 0];
+                use(codes_of[b], x_at + b * L::kBuffer, less_at + b * L::kBuffer);
+                fetch(codes_of[b], (round + b + 2 < last ? round + b + 2 : last) * WK + wk);
+                keep(after, 1 - b);
+                bring(after, round + b + 1 + DEEP < last ? round + b + 1 + DEEP : last, true);
+                __syncthreads();
+            }
         }
+        if (round == last) use(codes_of[0], x_at, less_at);
+        __syncthreads();
     }
-    if (round == last) use(codes_of[0], x_at, less_at);
-    __syncthreads();
+    if (p.k % (128 * WK)) {                                  // what is left behind the last whole round
+        bring(next[0], rounds, false);
+        fetch_rest(codes_of[0], rounds * WK + wk);
+        keep(next[0], 0);
+        __syncthreads();
+        use(codes_of[0], x_at, less_at);
+        __syncthreads();
+    }
     float* sums = reinterpret_cast<float*>(held);
     constexpr uint32_t kSumPitch = L::kCols + 4;
 #pragma unroll
@@ -534,22 +545,28 @@ void product_of_tiles(const Product& p, hipStream_t s) {
     using L = Tile<T, MT, NT, WM, WN, WK>;
     static_assert(L::kLds <= 160 * 1024, "LDS of a compute unit");
     const dim3 grid((p.n + L::kCols - 1) / L::kCols, (p.m + L::kRows - 1) / L::kRows);
-    if (p.k % (128 * WK) == 0) k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD, true><<<grid, L::kThreads, L::kLds, s>>>(p);
-    else k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, 1, false><<<grid, L::kThreads, L::kLds, s>>>(p);
+    k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD><<<grid, L::kThreads, L::kLds, s>>>(p);
 }
 
 template <int T, int G>
 void product(const Product& p, hipStream_t s) {
     const uint32_t steps = (p.k + 127) / 128;
     if (p.m > 16) {
-        // Tiles as large as still give every compute unit two workgroups (2048 rows by 4096x11008, us: 64 x 128 233, 64 x 64 338; 256 by
-        // 4096x4096: 37 and 30); few rows split the width over the wavefronts instead (32 rows by 4096x11008: 20).
-        if constexpr (T == LC_F32) product_of_tiles<T, G, 2, 2, 2, 2, 1, 1, 1>(p, s);
-        else {
-            const uint64_t blocks = (uint64_t)((p.m + 63) / 64) * ((p.n + 127) / 128);
+        // The smaller the tile, the more wavefronts share a tile's width: smaller tiles as long as they fit the chip in one go.  Measured, us
+        // (bf16, groups of 128): 64 rows by 4096x4096 in tiles of 32 x 32: 10.8, 32 x 64 14.1, 64 x 64 20.1, 64 x 128 36.9; 100 rows 20.1, 14.3, 20.1,
+        // 37.0; 256 rows 39.1, 27.3, 20.4, 36.8; 512 rows 76.5, 52.7, 39.1, 37.4; 32 by 4096x11008 in tiles of 32 x 16 20.3, 32 x 32 25.7.
+        // fp32, whose three parts take three times the LDS: 24 rows by 4096x4096 in tiles of 16 x 32 13.0, 32 x 64 23.8, 32 x 128 40.0; 100 rows 47.6,
+        // 24.1, 40.9; 256 rows 94.6, 46.9, 41.4; 1024 rows 373, 183, 115.
+        const auto fits = [&](uint32_t rows, uint32_t cols) { return (uint64_t)((p.m + rows - 1) / rows) * ((p.n + cols - 1) / cols) <= 256; };
+        if constexpr (T == LC_F32) {
+            if (fits(16, 32)) product_of_tiles<T, G, 1, 2, 1, 1, 4, 1, 1>(p, s);
+            else if (fits(32, 64)) product_of_tiles<T, G, 2, 1, 1, 4, 2, 1, 1>(p, s);
+            else product_of_tiles<T, G, 2, 2, 1, 4, 1, 1, 1>(p, s);
+        } else {
             if (p.m <= 32) product_of_tiles<T, G, 2, 1, 1, 1, 8, 1, 1>(p, s);
-            else if (p.m <= 64) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
-            else if (blocks < 512) product_of_tiles<T, G, 2, 2, 2, 2, 1, 1, 2>(p, s);
+            else if (fits(32, 32)) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
+            else if (fits(32, 64)) product_of_tiles<T, G, 2, 2, 1, 2, 4, 1, 1>(p, s);
+            else if (fits(64, 64)) product_of_tiles<T, G, 4, 1, 1, 4, 2, 1, 1>(p, s);
             else product_of_tiles<T, G, 4, 2, 1, 4, 1, 1, 2>(p, s);
         }
         return;
