@@ -217,133 +217,136 @@ template <int G> __device__ __forceinline__ u32x4 words_in_order(u32x4 w) {
 }
 template <int G> __device__ __forceinline__ uint32_t place(uint32_t h, uint32_t i) { return G == 128 ? 32 * h + 8 * i : 32 * i + 8 * h; }
 
-// Up to 16 MT rows of x by 16 NT rows of w a workgroup; its wavefronts take the width in turn, 128 elements (64 bytes of a row of codes)
-// at a time, and their sums meet in LDS.  Columns of the matrix instruction are rows of w, so a lane's four results share a scale.
-// x comes straight from memory into the operands, by every wavefront the part of the width that it works on.
-template <int T, int G, int MT, int NT, int WAVES, int AHEAD>
-__global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p) {
+// Few rows: up to 16 rows of x by 16 rows of w a workgroup; each wavefront has a part of the width of its own, `per` steps of 128 elements
+// (64 bytes of a row of codes), and their sums meet in LDS.  Columns of the matrix instruction are rows of w, so a lane's four results
+// share a scale.  S steps are asked for at once: 16 bytes of codes a lane and step, the scales of all S in one load, and x row by row, whole
+// lines, put into a piece of LDS of the wavefront's own and read from there as operands.  (Operands straight from memory and a scale at a
+// time, one row by 11008x4096: 10.0 us, of which the loads of x took 2.4 and those of scales 1.8; a bare read of the codes takes 4.9, of which
+// 2.3 are the launch.)
+template <int T, int MR, int WAVES, int S> struct Rows {
+    static constexpr int kSize = T == LC_F32 ? 4 : 2, kBytes = S * 128 * kSize, kPitch = kBytes + 16, kLoads = MR * kBytes / 1024;
+    static_assert(MR * kBytes % 1024 == 0, "whole loads");
+    static uint32_t lds(uint32_t rows) { const uint32_t x = WAVES * rows * kPitch, sums = WAVES * 1024; return x > sums ? x : sums; }
+};
+template <int T, int G, int MR, int WAVES, int S>
+__global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per) {
+    using L = Rows<T, MR, WAVES, S>;
     constexpr int PARTS = Num<T>::kParts, PER = G / 32, GROUPS = 128 / G;
-    __shared__ float sums[WAVES][4][64];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
-    const uint32_t n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
+    extern __shared__ __align__(16) uint8_t held[];
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 16, h = lane / 16;
+    const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * MR;
+    const uint32_t rows = p.m - m0 < MR ? p.m - m0 : MR;
     const uint32_t steps = p.k / 128;                       // whole ones
-    const uint8_t* codes[NT];
-    const uint16_t* scales[NT];
+    const uint32_t begin = wave * per, end = begin + per < steps ? begin + per : steps;
+    const uint32_t row = n0 + c < p.n ? n0 + c : p.n - 1;
+    const uint8_t* codes = p.codes + row * p.codes_pitch + 16 * h;
+    const uint16_t* scales = p.scales + row * p.scales_pitch;
+    uint8_t* own = held + wave * rows * L::kPitch;
+    const uint8_t* x_at = own + (c < rows ? c : 0) * L::kPitch;      // (a row beyond the last: any, its results go nowhere)
+    struct Batch { u32x4 w[S]; uint16_t s[S * GROUPS]; u32x4 x[L::kLoads]; };
+    auto fetch = [&](Batch& f, uint32_t first) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint32_t row = n0 + 16 * n + c < p.n ? n0 + 16 * n + c : p.n - 1;
-        codes[n] = p.codes + row * p.codes_pitch + 16 * h;
-        scales[n] = p.scales + row * p.scales_pitch;
-    }
-    uint64_t x_row[MT];
+        for (int i = 0; i < S; ++i)
+            if (first + i < end) f.w[i] = *reinterpret_cast<const u32x4*>(codes + (first + i) * 64);
+        if (first + S <= end) __builtin_memcpy(f.s, scales + first * GROUPS, sizeof(f.s));
+        else {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) x_row[m] = (m0 + 16 * m + c < p.m ? m0 + 16 * m + c : p.m - 1) * p.ldx;      // (a row beyond the last: any, its results go nowhere)
-    struct Step { u32x4 w[NT]; uint16_t s[NT][GROUPS]; Raw<T> x[MT][4]; };
-    Step ring[AHEAD];
-    auto fetch = [&](Step& f, uint32_t step) {              // a whole step
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = scales[n][step * GROUPS + g];
+            for (int g = 0; g < S * GROUPS; ++g)
+                if (first * GROUPS + g < end * GROUPS) f.s[g] = scales[first * GROUPS + g];
         }
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + step * 128 + place<G>(h, i), 8);
-    };
-    auto fetch_rest = [&](Step& f, uint32_t step) {         // what is left behind the last whole one
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            f.w[n] = u32x4{0, 0, 0, 0};
-            if (step * 64 + h * 16 < p.row_bytes) f.w[n] = *reinterpret_cast<const u32x4*>(codes[n] + step * 64);
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) f.s[n][g] = step * GROUPS + g < p.groups ? scales[n][step * GROUPS + g] : 0;
+        for (int l = 0; l < L::kLoads; ++l) {
+            const uint32_t at = (l * 64 + lane) * 16, r = at / L::kBytes, b = at % L::kBytes;
+            if (r < rows && b < (end - first) * 128 * L::kSize)
+                f.x[l] = load_any<u32x4>(static_cast<const uint8_t*>(p.x) + ((m0 + r) * p.ldx + first * 128) * L::kSize + b);
         }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = step * 128 + place<G>(h, i);
-                f.x[m][i] = x_as_it_is<T>(p.x, x_row[m] + at, at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
-            }
     };
-    f32x4 total[MT][NT];
+    auto keep = [&](const Batch& f) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) total[m][n] = f32x4{0, 0, 0, 0};
-    auto use = [&](const Step& f) {
-        u32x4 w[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) w[n] = words_in_order<G>(f.w[n]);
+        for (int l = 0; l < L::kLoads; ++l) {
+            const uint32_t at = (l * 64 + lane) * 16, r = at / L::kBytes, b = at % L::kBytes;
+            if (r < rows) *reinterpret_cast<u32x4*>(own + r * L::kPitch + b) = f.x[l];
+        }
+    };
+    f32x4 total = {0, 0, 0, 0};
+    auto use = [&](u32x4 codes16, const uint16_t (&s)[GROUPS], const Raw<T> (&raw)[4]) {
+        const u32x4 w = words_in_order<G>(codes16);
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-            f32x4 less[MT];
-            Operand<T> x[MT][PER];
+            f32x4 acc = {0, 0, 0, 0};
+            Operand<T> x[PER];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                less[m] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < PER; ++i) {
+                x[i] = x_as_operand<T>(raw[g * PER + i]);
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    x[m][i] = x_as_operand<T>(f.x[m][g * PER + i]);
-#pragma unroll
-                    for (int q = PARTS - 1; q >= 0; --q) less[m] = less_of<T>(x[m][i].part[q], less[m]);
-                }
+                for (int q = PARTS - 1; q >= 0; --q) acc = less_of<T>(x[i].part[q], acc);
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                f32x4 acc[MT];
+            for (int i = 0; i < PER; ++i) {
+                const u32x4 b = codes_as_operand<T>(w[g * PER + i]);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) acc[m] = less[m];
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const u32x4 b = codes_as_operand<T>(w[n][g * PER + i]);
-#pragma unroll
-                    for (int q = PARTS - 1; q >= 0; --q)
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) acc[m] = Num<T>::mfma(x[m][i].part[q], b, acc[m]);
-                }
-                const float s = of_bf16(f.s[n][g]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) total[m][n][r] = fmaf(acc[m][r], s, total[m][n][r]);
+                for (int q = PARTS - 1; q >= 0; --q) acc = Num<T>::mfma(x[i].part[q], b, acc);
             }
+            const float scale = of_bf16(s[g]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) total[r] = fmaf(acc[r], scale, total[r]);
         }
     };
+    auto use_batch = [&](const Batch& f, uint32_t first) {
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
-        if (wave + a * WAVES < steps) fetch(ring[a], wave + a * WAVES);
-    for (uint32_t step = wave; step < steps; step += AHEAD * WAVES) {
+        for (int i = 0; i < S; ++i) {
+            if (first + i >= end) break;
+            Raw<T> raw[4];
+            uint16_t s[GROUPS];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {                    // (each step's registers stay its own: moved on, they would have to be waited for)
-            const uint32_t now = step + a * WAVES;
-            if (now < steps) {
-                use(ring[a]);
-                if (now + AHEAD * WAVES < steps) fetch(ring[a], now + AHEAD * WAVES);
-            }
+            for (int g = 0; g < GROUPS; ++g) s[g] = f.s[i * GROUPS + g];
+#pragma unroll
+            for (int o = 0; o < 4; ++o)
+#pragma unroll
+                for (int q = 0; q < L::kSize / 2; ++q)
+                    raw[o].w[q] = *reinterpret_cast<const u32x4*>(x_at + (i * 128 + place<G>(h, o)) * L::kSize + 16 * q);
+            use(f.w[i], s, raw);
+        }
+    };
+    // (Each set of registers keeps its own loads: moved on to another, they would have to be waited for.)
+    Batch two[2];
+    if (begin < end) fetch(two[0], begin);
+    for (uint32_t first = begin; first < end; first += 2 * S) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const uint32_t now = first + b * S;
+            if (now >= end) break;
+            keep(two[b]);
+            if (now + S < end) fetch(two[1 - b], now + S);
+            use_batch(two[b], now);
         }
     }
-    if (p.k % 128 && wave == steps % WAVES) {
-        fetch_rest(ring[0], steps);
-        use(ring[0]);
-    }
+    if (p.k % 128 && wave == WAVES - 1) {                    // what is left behind the last whole step, straight from memory
+        u32x4 w = {0, 0, 0, 0};
+        if (steps * 64 + h * 16 < p.row_bytes) w = *reinterpret_cast<const u32x4*>(codes + steps * 64);
+        uint16_t s[GROUPS];
 #pragma unroll
-    for (int t = 0; t < MT * NT; ++t) {
-        if (t) __syncthreads();
+        for (int g = 0; g < GROUPS; ++g) s[g] = steps * GROUPS + g < p.groups ? scales[steps * GROUPS + g] : 0;
+        Raw<T> raw[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][r][lane] = total[t / NT][t % NT][r];
-        __syncthreads();
-        for (uint32_t e = threadIdx.x; e < 256; e += WAVES * 64) {
-            const uint32_t i = m0 + 16 * (t / NT) + 4 * (e / 64) + e % 64 / 16, j = n0 + 16 * (t % NT) + e % 16;      // neighbours write neighbours
-            const uint32_t from = (e / 64) * 16 + e % 16, r = e % 64 / 16;
-            if (i >= p.m || j >= p.n) continue;
-            float v = 0;
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) v += sums[q][r][from];
-            finish<T, G>(p, i, j, v);
+        for (int o = 0; o < 4; ++o) {
+            const uint32_t at = steps * 128 + place<G>(h, o);
+            raw[o] = x_as_it_is<T>(p.x, (m0 + (c < rows ? c : 0)) * p.ldx + at, at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
         }
+        use(w, s, raw);
+    }
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(held);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sums[(wave * 4 + r) * 64 + lane] = total[r];
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < 16 * rows; e += WAVES * 64) {                 // neighbours write neighbours
+        const uint32_t i = e / 16, j = e % 16;
+        if (n0 + j >= p.n) continue;
+        float v = 0;
+#pragma unroll
+        for (int q = 0; q < WAVES; ++q) v += sums[(q * 4 + i % 4) * 64 + i / 4 * 16 + j];
+        finish<T, G>(p, m0 + i, n0 + j, v);
     }
 }
 
@@ -535,9 +538,10 @@ __global__ __launch_bounds__(256) void k_w4_bias_only(Product p) {      // k = 0
     store_one<T>(p.y, i * p.ldy + j, p.bias ? load_one<T>(p.bias, j) : 0.0f);
 }
 
-template <int T, int G, int MT, int NT, int WAVES, int AHEAD>
+template <int T, int G, int MR, int WAVES, int S>
 void product_of_rows(const Product& p, hipStream_t s) {
-    k_w4_rows<T, G, MT, NT, WAVES, AHEAD><<<dim3((p.n + 16 * NT - 1) / (16 * NT), (p.m + 16 * MT - 1) / (16 * MT)), WAVES * 64, 0, s>>>(p);
+    const uint32_t steps = p.k / 128, rows = p.m < MR ? p.m : MR;
+    k_w4_rows<T, G, MR, WAVES, S><<<dim3((p.n + 15) / 16, (p.m + MR - 1) / MR), WAVES * 64, Rows<T, MR, WAVES, S>::lds(rows), s>>>(p, (steps + WAVES - 1) / WAVES);
 }
 
 template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD>
@@ -548,9 +552,22 @@ void product_of_tiles(const Product& p, hipStream_t s) {
     k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD><<<grid, L::kThreads, L::kLds, s>>>(p);
 }
 
+// More wavefronts a workgroup where there are few workgroups, as long as each has some steps to go, and two steps at a time where that leaves
+// enough wavefronts to a SIMD.  Measured with 4, 8 and 16 wavefronts a workgroup, us: one row by 4096x4096 (bf16, groups of 128) 4.6, 4.3, 4.4, by
+// 11008x4096 7.8, 8.9, 11.5, by 8192x8192 10.6, 9.6, 13.1, by 32000x4096 (groups of 32) 20.0, 21.6, 28.7, by 4096x11008 (32) 11.8, 9.0, 8.0; 13 rows
+// there 19.5, 12.5, 11.0; one row by 4096x4096 in fp32 8.8, 6.9, 6.9, 16 rows by 11008x4096 20.6, 24.4, 47.5.  Two steps instead of one: 11008x4096
+// 7.8 for 8.7 with 4 wavefronts, 8192x8192 9.6 for 11.0 with 8; but in groups of 32 32000x4096 21.1 for 20.0.
+template <int T, int G, int MR>
+void product_of_few(const Product& p, hipStream_t s) {
+    constexpr int FOUR = T != LC_F32 && G == 128 ? 2 : 1, EIGHT = T != LC_F32 && G == 128 && MR == 4 ? 2 : 1;
+    const uint32_t blocks = (p.n + 15) / 16;
+    if (T != LC_F32 && blocks <= 256 && p.k >= 8192) product_of_rows<T, G, MR, 16, 1>(p, s);
+    else if (blocks <= 512) product_of_rows<T, G, MR, 8, EIGHT>(p, s);
+    else product_of_rows<T, G, MR, 4, FOUR>(p, s);
+}
+
 template <int T, int G>
 void product(const Product& p, hipStream_t s) {
-    const uint32_t steps = (p.k + 127) / 128;
     if (p.m > 16) {
         // The smaller the tile, the more wavefronts share a tile's width: smaller tiles as long as they fit the chip in one go.  Measured, us
         // (bf16, groups of 128): 64 rows by 4096x4096 in tiles of 32 x 32: 10.8, 32 x 64 14.1, 64 x 64 20.1, 64 x 128 36.9; 100 rows 20.1, 14.3, 20.1,
@@ -571,8 +588,8 @@ void product(const Product& p, hipStream_t s) {
         }
         return;
     }
-    if (steps <= 4) product_of_rows<T, G, 1, 1, 4, 1>(p, s);
-    else product_of_rows<T, G, 1, 1, 8, 1>(p, s);
+    if (p.m <= 4) product_of_few<T, G, 4>(p, s);
+    else product_of_few<T, G, 16>(p, s);
 }
 
 // Whether a matrix in 4 bits is one the kernels can take.
