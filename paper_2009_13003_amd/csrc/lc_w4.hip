@@ -352,27 +352,45 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per)
 
 // More rows: a tile of 16 MT WM rows of x by 16 NT WN rows of w a workgroup of WM x WN x WK wavefronts, WK of them on different parts of the
 // width.  x passes through LDS, 128 WK elements of the width at a time, twice buffered: the next piece is under way in registers while this
-// one is worked on.  Codes come straight into registers and are unpacked by the wavefront that needs them.
+// one is worked on, and goes into the other buffer between two of the products of this one: what puts it there then waits in the products' shade.
+// Codes come straight into registers and are unpacked by the wavefront that needs them.
+// 2048 rows by 4096x11008 (bf16, groups of 128): 226 us, 816 TFLOP/s, 191 on constant data; a plain product of bf16 by the library takes 164.  x put
+// away behind all products 261; matrix instructions are under way a third of the time, vector instructions half of it: unpacking eight codes takes
+// eight of them and a scale one for each four sums, and the two share a wavefront's turn.  More loads ahead (three buffers, two pieces in registers)
+// cost the third wavefront a SIMD and were slower.
 template <int T, int MT, int NT, int WM, int WN, int WK> struct Tile {
     static constexpr int kThreads = 64 * WM * WN * WK, kRows = 16 * MT * WM, kCols = 16 * NT * WN, kParts = Num<T>::kParts;
-    static constexpr uint32_t kPitch = WK * 256 + 16, kPart = kRows * kPitch;       // 16 bytes beside a multiple of 256: sixteen rows in sixteen bank groups
-    // What is taken away: where several wavefronts work on the same rows of x, added up once by those who bring x in; else by each for itself, by
-    // the matrix instruction.  (2048 rows by 4096x11008 in tiles of 64 x 128: 233 us instead of 250; 32 rows in tiles of 32 x 16: 24.4 instead of 20.3.)
-    static constexpr bool kAdded = WN > 1;
-    static constexpr uint32_t kLess = kParts * kPart, kBuffer = kLess + WK * 4 * kRows * 4;      // behind x what is taken away for each of (at most four) groups and rows
+    // Of 128 elements of the width, kLanes threads bring in a row's, and each kEach rows'.
+    static constexpr int kLanes = WN > MT ? 4 * WN / MT : 4, kEach = kLanes * MT / (4 * WN), kItems = 16 / kLanes;
+    static_assert(kEach * 4 * WN == kLanes * MT && (kLanes == 4 || kLanes == 8), "whole items");
+    // In LDS they stand by fours of eights, and a four by rows, an eight's place in it crossed with the row's number: both the sixteen lanes that put
+    // four rows' eights there and the lanes that read sixteen rows' find all banks, whatever four they read.  (By rows of 272 bytes a third of the
+    // cycles that LDS was busy went on conflicts.)
+    static constexpr uint32_t kFour = kRows * 64, kPart = WK * 4 * kFour;
+    static __device__ uint32_t place_of(uint32_t r, uint32_t four, uint32_t eight) { return four * kFour + r * 64 + 16 * (eight ^ (r / 4 % 4)); }
+    static constexpr uint32_t kLess = kParts * kPart, kBuffer = kLess + WK * 4 * kRows * 4;      // behind x what is taken away for each of (at most four) groups and rows, added up by those who bring x in
     static constexpr uint32_t kSums = WK * kRows * (kCols + 4) * 4;
     static constexpr uint32_t kLds = 2 * kBuffer > kSums ? 2 * kBuffer : kSums;
-    static constexpr int kItems = kRows * WK * 16 / kThreads;            // eights of x a thread brings in at a time
-    static_assert(kRows * WK * 16 % kThreads == 0, "whole items");
 };
-template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD>
+// Which tile a workgroup takes.  Workgroups go round the eight dies, each with an L2 of its own: each die has one stretch of the tiles, ordered down
+// panels of kPanel tiles' height, so that those it works on at a time share both rows of x and rows of w.
+struct TileAt { uint32_t across, down; };
+__device__ __forceinline__ TileAt tile_of(uint32_t wide, uint32_t high) {
+    constexpr uint32_t kDies = 8, kPanel = 4;
+    const uint32_t tiles = wide * high, die = blockIdx.x % kDies, each = tiles / kDies, more = tiles % kDies;
+    const uint32_t t = die * each + (die < more ? die : more) + blockIdx.x / kDies;
+    const uint32_t panel = t / (kPanel * wide), in = t - panel * kPanel * wide, tall = high - panel * kPanel < kPanel ? high - panel * kPanel : kPanel;
+    return {in / tall, panel * kPanel + in % tall};
+}
+template <int T, int G, int MT, int NT, int WM, int WN, int WK, int PERSIMD>
 __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product p) {
     using L = Tile<T, MT, NT, WM, WN, WK>;
     constexpr int PARTS = L::kParts, PER = G / 32, GROUPS = 128 / G;
     extern __shared__ __align__(16) uint8_t held[];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
     const uint32_t wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
-    const uint32_t n0 = blockIdx.x * L::kCols, m0 = blockIdx.y * L::kRows;
+    const auto [across, down] = tile_of((p.n + L::kCols - 1) / L::kCols, (p.m + L::kRows - 1) / L::kRows);
+    const uint32_t n0 = across * L::kCols, m0 = down * L::kRows;
     const uint32_t rounds = p.k / (128 * WK);               // whole ones
     const uint8_t* codes[NT];
     const uint16_t* scales[NT];
@@ -400,31 +418,46 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
             for (int g = 0; g < GROUPS; ++g) f.s[n][g] = step * GROUPS + g < p.groups ? scales[n][step * GROUPS + g] : 0;
         }
     };
-    struct Piece { Raw<T> x[L::kItems]; };
-    const uint8_t* x_from[L::kItems];
+    struct Piece { Raw<T> x[L::kEach][L::kItems]; };
+    const uint32_t own = threadIdx.x % L::kLanes;
+    const uint8_t* x_from[L::kEach];
+    uint32_t first[L::kEach], row_of[L::kEach];
 #pragma unroll
-    for (int i = 0; i < L::kItems; ++i) {
-        const uint32_t item = threadIdx.x + i * L::kThreads, r = item / (WK * 16);
-        x_from[i] = static_cast<const uint8_t*>(p.x) + ((m0 + r < p.m ? m0 + r : p.m - 1) * p.ldx + 8 * (item % (WK * 16))) * (T == LC_F32 ? 4 : 2);      // (a row beyond the last: any, its results go nowhere)
+    for (int u = 0; u < L::kEach; ++u) {
+        const uint32_t unit = threadIdx.x / L::kLanes + u * (L::kThreads / L::kLanes), r = unit % L::kRows;
+        row_of[u] = r, first[u] = unit / L::kRows * 128 + 8 * own;
+        x_from[u] = static_cast<const uint8_t*>(p.x) + ((m0 + r < p.m ? m0 + r : p.m - 1) * p.ldx + first[u]) * (T == LC_F32 ? 4 : 2);      // (a row beyond the last: any, its results go nowhere)
     }
     auto bring = [&](Piece& next, uint32_t round, bool whole) {
         const uint32_t from = round * WK * 128;
 #pragma unroll
-        for (int i = 0; i < L::kItems; ++i) {
-            const uint32_t at = from + 8 * ((threadIdx.x + i * L::kThreads) % (WK * 16));
-            next.x[i] = x_as_it_is<T>(x_from[i], from, whole ? 8 : at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
-        }
+        for (int u = 0; u < L::kEach; ++u)
+#pragma unroll
+            for (int i = 0; i < L::kItems; ++i) {
+                const uint32_t at = from + first[u] + 8 * L::kLanes * i;
+                next.x[u][i] = x_as_it_is<T>(x_from[u], from + 8 * L::kLanes * i, whole ? 8 : at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
+            }
     };
     auto keep = [&](const Piece& next, uint32_t buffer) {
+        uint8_t* to = held + buffer * L::kBuffer;
 #pragma unroll
-        for (int i = 0; i < L::kItems; ++i) {
-            const uint32_t item = threadIdx.x + i * L::kThreads, r = item / (WK * 16), at = item % (WK * 16);
-            const Operand<T> x = x_as_operand<T>(next.x[i]);
+        for (int u = 0; u < L::kEach; ++u) {
+            const uint32_t at = L::place_of(row_of[u], first[u] / 32, own % 4);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4*>(held + buffer * L::kBuffer + q * L::kPart + r * L::kPitch + at * 16) = x.part[q];
-            if (!L::kAdded) continue;
-            const float taken = Num<T>::kTaken * sum_of_lanes<G / 8>(sum_of<T>(next.x[i]));
-            *reinterpret_cast<float*>(held + buffer * L::kBuffer + L::kLess + (at / (G / 8) * L::kRows + r) * 4) = taken;     // (a group's lanes all write it: no branch)
+            for (int i = 0; i < L::kItems; ++i) {
+                const Operand<T> x = x_as_operand<T>(next.x[u][i]);
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4*>(to + q * L::kPart + at + L::kLanes / 4 * i * L::kFour) = x.part[q];
+            }
+            constexpr int EIGHTS = G / 8, TOGETHER = EIGHTS > L::kLanes ? EIGHTS / L::kLanes : 1;
+#pragma unroll
+            for (int i = 0; i < L::kItems; i += TOGETHER) {
+                float sum = 0;
+#pragma unroll
+                for (int t = 0; t < TOGETHER; ++t) sum += sum_of<T>(next.x[u][i + t]);
+                const float taken = Num<T>::kTaken * sum_of_lanes<(EIGHTS < L::kLanes ? EIGHTS : L::kLanes)>(sum);
+                *reinterpret_cast<float*>(to + L::kLess + ((first[u] + 8 * L::kLanes * i) / G * L::kRows + row_of[u]) * 4) = taken;      // (a group's lanes all write it: no branch)
+            }
         }
     };
     f32x4 total[MT][NT];
@@ -432,83 +465,92 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) total[m][n] = f32x4{0, 0, 0, 0};
-    auto use = [&](const Step& f, const uint8_t* x_at, const uint8_t* less_at) {
+    uint32_t at_eight[G == 128 ? 4 : 1];                    // where the eights of the lane stand in LDS
+#pragma unroll
+    for (int o = 0; o < (G == 128 ? 4 : 1); ++o) at_eight[o] = L::place_of(16 * MT * wm + c, 4 * wk + (G == 128 ? h : 0), G == 128 ? o : h);
+    auto use = [&](const Step& f, const uint8_t* x_at, const uint8_t* less_at, auto meanwhile) {
         u32x4 w[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) w[n] = words_in_order<G>(f.w[n]);
+        u32x4 x[2][MT][PARTS];
+        auto read = [&](u32x4 (&to)[MT][PARTS], int o) {
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            f32x4 less[MT];
-            u32x4 x[MT][PER][PARTS];
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                less[m] = L::kAdded ? *reinterpret_cast<const f32x4*>(less_at + (g * L::kRows + 16 * m) * 4) : f32x4{0, 0, 0, 0};
+                for (int q = 0; q < PARTS; ++q) to[m][q] = *reinterpret_cast<const u32x4*>(x_at + (G == 128 ? at_eight[o] : at_eight[0] + o * L::kFour) + m * 1024 + q * L::kPart);
+        };
+        read(x[0], 0);
+        f32x4 acc[NT][MT];
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
+        for (int o = 0; o < 4; ++o) {                       // eights of the width, the next one's x on its way while one is worked on
+            const int g = o / PER;
+            if (o < 3) read(x[(o + 1) % 2], o + 1);
+            if (o % PER == 0) {
+                f32x4 less[MT];
 #pragma unroll
-                    for (int q = PARTS - 1; q >= 0; --q) {
-                        x[m][i][q] = *reinterpret_cast<const u32x4*>(x_at + 16 * m * L::kPitch + q * L::kPart + 2 * place<G>(h, g * PER + i));
-                        if (!L::kAdded) less[m] = less_of<T>(x[m][i][q], less[m]);
-                    }
+                for (int m = 0; m < MT; ++m) {
+                    less[m] = *reinterpret_cast<const f32x4*>(less_at + (g * L::kRows + 16 * m) * 4);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][m] = less[m];
+                }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                f32x4 acc[MT];
+                const u32x4 b = codes_as_operand<T>(w[n][o]);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) acc[m] = less[m];
+                for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const u32x4 b = codes_as_operand<T>(w[n][g * PER + i]);
+                    for (int m = 0; m < MT; ++m) acc[n][m] = Num<T>::mfma(x[o % 2][m][q], b, acc[n][m]);
+            }
+            __builtin_amdgcn_sched_barrier(0);              // (else all reads of x come first, and their registers)
+            if (o == 1) meanwhile();
+            if (o % PER == PER - 1) {
 #pragma unroll
-                    for (int q = PARTS - 1; q >= 0; --q)
+                for (int n = 0; n < NT; ++n) {
+                    const float s = of_bf16(f.s[n][g]);
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) acc[m] = Num<T>::mfma(x[m][i][q], b, acc[m]);
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) total[m][n][r] = fmaf(acc[n][m][r], s, total[m][n][r]);
                 }
-                const float s = of_bf16(f.s[n][g]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) total[m][n][r] = fmaf(acc[m][r], s, total[m][n][r]);
             }
         }
     };
     // Round r works on buffer r % 2 and on the codes that were asked for two rounds before; x of round r + 1 is put into the other buffer
-    // behind it.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on, and the
+    // meanwhile.  Two rounds are written out, so that every set of registers keeps its own loads and none has to be moved on, and the
     // last rounds ask for the last piece again instead of asking whether there is one: a branch there costs more than the loads.
-    Piece next[DEEP];
+    Piece next;
     Step codes_of[2];
-    const uint8_t* x_at = held + (16 * MT * wm + c) * L::kPitch + wk * 256;
     const uint8_t* less_at = held + L::kLess + (wk * GROUPS * L::kRows + 16 * MT * wm + 4 * h) * 4;
     if (rounds) {
         const uint32_t last = rounds - 1;
-        bring(next[0], 0, true);
+        bring(next, 0, true);
         fetch(codes_of[0], wk);
-        keep(next[0], 0);
+        keep(next, 0);
         fetch(codes_of[1], (last < 1 ? last : 1) * WK + wk);
-        bring(next[DEEP - 1], last < 1 ? last : 1, true);
-        if (DEEP == 2) bring(next[0], last < 2 ? last : 2, true);
+        bring(next, last < 1 ? last : 1, true);
         __syncthreads();
         uint32_t round = 0;
         for (; round < last; round += 2) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                Piece& after = next[DEEP == 2 ? 1 - b : 0];
-                use(codes_of[b], x_at + b * L::kBuffer, less_at + b * L::kBuffer);
+                use(codes_of[b], held + b * L::kBuffer, less_at + b * L::kBuffer, [&]() {
+                    keep(next, 1 - b);
+                    bring(next, round + b + 2 < last ? round + b + 2 : last, true);
+                });
                 fetch(codes_of[b], (round + b + 2 < last ? round + b + 2 : last) * WK + wk);
-                keep(after, 1 - b);
-                bring(after, round + b + 1 + DEEP < last ? round + b + 1 + DEEP : last, true);
                 __syncthreads();
             }
         }
-        if (round == last) use(codes_of[0], x_at, less_at);
+        if (round == last) use(codes_of[0], held, less_at, []() {});
         __syncthreads();
     }
     if (p.k % (128 * WK)) {                                  // what is left behind the last whole round
-        bring(next[0], rounds, false);
+        bring(next, rounds, false);
         fetch_rest(codes_of[0], rounds * WK + wk);
-        keep(next[0], 0);
+        keep(next, 0);
         __syncthreads();
-        use(codes_of[0], x_at, less_at);
+        use(codes_of[0], held, less_at, []() {});
         __syncthreads();
     }
     float* sums = reinterpret_cast<float*>(held);
@@ -544,12 +586,12 @@ void product_of_rows(const Product& p, hipStream_t s) {
     k_w4_rows<T, G, MR, WAVES, S><<<dim3((p.n + 15) / 16, (p.m + MR - 1) / MR), WAVES * 64, Rows<T, MR, WAVES, S>::lds(rows), s>>>(p, (steps + WAVES - 1) / WAVES);
 }
 
-template <int T, int G, int MT, int NT, int WM, int WN, int WK, int DEEP, int PERSIMD>
+template <int T, int G, int MT, int NT, int WM, int WN, int WK, int PERSIMD>
 void product_of_tiles(const Product& p, hipStream_t s) {
     using L = Tile<T, MT, NT, WM, WN, WK>;
     static_assert(L::kLds <= 160 * 1024, "LDS of a compute unit");
-    const dim3 grid((p.n + L::kCols - 1) / L::kCols, (p.m + L::kRows - 1) / L::kRows);
-    k_w4_tiles<T, G, MT, NT, WM, WN, WK, DEEP, PERSIMD><<<grid, L::kThreads, L::kLds, s>>>(p);
+    const uint32_t grid = (p.n + L::kCols - 1) / L::kCols * ((p.m + L::kRows - 1) / L::kRows);
+    k_w4_tiles<T, G, MT, NT, WM, WN, WK, PERSIMD><<<grid, L::kThreads, L::kLds, s>>>(p);
 }
 
 // More wavefronts a workgroup where there are few workgroups, as long as each has some steps to go, and two steps at a time where that leaves
@@ -569,22 +611,23 @@ void product_of_few(const Product& p, hipStream_t s) {
 template <int T, int G>
 void product(const Product& p, hipStream_t s) {
     if (p.m > 16) {
-        // The smaller the tile, the more wavefronts share a tile's width: smaller tiles as long as they fit the chip in one go.  Measured, us
-        // (bf16, groups of 128): 64 rows by 4096x4096 in tiles of 32 x 32: 10.8, 32 x 64 14.1, 64 x 64 20.1, 64 x 128 36.9; 100 rows 20.1, 14.3, 20.1,
-        // 37.0; 256 rows 39.1, 27.3, 20.4, 36.8; 512 rows 76.5, 52.7, 39.1, 37.4; 32 by 4096x11008 in tiles of 32 x 16 20.3, 32 x 32 25.7.
-        // fp32, whose three parts take three times the LDS: 24 rows by 4096x4096 in tiles of 16 x 32 13.0, 32 x 64 23.8, 32 x 128 40.0; 100 rows 47.6,
-        // 24.1, 40.9; 256 rows 94.6, 46.9, 41.4; 1024 rows 373, 183, 115.
-        const auto fits = [&](uint32_t rows, uint32_t cols) { return (uint64_t)((p.m + rows - 1) / rows) * ((p.n + cols - 1) / cols) <= 256; };
+        // The smaller the tile, the more wavefronts share a tile's width: smaller tiles as long as they fit the chip in one go, those of 64 x 64 two a
+        // compute unit.  Measured in tiles of 32 x 16, 32 x 32, 32 x 64, 64 x 64 and 64 x 128, us (bf16, groups of 128): 24 rows by 4096x4096 8.4, 10.3,
+        // 13.2, 16.1, 29.8; 64 rows 15.7, 10.9, 13.9, 16.7, 32.8; 100 rows 29.4, 20.3, 14.0, 16.8, 32.9; 256 rows 57.2, 38.9, 26.8, 17.1, 32.8; 512
+        // rows 113, 75.9, 52.0, 28.8, 33.4; 1024 rows 223, 150, 102, 53.3, 48.2; 128 by 11008x4096 77.8, 57.1, 39.4, 28.5, 33.1.
+        // fp32, whose three parts take three times the LDS, in tiles of 16 x 32, 32 x 64 and 32 x 128: 24 rows by 4096x4096 13.9, 21.0, 37.6; 100 rows
+        // 51.0, 21.9, 38.3; 256 rows 101, 42.0, 39.3; 1024 rows 400, 163, 97.7.
+        const auto fits = [&](uint32_t rows, uint32_t cols, uint32_t blocks = 256) { return (uint64_t)((p.m + rows - 1) / rows) * ((p.n + cols - 1) / cols) <= blocks; };
         if constexpr (T == LC_F32) {
-            if (fits(16, 32)) product_of_tiles<T, G, 1, 2, 1, 1, 4, 1, 1>(p, s);
-            else if (fits(32, 64)) product_of_tiles<T, G, 2, 1, 1, 4, 2, 1, 1>(p, s);
-            else product_of_tiles<T, G, 2, 2, 1, 4, 1, 1, 1>(p, s);
+            if (fits(16, 32)) product_of_tiles<T, G, 1, 2, 1, 1, 4, 1>(p, s);
+            else if (fits(32, 64)) product_of_tiles<T, G, 2, 1, 1, 4, 2, 1>(p, s);
+            else product_of_tiles<T, G, 2, 2, 1, 4, 1, 1>(p, s);
         } else {
-            if (p.m <= 32) product_of_tiles<T, G, 2, 1, 1, 1, 8, 1, 1>(p, s);
-            else if (fits(32, 32)) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1, 1>(p, s);
-            else if (fits(32, 64)) product_of_tiles<T, G, 2, 2, 1, 2, 4, 1, 1>(p, s);
-            else if (fits(64, 64)) product_of_tiles<T, G, 4, 1, 1, 4, 2, 1, 1>(p, s);
-            else product_of_tiles<T, G, 4, 2, 1, 4, 1, 1, 2>(p, s);
+            if (p.m <= 32) product_of_tiles<T, G, 2, 1, 1, 1, 8, 1>(p, s);
+            else if (fits(32, 32)) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1>(p, s);
+            else if (fits(32, 64)) product_of_tiles<T, G, 2, 2, 1, 2, 4, 1>(p, s);
+            else if (fits(64, 64, 512)) product_of_tiles<T, G, 4, 1, 1, 4, 2, 1>(p, s);
+            else product_of_tiles<T, G, 4, 2, 1, 4, 1, 3>(p, s);
         }
         return;
     }
@@ -660,9 +703,17 @@ int lc_w4_matmul(const void* x, uint64_t ldx, uint64_t m, const lc_w4* w4, const
         else k_w4_bias_only<LC_F16><<<(uint32_t)blocks, 256, 0, s>>>(p);
         return launched();
     }
-#define CALL(T, G) product<T, G>(p, s)
-    LC_BY_TYPE(CALL, dtype, q);
+    // Over at most this many rows of w at once, so that a launch's threads are counted in 32 bits.
+    const uint64_t step = m > 16 ? 1ull << 17 : 1ull << 22;
+    for (uint64_t j = 0; j < q.n; j += step) {
+        Product some = p;
+        some.codes += j * q.codes_pitch, some.scales += j * q.scales_pitch, some.n = (uint32_t)(q.n - j < step ? q.n - j : step);
+        some.y = static_cast<uint8_t*>(y) + j * size;
+        if (bias) some.bias = static_cast<const uint8_t*>(bias) + j * size;
+#define CALL(T, G) product<T, G>(some, s)
+        LC_BY_TYPE(CALL, dtype, q);
 #undef CALL
+    }
     return launched();
 }
 

@@ -154,6 +154,18 @@ def test_product(lc, dtype, group, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,group", [(1, 64, 8320, 32), (3, 40, 8200, 128), (14, 70, 9000, 64), (2, 8300, 300, 128), (13, 8300, 520, 32), (4, 8200, 2700, 128),
+                                         (600, 4000, 384, 64), (601, 4010, 650, 128), (300, 1500, 520, 32), (17, (1 << 17) + 40, 32, 32)])
+def test_product_however_split(lc, dtype, m, n, k, group):
+    """Wide and narrow, few rows and many: each way of sharing a product out between wavefronts, workgroups and launches."""
+    g = torch.Generator(device=DEV); g.manual_seed(m + n + k)
+    w4 = random_w4(lc, n, k, group, m + k)
+    x = torch.randn(m, k, generator=g, device=DEV).to(dtype)
+    bias = torch.randn(n, generator=g, device=DEV).to(dtype)
+    check(x, w4, bias, lc.lc_w4_matmul(x, w4, bias))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,n,k,group", [(1, 33, 200, 64), (6, 20, 511, 32), (18, 40, 130, 128), (150, 140, 258, 64)])
 def test_product_of_views(lc, dtype, m, n, k, group):
     """Pitches and first elements off every alignment; nothing beside the output is written."""
