@@ -134,10 +134,6 @@ template <bool HALF> __device__ __forceinline__ uint32_t pair_of(float a, float 
     if (HALF) { const auto h = __builtin_amdgcn_cvt_pkrtz(a, b); uint32_t u; __builtin_memcpy(&u, &h, 4); return u; }
     return high_halves(bits_of(a), bits_of(b));
 }
-// Nibble j of a word of 4-bit codes as a sixteenth of what it stands for: the instruction reads four bits as a two's complement number
-// of sixteenths, which the code with its top bit turned round is.
-__device__ __forceinline__ uint32_t turned(uint32_t w) { return w ^ 0x88888888u; }
-__device__ __forceinline__ float nibble_of(uint32_t w, int j) { return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * j))); }
 template <int BYTE> __device__ __forceinline__ float byte_of(uint32_t w) { return (float)(int8_t)(w >> (8 * BYTE)); }
 
 // A bf16 operand of the values of eight tokens at element j of each token's `w` (4 bits: turned words, and sixteenths).

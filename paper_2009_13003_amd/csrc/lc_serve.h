@@ -146,6 +146,11 @@ template <int LANES> __device__ __forceinline__ float sum_of_lanes(float v) {
 // one to nearest even.
 __device__ __forceinline__ uint32_t rounded(float t, float bias) { return bits_of(t + (12582912.0f + bias)); }
 
+// Nibble j of a word of 4-bit codes as a sixteenth of what it stands for: the instruction reads four bits as a two's complement number
+// of sixteenths, which the code with its top bit turned round is.
+__device__ __forceinline__ uint32_t turned(uint32_t w) { return w ^ 0x88888888u; }
+__device__ __forceinline__ float nibble_of(uint32_t w, int j) { return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * j))); }
+
 // D = A B + C, 16 x 16 x 32: lane l gives row l % 16 of A and column l % 16 of B, eight places of the inner dimension of its
 // own (the same ones for A and B) per quarter l / 16, and receives column l % 16, rows 4 (l / 16) + 0..3 of D.
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {

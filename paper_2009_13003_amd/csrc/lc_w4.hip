@@ -82,28 +82,33 @@ void dequantize(const lc_w4& q, void* w, uint64_t ldw, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- the product
-// Codes enter the matrix instructions as whole numbers: a nibble c put into the lowest bits of the mantissa of 2^7 (bf16) or 2^10
-// (fp16) makes 128 + c = q + 136, or 1024 + c = q + 1032, in little more than two operations for two codes, and the same instruction with
-// a constant for B takes 136 (1032) times the sum of x away first (or those who bring x into LDS add it up).  All of that is exact but for the sums' own rounding in 32 bits, which
-// this makes some 136 / 4 (1032 / 4) times that of the sum of q x: 2e-6 (2e-5) of it, nothing beside the result's rounding to 16 bits.  fp32
-// takes 16 + c = q + 24 and a shift for each two codes more, and three bf16 parts of x that add up to it exactly.
+// For 16-bit types codes enter the matrix instructions as whole numbers: a nibble c put into the lowest bits of the mantissa of 2^7 (bf16) or
+// 2^10 (fp16) makes 128 + c = q + 136, or 1024 + c = q + 1032, in little more than two operations for two codes, and 136 (1032) times the sum of x
+// is taken away first, by the same instruction with a constant for B or as x is brought into LDS.  All of that is exact but for the sums' own
+// rounding in 32 bits, which this makes some 136 / 4 (1032 / 4) times that of the sum of q x: 2e-6 (2e-5) of it, nothing beside the result's rounding to
+// 16 bits.  fp32 has no such rounding behind it: there codes are converted to sixteenths of q, which bf16 holds exactly (three operations for two
+// codes), and x is three bf16 parts that add up to it.  (Lifted codes, 16 + c, left 9e-7
+// of the result at a width of 2043 instead of 1e-7.)
 template <int T> struct Num;
 template <> struct Num<LC_BF16> {
-    static constexpr float kTaken = -136.0f;
-    static constexpr int kParts = 1, kUp = 0;               // how far a nibble is moved up into the mantissa
-    static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x43004300u, kLess = 0xC308C308u;        // 128, -136
+    static constexpr bool kLifted = true;
+    static constexpr float kTaken = -136.0f, kUnit = 1.0f;  // what is taken away, and what the operand counts in
+    static constexpr int kParts = 1;
+    static constexpr uint32_t kBase = 0x43004300u, kLess = 0xC308C308u;        // 128, -136
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F32> {
-    static constexpr float kTaken = -24.0f;
-    static constexpr int kParts = 3, kUp = 3;
-    static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u, kLess = 0xC1C0C1C0u;        // 16, -24
+    static constexpr bool kLifted = false;
+    static constexpr float kTaken = 0.0f, kUnit = 16.0f;
+    static constexpr int kParts = 3;
+    static constexpr uint32_t kBase = 0, kLess = 0;
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F16> {
-    static constexpr float kTaken = -1032.0f;
-    static constexpr int kParts = 1, kUp = 0;
-    static constexpr uint32_t kMask = 0x000F000Fu, kBase = 0x64006400u, kLess = 0xE408E408u;        // 1024, -1032
+    static constexpr bool kLifted = true;
+    static constexpr float kTaken = -1032.0f, kUnit = 1.0f;
+    static constexpr int kParts = 1;
+    static constexpr uint32_t kBase = 0x64006400u, kLess = 0xE408E408u;        // 1024, -1032
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16(a, b, c); }
 };
 template <int T> __device__ __forceinline__ f32x4 less_of(u32x4 x, f32x4 c) { return Num<T>::mfma(x, u32x4{Num<T>::kLess, Num<T>::kLess, Num<T>::kLess, Num<T>::kLess}, c); }
@@ -113,12 +118,18 @@ template <int T> __device__ __forceinline__ f32x4 less_of(u32x4 x, f32x4 c) { re
 template <int T> __device__ __forceinline__ u32x4 codes_as_operand(uint32_t w) {
     u32x4 r;
     const uint32_t odd = w >> 4;
-    uint32_t mask = Num<T>::kMask;
+    uint32_t mask = 0x000F000Fu;
     asm("" : "+v"(mask));
+    if (!Num<T>::kLifted) {
+        const uint32_t t = turned(w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = high_halves(bits_of(nibble_of(t, 2 * j)), bits_of(nibble_of(t, 2 * j + 1)));
+        return r;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t pair = __builtin_amdgcn_perm(odd, w, 0x0C000C00u | (uint32_t)j | (uint32_t)(4 + j) << 16);      // byte j of w, byte j of odd
-        r[j] = (pair << Num<T>::kUp & mask) | Num<T>::kBase;
+        r[j] = (pair & mask) | Num<T>::kBase;
     }
     return r;
 }
@@ -162,16 +173,11 @@ template <int T> __device__ __forceinline__ Operand<T> x_as_operand(const Raw<T>
     return r;
 }
 
-// The sum of an operand's eight elements (fp32: of the elements themselves), in 32 bits.
+// The sum of an operand's eight elements (of 16 bits), in 32 bits.
 template <int T> __device__ __forceinline__ float sum_of(const Raw<T>& x) {
     float s = 0;
-    if (T == LC_F32) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += float_of(x.w[e / 4][e % 4]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s = dot_16<T == LC_F16>(x.w[0][j], T == LC_F16 ? 0x3C003C00u : 0x3F803F80u, s);
-    }
+    for (int j = 0; j < 4; ++j) s = dot_16<T == LC_F16>(x.w[0][j], T == LC_F16 ? 0x3C003C00u : 0x3F803F80u, s);
     return s;
 }
 
@@ -185,7 +191,7 @@ struct Product {
 };
 
 // One element of y straight from the formula, where the sums above are not finite: infinity - infinity is not what an infinity in
-// x gives, and 24 times a group's sum, or the sum before its scale, may be out of range where the result is not.
+// x gives, and what is taken away, the sum before its scale or sixteen times a scale may be out of range where the result is not.
 template <int T, int G>
 __device__ __forceinline__ float one_by_formula(const Product& p, uint32_t i, uint32_t j) {
     float total = 0;
@@ -279,7 +285,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per)
             for (int i = 0; i < PER; ++i) {
                 x[i] = x_as_operand<T>(raw[g * PER + i]);
 #pragma unroll
-                for (int q = PARTS - 1; q >= 0; --q) acc = less_of<T>(x[i].part[q], acc);
+                for (int q = PARTS - 1; q >= 0 && Num<T>::kLifted; --q) acc = less_of<T>(x[i].part[q], acc);
             }
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
@@ -287,7 +293,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per)
 #pragma unroll
                 for (int q = PARTS - 1; q >= 0; --q) acc = Num<T>::mfma(x[i].part[q], b, acc);
             }
-            const float scale = of_bf16(s[g]);
+            const float scale = of_bf16(s[g]) * Num<T>::kUnit;
 #pragma unroll
             for (int r = 0; r < 4; ++r) total[r] = fmaf(acc[r], scale, total[r]);
         }
@@ -368,7 +374,7 @@ template <int T, int MT, int NT, int WM, int WN, int WK> struct Tile {
     // cycles that LDS was busy went on conflicts.)
     static constexpr uint32_t kFour = kRows * 64, kPart = WK * 4 * kFour;
     static __device__ uint32_t place_of(uint32_t r, uint32_t four, uint32_t eight) { return four * kFour + r * 64 + 16 * (eight ^ (r / 4 % 4)); }
-    static constexpr uint32_t kLess = kParts * kPart, kBuffer = kLess + WK * 4 * kRows * 4;      // behind x what is taken away for each of (at most four) groups and rows, added up by those who bring x in
+    static constexpr uint32_t kLess = kParts * kPart, kBuffer = kLess + (Num<T>::kLifted ? WK * 4 * kRows * 4 : 0);      // behind x what is taken away for each of (at most four) groups and rows, added up by those who bring x in
     static constexpr uint32_t kSums = WK * kRows * (kCols + 4) * 4;
     static constexpr uint32_t kLds = 2 * kBuffer > kSums ? 2 * kBuffer : kSums;
 };
@@ -449,6 +455,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
 #pragma unroll
                 for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4*>(to + q * L::kPart + at + L::kLanes / 4 * i * L::kFour) = x.part[q];
             }
+            if (!Num<T>::kLifted) continue;
             constexpr int EIGHTS = G / 8, TOGETHER = EIGHTS > L::kLanes ? EIGHTS / L::kLanes : 1;
 #pragma unroll
             for (int i = 0; i < L::kItems; i += TOGETHER) {
@@ -489,7 +496,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
                 f32x4 less[MT];
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    less[m] = *reinterpret_cast<const f32x4*>(less_at + (g * L::kRows + 16 * m) * 4);
+                    less[m] = Num<T>::kLifted ? *reinterpret_cast<const f32x4*>(less_at + (g * L::kRows + 16 * m) * 4) : f32x4{0, 0, 0, 0};
 #pragma unroll
                     for (int n = 0; n < NT; ++n) acc[n][m] = less[m];
                 }
@@ -507,7 +514,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
             if (o % PER == PER - 1) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float s = of_bf16(f.s[n][g]);
+                    const float s = of_bf16(f.s[n][g]) * Num<T>::kUnit;
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -603,8 +610,9 @@ template <int T, int G, int MR>
 void product_of_few(const Product& p, hipStream_t s) {
     constexpr int FOUR = T != LC_F32 && G == 128 ? 2 : 1, EIGHT = T != LC_F32 && G == 128 && MR == 4 ? 2 : 1;
     const uint32_t blocks = (p.n + 15) / 16;
-    if (T != LC_F32 && blocks <= 256 && p.k >= 8192) product_of_rows<T, G, MR, 16, 1>(p, s);
-    else if (blocks <= 512) product_of_rows<T, G, MR, 8, EIGHT>(p, s);
+    if constexpr (T != LC_F32)
+        if (blocks <= 256 && p.k >= 8192) return product_of_rows<T, G, MR, 16, 1>(p, s);
+    if (blocks <= 512) product_of_rows<T, G, MR, 8, EIGHT>(p, s);
     else product_of_rows<T, G, MR, 4, FOUR>(p, s);
 }
 
