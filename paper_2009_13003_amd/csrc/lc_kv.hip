@@ -21,7 +21,9 @@ __device__ __forceinline__ uint64_t row_of(const Cache& c, uint64_t page, uint32
 
 // ---------------------------------------------------------------- writing and reading back
 // A lane takes eight elements of a token's head, a power of two of lanes (those behind the last element idle) the whole head; the
-// keys are the first half of the grid, the values the second.
+// keys are the first half of the grid, the values the second.  s = max |x| / 127 (or 7) over the head in fp32, q = rint(x (1 / s)).  Bound by memory:
+// 2000 tokens of 8 heads of 128 in fp16 to 4 bits 4.7 us, of which 2.3 are the launch; 30011 tokens read back, keys and values by the same lane,
+// 26 to 29 us, 5.4 to 6 TB/s, past the caches.
 template <int T, int BITS, int LANES>
 __global__ __launch_bounds__(256) void k_kv_write(Cache c, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots,
                                                   uint32_t items, FastDiv by_heads) {
@@ -98,7 +100,13 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 //   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens
 //                    in the order 4 h + 0..3, 16 + 4 h + 0..3, in which the values are then loaded too
 // so the running maximum, the sum and the factors of the rescaling are one number a lane, and nothing passes through LDS.
-// Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly.
+// Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly, and
+// probabilities times scales as two bf16 parts (three for fp32): one part alone, 2^-9 of each, would show beside a result in fp16.
+// One token of 16 sequences of up to 4096 tokens of 32 heads (8 bits): 63 us, 4.7 TB/s of the cache, which is near what memory gives.  24 drafted
+// tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 45 us for what memory would give in 6: each tile of 32 tokens by 32 queries
+// takes 400 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
+// three workgroups convert a head's codes each for its own rows.  One token of one sequence of 1000: 9 us, latencies in a row: launch 2.3, lengths,
+// pages, tiles, and a meeting of the parts.
 constexpr int kTile = 32, kWaves = 4;
 constexpr float kLog2e = 1.44269504088896340736f;
 // A sequence whose heads and queries alone do not give the chip kWantBlocks workgroups (two a compute unit) is split along its tokens.
@@ -698,9 +706,12 @@ void attend_of(const Attend& a, hipStream_t s) {
 }
 template <int T, int BITS>
 void attend(const Attend& a, hipStream_t s) {
+    // Two tiles of 16 rows a wavefront where there are more rows than one: codes are converted once for both (24 drafted tokens as above 46 us
+    // for 59, in 8 bits 50 for 68, 64 tokens of 4 queries to a head of 64 over 20000 49 for 63).  Two tiles of tokens under way where the registers of
+    // two wavefronts a SIMD hold them: not for 8 bits and two tiles of rows (49 us either way), nor from 129 elements on.
     const bool two = tiles_of_rows(a.rows, (int)a.c.dim, T) == 2;
     if (a.c.dim <= 64) two ? attend_of<T, BITS, 64, 2, 2, 2>(a, s) : attend_of<T, BITS, 64, 1, 2, 3>(a, s);
-    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2, 2, 2>(a, s) : attend_of<T, BITS, 128, 1, 2, 2>(a, s);
+    else if (a.c.dim <= 128) two ? attend_of<T, BITS, 128, 2, BITS == 8 ? 1 : 2, 2>(a, s) : attend_of<T, BITS, 128, 1, 2, 2>(a, s);
     else attend_of<T, BITS, 256, 1, 1, 1>(a, s);
 }
 

@@ -7,7 +7,10 @@ namespace {
 
 // ---------------------------------------------------------------- quantising and reading back
 // A lane takes eight elements (4 bytes of codes), a group is 4, 8 or 16 neighbouring lanes, and a row's lanes are rounded up to whole
-// groups, so that no group is split over wavefronts.
+// groups, so that no group is split over wavefronts.  s = bf16(max |w| / 7), q = rint(w (1 / s)) held to +-7; a group too small for 1 / s to be a
+// number has scale 0, one that holds what is not finite a NaN for a scale.  Bound by memory: 11008x4096 in fp32 38 us, 5.4 TB/s of what is
+// read and written, and read back 29 us, 7 TB/s; both stream past the caches, 16 bytes a lane at a time (through them, and 32 at a time, the two
+// took 78 us together).
 template <int T, int LANES>
 __global__ __launch_bounds__(256) void k_w4_quantize(const void* w, uint64_t ldw, uint8_t* codes, uint64_t codes_pitch, uint16_t* scales,
                                                      uint64_t scales_pitch, uint32_t rows, uint32_t k, uint32_t row_bytes, uint32_t row_lanes, FastDiv div) {
