@@ -108,6 +108,7 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 // three workgroups convert a head's codes each for its own rows.  One token of one sequence of 1000: 9 us, latencies in a row: launch 2.3, lengths,
 // pages, tiles, and a meeting of the parts.
 constexpr int kTile = 32, kWaves = 4;
+constexpr float kFar = 8.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 // A sequence whose heads and queries alone do not give the chip kWantBlocks workgroups (two a compute unit) is split along its tokens.
 constexpr uint32_t kMostSplits = 60, kWantBlocks = 512, kLeastTokens = kWaves * kTile;
@@ -151,7 +152,7 @@ template <int BITS> __device__ __forceinline__ u32x4 values_at(const uint32_t (&
     for (int e = 0; e < 4; ++e) {
         float a, b;
         if (BITS == 8) { a = (float)(int8_t)(w[2 * e] >> (8 * j)); b = (float)(int8_t)(w[2 * e + 1] >> (8 * j)); }
-        else { a = nibble_of(w[2 * e], j); b = nibble_of(w[2 * e + 1], j); }
+        else { a = low_nibble_of(w[2 * e], j); b = low_nibble_of(w[2 * e + 1], j); }
         r[e] = high_halves(bits_of(a), bits_of(b));
     }
     return r;
@@ -398,11 +399,11 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
     }
 
     f32x4 acc[NT][VD];
-    float top[NT], sum[NT];
+    float top[NT], from[NT], sum[NT];                       // the largest score so far (or about that), what probabilities are measured from, their sum
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         top[n] = -__builtin_inff();
-        sum[n] = 0;
+        from[n] = sum[n] = 0;
 #pragma unroll
         for (int j = 0; j < VD; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
     }
@@ -455,34 +456,34 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
         u32x4 pp[NT][NP];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float x[8], weight[8];
+            float p[8], weight[8];                           // scores less what probabilities are measured from, then probabilities
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { x[i] = score[n][i / 4][i % 4] * ks[i]; weight[i] = vs[i]; }
+            for (int i = 0; i < 8; ++i) { p[i] = fmaf(score[n][i / 4][i % 4], ks[i], -from[n]); weight[i] = vs[i]; }
             if (!whole) {                                    // (what is not seen may have any scale)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int32_t t = tb + 16 * (i / 4) + 4 * h + i % 4, j = t - base;
                     const bool there = at.there >> (2 * (i / 4) + h / 2) & 1, seen = there && t < end && (j < 0 || (mask[n] >> (j & 63) & 1));
-                    x[i] = seen ? x[i] : -__builtin_inff();
+                    p[i] = seen ? p[i] : -__builtin_inff();
                     weight[i] = seen ? weight[i] : 0.0f;
                 }
             }
-            float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
             // What probabilities are measured from moves only when one would pass 2^8, so that the sums are seldom rescaled.
-            most = max_over_quarters(most);
-            if (__any(most > top[n] + 8.0f)) {
-                most = fmaxf(most, top[n]);
-                const float shrink = __builtin_amdgcn_exp2f(top[n] - (most == -__builtin_inff() ? 0.0f : most));
+            float most = fmaxf(fmaxf(fmaxf(p[0], p[1]), p[2]), fmaxf(fmaxf(fmaxf(p[3], p[4]), p[5]), fmaxf(p[6], p[7])));
+            if (__any(most > kFar || top[n] == -__builtin_inff())) {
+                most = fmaxf(max_over_quarters(most) + from[n], top[n]);
+                const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top[n] - then);
                 sum[n] *= shrink;
 #pragma unroll
                 for (int j = 0; j < VD; ++j) acc[n][j] *= shrink;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] -= then - from[n];
                 top[n] = most;
+                from[n] = then;
             }
-            const float from = top[n] == -__builtin_inff() ? 0.0f : top[n];
-            float p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(x[i] - from);
+                p[i] = __builtin_amdgcn_exp2f(p[i]);
                 sum[n] += p[i];
                 p[i] *= weight[i];
             }
@@ -503,12 +504,19 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
                 if (BITS == 4) asm("" : "+v"(w[i]));         // (turned once, not again for every element)
             }
 #pragma unroll
-            for (int j = 0; j < Raw::kPerWord; ++j) {
-                const u32x4 v = values_at<BITS>(w, j);
+            for (int half = 0; half < (BITS == 4 ? 2 : 1); ++half) {
+                if (half)
 #pragma unroll
-                for (int k = NP - 1; k >= 0; --k)
+                    for (int i = 0; i < 8; ++i) w[i] = upper_nibbles(w[i]);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[n][o * Raw::kPerWord + j] = mfma_bf16(v, pp[n][k], acc[n][o * Raw::kPerWord + j]);
+                for (int j = 0; j < Raw::kPerWord * BITS / 8; ++j) {
+                    const u32x4 v = values_at<BITS>(w, j);
+                    const int at = o * Raw::kPerWord + (BITS == 4 ? 2 * j + half : j);
+#pragma unroll
+                    for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[n][at] = mfma_bf16(v, pp[n][k], acc[n][at]);
+                }
             }
         }
         load_values(f, next);

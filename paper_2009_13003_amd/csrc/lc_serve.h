@@ -150,6 +150,14 @@ __device__ __forceinline__ uint32_t rounded(float t, float bias) { return bits_o
 // of sixteenths, which the code with its top bit turned round is.
 __device__ __forceinline__ uint32_t turned(uint32_t w) { return w ^ 0x88888888u; }
 __device__ __forceinline__ float nibble_of(uint32_t w, int j) { return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * j))); }
+// ... and the lower nibble of byte j, which the instruction picks by itself; the upper ones' word, which the compiler does not see through, so
+// that it is shifted once and not for every byte.
+__device__ __forceinline__ float low_nibble_of(uint32_t w, int j) { return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (8 * j) & 255u)); }
+__device__ __forceinline__ uint32_t upper_nibbles(uint32_t w) {
+    w >>= 4;
+    asm("" : "+v"(w));
+    return w;
+}
 
 // D = A B + C, 16 x 16 x 32: lane l gives row l % 16 of A and column l % 16 of B, eight places of the inner dimension of its
 // own (the same ones for A and B) per quarter l / 16, and receives column l % 16, rows 4 (l / 16) + 0..3 of D.

@@ -124,9 +124,9 @@ template <int T> __device__ __forceinline__ u32x4 codes_as_operand(uint32_t w) {
     uint32_t mask = 0x000F000Fu;
     asm("" : "+v"(mask));
     if (!Num<T>::kLifted) {
-        const uint32_t t = turned(w);
+        const uint32_t t = turned(w), u = upper_nibbles(t);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = high_halves(bits_of(nibble_of(t, 2 * j)), bits_of(nibble_of(t, 2 * j + 1)));
+        for (int j = 0; j < 4; ++j) r[j] = high_halves(bits_of(low_nibble_of(t, j)), bits_of(low_nibble_of(u, j)));
         return r;
     }
 #pragma unroll
