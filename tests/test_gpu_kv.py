@@ -226,6 +226,18 @@ def test_attention_of_trees(lc, dtype, bits, lens, nq, heads, kv, dim, page):
     case.check(case.run(lc))                                 # and one behind the other
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("lens,nq,heads,kv,dim,page", [([512], 1, 8, 8, 128, 16), ([513, 2], 1, 8, 8, 128, 16), ([513], 40, 4, 2, 64, 32), ([512, 500, 0], 40, 4, 2, 64, 32),
+                                                       ([641, 640, 639], 7, 18, 9, 96, 8), ([256, 257], 3, 6, 3, 256, 16), ([256, 255], 3, 6, 3, 192, 16),
+                                                       ([530], 64, 16, 8, 128, 8), ([1, 1025, 7], 20, 20, 10, 128, 64)])
+def test_attention_split_or_not(lc, dtype, bits, lens, nq, heads, kv, dim, page):
+    """Lengths at which sequences begin to be split, and at the ends of the parts: some rows see nothing of the last."""
+    case = Case(lc, sum(lens) + nq + dim, lens, nq, heads, kv, dim, page, bits, dtype)
+    mask = tree(len(lens), nq, nq)
+    case.check(case.run(lc, mask), mask)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_rows_that_see_nothing(lc, bits):
     case = Case(lc, 5, [6, 3, 0, 90], 6, 4, 2, 64, 16, bits, torch.float32)
