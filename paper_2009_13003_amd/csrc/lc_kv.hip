@@ -103,15 +103,15 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 // Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly, and
 // probabilities times scales as two bf16 parts (three for fp32): one part alone, 2^-9 of each, would show beside a result in fp16.
 // One token of 16 sequences of up to 4096 tokens of 32 heads (8 bits): 63 us, 4.7 TB/s of the cache, which is near what memory gives.  24 drafted
-// tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 45 us for what memory would give in 6: each tile of 32 tokens by 32 queries
-// takes 400 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
+// tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 43 us for what memory would give in 6: each tile of 32 tokens by 32 queries
+// takes 350 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
 // three workgroups convert a head's codes each for its own rows.  One token of one sequence of 1000: 9 us, latencies in a row: launch 2.3, lengths,
 // pages, tiles, and a meeting of the parts.
 constexpr int kTile = 32, kWaves = 4;
-constexpr float kFar = 8.0f;
+constexpr float kFar = 8.0f;                                // by how much, in powers of two, a score may pass what probabilities are measured from
 constexpr float kLog2e = 1.44269504088896340736f;
-// A sequence whose heads and queries alone do not give the chip kWantBlocks workgroups (two a compute unit) is split along its tokens.
-constexpr uint32_t kMostSplits = 60, kWantBlocks = 512, kLeastTokens = kWaves * kTile;
+// A sequence whose heads and queries alone do not give the chip as many workgroups as fit it at once is split along its tokens.
+constexpr uint32_t kMostSplits = 60, kLeastTokens = kWaves * kTile;
 
 struct Attend {
     Cache c;
@@ -655,9 +655,9 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
 }
 
 // Slots for the parts of all sequences: one a sequence, or as many more as all fit the chip together.
-uint64_t slots_of(uint64_t batch, uint32_t kv_heads, uint64_t row_groups) {
+uint64_t slots_of(uint64_t batch, uint32_t kv_heads, uint64_t row_groups, uint32_t want) {
     const uint64_t blocks = kv_heads * row_groups;
-    const uint64_t slots = batch * blocks >= kWantBlocks ? batch : kWantBlocks / blocks;
+    const uint64_t slots = batch * blocks >= want ? batch : want / blocks;
     return slots < batch * kMostSplits ? slots : batch * kMostSplits;
 }
 struct Scratch { uint64_t stats, part, bytes; };            // where the parts of the scratch memory begin
@@ -670,6 +670,10 @@ Scratch scratch_of(uint64_t batch, uint64_t slots, uint64_t groups, uint64_t nq,
     return s;
 }
 int tiles_of_rows(uint64_t rows, int dim, int dtype) { return rows > 16 && dtype != LC_F32 && dim <= 128 ? 2 : 1; }
+// How many workgroups: two a compute unit, which is what most kernels' registers leave room for; three for one tile of rows of 4-bit codes, where that
+// pays (one token of 16 sequences of up to 16384 of 8 heads of 128 47.0 us for 50.5, of 40 of up to 2000 of 2 heads of 96 16.1 for 15.6; one over 32000 of
+// 16 heads of 64 25.0 for 22.9).
+uint32_t workgroups_of(int bits, int dim, int dtype, int tiles) { return bits == 4 && dim > 64 && dim <= 128 && dtype != LC_F32 && tiles == 1 ? 768 : 512; }
 
 bool bad(const lc_kv_cache* c) {
     if (!c || c->heads < 1 || c->heads > 1024 || c->dim < 32 || c->dim > 256 || c->dim % 32 || (c->bits != 8 && c->bits != 4)) return true;
@@ -731,7 +735,7 @@ void attend(const Attend& a, hipStream_t s) {
             return;
         }
     if (a.c.dim <= 64) attend_of<T, BITS, 64, 1, 2, 3>(a, s);
-    else if (a.c.dim <= 128) attend_of<T, BITS, 128, 1, 2, 2>(a, s);
+    else if (a.c.dim <= 128) attend_of<T, BITS, 128, 1, 2, BITS == 4 && T != LC_F32 ? 3 : 2>(a, s);
     else attend_of<T, BITS, 256, 1, 1, 1>(a, s);
 }
 
@@ -776,11 +780,14 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
 size_t lc_kv_workspace_bytes(uint64_t batch, int nq, int heads, int kv_heads, int dim) {
     if (batch > 65535 || nq < 1 || nq > 64 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 ||
         dim > 256 || dim % 32) return 0;
-    uint64_t most = 0;                                      // (of the ways the rows may be grouped, whatever the type)
+    uint64_t most = 0;                                      // (of the ways the rows may be grouped and split, whatever the type)
     for (int tiles = 1; tiles <= 2; ++tiles) {
         const uint64_t rows = (uint64_t)nq * (heads / kv_heads), groups = (rows + 16 * tiles - 1) / (16 * tiles);
-        const uint64_t bytes = scratch_of(batch, slots_of(batch, (uint32_t)kv_heads, groups), kv_heads * groups, nq, heads, dim).bytes;
-        most = bytes > most ? bytes : most;
+        for (int bits = 4; bits <= 8; bits += 4) {
+            const uint64_t slots = slots_of(batch, (uint32_t)kv_heads, groups, workgroups_of(bits, dim, LC_BF16, tiles));
+            const uint64_t bytes = scratch_of(batch, slots, kv_heads * groups, nq, heads, dim).bytes;
+            most = bytes > most ? bytes : most;
+        }
     }
     return (size_t)most;
 }
@@ -803,7 +810,7 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
     a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
     const int tiles = tiles_of_rows(a.rows, cache->dim, dtype);
     const uint64_t groups = (a.rows + 16 * tiles - 1) / (16 * tiles);
-    a.slots = (uint32_t)slots_of(batch, a.c.heads, groups);
+    a.slots = (uint32_t)slots_of(batch, a.c.heads, groups, workgroups_of(cache->bits, cache->dim, dtype, tiles));
     if ((a.table_pages << a.c.page_shift) <= kLeastTokens) a.slots = a.batch;      // (nothing to split)
     const Scratch at = scratch_of(batch, a.slots, a.c.heads * groups, nq, heads, a.c.dim);
     a.marks = static_cast<unsigned long long*>(ws);
