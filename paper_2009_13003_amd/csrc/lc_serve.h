@@ -37,7 +37,6 @@ struct FastDiv {
 
 // 16 bytes from anywhere that suits the element (global loads need no more than that here).
 template <typename V> __device__ __forceinline__ V load_any(const void* p) { V v; __builtin_memcpy(&v, p, sizeof(V)); return v; }
-template <typename V> __device__ __forceinline__ void store_any(void* p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
 // ... and the same past the caches, for what is read or written once and too long to stay in them.
 template <typename V> __device__ __forceinline__ V load_once(const void* p) {
     typedef V __attribute__((aligned(2))) Any;
@@ -182,8 +181,7 @@ template <bool HALF> __device__ __forceinline__ float dot_16(uint32_t a, uint32_
     return __builtin_amdgcn_fdot2_f32_bf16(x, y, c, false);
 }
 
-// The low (0x05040100) or high (0x07060302) halves of a and b, a's below b's.
-__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+// The high halves of a and b, a's below b's.
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 }  // namespace serve
