@@ -504,6 +504,9 @@ def alloc_out(n, nbits, device="cuda"):
 
 
 # ---------------------------------------------------------------- serving a restored checkpoint (include/lc_serve.h)
+# `stream` (None: the current one) is where a call's work is enqueued, and nothing else is waited for.  On another stream than the current one the
+# caller sees to it that inputs, and an `out` or `ws` that is given, are ready there, and keeps them until that stream is done with them (or calls
+# their record_stream).  What a call allocates belongs to `stream`: the current stream, or any other, has to wait for it before it uses the result.
 SERVED = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -547,12 +550,23 @@ def _matrix(t):
     return t.data_ptr(), (t.stride(0) if n > 1 else k)
 
 
-def _own(t, stream):
-    """An output allocated here is used on `stream`, whose work the allocator has to know of where it is not the current one."""
-    if stream is not None:
-        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
-        if s != torch.cuda.current_stream():
-            t.record_stream(s)
+def _torch_stream(stream):
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _handle(stream)
+    return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+
+
+def _empty_on(stream, *size, dtype, device):
+    """torch.empty for a call on `stream`, which need not be the current one: from that stream's memory, since a block of the current one's may
+    still be in use by what is enqueued there, which `stream` does not wait for.  Freed, it waits for the current stream's work too, where
+    the caller is most likely to use it."""
+    s, now = _torch_stream(stream), torch.cuda.current_stream()
+    if s == now:
+        return torch.empty(*size, dtype=dtype, device=device)
+    with torch.cuda.stream(s):
+        t = torch.empty(*size, dtype=dtype, device=device)
+    t.record_stream(now)
     return t
 
 
@@ -564,11 +578,12 @@ def lc_w4_quantize(w, group, out=None, stream=None):
         if group not in (32, 64, 128):
             raise LcError(ERR_BADARG)
         row, groups, device = (k + 31) // 32 * 16, -(-k // group), w.device
-        codes = torch.empty(n, row, dtype=torch.uint8, device=device)
-        scales = torch.empty(n, groups, dtype=torch.bfloat16, device=device)
-        if stream is not None:
-            _own(codes, stream)
-            _own(scales, stream)
+        if stream is None:
+            codes = torch.empty(n, row, dtype=torch.uint8, device=device)
+            scales = torch.empty(n, groups, dtype=torch.bfloat16, device=device)
+        else:
+            codes = _empty_on(stream, n, row, dtype=torch.uint8, device=device)
+            scales = _empty_on(stream, n, groups, dtype=torch.bfloat16, device=device)
         out = W4.__new__(W4)
         out._describe(codes, scales, n, k, group, row, groups)
     else:
@@ -583,9 +598,10 @@ def lc_w4_dequantize(w4, dtype=None, out=None, stream=None):
     """The values that w4 stands for, as a matrix of `dtype` (or in `out`)."""
     if out is None:
         dtype = torch.float32 if dtype is None else dtype
-        out = torch.empty(w4.n, w4.k, dtype=dtype, device=w4.codes.device)
-        if stream is not None:
-            _own(out, stream)
+        if stream is None:
+            out = torch.empty(w4.n, w4.k, dtype=dtype, device=w4.codes.device)
+        else:
+            out = _empty_on(stream, w4.n, w4.k, dtype=dtype, device=w4.codes.device)
         p, ld = out.data_ptr(), w4.k
     else:
         p, ld = _matrix(out)
@@ -607,9 +623,7 @@ def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
         assert bias.is_cuda and bias.dtype == dtype and bias.shape == (n,) and (bias.stride(0) == 1 or n <= 1)
         bias = bias.data_ptr()
     if out is None:
-        out = x.new_empty(m, n)
-        if stream is not None:
-            _own(out, stream)
+        out = x.new_empty(m, n) if stream is None else _empty_on(stream, m, n, dtype=dtype, device=x.device)
         q, ldq = out.data_ptr(), n
     else:
         q, ldq = _matrix(out)
@@ -675,11 +689,11 @@ def lc_kv_read(cache, slots, dtype=None, out=None, stream=None):
     tokens = slots.shape[0]
     if out is None:
         heads, dim, dtype = cache.heads, cache.dim, torch.float32 if dtype is None else dtype
-        k = torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device)
-        v = torch.empty_like(k)
-        if stream is not None:
-            _own(k, stream)
-            _own(v, stream)
+        if stream is None:
+            k = torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device)
+            v = torch.empty_like(k)
+        else:
+            k, v = (_empty_on(stream, tokens, heads, dim, dtype=dtype, device=slots.device) for _ in range(2))
         ldt, ldh = heads * dim, dim
     else:
         k, v = out
@@ -696,9 +710,12 @@ def lc_kv_workspace_bytes(batch, nq, heads, kv_heads, dim):
     return int(_lib.lc_kv_workspace_bytes(batch, nq, heads, kv_heads, dim))
 
 
-def new_kv_workspace(cache, batch, nq, heads):
-    """Scratch for lc_kv_attend with these sizes; calls that may run at the same time need one each."""
-    return torch.empty(lc_kv_workspace_bytes(batch, nq, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device)
+def new_kv_workspace(cache, batch, nq, heads, stream=None):
+    """Scratch for lc_kv_attend with these sizes, to be used on `stream` (None: the current one); calls that may run at the same time need one each."""
+    size = lc_kv_workspace_bytes(batch, nq, heads, cache.heads, cache.dim)
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=cache.k.device)
+    return _empty_on(stream, size, dtype=torch.uint8, device=cache.k.device)
 
 
 def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None, stream=None):
@@ -713,15 +730,11 @@ def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None
         assert mask.is_cuda and mask.dtype == torch.int64 and mask.shape == (batch, nq) and mask.is_contiguous()
         mask = mask.data_ptr()
     if out is None:
-        out = torch.empty_like(q)
-        if stream is not None:
-            _own(out, stream)
+        out = torch.empty_like(q) if stream is None else _empty_on(stream, batch, nq, heads, dim, dtype=q.dtype, device=q.device)
     else:
         assert out.is_cuda and out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
     if ws is None:
-        ws = new_kv_workspace(cache, batch, nq, heads)
-        if stream is not None:
-            _own(ws, stream)
+        ws = new_kv_workspace(cache, batch, nq, heads, stream)
     assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
     st = _lib.lc_kv_attend(cache._p, q.data_ptr(), batch, nq, heads, table.data_ptr(), table.stride(0) if batch > 1 else table.shape[1], table.shape[1],
                            lens.data_ptr(), mask, dim ** -0.5 if scale is None else scale, out.data_ptr(), SERVED[q.dtype], ws.data_ptr(), ws.numel(),

@@ -1,0 +1,75 @@
+"""Calls on another stream than the current one: what they allocate comes from that stream's memory, so that nothing which the current stream still
+works on is written over."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+M, N, K = 300, 2000, 1024                                   # sizes that no block of the small pools serves
+
+
+@pytest.fixture(scope="module")
+def calls():
+    from paper_2009_13003_amd import lc
+    g = torch.Generator(device=DEV); g.manual_seed(1)
+    w, x = torch.randn(N, K, generator=g, device=DEV), torch.randn(M, K, generator=g, device=DEV)
+    w4 = lc.lc_w4_quantize(w, 64)
+    cache = lc.new_kv_cache(70, 8, 64, 128, 8, DEV)
+    slots = torch.arange(70 * 64, device=DEV)
+    kv = torch.randn(2, 70 * 64, 8, 128, generator=g, device=DEV)
+    lc.lc_kv_write(cache, kv[0], kv[1], slots)
+    table = torch.arange(70, dtype=torch.int32, device=DEV)[None]
+    lens, q = torch.tensor([4400], dtype=torch.int32, device=DEV), torch.randn(1, 64, 32, 128, generator=g, device=DEV)
+    of = lambda t: (t.codes, t.scales) if isinstance(t, lc.W4) else t if isinstance(t, tuple) else (t,)
+    return {"quantize": lambda **kw: of(lc.lc_w4_quantize(w, 64, **kw)), "dequantize": lambda **kw: of(lc.lc_w4_dequantize(w4, **kw)),
+            "matmul": lambda **kw: of(lc.lc_w4_matmul(x, w4, **kw)), "read": lambda **kw: of(lc.lc_kv_read(cache, slots, **kw)),
+            "attend": lambda **kw: of(lc.lc_kv_attend(cache, q, table, lens, **kw))}
+
+
+def stream_of(t):
+    """The stream whose memory a tensor lies in."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+
+
+NAMES = ["quantize", "dequantize", "matmul", "read", "attend"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("raw", [False, True])
+def test_outputs_lie_in_the_streams_own_memory(calls, name, raw, monkeypatch):
+    from paper_2009_13003_amd import lc
+    spaces = []
+    new = lc.new_kv_workspace
+    monkeypatch.setattr(lc, "new_kv_workspace", lambda *a: spaces.append(new(*a)) or spaces[-1])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = calls[name](stream=side.cuda_stream if raw else side)
+    side.synchronize()
+    assert all(stream_of(t) == side.cuda_stream for t in out + tuple(spaces)) and len(spaces) == (name == "attend")
+    here = calls[name]()
+    assert all(stream_of(t) == torch.cuda.current_stream().cuda_stream for t in here)
+    assert all(torch.equal(a, b) for a, b in zip(out, here))
+    with torch.cuda.stream(side):                            # and from there on the null stream, by its number
+        back = calls[name](stream=0)
+    torch.cuda.synchronize()
+    assert all(stream_of(t) == 0 for t in back) and all(torch.equal(a, b) for a, b in zip(back, here))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_what_the_current_stream_works_on_stays(calls, name):
+    side = torch.cuda.Stream()
+    want = calls[name]()
+    torch.cuda.synchronize()
+    work = torch.randn(4096, 4096, device=DEV).to(torch.bfloat16)
+    held = [torch.full_like(t.view(torch.uint8) if t.dtype == torch.bfloat16 else t, 3) for t in want]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        torch.mm(work, work)
+    kept = [t.clone() for t in held]                         # enqueued behind that
+    del held                                                 # ... so its memory is free for the current stream alone
+    out = calls[name](stream=side)
+    torch.cuda.synchronize()
+    assert all((t == 3).all() for t in kept) and all(torch.equal(a, b) for a, b in zip(out, want))
