@@ -85,33 +85,34 @@ void dequantize(const lc_w4& q, void* w, uint64_t ldw, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- the product
-// For 16-bit types codes enter the matrix instructions as whole numbers: a nibble c put into the lowest bits of the mantissa of 2^7 (bf16) or
-// 2^10 (fp16) makes 128 + c = q + 136, or 1024 + c = q + 1032, in little more than two operations for two codes, and 136 (1032) times the sum of x
-// is taken away first, by the same instruction with a constant for B or as x is brought into LDS.  All of that is exact but for the sums' own
-// rounding in 32 bits, which this makes some 136 / 4 (1032 / 4) times that of the sum of q x: 2e-6 (2e-5) of it, nothing beside the result's rounding to
-// 16 bits.  fp32 has no such rounding behind it: there codes are converted to sixteenths of q, which bf16 holds exactly (three operations for two
-// codes), and x is three bf16 parts that add up to it.  (Lifted codes, 16 + c, left 9e-7
+// For 16-bit types codes enter the matrix instructions as whole numbers: a nibble c put where the mantissa of 2^7 (bf16) or 2^6 (fp16) counts
+// whole numbers makes 128 + c = q + 136, or 64 + c = q + 72, in little more than two operations for two codes, and 136 (72) times the sum of x is taken
+// away first, by the same instruction with a constant for B or as x is brought into LDS.  All of that is exact but for the sums' own rounding in 32 bits,
+// which this makes larger by as much as a group's 136 (72) sum |x| is larger than its sum of q x: for x without a mean it leaves some 3e-6 (1e-6) of the
+// result, in groups of 128 for |x| and for x with an offset 2e-5 (1e-5), beside the result's own rounding of 1.6e-3 (2e-4).  (fp16 has room for 1024 + c as
+// well, but 1032 sum |x| left 1.4e-4.)  fp32 has no such rounding behind it: there codes are converted to sixteenths of q, which bf16 holds exactly
+// (three operations for two codes), and x is three bf16 parts that add up to it.  (Lifted codes, 16 + c, left 9e-7
 // of the result at a width of 2043 instead of 1e-7.)
 template <int T> struct Num;
 template <> struct Num<LC_BF16> {
     static constexpr bool kLifted = true;
     static constexpr float kTaken = -136.0f, kUnit = 1.0f;  // what is taken away, and what the operand counts in
     static constexpr int kParts = 1;
-    static constexpr uint32_t kBase = 0x43004300u, kLess = 0xC308C308u;        // 128, -136
+    static constexpr uint32_t kBase = 0x43004300u, kLess = 0xC308C308u, kCode = 0x000F000Fu;        // 128, -136, where a code's bits go
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F32> {
     static constexpr bool kLifted = false;
     static constexpr float kTaken = 0.0f, kUnit = 16.0f;
     static constexpr int kParts = 3;
-    static constexpr uint32_t kBase = 0, kLess = 0;
+    static constexpr uint32_t kBase = 0, kLess = 0, kCode = 0;
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_bf16(a, b, c); }
 };
 template <> struct Num<LC_F16> {
     static constexpr bool kLifted = true;
-    static constexpr float kTaken = -1032.0f, kUnit = 1.0f;
+    static constexpr float kTaken = -72.0f, kUnit = 1.0f;
     static constexpr int kParts = 1;
-    static constexpr uint32_t kBase = 0x64006400u, kLess = 0xE408E408u;        // 1024, -1032
+    static constexpr uint32_t kBase = 0x54005400u, kLess = 0xD480D480u, kCode = 0x00F000F0u;        // 64, -72
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16(a, b, c); }
 };
 template <int T> __device__ __forceinline__ f32x4 less_of(u32x4 x, f32x4 c) { return Num<T>::mfma(x, u32x4{Num<T>::kLess, Num<T>::kLess, Num<T>::kLess, Num<T>::kLess}, c); }
@@ -120,8 +121,7 @@ template <int T> __device__ __forceinline__ f32x4 less_of(u32x4 x, f32x4 c) { re
 // base would take an instruction each.)
 template <int T> __device__ __forceinline__ u32x4 codes_as_operand(uint32_t w) {
     u32x4 r;
-    const uint32_t odd = w >> 4;
-    uint32_t mask = 0x000F000Fu;
+    uint32_t mask = Num<T>::kCode;
     asm("" : "+v"(mask));
     if (!Num<T>::kLifted) {
         const uint32_t t = turned(w), u = upper_nibbles(t);
@@ -129,9 +129,12 @@ template <int T> __device__ __forceinline__ u32x4 codes_as_operand(uint32_t w) {
         for (int j = 0; j < 4; ++j) r[j] = high_halves(bits_of(low_nibble_of(t, j)), bits_of(low_nibble_of(u, j)));
         return r;
     }
+    // The lower nibble of byte j and the upper one, in words in which they stand in that byte as they go into a half: bf16 in its lower four bits, fp16 in
+    // its upper ones.
+    const uint32_t low = T == LC_F16 ? w << 4 : w, high = T == LC_F16 ? w : w >> 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t pair = __builtin_amdgcn_perm(odd, w, 0x0C000C00u | (uint32_t)j | (uint32_t)(4 + j) << 16);      // byte j of w, byte j of odd
+        const uint32_t pair = __builtin_amdgcn_perm(high, low, 0x0C000C00u | (uint32_t)j | (uint32_t)(4 + j) << 16);      // byte j of low, byte j of high
         r[j] = (pair & mask) | Num<T>::kBase;
     }
     return r;
