@@ -118,6 +118,14 @@ template <int T> __device__ __forceinline__ void store_four(void* p, uint64_t i,
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + i) = w;
 }
 
+// Between what lanes of a wavefront put into LDS and what others of it read there, or the other way round: the compiler moves neither past it.  (A wavefront's
+// LDS operations come about in their order, so it takes no instruction.)
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // The largest of `lanes` neighbouring lanes' values in every one of them (lanes: 4, 8, 16 or 32, aligned).
 template <int LANES> __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
 #define LC_DPP_MAX(ctrl) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false); v = v > o ? v : o; }

@@ -329,8 +329,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per)
             const uint32_t now = first + b * S;
             if (now >= end) break;
             keep(two[b]);
+            lanes_meet();                                    // (a lane reads what others of its wavefront put there ...)
             if (now + S < end) fetch(two[1 - b], now + S);
             use_batch(two[b], now);
+            lanes_meet();                                    // (... which is read before the next batch takes its place)
         }
     }
     if (p.k % 128 && wave == WAVES - 1) {                    // what is left behind the last whole step, straight from memory
