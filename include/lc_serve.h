@@ -100,7 +100,8 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
  *   mask    NULL, or uint64 [batch][nq]: drafted token i sees drafted token j iff bit j of mask[i] is set (a tree's ancestors and
  *           itself).  NULL: j <= i.  Everything before the drafted tokens is seen by all of them.  nq is at most 64; nq = 1 is
  *           the step of one token.
- *   out     softmax over the seen tokens of (scale * q . k), times v; zeros where a token sees nothing.  Sums, maxima and
+ *   out     softmax over the seen tokens of (scale * q . k), times v; zeros where a token sees nothing, NaN where it sees anything with
+ *           an infinity or NaN in q.  (Scores are summed as multiples of a key's scale: a head's sum of |q| has to stay below 2^120.)  Sums, maxima and
  *           products with the probabilities are held in 32 bits.  Keys and values that are not seen do not matter, whatever they hold.
  *   ws      scratch, 256-byte aligned, lc_kv_workspace_bytes; its content need not be anything.  Calls that may run at the same
  *           time (on different streams) need areas of their own.

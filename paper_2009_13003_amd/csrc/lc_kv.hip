@@ -382,6 +382,10 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
             else d = 2 * Raw::kKey * h + 8 * Raw::kKey * (o / Raw::kKeyWords) + 8 * (o % Raw::kKeyWords);
             float v[8];
             load_eight<T>(a.q, q_at + d, has_row && d < a.c.dim ? 8 : 0, v);
+            // An infinity is taken as NaN: the score of whatever is seen is infinite or NaN, so the softmax of any set of them is NaN, and scores that are
+            // all minus infinity would look like those of what is not seen.
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += v[e] - v[e];
 #pragma unroll
             for (int p = 0; p < NQ; ++p) {
 #pragma unroll
