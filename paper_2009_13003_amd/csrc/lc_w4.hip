@@ -197,13 +197,32 @@ struct Product {
 };
 
 // One element of y straight from the formula, where the sums above are not finite: infinity - infinity is not what an infinity in
-// x gives, and what is taken away, the sum before its scale or sixteen times a scale may be out of range where the result is not.
+// x gives, and what is taken away, the sum before its scale or sixteen times a scale may be out of range where the result is not.  One sum after
+// another, 32 elements of the width to a step, up to the first NaN, behind which nothing changes any more; a NaN among the scales is looked for first.
+// (Element by element to the end an infinity in one row of 4096 took 400 us, 256 rows of NaN by 4096x4096 14.5 ms.)
 template <int T, int G>
 __device__ __forceinline__ float one_by_formula(const Product& p, uint32_t i, uint32_t j) {
+    const uint8_t* codes = p.codes + j * p.codes_pitch;
+    const uint16_t* scales = p.scales + j * p.scales_pitch;
     float total = 0;
-    for (uint32_t l = 0; l < p.k; ++l) {
-        const uint32_t c = p.codes[j * p.codes_pitch + l / 2] >> (4 * (l % 2)) & 15u;
-        total = fmaf(load_one<T>(p.x, i * p.ldx + l), (float)((int)c - 8) * of_bf16(p.scales[j * p.scales_pitch + l / G]), total);   // (q s is exact)
+#pragma unroll 4
+    for (uint32_t g = 0; g < p.groups; ++g)
+        if ((scales[g] & 0x7fffu) > 0x7f80u) total = __builtin_nanf("");
+    for (uint32_t l = 0; l < p.k && total == total; l += 32) {
+        const u32x4 words = *reinterpret_cast<const u32x4*>(codes + l / 2);
+        const float s = of_bf16(scales[l / G]);
+        Raw<T> raw[4];
+#pragma unroll
+        for (uint32_t o = 0; o < 4; ++o) {
+            const uint32_t at = l + 8 * o;
+            raw[o] = x_as_it_is<T>(p.x, i * p.ldx + at, at < p.k ? (int)(p.k - at < 8 ? p.k - at : 8) : 0);
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 32; ++e) {
+            const uint32_t at = e % 8, bits = T == LC_F32 ? raw[e / 8].w[at / 4][at % 4] : raw[e / 8].w[0][at / 2] >> (16 * (at % 2)) & 0xffffu;
+            const float x = T == LC_F32 ? float_of(bits) : T == LC_BF16 ? of_bf16(bits) : of_f16(bits);
+            if (l + e < p.k) total = fmaf(x, (float)((int)(words[e / 8] >> (4 * at) & 15u) - 8) * s, total);      // (q s is exact)
+        }
     }
     return total;
 }
