@@ -608,11 +608,17 @@ __global__ __launch_bounds__(64 * WM * WN * WK, PERSIMD) void k_w4_tiles(Product
 
 template <int T>
 __global__ __launch_bounds__(256) void k_w4_bias_only(Product p) {      // k = 0
-    const uint64_t e = blockIdx.x * 256ull + threadIdx.x;
-    if (e >= (uint64_t)p.m * p.n) return;
-    const uint64_t i = e / p.n, j = e % p.n;
-    store_one<T>(p.y, i * p.ldy + j, p.bias ? load_one<T>(p.bias, j) : 0.0f);
+    for (uint64_t e = blockIdx.x * 256ull + threadIdx.x; e < (uint64_t)p.m * p.n; e += gridDim.x * 256ull) {
+        const uint64_t i = e / p.n, j = e % p.n;
+        store_one<T>(p.y, i * p.ldy + j, p.bias ? load_one<T>(p.bias, j) : 0.0f);
+    }
 }
+
+// A launch's threads have to be fewer than 2^32.
+constexpr uint64_t kMostRows = 1ull << 19;                  // of x
+constexpr uint64_t kAtOnce16 = 1ull << 22, kAtOnceTiles = (1ull << 17) - 128;      // rows of w in a launch, for up to 16 rows of x and for more
+constexpr uint32_t kMostBiasBlocks = 1u << 22;
+template <typename L> constexpr bool kLaunches = (kMostRows + L::kRows - 1) / L::kRows * ((kAtOnceTiles + L::kCols - 1) / L::kCols) * L::kThreads < 1ull << 32;
 
 template <int T, int G, int MR, int WAVES, int S>
 void product_of_rows(const Product& p, hipStream_t s) {
@@ -657,12 +663,14 @@ void product(const Product& p, hipStream_t s) {
             if (fits(16, 32)) product_of_tiles<T, G, 1, 2, 1, 1, 4, 1>(p, s);
             else if (fits(32, 64)) product_of_tiles<T, G, 2, 1, 1, 4, 2, 1>(p, s);
             else product_of_tiles<T, G, 2, 2, 1, 4, 1, 1>(p, s);
+            static_assert(kLaunches<Tile<T, 2, 2, 1, 4, 1>>, "threads of the largest launch");      // (the others' tiles are a few hundred)
         } else {
             if (p.m <= 32) product_of_tiles<T, G, 2, 1, 1, 1, 8, 1>(p, s);
             else if (fits(32, 32)) product_of_tiles<T, G, 2, 2, 1, 1, 8, 1>(p, s);
             else if (fits(32, 64)) product_of_tiles<T, G, 2, 2, 1, 2, 4, 1>(p, s);
             else if (fits(64, 64, 512)) product_of_tiles<T, G, 4, 1, 1, 4, 2, 1>(p, s);
             else product_of_tiles<T, G, 4, 2, 1, 4, 1, 3>(p, s);
+            static_assert(kLaunches<Tile<T, 4, 2, 1, 4, 1>>, "threads of the largest launch");
         }
         return;
     }
@@ -721,7 +729,7 @@ int lc_w4_dequantize(const lc_w4* w4, void* w, uint64_t ldw, int dtype, void* st
 }
 
 int lc_w4_matmul(const void* x, uint64_t ldx, uint64_t m, const lc_w4* w4, const void* bias, void* y, uint64_t ldy, int dtype, void* stream) {
-    if (!served_type(dtype) || bad(w4) || m > (1u << 19)) return LC_ERR_BADARG;
+    if (!served_type(dtype) || bad(w4) || m > kMostRows) return LC_ERR_BADARG;
     if (m == 0 || w4->n == 0) return LC_OK;
     const uintptr_t size = size_of(dtype);
     if (!y || off(y, size) || ldy < w4->n || ldy > (1ull << 40) || (bias && off(bias, size))) return LC_ERR_BADARG;
@@ -731,15 +739,14 @@ int lc_w4_matmul(const void* x, uint64_t ldx, uint64_t m, const lc_w4* w4, const
                        (uint32_t)m, (uint32_t)q.n, (uint32_t)q.k, (uint32_t)lc_w4_row_bytes(q.k), (uint32_t)((q.k + q.group - 1) / q.group)};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (q.k == 0) {
-        const uint64_t blocks = ((uint64_t)p.m * p.n + 255) / 256;
-        if (blocks > 0x7fffffffull) return LC_ERR_BADARG;
-        if (dtype == LC_F32) k_w4_bias_only<LC_F32><<<(uint32_t)blocks, 256, 0, s>>>(p);
-        else if (dtype == LC_BF16) k_w4_bias_only<LC_BF16><<<(uint32_t)blocks, 256, 0, s>>>(p);
-        else k_w4_bias_only<LC_F16><<<(uint32_t)blocks, 256, 0, s>>>(p);
+        const uint64_t all = ((uint64_t)p.m * p.n + 255) / 256;
+        const uint32_t blocks = all < kMostBiasBlocks ? (uint32_t)all : kMostBiasBlocks;
+        if (dtype == LC_F32) k_w4_bias_only<LC_F32><<<blocks, 256, 0, s>>>(p);
+        else if (dtype == LC_BF16) k_w4_bias_only<LC_BF16><<<blocks, 256, 0, s>>>(p);
+        else k_w4_bias_only<LC_F16><<<blocks, 256, 0, s>>>(p);
         return launched();
     }
-    // Over at most this many rows of w at once, so that a launch's threads are counted in 32 bits.
-    const uint64_t step = m > 16 ? 1ull << 17 : 1ull << 22;
+    const uint64_t step = m > 16 ? kAtOnceTiles : kAtOnce16;
     for (uint64_t j = 0; j < q.n; j += step) {
         Product some = p;
         some.codes += j * q.codes_pitch, some.scales += j * q.scales_pitch, some.n = (uint32_t)(q.n - j < step ? q.n - j : step);
