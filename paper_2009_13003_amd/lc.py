@@ -550,6 +550,10 @@ def _matrix(t):
     return t.data_ptr(), (t.stride(0) if n > 1 else k)
 
 
+# The calls below have no backward pass: where a gradient is asked for through one it is refused, instead of a result that none flows through.
+_NO_GRADIENT = "no gradient flows through this call: detach its inputs, or call it under torch.no_grad()"
+
+
 def _torch_stream(stream):
     if isinstance(stream, torch.cuda.Stream):
         return stream
@@ -614,12 +618,14 @@ def lc_w4_dequantize(w4, dtype=None, out=None, stream=None):
 
 
 def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
-    """x [m][k] times w4 [n][k] transposed, plus bias [n]: a matrix [m][n] of x's dtype (or in `out`)."""
+    """x [m][k] times w4 [n][k] transposed, plus bias [n]: a matrix [m][n] of x's dtype (or in `out`).  No gradient flows through it."""
     p, ld = _matrix(x)
     m, k = x.shape
     dtype, n = x.dtype, w4.n
     assert k == w4.k
+    assert not x.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
     if bias is not None:
+        assert not bias.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
         assert bias.is_cuda and bias.dtype == dtype and bias.shape == (n,) and (bias.stride(0) == 1 or n <= 1)
         bias = bias.data_ptr()
     if out is None:
@@ -678,6 +684,7 @@ def _slots(slots, tokens):
 def lc_kv_write(cache, k, v, slots, stream=None):
     """Quantises k and v [tokens][heads][dim] into the cache at `slots` (int64 [tokens]; a negative one is passed over)."""
     ldt, ldh = _vectors(cache, k, v)
+    assert not (k.requires_grad or v.requires_grad) or not torch.is_grad_enabled(), _NO_GRADIENT
     tokens = k.shape[0]
     st = _lib.lc_kv_write(cache._p, k.data_ptr(), v.data_ptr(), ldt, ldh, _slots(slots, tokens), tokens, SERVED[k.dtype], _handle(stream))
     if st != OK:
@@ -721,9 +728,10 @@ def new_kv_workspace(cache, batch, nq, heads, stream=None):
 def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None, stream=None):
     """Attention of q [batch][nq][heads][dim] over the cache: table int32 [batch][pages a sequence], lens int32 [batch] (the nq
     newest tokens are the drafted ones), mask int64 [batch][nq] of the bits that each drafted token sees (None: itself and
-    those before it).  scale: 1 / sqrt(dim) if None.  ws: a tensor from new_kv_workspace (None: allocated for this call)."""
+    those before it).  scale: 1 / sqrt(dim) if None.  ws: a tensor from new_kv_workspace (None: allocated for this call).  No gradient flows through it."""
     batch, nq, heads, dim = q.shape
     assert q.is_cuda and q.dtype in SERVED and q.is_contiguous() and dim == cache.dim
+    assert not q.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
     assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == batch and (table.stride(1) == 1 or table.shape[1] <= 1)
     assert lens.is_cuda and lens.dtype == torch.int32 and lens.shape == (batch,) and lens.is_contiguous()
     if mask is not None:
