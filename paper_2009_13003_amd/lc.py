@@ -671,8 +671,8 @@ def _vectors(cache, k, v):
     assert k.is_cuda and v.is_cuda and k.dtype in SERVED and v.dtype == k.dtype and k.dim() == 3 and v.shape == k.shape
     tokens, heads, dim = k.shape
     assert heads == cache.heads and dim == cache.dim
-    st, sh, s1 = k.stride()
-    assert s1 == 1 and (v.stride() == k.stride() or tokens == 0), "keys and values need contiguous heads and the same pitches"
+    (st, sh, s1), (vt, vh, v1) = k.stride(), v.stride()      # (the pitch of an axis of one element says nothing)
+    assert tokens == 0 or s1 == v1 == 1 and (st == vt or tokens == 1) and (sh == vh or heads == 1), "keys and values need contiguous heads and the same pitches"
     return (st if tokens > 1 else heads * dim), (sh if heads > 1 else dim)
 
 
