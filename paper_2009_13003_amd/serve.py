@@ -124,7 +124,7 @@ def seen_before(b, known):
 def write_on(model, prompt, count, drafts=2, guess=seen_before):
     """The `count` tokens a sequence that model writes behind prompt [batch][n], each the likeliest; and the number of passes it took.  With drafts,
     a pass judges the known next token and, below it, a tree: `drafts` of the tokens that guess(b, tokens of sequence b) lists to follow, and
-    one below each."""
+    one below each, as long as the model's context has room for the tree."""
     batch, device = model.batch, prompt.device
     known = [p.tolist() for p in prompt]
     for b, t in enumerate(model.read_in(prompt).argmax(-1).tolist()):
@@ -138,10 +138,12 @@ def write_on(model, prompt, count, drafts=2, guess=seen_before):
         sees.append((sees[a] if a >= 0 else 0) | 1 << i)
     mask = torch.tensor([sees] * batch, dtype=torch.int64, device=device)
     while min(map(len, known)) < goal:
+        if max(model.count) + len(above) > model.shape.context:              # no room for the tree any more: the known token alone
+            drafts, above, depth, mask = 0, above[:1], depth[:1], mask[:, :1].contiguous()
         rows = []
         for b, k in enumerate(known):
-            below = guess(b, k)
-            below = (below + [below[-1]] * drafts)[:drafts]
+            below = guess(b, k) if drafts else []
+            below = (below + below[-1:] * drafts)[:drafts]
             rows.append([k[-1]] + below + [guess(b, k + [t])[0] for t in below])
         first = model.count
         best = model.step(torch.tensor(rows, device=device), depth, mask).argmax(-1).tolist()
