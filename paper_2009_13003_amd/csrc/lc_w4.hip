@@ -639,12 +639,17 @@ void product_of_tiles(const Product& p, hipStream_t s) {
 // 11008x4096 7.8, 8.9, 11.5, by 8192x8192 10.6, 9.6, 13.1, by 32000x4096 (groups of 32) 20.0, 21.6, 28.7, by 4096x11008 (32) 11.8, 9.0, 8.0; 13 rows
 // there 19.5, 12.5, 11.0; one row by 4096x4096 in fp32 8.8, 6.9, 6.9, 16 rows by 11008x4096 20.6, 24.4, 47.5.  Two steps instead of one: 11008x4096
 // 7.8 for 8.7 with 4 wavefronts, 8192x8192 9.6 for 11.0 with 8; but in groups of 32 32000x4096 21.1 for 20.0.
+// Sixteen for eight where workgroups are no more than compute units (kernels in a row, bf16, groups of 128): 13 rows by 4096x1500 4.0 for 3.8, x2048 3.9
+// for 4.1, x4096 6.0 for 6.5, x8192 9.4 for 10.0, x16384 15.1 for 16.7, by 512x2048 3.6 for 3.8; so from a step for each on.  One row by 4096x2048 3.4 for
+// 3.3, x4096 4.9 for 5.2, x8192 7.5 for 7.3, x11008 7.5 for 8.4, x16384 11.4 for 10.9, by 1000x8192 6.3 for 5.7, x11008 6.5 for 7.0, in groups of 32 by
+// 4096x4096 5.2 for 5.4, x8192 7.9 for 7.9, x11008 8.3 for 9.3, x16384 12.0 for 12.6, by 1000x4096 4.5 for 4.4, x8192 6.7 for 7.0: from four steps for each on.  By
+// 6144 and more columns of y sixteen are slower at any width (13 rows by 6144x11008 17.4 for 16.8).
 template <int T, int G, int MR>
 void product_of_few(const Product& p, hipStream_t s) {
     constexpr int FOUR = T != LC_F32 && G == 128 ? 2 : 1, EIGHT = T != LC_F32 && G == 128 && MR == 4 ? 2 : 1;
     const uint32_t blocks = (p.n + 15) / 16;
     if constexpr (T != LC_F32)
-        if (blocks <= 256 && p.k >= 8192) return product_of_rows<T, G, MR, 16, 1>(p, s);
+        if (blocks <= 256 && p.k >= (MR == 16 ? 1 : 4) * 16 * 128) return product_of_rows<T, G, MR, 16, 1>(p, s);
     if (blocks <= 512) product_of_rows<T, G, MR, 8, EIGHT>(p, s);
     else product_of_rows<T, G, MR, 4, FOUR>(p, s);
 }
