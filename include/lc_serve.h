@@ -81,7 +81,7 @@ typedef struct lc_kv_cache {
  * Quantises the keys and values of `tokens` tokens into the cache: k and v are [tokens][heads][dim] of type dtype, token i at
  * element i * ld_token, head h at h * ld_head behind that (both may be any multiple of 1 that keeps vectors apart).
  * slots: int64 [tokens], the slot of each token; a slot outside [0, pages * page_tokens) is passed over.  If a slot
- * occurs twice, which of its tokens it holds afterwards is not defined.
+ * occurs twice, what it holds afterwards is not defined: its codes and scales may come from either of the tokens.
  */
 int lc_kv_write(const lc_kv_cache* cache, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots,
                 uint64_t tokens, int dtype, void* stream);
@@ -102,8 +102,10 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
  *           itself).  NULL: j <= i.  Everything before the drafted tokens is seen by all of them.  nq is at most 64; nq = 1 is
  *           the step of one token.
  *   out     softmax over the seen tokens of (scale * q . k), times v; zeros where a token sees nothing, NaN where it sees anything with
- *           an infinity or NaN in q.  (Scores are summed as multiples of a key's scale: a head's sum of |q| has to stay below 2^120.)  Sums, maxima and
- *           products with the probabilities are held in 32 bits.  Keys and values that are not seen do not matter, whatever they hold.
+ *           an infinity or NaN in q.  Scores, maxima and sums are held in 32 bits; probabilities, times the values' scales, enter the product with the values
+ *           with their first 16 bits or more (fp32: all 24), the rest cut off, which leaves results up to 2^-15 too small, and half a unit of 16 bits is
+ *           2^-11 or more.  A head's sum of |q|, and |v| summed over the tokens seen, have to stay below 2^120.  Keys and values that are not seen do
+ *           not matter, whatever they hold.
  *   ws      scratch, 256-byte aligned, lc_kv_workspace_bytes; its content need not be anything.  Calls that may run at the same
  *           time (on different streams) need areas of their own.
  */

@@ -73,3 +73,22 @@ def test_what_the_current_stream_works_on_stays(calls, name):
     out = calls[name](stream=side)
     torch.cuda.synchronize()
     assert all((t == 3).all() for t in kept) and all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_on_a_side_stream_of_a_graph(calls, name):
+    want = calls[name]()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        out = calls[name](stream=side)
+        here.wait_stream(side)
+    for _ in range(3):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert all(torch.equal(a, b) for a, b in zip(calls[name](), want))
