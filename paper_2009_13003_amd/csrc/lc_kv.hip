@@ -87,7 +87,10 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[n][e] = (BITS == 8 ? (float)(int8_t)(w[n] >> (8 * e)) : (float)((int)(w[n] >> (4 * e) & 15u) - 8)) * s[n];
+            for (int e = 0; e < N; ++e) {
+                x[n][e] = (BITS == 8 ? (float)(int8_t)(w[n] >> (8 * e)) : (float)((int)(w[n] >> (4 * e) & 15u) - 8)) * s[n];
+                if (T == LC_F16) asm("" : "+v"(x[n][e]));    // (else product and conversion become one instruction, with one rounding for the two)
+            }
     }
     store_some<T>(k, token * ld_token + head * ld_head + at, N, x[0]);
     store_some<T>(v, token * ld_token + head * ld_head + at, N, x[1]);
