@@ -103,9 +103,8 @@ int lc_kv_read(const lc_kv_cache* cache, const int64_t* slots, uint64_t tokens, 
  *           the step of one token.
  *   out     softmax over the seen tokens of (scale * q . k), times v; zeros where a token sees nothing, NaN where it sees anything with
  *           an infinity or NaN in q.  Scores, maxima and sums are held in 32 bits; probabilities, times the values' scales, enter the product with the values
- *           with their first 16 bits or more (fp32: all 24), the rest cut off, which leaves results up to 2^-15 too small, and half a unit of 16 bits is
- *           2^-11 or more.  A head's sum of |q|, and |v| summed over the tokens seen, have to stay below 2^120.  Keys and values that are not seen do
- *           not matter, whatever they hold.
+ *           rounded to nearest with 16 bits or more (fp32: 24), 2^-16 of each at most.  A head's sum of |q|, and |v| summed over the tokens
+ *           seen, have to stay below 2^120.  Keys and values that are not seen do not matter, whatever they hold.
  *   ws      scratch, 256-byte aligned, lc_kv_workspace_bytes; its content need not be anything.  Calls that may run at the same
  *           time (on different streams) need areas of their own.
  */

@@ -104,7 +104,8 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 //                    in the order 4 h + 0..3, 16 + 4 h + 0..3, in which the values are then loaded too
 // so the running maximum, the sum and the factors of the rescaling are one number a lane, and nothing passes through LDS.
 // Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly, and
-// probabilities times scales as two bf16 parts (three for fp32): one part alone, 2^-9 of each, would show beside a result in fp16.
+// probabilities times scales as two bf16 parts (three for fp32), the first cut off and the last rounded to nearest: 2^-16 of each at most, either way.  One
+// part alone, 2^-9 of each, would show beside a result in fp16; with the last one cut off as well results were 7e-6 too small on average.
 // One token of 16 sequences of up to 4096 tokens of 32 heads (8 bits): 63 us, 4.7 TB/s of the cache, which is near what memory gives.  24 drafted
 // tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 43 us for what memory would give in 6: each tile of 32 tokens by 32 queries
 // takes 350 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
@@ -500,9 +501,10 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_attend(Attend a) {
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pp[n][k][i] = high_halves(bits_of(p[2 * i]), bits_of(p[2 * i + 1]));
+                for (int i = 0; i < 4; ++i) pp[n][k][i] = k == NP - 1 ? rounded_halves(p[2 * i], p[2 * i + 1]) : high_halves(bits_of(p[2 * i]), bits_of(p[2 * i + 1]));
+                if (k < NP - 1)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] -= float_of(bits_of(p[i]) & 0xffff0000u);
+                    for (int i = 0; i < 8; ++i) p[i] -= float_of(bits_of(p[i]) & 0xffff0000u);
             }
         }
 #pragma unroll

@@ -189,6 +189,13 @@ template <bool HALF> __device__ __forceinline__ float dot_16(uint32_t a, uint32_
     return __builtin_amdgcn_fdot2_f32_bf16(x, y, c, false);
 }
 
+// a and b rounded to bf16 (to nearest even), a below b.
+__device__ __forceinline__ uint32_t rounded_halves(float a, float b) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    const bf16x2 r = __builtin_convertvector(f32x2{a, b}, bf16x2);
+    uint32_t u; __builtin_memcpy(&u, &r, 4);
+    return u;
+}
 // The high halves of a and b, a's below b's.
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
