@@ -106,15 +106,20 @@ __global__ __launch_bounds__(256) void k_kv_read(Cache c, const int64_t* slots, 
 // Scales of keys multiply the scores, scales of values the probabilities; codes enter the matrix instructions as whole numbers, exactly, and
 // probabilities times scales as two bf16 parts (three for fp32), the first cut off and the last rounded to nearest: 2^-16 of each at most, either way.  One
 // part alone, 2^-9 of each, would show beside a result in fp16; with the last one cut off as well results were 7e-6 too small on average.
-// One token of 16 sequences of up to 4096 tokens of 32 heads (8 bits): 63 us, 4.7 TB/s of the cache, which is near what memory gives.  24 drafted
-// tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 43 us for what memory would give in 6: each tile of 32 tokens by 32 queries
-// takes 350 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
-// three workgroups convert a head's codes each for its own rows.  One token of one sequence of 1000: 9 us, latencies in a row: launch 2.3, lengths,
-// pages, tiles, and a meeting of the parts.
+// One token of 16 sequences of up to 4096 tokens of 32 heads (8 bits): 63 to 67 us, 4.4 to 4.7 TB/s of the cache, two thirds of the 7 that a bare read
+// reaches (42 us); vector instructions half of its cycles; fp32 68.  The same in 4 bits 50 us (fp32 54), of 8 heads for 32 queries up to 16384 46 (59), where the
+// bytes take 21.  Heads of 160, 192 and 256 (16 of them, 8 bits) 50, 55 and 67 us, in 4 bits 40,
+// 43 and 44: all are worked on as 256.  24 drafted
+// tokens of 5 sequences of up to 8191, 4 queries to a head (4 bits): 43 us for what memory would give in 4 to 6 and products at the rate of large ones in 8: each tile of
+// 32 tokens by 32 queries takes 350 vector instructions, half of them to convert codes and half for the softmax, beside 48 of the matrix unit's (16% of the time), and
+// three workgroups convert a head's codes each for its own rows; 8 bits 48 us, fp32 66 to 68.  One token of one sequence of 1000: 9 us, latencies in a row: launch 2.3,
+// lengths, pages, tiles, and a meeting of the parts.
 constexpr int kTile = 32, kWaves = 4;
 constexpr float kFar = 8.0f;                                // by how much, in powers of two, a score may pass what probabilities are measured from
 constexpr float kLog2e = 1.44269504088896340736f;
-// A sequence whose heads and queries alone do not give the chip as many workgroups as fit it at once is split along its tokens.
+// A sequence whose heads and queries alone do not give the chip as many workgroups as fit it at once is split along its tokens, into as many parts at most as
+// a wavefront has lanes to look at the parts' marks with, less a few.  (One sequence of 32768 tokens of one head, 8 queries: 60 workgroups, 24 us in 8 bits; of 8
+// heads, 480 of them, 30 us.)
 constexpr uint32_t kMostSplits = 60, kLeastTokens = kWaves * kTile;
 
 struct Attend {

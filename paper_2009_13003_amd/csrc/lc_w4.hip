@@ -387,7 +387,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_w4_rows(Product p, uint32_t per)
 // width.  x passes through LDS, 128 WK elements of the width at a time, twice buffered: the next piece is under way in registers while this
 // one is worked on, and goes into the other buffer between two of the products of this one: what puts it there then waits in the products' shade.
 // Codes come straight into registers and are unpacked by the wavefront that needs them.
-// 2048 rows by 4096x11008 (bf16, groups of 128): 226 us, 816 TFLOP/s, 191 on constant data; a plain product of bf16 by the library takes 164.  x put
+// 2048 rows by 4096x11008 (bf16, groups of 128): 224 to 234 us from run to run, 790 to 825 TFLOP/s, 191 on constant data; a plain product of bf16 by the library takes 164 to 167.  x put
 // away behind all products 261; matrix instructions are under way a third of the time, vector instructions half of it: unpacking eight codes takes
 // eight of them and a scale one for each four sums, and the two share a wavefront's turn.  More loads ahead (three buffers, two pieces in registers)
 // cost the third wavefront a SIMD and were slower.
