@@ -561,17 +561,21 @@ def _torch_stream(stream):
     return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
 
 
-def _empty_on(stream, *size, dtype, device):
-    """torch.empty for a call on `stream`, which need not be the current one: from that stream's memory, since a block of the current one's may
-    still be in use by what is enqueued there, which `stream` does not wait for.  Freed, it waits for the current stream's work too, where
+def _made_on(stream, make):
+    """What make() allocates for a call on `stream`, which need not be the current one: from that stream's memory, since a block of the current one's
+    may still be in use by what is enqueued there, which `stream` does not wait for.  Freed, it waits for the current stream's work too, where
     the caller is most likely to use it."""
     s, now = _torch_stream(stream), torch.cuda.current_stream()
     if s == now:
-        return torch.empty(*size, dtype=dtype, device=device)
-    with torch.cuda.stream(s):
-        t = torch.empty(*size, dtype=dtype, device=device)
-    t.record_stream(now)
-    return t
+        return make()
+    torch.cuda.set_stream(s)                                 # (the context manager for it takes 6 us more)
+    try:
+        made = make()
+    finally:
+        torch.cuda.set_stream(now)
+    for t in made:
+        t.record_stream(now)
+    return made
 
 
 def lc_w4_quantize(w, group, out=None, stream=None):
@@ -582,12 +586,8 @@ def lc_w4_quantize(w, group, out=None, stream=None):
         if group not in (32, 64, 128):
             raise LcError(ERR_BADARG)
         row, groups, device = (k + 31) // 32 * 16, -(-k // group), w.device
-        if stream is None:
-            codes = torch.empty(n, row, dtype=torch.uint8, device=device)
-            scales = torch.empty(n, groups, dtype=torch.bfloat16, device=device)
-        else:
-            codes = _empty_on(stream, n, row, dtype=torch.uint8, device=device)
-            scales = _empty_on(stream, n, groups, dtype=torch.bfloat16, device=device)
+        make = lambda: (torch.empty(n, row, dtype=torch.uint8, device=device), torch.empty(n, groups, dtype=torch.bfloat16, device=device))
+        codes, scales = make() if stream is None else _made_on(stream, make)
         out = W4.__new__(W4)
         out._describe(codes, scales, n, k, group, row, groups)
     else:
@@ -602,10 +602,8 @@ def lc_w4_dequantize(w4, dtype=None, out=None, stream=None):
     """The values that w4 stands for, as a matrix of `dtype` (or in `out`)."""
     if out is None:
         dtype = torch.float32 if dtype is None else dtype
-        if stream is None:
-            out = torch.empty(w4.n, w4.k, dtype=dtype, device=w4.codes.device)
-        else:
-            out = _empty_on(stream, w4.n, w4.k, dtype=dtype, device=w4.codes.device)
+        make = lambda: (torch.empty(w4.n, w4.k, dtype=dtype, device=w4.codes.device),)
+        out, = make() if stream is None else _made_on(stream, make)
         p, ld = out.data_ptr(), w4.k
     else:
         p, ld = _matrix(out)
@@ -629,7 +627,7 @@ def lc_w4_matmul(x, w4, bias=None, out=None, stream=None):
         assert bias.is_cuda and bias.dtype == dtype and bias.shape == (n,) and (bias.stride(0) == 1 or n <= 1)
         bias = bias.data_ptr()
     if out is None:
-        out = x.new_empty(m, n) if stream is None else _empty_on(stream, m, n, dtype=dtype, device=x.device)
+        out = x.new_empty(m, n) if stream is None else _made_on(stream, lambda: (x.new_empty(m, n),))[0]
         q, ldq = out.data_ptr(), n
     else:
         q, ldq = _matrix(out)
@@ -696,11 +694,8 @@ def lc_kv_read(cache, slots, dtype=None, out=None, stream=None):
     tokens = slots.shape[0]
     if out is None:
         heads, dim, dtype = cache.heads, cache.dim, torch.float32 if dtype is None else dtype
-        if stream is None:
-            k = torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device)
-            v = torch.empty_like(k)
-        else:
-            k, v = (_empty_on(stream, tokens, heads, dim, dtype=dtype, device=slots.device) for _ in range(2))
+        make = lambda: (torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device), torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device))
+        k, v = make() if stream is None else _made_on(stream, make)
         ldt, ldh = heads * dim, dim
     else:
         k, v = out
@@ -719,10 +714,8 @@ def lc_kv_workspace_bytes(batch, nq, heads, kv_heads, dim):
 
 def new_kv_workspace(cache, batch, nq, heads, stream=None):
     """Scratch for lc_kv_attend with these sizes, to be used on `stream` (None: the current one); calls that may run at the same time need one each."""
-    size = lc_kv_workspace_bytes(batch, nq, heads, cache.heads, cache.dim)
-    if stream is None:
-        return torch.empty(size, dtype=torch.uint8, device=cache.k.device)
-    return _empty_on(stream, size, dtype=torch.uint8, device=cache.k.device)
+    make = lambda: (torch.empty(lc_kv_workspace_bytes(batch, nq, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device),)
+    return (make() if stream is None else _made_on(stream, make))[0]
 
 
 def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None, stream=None):
@@ -738,7 +731,7 @@ def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None
         assert mask.is_cuda and mask.dtype == torch.int64 and mask.shape == (batch, nq) and mask.is_contiguous()
         mask = mask.data_ptr()
     if out is None:
-        out = torch.empty_like(q) if stream is None else _empty_on(stream, batch, nq, heads, dim, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q) if stream is None else _made_on(stream, lambda: (torch.empty_like(q),))[0]
     else:
         assert out.is_cuda and out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
     if ws is None:
