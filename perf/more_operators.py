@@ -1,0 +1,513 @@
+"""The operators that take prompts in and drafted tokens out of a served checkpoint, as they are measured: weights and activations
+in 8 bits and their products, the pages and slots of a paged cache given out and taken back on the card, the attention of a prompt's piece over
+that cache, and drafted tokens judged against the model's probabilities.
+
+`run` computes them in their plain form (elementary torch operations in 32 bits, 64 where a whole number hangs on the result, rounded
+once at the end) or, where `own` is true, by the calls that a user makes of the package's operators.  `exact` computes the same in 64 bits from the
+definitions:
+
+  product   a row of x or w shares a scale s = fl32(max|x| * fl32(1/127)), q = rint(fl32(x * fl32(1/s))) in [-127, 127];
+            y[i][j] = (sum_l qx[i][l] qw[j][l]) * sx[i] * sw[j] + bias[j]
+  pages     sequence b of lens[b] cached tokens gets add[b] more: the pages behind ceil(lens / page) come off the end of a list of free
+            ones, in order of the sequences; the leading sequences for which pages, table and room for new tokens suffice.  Of every new
+            token its slot (page * tokens a page + token), its place in the sequence and its sequence.  Taken back: sequences keep
+            their first tokens, and the pages behind them return to the list, last ones first
+  prompts   attention of the n new tokens of each sequence, the newest of its `lens` cached ones, over what is cached up to themselves:
+            softmax(scale * q . k) . v; codes of 8 or 4 bits with a scale per token and head
+  drafts    node 0 of a sequence is known; node i was drafted below parent[i] (one behind the other without parents).  Below the node where
+            the path stands nodes are tried in order: i is taken if u[i] * q(token i) < p(token i), q being what it was drawn from
+            (without it: u[i] * what p has left once the siblings before it are taken away < p(token i)).  Behind the path the next token is
+            the first whose running sum of what is left, max(p - q, 0) or p without what was refused, exceeds u[0] of the whole sum
+"""
+import math
+
+import torch
+
+own = False
+
+_TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+_SMALLEST = 2.0 ** -126
+
+
+# ---------------------------------------------------------------- the cases
+def listed():
+    return [
+        # one token through the widest matrix of a 6.7 B parameter model's layer
+        {"name": "product 1x11008x4096 bf16", "op": "product", "m": 1, "n": 11008, "k": 4096, "dtype": "bf16", "bias": False},
+        # odd sizes in 32 bits: a classifier's rows over a width that is no multiple of anything
+        {"name": "product 7x1000x2043 f32", "op": "product", "m": 7, "n": 1000, "k": 2043, "dtype": "f32", "bias": True},
+        # a prompt of 2048 tokens through the way back
+        {"name": "product 2048x4096x11008 bf16", "op": "product", "m": 2048, "n": 4096, "k": 11008, "dtype": "bf16", "bias": False},
+        # the step of a batch that decodes: one token each, a page for every sixteenth sequence
+        {"name": "pages 48 x 1 token", "op": "pages", "batch": 48, "add": 1, "longest": 4096, "page": 16, "room": 48},
+        # a wave of prompts for which the free pages do not suffice, in an array with room to spare
+        {"name": "pages 300 prompts", "op": "pages", "batch": 300, "add": 211, "longest": 700, "page": 32, "room": 40000},
+        # a short question to a small model: latency counts
+        {"name": "prompt 100 of 100", "op": "prompt", "batch": 1, "new": 100, "longest": 100, "heads": 16, "kv": 16, "dim": 64, "page": 16, "bits": 8,
+         "dtype": "bf16"},
+        # a piece of a long prompt, four queries to a cached head
+        {"name": "prompt 2048 of 10000", "op": "prompt", "batch": 1, "new": 2048, "longest": 10000, "heads": 32, "kv": 8, "dim": 128, "page": 16, "bits": 8,
+         "dtype": "bf16"},
+        # pieces of unlike prompts together, 4 bits
+        {"name": "prompt 9 to 517 of 3001", "op": "prompt", "batch": 9, "new": 517, "longest": 3001, "heads": 32, "kv": 32, "dim": 128, "page": 64, "bits": 4,
+         "dtype": "f16"},
+        # in 32 bits, heads that are no power of two
+        {"name": "prompt 2 to 333 of 1500 f32", "op": "prompt", "batch": 2, "new": 333, "longest": 1500, "heads": 12, "kv": 4, "dim": 96, "page": 32, "bits": 8,
+         "dtype": "f32"},
+        # four drafted tokens of one sequence
+        {"name": "drafts 1x5 of 32000", "op": "drafts", "batch": 1, "nodes": 5, "vocab": 32000, "tree": False, "dtype": "f32"},
+        # eight drafted tokens of every sequence of a batch
+        {"name": "drafts 48x9 of 50257", "op": "drafts", "batch": 48, "nodes": 9, "vocab": 50257, "tree": False, "dtype": "f32"},
+        # trees of guesses out of what was written before
+        {"name": "trees 5x24 of 50257", "op": "drafts", "batch": 5, "nodes": 24, "vocab": 50257, "tree": True, "dtype": "bf16"},
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.5)))))))
+
+
+def draw(rng):
+    op = rng.choice(["product", "product", "pages", "prompt", "prompt", "drafts"])
+    dtype = rng.choice(["f32", "bf16", "f16"])
+    if op == "product":
+        m, k = _log(rng, 1, 2048), _log(rng, 16, 11008)
+        n = _log(rng, 16, min(32000, 2048 * 4096 * 11008 // (m * k)))
+        return {"op": op, "m": m, "n": n, "k": k, "dtype": dtype, "bias": rng.random() < 0.5}
+    if op == "pages":
+        batch = _log(rng, 1, 300)
+        add = _log(rng, 1, 40000 // batch)
+        return {"op": op, "batch": batch, "add": add, "longest": _log(rng, 1, 4096), "page": rng.choice([8, 16, 32, 64, 128]),
+                "room": _log(rng, batch * add // 2 + 1, 40000)}
+    if op == "drafts":
+        batch, nodes = _log(rng, 1, 48), _log(rng, 1, 24)
+        vocab = _log(rng, 100, min(130000, 48 * 9 * 50257 // (batch * nodes)))
+        return {"op": op, "batch": batch, "nodes": nodes, "vocab": vocab, "tree": rng.random() < 0.5, "dtype": dtype}
+    dim, kv = rng.choice([32, 64, 96, 128, 160, 256]), rng.choice([1, 2, 4, 8, 16, 32])
+    heads = kv * rng.choice([1, 1, 2, 4, 7, 8])
+    batch, new = _log(rng, 1, 24), _log(rng, 1, 4096)
+    most = 2048 * 8976 * 32 * 128 // (4 if dtype == "f32" else 1)
+    longest = max(16, most // (batch * new * heads * dim))
+    if longest < new:
+        new = max(1, int(math.sqrt(most // (batch * heads * dim))))
+        longest = new
+    return {"op": op, "batch": batch, "new": new, "longest": _log(rng, new, max(new, min(32768, longest))), "heads": heads, "kv": kv, "dim": dim,
+            "page": rng.choice([8, 16, 32, 64, 128]), "bits": rng.choice([8, 4]), "dtype": dtype}
+
+
+def _shares(most, batch):
+    """Unlike sizes of `batch` sequences: from the largest down to a share of it, at least 1."""
+    return [max(1, most * (batch - i) // batch) for i in range(batch)]
+
+
+def _prompts(case):
+    """New and cached tokens of each sequence, the new ones counted among the cached."""
+    new = _shares(case["new"], case["batch"])
+    return new, [max(n, t) for n, t in zip(new, _shares(case["longest"], case["batch"])[::-1])]
+
+
+def work(case):
+    if case["op"] == "pages":
+        b, page = case["batch"], case["page"]
+        return {"bytes": b * 24 + case["room"] * 16 + b * (case["add"] // page + case["longest"] // page) * 8, "flops": 4 * (b + case["room"])}
+    size = 4 if case["dtype"] == "f32" else 2
+    if case["op"] == "product":
+        m, n, k = case["m"], case["n"], case["k"]
+        return {"bytes": n * (k + 4) + (m * k + m * n + n * case["bias"]) * size, "flops": 2 * m * n * k}
+    if case["op"] == "drafts":
+        rows = case["batch"] * (1 if case["tree"] else 2)
+        return {"bytes": rows * case["vocab"] * size + case["batch"] * case["nodes"] * (16 + 2 * size), "flops": 2 * rows * case["vocab"]}
+    new, lens = _prompts(case)
+    held = 2 * case["kv"] * (case["dim"] * case["bits"] // 8 + 4)
+    pairs = sum(n * (t - n) + n * (n + 1) // 2 for n, t in zip(new, lens))
+    return {"bytes": sum(lens) * held + sum(lens) // case["page"] * 4 + 2 * sum(new) * case["heads"] * case["dim"] * size,
+            "flops": 4 * pairs * case["heads"] * case["dim"]}
+
+
+# ---------------------------------------------------------------- inputs
+def _nibbles(q):
+    """Two values of [-7, 7] a byte, the first in the low half."""
+    c = (q + 8).to(torch.uint8)
+    return c[..., 0::2] | (c[..., 1::2] << 4)
+
+
+def _cache(g, pages, page, heads, dim, bits, dev):
+    """A cache of normal keys and values: codes as quantising 128 normal numbers by the largest of them leaves them."""
+    most = 127 if bits == 8 else 7
+
+    def codes():
+        q = (torch.randn(pages, heads, page, dim, generator=g, device=dev) * (most / 2.7)).round_().clamp_(-most, most).to(torch.int8)
+        return q.view(torch.uint8) if bits == 8 else _nibbles(q)
+
+    def scales():
+        return torch.exp(0.2 * torch.randn(pages, heads, page, generator=g, device=dev)) * (2.7 / most)
+
+    return {"k": codes(), "v": codes(), "k_scale": scales(), "v_scale": scales()}
+
+
+def _pages(c, lens, more, page, wide, spare):
+    """The table of sequences of these lengths with pages in any order, and a list of `spare` free ones with room for all there are."""
+    have = [-(-t // page) for t in lens]
+    total = len(lens) * wide + 8
+    order = torch.randperm(total, generator=c).to(torch.int32)
+    table, at = torch.full((len(lens), wide), -1, dtype=torch.int32), 0
+    for b, n in enumerate(have):
+        table[b, :n] = order[at:at + n]
+        at += n
+    free = torch.full((total,), -1, dtype=torch.int32)
+    free[:spare] = order[at:at + spare]
+    return {"table": table.to("cuda"), "lens": torch.tensor(lens, dtype=torch.int32, device="cuda"), "free": free.to("cuda"),
+            "count": torch.tensor([spare], dtype=torch.int32, device="cuda"), "change": torch.tensor(more, dtype=torch.int32, device="cuda")}
+
+
+def _integers(c, lo, hi, n):
+    return torch.randint(lo, hi + 1, (n,), generator=c).tolist()
+
+
+def _tree(c, nodes):
+    """Parents: a few below the known token, the others below any before them."""
+    return [-1] + [0 if i < 4 else int(torch.randint(0, i, (1,), generator=c)) for i in range(1, nodes)]
+
+
+def prepare(case, seed):
+    dev = "cuda"
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    c = torch.Generator()
+    c.manual_seed(seed)
+    s = {"case": case}
+    if case["op"] == "pages":
+        batch, page = case["batch"], case["page"]
+        lens = _integers(c, 0, case["longest"], batch)
+        add = _integers(c, max(1, case["add"] // 2), case["add"], batch)
+        wide = -(-(case["longest"] + case["add"]) // page)
+        spare = sum(-(-(t + a) // page) - -(-t // page) for t, a in zip(lens, add)) * 15 // 16 + 1       # a little short of what is asked for
+        s["grow"] = _pages(c, lens, add, page, wide, spare)
+        lens = _integers(c, 1, case["longest"], batch)
+        keep = [0 if int(torch.randint(0, 4, (1,), generator=c)) == 0 else max(0, t - int(torch.randint(0, 24, (1,), generator=c))) for t in lens]
+        s["end"] = _pages(c, lens, keep, page, wide, 7)
+    elif case["op"] == "product":
+        m, n, k = case["m"], case["n"], case["k"]
+        dtype = _TYPES[case["dtype"]]
+        s["w"] = torch.zeros(n, (k + 15) // 16 * 16, dtype=torch.int8, device=dev)
+        s["w"][:, :k] = (torch.randn(n, k, generator=g, device=dev) * 32).round_().clamp_(-127, 127).to(torch.int8)
+        s["scales"] = torch.exp(0.2 * torch.randn(n, generator=g, device=dev)) * (0.05 / 32)
+        s["x"] = torch.randn(m, k, generator=g, device=dev).to(dtype)
+        s["bias"] = (0.1 * torch.randn(n, generator=g, device=dev)).to(dtype) if case["bias"] else None
+    elif case["op"] == "drafts":
+        batch, nodes, vocab = case["batch"], case["nodes"], case["vocab"]
+        dtype = _TYPES[case["dtype"]]
+        logits = 2.5 * torch.randn(batch, nodes, vocab, generator=g, device=dev)
+        s["target"] = torch.softmax(logits, -1).to(dtype)
+        s["uniform"] = torch.rand(batch, nodes, generator=g, device=dev)
+        s["draft"] = s["parent"] = None
+        if case["tree"]:            # guesses, the better half among the likely ones
+            likely = s["target"].float().topk(min(vocab, 8), -1).indices
+            s["parent"] = torch.tensor([_tree(c, nodes) for _ in range(batch)], dtype=torch.int32, device=dev)
+            pick = torch.randint(0, likely.shape[-1], (batch, nodes, 1), generator=g, device=dev)
+            above = s["parent"].long().clamp(min=0)[..., None].expand(-1, -1, likely.shape[-1])
+            s["tokens"] = torch.gather(torch.gather(likely, 1, above), 2, pick)[..., 0].to(torch.int32)
+        else:                       # drawn from a smaller model's probabilities, which are near the model's own
+            near = torch.softmax(logits[:, :nodes - 1] + 0.5 * torch.randn(batch, nodes - 1, vocab, generator=g, device=dev), -1)
+            s["draft"] = near.to(dtype)
+            s["tokens"] = torch.zeros(batch, nodes, dtype=torch.int32, device=dev)
+            if nodes > 1:
+                s["tokens"][:, 1:] = torch.multinomial(near.view(-1, vocab), 1, generator=g).view(batch, nodes - 1).to(torch.int32)
+        del logits
+    else:
+        page, dim, bits, kv = case["page"], case["dim"], case["bits"], case["kv"]
+        new, lens = _prompts(case)
+        need = sum(-(-t // page) for t in lens)
+        s["cache"] = _cache(g, need + need // 8 + 1, page, kv, dim, bits, dev)
+        order, at = torch.randperm(need + need // 8 + 1, generator=c).to(torch.int32), 0
+        table = torch.zeros(case["batch"], max(-(-t // page) for t in lens), dtype=torch.int32)
+        for b, t in enumerate(lens):
+            table[b, :-(-t // page)] = order[at:at - (-t // page)]
+            at -= -t // page
+        s["table"], s["lens"] = table.to(dev), torch.tensor(lens, dtype=torch.int32, device=dev)
+        starts = [0]
+        for n in new:
+            starts.append(starts[-1] + n)
+        s["starts"] = torch.tensor(starts, dtype=torch.int32, device=dev)
+        s["q"] = (1.5 * torch.randn(starts[-1], case["heads"], dim, generator=g, device=dev)).to(_TYPES[case["dtype"]])
+        s["scale"] = dim ** -0.5
+    if own:                         # what a serving program keeps: the handles that name its weights, its pages and its cache, and scratch memory
+        from paper_2009_13003_amd import lc
+        if case["op"] == "product":
+            s["w8"] = lc.I8(s["w"], s["scales"], case["k"])
+        elif case["op"] == "pages":
+            for name in ("grow", "end"):
+                p = s[name]
+                p["pages"] = lc.KvPages(p["table"], p["lens"], p["free"], p["count"], case["page"])
+                p["new_lens"], p["new_count"] = torch.empty_like(p["lens"]), torch.empty_like(p["count"])
+        elif case["op"] == "drafts":
+            s["ws"] = lc.new_draft_workspace(case["batch"])
+        else:
+            s["kv"] = lc.KvCache(bits=case["bits"], **s["cache"])
+            s["ws"] = lc.new_prompt_workspace(s["kv"], s["q"].shape[0], case["batch"], case["heads"])
+    return s
+
+
+# ---------------------------------------------------------------- one pass
+def run(s):
+    case = s["case"]
+    if own:
+        from paper_2009_13003_amd import lc
+        if case["op"] == "product":
+            return lc.lc_i8_matmul(lc.lc_i8_quantize(s["x"]), s["w8"], s["bias"], s["x"].dtype)
+        if case["op"] == "pages":
+            g, e = s["grow"], s["end"]
+            starts, slots, places, owners = lc.lc_kv_extend(g["pages"], g["change"], case["room"], g["new_lens"], g["new_count"])
+            lc.lc_kv_trim(e["pages"], e["change"], e["new_lens"], e["new_count"])
+            return {"table": g["table"], "lens": g["new_lens"], "count": g["new_count"], "starts": starts, "slots": slots, "places": places,
+                    "owners": owners, "kept": e["new_lens"], "free": e["free"], "free count": e["new_count"]}
+        if case["op"] == "drafts":
+            return lc.lc_draft_verify(s["target"], s["tokens"], s["uniform"], s["draft"], s["parent"], ws=s["ws"])
+        return lc.lc_kv_attend_prompt(s["kv"], s["q"], s["starts"], s["table"], s["lens"], s["scale"], ws=s["ws"])
+    return {"product": _product, "pages": _extend_and_trim, "drafts": _judge, "prompt": _attention}[case["op"]](s, case)
+
+
+def _product(s, case):
+    x = s["x"].float()
+    share = torch.tensor(1.0 / 127.0, dtype=torch.float32, device=x.device)
+    most = x.abs().amax(-1, keepdim=True)
+    scale = most * share
+    tiny = scale < _SMALLEST
+    inv = torch.where(tiny, 0.0, torch.ones_like(scale) / torch.where(tiny, 1.0, scale))
+    q = (x * inv).round().clamp(-127, 127)
+    y = (q @ s["w"][:, :case["k"]].float().t()) * torch.where(tiny, 0.0, scale) * s["scales"]
+    if s["bias"] is not None:
+        y = y + s["bias"].float()
+    return y.to(s["x"].dtype)
+
+
+def _extend_and_trim(s, case):
+    page, room, p = case["page"], case["room"], s["grow"]
+    dev = p["lens"].device
+    lens, add = p["lens"].long().clamp(min=0), p["change"].long().clamp(min=0)
+    have = (lens + page - 1) // page
+    need = (lens + add + page - 1) // page - have
+    pages, ends = need.cumsum(0), add.cumsum(0)
+    fits = (pages <= p["count"]) & (ends <= room) & (have + need <= p["table"].shape[1])
+    fits = fits.long().cumprod(0)                                # the leading ones
+    add, taken = add * fits, need * fits
+    starts = torch.cat([torch.zeros(1, dtype=torch.long, device=dev), add.cumsum(0)])
+    j = torch.arange(p["table"].shape[1], device=dev)[None]
+    rank = (pages - need)[:, None] + j - have[:, None]
+    given = (j >= have[:, None]) & (j < (have + taken)[:, None])
+    p["table"].copy_(torch.where(given, p["free"][(p["count"] - 1 - rank).clamp(min=0, max=p["free"].shape[0] - 1)], p["table"]))
+    t = torch.arange(room, device=dev)
+    owner = torch.searchsorted(starts[1:].contiguous(), t, right=True)
+    there = owner < case["batch"]
+    owner = torch.where(there, owner, 0)
+    place = lens[owner] + t - starts[owner]
+    slot = p["table"][owner, torch.where(there, place // page, 0)].long() * page + place % page
+    out = {"table": p["table"], "lens": (p["lens"] + add).to(torch.int32), "count": (p["count"] - taken.sum()).to(torch.int32), "starts": starts.to(torch.int32),
+           "slots": torch.where(there, slot, -1), "places": torch.where(there, place, -1).to(torch.int32),
+           "owners": torch.where(there, owner, -1).to(torch.int32)}
+    p = s["end"]
+    lens = p["lens"].long().clamp(min=0)
+    keep = torch.minimum(p["change"].long().clamp(min=0), lens)
+    first, last = (keep + page - 1) // page, (lens + page - 1) // page
+    back = (last - first).cumsum(0)
+    rank = (back - (last - first))[:, None] + j - first[:, None]
+    given = (j >= first[:, None]) & (j < last[:, None])
+    at = p["count"] + back[-1] - 1 - rank                         # the last page first
+    at = torch.where(given, at, p["free"].shape[0])               # (a place of its own for what stays)
+    more = torch.cat([p["free"], p["free"][:1]])
+    more[at.flatten()] = p["table"].flatten()
+    p["free"].copy_(more[:-1])
+    out.update({"kept": keep.to(torch.int32), "free": p["free"], "free count": (p["count"] + back[-1]).to(torch.int32)})
+    return out
+
+
+def _judge(s, case):
+    target, tokens, u, draft, parent = s["target"], s["tokens"].long(), s["uniform"].double(), s["draft"], s["parent"]
+    batch, nodes, vocab = target.shape
+    dev = target.device
+    every = torch.arange(batch, device=dev)
+    cur, count = torch.zeros(batch, dtype=torch.long, device=dev), torch.ones(batch, dtype=torch.long, device=dev)
+    path = torch.full((batch, nodes), -1, dtype=torch.int32, device=dev)
+    path[:, 0] = 0
+    refused = torch.zeros(batch, nodes, dtype=torch.bool, device=dev)       # children of the path's end that were not taken
+    left = torch.ones(batch, dtype=torch.float64, device=dev)
+    for i in range(1, nodes):
+        here = cur == (i - 1 if parent is None else parent[:, i])
+        p = target[every, cur, tokens[:, i]].double()
+        if draft is not None:
+            take = here & (u[:, i] * draft[every, i - 1, tokens[:, i]].double() < p)
+        else:
+            again = (refused & (tokens == tokens[:, i:i + 1])).any(1)       # what a sibling was refused for is gone already
+            p = torch.where(again, 0.0, p)
+            take = here & (u[:, i] * left < p)
+            left = torch.where(take, 1.0, torch.where(here, left - p, left))
+        refused[:, i] = here
+        refused = refused & ~take[:, None]
+        path[every, torch.where(take, count, 0)] = torch.where(take, i, 0).to(torch.int32)
+        cur, count = torch.where(take, i, cur), count + take
+    p = target[every, cur].double()
+    if draft is not None and nodes > 1:
+        q = draft[every, cur.clamp(max=nodes - 2)].double()
+        rest = torch.where(refused.any(1)[:, None], (p - q).clamp(min=0), p)
+    elif draft is None:
+        rest = p.scatter(1, torch.where(refused, tokens, tokens[:, :1] * 0 + vocab - 1), torch.where(refused, 0.0, p[:, -1:]))
+        rest[:, -1] = torch.where((refused & (tokens == vocab - 1)).any(1), 0.0, p[:, -1])
+    else:
+        rest = p
+    rest = torch.where(rest.sum(-1, keepdim=True) > 0, rest, p)
+    run_up = rest.cumsum(-1)
+    following = (run_up <= u[:, :1] * run_up[:, -1:]).sum(-1).clamp(max=vocab - 1)
+    return {"path": path, "count": count.to(torch.int32), "next": following.to(torch.int32)}
+
+
+def _codes(codes, bits, dim):
+    if bits == 8:
+        return codes.view(torch.int8).float()
+    return torch.stack((codes & 15, codes >> 4), -1).flatten(-2)[..., :dim].float() - 8
+
+
+def _attention(s, case):
+    page, dim, bits, kv, c, q = case["page"], case["dim"], case["bits"], case["kv"], s["cache"], s["q"]
+    g = case["heads"] // kv
+    new, lens = _prompts(case)
+    out, first = torch.empty_like(q), 0
+    for b, (n, length) in enumerate(zip(new, lens)):
+        t = torch.arange(length, device=q.device)
+        at, off = s["table"][b].long()[t // page], t % page
+        k, v = ((_codes(c[x][at, :, off], bits, dim) * c[x + "_scale"][at, :, off][..., None]).transpose(0, 1).contiguous() for x in ("k", "v"))
+        rows = max(1, (1 << 28) // (case["heads"] * length))        # pieces of the new tokens whose scores take a gigabyte
+        for i in range(0, n, rows):
+            m = min(rows, n - i)
+            x = q[first + i:first + i + m].float().view(m, kv, g, dim).permute(1, 0, 2, 3).reshape(kv, m * g, dim)
+            score = (x @ k.transpose(1, 2).contiguous()).view(kv, m, g, length) * s["scale"]
+            last = length - n + i + torch.arange(m, device=q.device)
+            score = torch.where((t[None] <= last[:, None])[None, :, None], score, -math.inf)
+            p = torch.exp(score - score.amax(-1, keepdim=True))
+            o = (p.view(kv, m * g, length) @ v).view(kv, m, g, dim) / p.sum(-1, keepdim=True)
+            out[first + i:first + i + m] = o.permute(1, 0, 2, 3).reshape(m, case["heads"], dim).to(q.dtype)
+        first += n
+    return out
+
+
+# ---------------------------------------------------------------- the same from the definitions, in 64 bits
+def _product64(s, case):
+    x, k = s["x"].double(), case["k"]
+    one = torch.ones((), dtype=torch.float64, device="cuda")
+    scale = (x.abs().max(1).values * (one / 127).float().double()).float()
+    scale[scale < _SMALLEST] = 0
+    inv = torch.where(scale > 0, (one / scale.double()).float(), torch.zeros_like(scale))
+    q = torch.round((x * inv.double()[:, None]).float()).double().clamp(-127, 127)
+    y = torch.zeros(case["m"], case["n"], dtype=torch.float64, device="cuda")
+    for at in range(0, k, 1024):                            # a piece of the width at a time: whole numbers, exactly
+        y += q[:, at:at + 1024] @ s["w"][:, at:min(at + 1024, k)].double().t().contiguous()
+    y *= scale.double()[:, None] * s["scales"].double()[None]
+    return y if s["bias"] is None else y + s["bias"].double()
+
+
+def _pages64(s, case):
+    """One sequence after the other, with a list as the stack of free pages."""
+    page, room = case["page"], case["room"]
+
+    def lists(p):
+        return [p[x].tolist() for x in ("table", "lens", "free", "count", "change")]
+
+    table, lens, free, (count,), add = lists(s["grow"])
+    stack, wide = free[:count], len(table[0])
+    starts, new, waits = [0], [], False
+    slots, places, owners = [], [], []
+    for b, (t, a) in enumerate(zip(lens, add)):
+        have, want = -(-t // page), -(-(t + a) // page)
+        waits = waits or want > wide or want - have > len(stack) or starts[-1] + a > room
+        a = 0 if waits else a
+        for j in range(have, -(-(t + a) // page) if a else have):
+            table[b][j] = stack.pop()
+        for i in range(t, t + a):
+            slots.append(table[b][i // page] * page + i % page)
+            places.append(i)
+            owners.append(b)
+        starts.append(starts[-1] + a)
+        new.append(t + a)
+    pad = [-1] * (room - len(slots))
+    out = {"table": table, "lens": new, "count": [len(stack)], "starts": starts, "slots": slots + pad, "places": places + pad, "owners": owners + pad}
+    table, lens, free, (count,), keep = lists(s["end"])
+    back, kept = [], []
+    for b, (t, n) in enumerate(zip(lens, keep)):
+        kept.append(min(t, n))
+        back += table[b][-(-kept[-1] // page):-(-t // page)]
+    free[count:count + len(back)] = back[::-1]
+    out.update({"kept": kept, "free": free, "free count": [count + len(back)]})
+    return {n: torch.tensor(v, dtype=torch.int64 if n == "slots" else torch.int32, device="cuda") for n, v in out.items()}
+
+
+def _judge64(s, case):
+    import numpy as np
+    tokens, u = s["tokens"].cpu().tolist(), s["uniform"].cpu().double().tolist()
+    above = s["parent"].cpu().tolist() if s["parent"] is not None else None
+    paths, counts, nexts = [], [], []
+
+    def row(t, b, i):
+        return t[b, i].double().cpu().numpy()
+
+    for b in range(case["batch"]):
+        path, going = [0], True
+        while going:                                        # from node to node
+            p, going = row(s["target"], b, path[-1]), False
+            rest, left = p.copy(), 1.0
+            for i in range(path[-1] + 1, case["nodes"]):
+                if (i - 1 if above is None else above[b][i]) != path[-1]:
+                    continue
+                t = tokens[b][i]
+                if s["draft"] is not None:
+                    q = row(s["draft"], b, i - 1)
+                    taken = u[b][i] * q[t] < p[t]
+                    rest = np.maximum(p - q, 0.0)
+                else:
+                    taken = u[b][i] * left < rest[t]
+                    left -= rest[t]
+                    rest[t] = 0.0
+                if taken:
+                    path.append(i)
+                    going = True
+                    break
+        if not rest.sum() > 0:
+            rest = p
+        run_up = np.cumsum(rest)
+        paths.append(path + [-1] * (case["nodes"] - len(path)))
+        counts.append(len(path))
+        nexts.append(int(np.argmax(run_up > u[b][0] * run_up[-1])))
+    return {n: torch.tensor(v, dtype=torch.int32, device="cuda") for n, v in (("path", paths), ("count", counts), ("next", nexts))}
+
+
+def _attention64(s, case):
+    page, bits, kv, c = case["page"], case["bits"], case["kv"], s["cache"]
+    g = case["heads"] // kv
+    new, lens = _prompts(case)
+    flat = {n: c[n].transpose(1, 2).flatten(0, 1) for n in ("k", "v", "k_scale", "v_scale")}       # by slot
+    out, first = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda"), 0
+
+    def values(name, slots, h):
+        b = flat[name][slots, h].to(torch.int64)
+        if bits == 8:
+            q = torch.where(b > 127, b - 256, b)
+        else:
+            q = torch.empty(b.shape[0], 2 * b.shape[1], dtype=torch.int64, device="cuda")
+            q[:, 0::2] = b % 16 - 8
+            q[:, 1::2] = b // 16 - 8
+        return q.double() * flat[name + "_scale"][slots, h].double()[:, None]
+
+    for b, (n, length) in enumerate(zip(new, lens)):
+        t = torch.arange(length, device="cuda")
+        slots = s["table"][b].long()[t // page] * page + t % page
+        hide = t[None] > (length - n + torch.arange(n, device="cuda"))[:, None]
+        for h in range(kv):
+            keys, vals = values("k", slots, h).t().contiguous(), values("v", slots, h)
+            for x in range(h * g, (h + 1) * g):
+                for i in range(0, n, 4096):
+                    score = (s["q"][first + i:first + min(n, i + 4096), x].double() @ keys) * s["scale"]
+                    out[first + i:first + min(n, i + 4096), x] = torch.softmax(score.masked_fill(hide[i:i + 4096], -math.inf), -1) @ vals
+        first += n
+    return out
+
+
+def exact(case, seed):
+    return {"product": _product64, "pages": _pages64, "drafts": _judge64, "prompt": _attention64}[case["op"]](prepare(case, seed), case)
