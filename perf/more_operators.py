@@ -235,6 +235,7 @@ def prepare(case, seed):
         from paper_2009_13003_amd import lc
         if case["op"] == "product":
             s["w8"] = lc.I8(s["w"], s["scales"], case["k"])
+            s["ws"] = lc.new_i8_workspace(case["m"], case["k"])
         elif case["op"] == "pages":
             for name in ("grow", "end"):
                 p = s[name]
@@ -254,7 +255,7 @@ def run(s):
     if own:
         from paper_2009_13003_amd import lc
         if case["op"] == "product":
-            return lc.lc_i8_matmul(lc.lc_i8_quantize(s["x"]), s["w8"], s["bias"], s["x"].dtype)
+            return lc.lc_i8_linear(s["x"], s["w8"], s["bias"], ws=s["ws"])
         if case["op"] == "pages":
             g, e = s["grow"], s["end"]
             starts, slots, places, owners = lc.lc_kv_extend(g["pages"], g["change"], case["room"], g["new_lens"], g["new_count"])
