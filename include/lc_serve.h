@@ -1,7 +1,7 @@
 /*
  * lc_serve.h -- what a program that answers with a restored checkpoint needs next to lc.h: weights held in 4 bits with
- * group scales and their products with activations, and a paged cache of keys and values in 8 or 4 bits, written, read
- * back and attended to.  Hand-written HIP kernels for MI355X (gfx950) behind the same C ABI as lc.h.
+ * group scales or in 8 with one a row, and their products with activations; a paged cache of keys and values in 8 or 4 bits,
+ * its pages given out and taken back, written, read back and attended to; and drafted tokens judged.  Hand-written HIP kernels for MI355X (gfx950) behind the same C ABI as lc.h.
  *
  * As in lc.h: every pointer is a DEVICE pointer unless a parameter says "host"; `stream` is a hipStream_t passed as
  * void* (NULL = the null stream).  Every call here enqueues on `stream` and returns at once with an lc_status; it
@@ -61,6 +61,42 @@ int lc_w4_matmul(const void* x, uint64_t ldx, uint64_t m, const lc_w4* w4, const
                  int dtype, void* stream);
 
 /*
+ * A matrix q[n][k] in 8 bits, one scale a row: weights (a row is an output channel) or activations (a row is a token).
+ *     s = max |w| * fl32(1/127),  q = rint(fl32(w * fl32(1/s))) limited to [-127, 127], a two's complement byte;  the value meant is q * s.
+ * Scales below 2^-126 and rows that are not finite as for lc_w4.  A byte of -128 is never written but is read as what it stands for.
+ */
+typedef struct lc_i8 {
+    void* codes;            /* int8, 16-byte aligned; row i begins at codes + i * pitch */
+    float* scales;          /* [n] */
+    uint64_t n, k;          /* n at most 2^31 - 1, k at most LC_I8_MAX_K */
+    uint64_t pitch;         /* bytes: a multiple of 16, at least k */
+} lc_i8;
+#define LC_I8_MAX_K 131072  /* so that a sum of k products of codes, of which one side is never -128, fits 32 bits */
+
+/* w [n][k] of type dtype, row i at element i * ldw (ldw >= k), into w8's codes and scales.  Bytes behind a row's end are written as zeros up to the
+ * next multiple of 16. */
+int lc_i8_quantize(const void* w, uint64_t ldw, int dtype, const lc_i8* w8, void* stream);
+
+/* The values that w8 stands for, each fl32(q * s) rounded once to dtype, into w [n][k] (row i at element i * ldw). */
+int lc_i8_dequantize(const lc_i8* w8, void* w, uint64_t ldw, int dtype, void* stream);
+
+/*
+ * y[i][j] = (sum over l of qx[i][l] * qw[j][l]) * sx[i] * sw[j], plus bias[j] if bias is not NULL: x8 [m][k] with m at most 2^19, w8 [n][k], bias [n] and
+ * y [m][n] (row i at element i * ldy) of type dtype.  The sum of codes is exact, rounded once to 32 bits, multiplied by x's scale and then by w's in 32 bits (the sum times
+ * x's scale has to stay below 2^128), and y is rounded once more.  Bytes of a row of x8 behind k
+ * have to be zeros up to the next multiple of 16, as lc_i8_quantize leaves them; those of w8 may be anything.
+ */
+int lc_i8_matmul(const lc_i8* x8, const lc_i8* w8, const void* bias, void* y, uint64_t ldy, int dtype, void* stream);
+
+/*
+ * The same for x [m][k] of type dtype, row i at element i * ldx: its rows are put into 8 bits first, as by lc_i8_quantize, with the same results.  ws: scratch,
+ * 256-byte aligned, lc_i8_workspace_bytes(m, k); its content need not be anything.  Calls that may run at the same time need areas of their own.
+ */
+size_t lc_i8_workspace_bytes(uint64_t m, uint64_t k);
+int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const void* bias, void* y, uint64_t ldy, int dtype, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/*
  * A paged cache of keys and values.  A slot is page * page_tokens + token.  Codes lie as [page][head][token][dim],
  * dim elements in dim * bits / 8 bytes; scales as [page][head][token], one fp32 for the dim elements of a key or value:
  *     s = max |v| * fl32(1/most),  q = rint(v * fl32(1/s)) limited to [-most, most],  the value meant is q * s,
@@ -112,6 +148,82 @@ size_t lc_kv_workspace_bytes(uint64_t batch, int nq, int heads, int kv_heads, in
 int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq, int heads, const int32_t* table, uint64_t ld_table,
                  uint64_t table_pages, const int32_t* lens, const uint64_t* mask, float scale, void* out, int dtype, void* ws,
                  size_t ws_bytes, void* stream);
+
+/*
+ * The same attention for the new tokens of several prompts, or pieces of them, of any number each:
+ *   q, out  [tokens][heads][dim] of type dtype, token i at element i * ld (a multiple of 8; of 4 for LC_F32), 16-byte aligned; tokens at most 2^24, heads as above,
+ *           tokens * heads at most 2^30
+ *   starts  int32 [batch + 1], none below the one before it, in [0, tokens]: sequence b's new tokens are starts[b] .. starts[b + 1] - 1, in order.  Rows of out that
+ *           belong to no sequence are left as they were.
+ *   table, lens, scale: as above; the newest cached tokens of a sequence are the new ones, and each sees what is cached up to itself.  A new token
+ *           that would lie before the first cached one gets zeros.
+ * Roundings: bf16 probabilities times the values' scales are rounded to 8 bits, once each; in fp16 the probabilities to 11 bits (2^-25 at least) and the values, as
+ * lc_kv_read gives them, to fp16 (those beyond 65504 count as 65504); fp32 as above.  Sums, maxima and scores are held in 32 bits.
+ */
+size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim);
+int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,
+                        const int32_t* table, uint64_t ld_table, uint64_t table_pages, const int32_t* lens, float scale, void* out, uint64_t ld_out, int dtype,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The pages of sequences that share a cache.  table and lens are those that attention takes; free_pages is a stack of the pages that nobody has, with
+ * *free_count of them (both on the device), the next one to be given out last.
+ */
+typedef struct lc_kv_pages {
+    int32_t* table;         /* [batch][ld_table]; entries behind a sequence's pages may hold anything */
+    int32_t* lens;          /* [batch] cached tokens, a negative number counts as 0 */
+    int32_t* free_pages;    /* [free_room] */
+    int32_t* free_count;    /* [1], held to [0, free_room] */
+    uint64_t batch;         /* at most 65535 */
+    uint64_t ld_table, table_pages;     /* table_pages * page_tokens at most 2^30 */
+    uint64_t free_room;     /* at most 2^31 - 1 */
+    int page_tokens;        /* a power of two, 8 to 1024 */
+} lc_kv_pages;
+
+/*
+ * Room for add[b] (int32 [batch]; not above 0: none) more tokens of every sequence: the pages that it needs are taken off the stack, in order of the sequences and of
+ * the tokens, and written into the table.  A sequence that has no room in its row of the table, for which the stack does not suffice, or whose tokens would pass
+ * `room`, gets nothing, and neither do those behind it.  Then
+ *   new_lens [batch], new_count [1]   the lengths with the tokens that found room, and what is left on the stack; may be lens and free_count themselves
+ *   starts   int32 [batch + 1]        where each sequence's new tokens begin among all that found room
+ *   slots    int64 [room]             of each new token its slot (page * page_tokens + token), -1 behind the last one
+ *   places   int32 [room]             its place in the sequence, or -1;  owners int32 [room]: the sequence, or -1.  Either may be NULL.
+ * The stack itself is read only.  One call at a time on the same pages.
+ */
+int lc_kv_extend(const lc_kv_pages* pages, const int32_t* add, uint64_t room, int32_t* new_lens, int32_t* new_count, int32_t* starts, int64_t* slots,
+                 int32_t* places, int32_t* owners, void* stream);
+
+/*
+ * Of every sequence the first keep[b] tokens stay (int32 [batch]; at most its length, a negative number counts as 0), and the pages behind them go back on the stack, the
+ * last one first: what an extension took, taken back, leaves the stack as it was.  The table is read only.  Pages for which the stack has no room are lost.
+ * new_lens and new_count as for lc_kv_extend.
+ */
+int lc_kv_trim(const lc_kv_pages* pages, const int32_t* keep, int32_t* new_lens, int32_t* new_count, void* stream);
+
+/*
+ * Drafted tokens judged against the model's probabilities, with given random numbers, so that what is written has the model's distribution:
+ *   target  [batch][nodes][vocab] of type dtype: the model's probabilities behind each node; row (b, i) at element b * ld_batch + i * ld_row (rows may share memory).  nodes 1 to 64, vocab 1 to 2^24.
+ *           Values that are negative or not finite count as zero.
+ *   tokens  int32 [batch][nodes].  Node 0 is the token that is known (its number is not looked at); a number outside the vocabulary has probability zero.
+ *   draft   the probabilities that the tokens of nodes 1, 2 ... were drawn from, [batch][nodes - 1][vocab] with pitches of its own, or NULL: the tokens are
+ *           guesses that nothing was drawn for
+ *   parent  int32 [batch][nodes], only without draft: the node below which each was drafted, smaller than itself; NULL: the one before.
+ *   count   NULL, or int32 [batch]: how many of the nodes exist (held to 1 .. nodes)
+ *   uniform fp32 [batch][nodes], in [0, 1)
+ * The path begins with node 0.  Below its end nodes are tried in order.  With draft, i is taken if uniform[i] * q(token i) < p(token i), with p behind the path's end and
+ * q that i was drawn from; else the path ends, and what is left is max(p - q, 0).  Without, i is taken if uniform[i] * rest < p(token i), where rest is 1 less the
+ * probabilities of what was refused here before, and those tokens are left out of p (the same token refused again has probability zero).  A node without
+ * nodes below it leaves p.  Then
+ *   path    int32 [batch][nodes]: the nodes of the path, -1 behind them;  length int32 [batch]: how many
+ *   next    int32 [batch]: the first token at which the running sum of what is left exceeds uniform[0] times all of it; where nothing is left, of p; where that is zero
+ *           everywhere, -1
+ * Sums are held in 64 bits.  ws: scratch, 256-byte aligned, lc_draft_workspace_bytes(batch); its content need not be anything.  Calls that may run
+ * at the same time need areas of their own.
+ */
+size_t lc_draft_workspace_bytes(uint64_t batch);
+int lc_draft_verify(const void* target, uint64_t ld_batch, uint64_t ld_row, uint64_t batch, int nodes, uint64_t vocab, const int32_t* tokens, const void* draft,
+                    uint64_t ld_draft_batch, uint64_t ld_draft_row, const int32_t* parent, const int32_t* count, const float* uniform, int dtype,
+                    int32_t* path, int32_t* length, int32_t* next, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -5,13 +5,14 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblc.so")
-SOURCES = ["lc_encode.hip", "lc_decode.hip", "lc_decode_one.hip", "lc_api.hip", "lc_w4.hip", "lc_kv.hip"]
+SOURCES = ["lc_encode.hip", "lc_decode.hip", "lc_decode_one.hip", "lc_api.hip", "lc_w4.hip", "lc_i8.hip", "lc_kv.hip", "lc_prompt.hip", "lc_pages.hip",
+           "lc_draft.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC", "-ffp-contract=off",
          # packed fp32 instructions stay off: some of their forms have given wrong results on this hardware
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # the attention's sums live in vector registers from end to end; left to itself the compiler moves them to the accumulation
 # registers and back for every tile
-MORE_FLAGS = {"lc_kv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+MORE_FLAGS = {"lc_kv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "lc_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _run(cmd, verbose):

@@ -1,0 +1,358 @@
+// Matrices in 8 bits with a scale a row: quantising, reading back, and the products of two of them (include/lc_serve.h).
+#include "lc_serve.h"
+
+#include <type_traits>
+
+namespace lc {
+namespace serve {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(16))) int i32x16;
+
+// ---------------------------------------------------------------- quantising and reading back
+// A row to a workgroup, or of short rows to a wavefront: 8 elements a lane at a time, kept in registers between the search for the largest and the rounding
+// (rows too long for that are read again).  s = max |w| / 127, q = rint(w (1 / s)).
+template <int T, int WAVES, int R>
+__global__ __launch_bounds__(256) void k_i8_quantize(const void* w, uint64_t ldw, uint8_t* codes, uint64_t pitch, float* scales, uint32_t rows, uint32_t k) {
+    __shared__ uint32_t tops[4];
+    constexpr uint32_t LANES = WAVES * 64;
+    const uint32_t row = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + threadIdx.x / 64, lane = WAVES == 4 ? threadIdx.x : threadIdx.x % 64;
+    if (row >= rows) return;
+    float v[R][8];
+    uint32_t most = 0;
+    auto load = [&](uint32_t at, float x[8]) { load_eight<T>(w, row * ldw + at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, x); };
+    auto look = [&](const float x[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { const uint32_t a = bits_of(x[e]) & 0x7fffffffu; most = a > most ? a : most; }
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) load((r * LANES + lane) * 8, v[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) look(v[r]);
+    for (uint32_t at = (R * LANES + lane) * 8; at < k; at += LANES * 8) {
+        float x[8];
+        load(at, x);
+        look(x);
+    }
+    most = max_of_lanes<32>(most);
+    { const uint32_t o = (uint32_t)__shfl_xor((int)most, 32); most = o > most ? o : most; }
+    if (WAVES == 4) {
+        if (lane % 64 == 0) tops[lane / 64] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = tops[i] > most ? tops[i] : most;
+    }
+    float s = float_of(most) * (1.0f / 127.0f), inv = 0.0f;
+    if (most >= 0x7f800000u) s = __builtin_nanf("");
+    else if (s < kSmallest) s = 0.0f;
+    else inv = 1.0f / s;
+    const uint32_t end = (k + 15) & ~15u;
+    auto store = [&](uint32_t at, const float x[8]) {
+        if (at >= end) return;
+        u32x2 q = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e / 4] |= (rounded(fminf(fmaxf(inv == 0.0f ? 0.0f : x[e] * inv, -127.0f), 127.0f), 0.0f) & 255u) << (8 * (e % 4));
+        *reinterpret_cast<u32x2*>(codes + row * pitch + at) = q;
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) store((r * LANES + lane) * 8, v[r]);
+    for (uint32_t at = (R * LANES + lane) * 8; at < end; at += LANES * 8) {
+        float x[8];
+        load(at, x);
+        store(at, x);
+    }
+    if (lane == 0) scales[row] = s;
+}
+
+template <int T>
+__global__ __launch_bounds__(256) void k_i8_dequantize(const uint8_t* codes, uint64_t pitch, const float* scales, void* w, uint64_t ldw, uint32_t lanes, uint32_t k,
+                                                       FastDiv by_row) {
+    constexpr int N = kAtOnce<T>;
+    const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
+    if (lane >= lanes) return;
+    const uint32_t row = by_row(lane), at = N * (lane - row * by_row.d);
+    typedef typename std::conditional<N == 8, uint64_t, uint32_t>::type Word;
+    const Word q = *reinterpret_cast<const Word*>(codes + row * pitch + at);
+    const float s = scales[row];
+    float v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        v[e] = (float)(int8_t)(q >> (8 * e)) * s;
+        if (T == LC_F16) asm("" : "+v"(v[e]));              // (else product and conversion become one instruction, with one rounding for the two)
+    }
+    store_some<T>(w, row * ldw + at, (int)(k - at < N ? k - at : N), v);
+}
+
+// ---------------------------------------------------------------- the product
+struct Product {
+    const uint8_t *x, *w;
+    const float *sx, *sw;
+    const void* bias;
+    void* y;
+    uint64_t x_pitch, w_pitch, ldy;
+    uint32_t m, n, k16;         // k16: bytes of a row, a multiple of 16
+    int dtype;
+};
+
+__device__ __forceinline__ float result_of(const Product& p, int sum, float sx, float sw, uint32_t j) {
+    float v = (float)sum * sx * sw;
+    if (p.bias) v += p.dtype == LC_F32 ? load_one<LC_F32>(p.bias, j) : p.dtype == LC_BF16 ? load_one<LC_BF16>(p.bias, j) : load_one<LC_F16>(p.bias, j);
+    return v;
+}
+__device__ __forceinline__ void put(const Product& p, uint64_t at, float v) {
+    if (p.dtype == LC_F32) store_one<LC_F32>(p.y, at, v);
+    else if (p.dtype == LC_BF16) store_one<LC_BF16>(p.y, at, v);
+    else store_one<LC_F16>(p.y, at, v);
+}
+
+// D = A B^T + C in whole numbers, 16 x 16 x 64: lane l gives row l % 16 of A and of B, 16 bytes of the inner dimension per quarter (the same ones for both), and
+// receives column l % 16, rows 4 (l / 16) + 0..3.  And 32 x 32 x 32: row l % 32, 16 bytes per half; column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4.
+__device__ __forceinline__ i32x4 mfma_16(u32x4 a, u32x4 b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ i32x16 mfma_32(u32x4 a, u32x4 b, i32x16 c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+// Few rows: MT tiles of 16 rows of x by 16 rows of w a workgroup, whose wavefronts take steps of 128 bytes of the width in turn; a lane loads 32 bytes of a row, so
+// that four lanes have a whole line, and their sums meet in LDS.
+template <int MT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_i8_rows(Product p) {
+    __shared__ int sums[WAVES][MT * 16][17];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
+    const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+    const uint32_t j = n0 + c < p.n ? n0 + c : p.n - 1;
+    const uint8_t* w = p.w + j * p.w_pitch;
+    const uint8_t* x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) { const uint32_t i = m0 + 16 * t + c < p.m ? m0 + 16 * t + c : p.m - 1; x[t] = p.x + i * p.x_pitch; }
+    i32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+    constexpr int S = 4;
+    for (uint32_t k0 = wave * 128; k0 < p.k16; k0 += S * WAVES * 128) {
+        u32x4 a[S][2], b[S][MT][2];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t at = k0 + s * WAVES * 128 + 32 * h + 16 * i;
+                const bool in = at < p.k16;
+                a[s][i] = load_once<u32x4>(w + (in ? at : 0));
+#pragma unroll
+                for (int t = 0; t < MT; ++t) { b[s][t][i] = *reinterpret_cast<const u32x4*>(x[t] + (in ? at : 0)); if (!in) b[s][t][i] = u32x4{0, 0, 0, 0}; }
+            }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) acc[t] = mfma_16(b[s][t][i], a[s][i], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][16 * t + 4 * h + r][c] = acc[t][r];
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < MT * 256; e += WAVES * 64) {
+        const uint32_t r = e / 16, i = m0 + r, col = n0 + e % 16;
+        if (i >= p.m || col >= p.n) continue;
+        int sum = 0;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) sum += sums[v][r][e % 16];
+        put(p, i * p.ldy + col, result_of(p, sum, p.sx[i], p.sw[col], col));
+    }
+}
+
+__device__ const u32x4 zeros16 = {0, 0, 0, 0};
+
+// 16 bytes of each lane's own place into LDS at `to` + 16 lane, without passing through registers.
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Many rows: TM rows of x by TN rows of w a workgroup, WM x WN wavefronts, 128 bytes of the width at a time in LDS, twice buffered.  A row is eight units
+// of 16 bytes, stored at unit ^ row % 8, so that the lanes that read a column of units from eight rows have eight places; loads that go to LDS write it lane by lane, so
+// it is where each lane loads from that is turned.
+template <int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
+    constexpr int WAVES = WM * WN, MT = TM / WM / 32, NT = TN / WN / 32, BYTES = (TM + TN) * 128, LOADS = (TM + TN) / 8 / WAVES;
+    static_assert((TM + TN) % (8 * WAVES) == 0, "whole loads");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][BYTES];
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
+    const uint32_t tiles_m = (p.m + TM - 1) / TM;
+    const uint32_t m0 = blockIdx.x % tiles_m * TM, n0 = blockIdx.x / tiles_m * TN;
+    const uint8_t* from[LOADS];
+    uint32_t unit = (lane % 8) ^ (lane / 8);
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) {
+        const uint32_t row = (wave * LOADS + l) * 8 + lane / 8;     // of x, and behind them of w
+        if (row < TM) { const uint32_t i = m0 + row < p.m ? m0 + row : p.m - 1; from[l] = p.x + i * p.x_pitch; }
+        else { const uint32_t i = n0 + row - TM < p.n ? n0 + row - TM : p.n - 1; from[l] = p.w + i * p.w_pitch; }
+    }
+    const uint32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
+    i32x16 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    auto ask = [&](uint32_t k0, uint32_t buffer) {
+        const uint32_t at = k0 + unit * 16;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) load_to_lds(at < p.k16 ? (const void*)(from[l] + at) : (const void*)&zeros16, &lds[buffer][(wave * LOADS + l) * 1024]);
+    };
+    ask(0, 0);
+    uint32_t buffer = 0;
+    for (uint32_t k0 = 0; k0 < p.k16; k0 += 128, buffer ^= 1) {
+        __syncthreads();                                    // (what was asked for is there, and the other buffer is free)
+        if (k0 + 128 < p.k16) ask(k0 + 128, buffer ^ 1);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            u32x4 a[MT], b[NT];
+            const uint32_t u = ((2 * s + h) ^ (c % 8)) * 16;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = *reinterpret_cast<const u32x4*>(&lds[buffer][(wm + 32 * i + c) * 128 + u]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = *reinterpret_cast<const u32x4*>(&lds[buffer][(TM + wn + 32 * j + c) * 128 + u]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_32(a[i], b[j], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const uint32_t col = n0 + wn + 32 * j + c;
+        if (col >= p.n) continue;
+        const float sw = p.sw[col];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t row = m0 + wm + 32 * i + 8 * (e / 4) + 4 * h + e % 4;
+                if (row < p.m) put(p, row * p.ldy + col, result_of(p, acc[i][j][e], p.sx[row], sw, col));
+            }
+    }
+}
+
+bool bad(const lc_i8* q) {
+    if (!q || q->n > 0x7fffffffull || q->k > LC_I8_MAX_K) return true;
+    if (q->n == 0 || q->k == 0) return q->n != 0 && (!q->scales || off(q->scales, 4));
+    return !q->codes || !q->scales || off(q->codes, 16) || off(q->scales, 4) || q->pitch % 16 || q->pitch < q->k || q->pitch > (1ull << 40);
+}
+
+template <int T, int WAVES, int R>
+void quantize_of(const void* w, uint64_t ldw, const lc_i8& q, hipStream_t s) {
+    const uint64_t step = 1ull << 23;                       // rows: a launch's lanes are counted in 32 bits
+    for (uint64_t r = 0; r < q.n; r += step) {
+        const uint32_t rows = (uint32_t)(q.n - r < step ? q.n - r : step);
+        k_i8_quantize<T, WAVES, R><<<WAVES == 4 ? rows : (rows + 3) / 4, 256, 0, s>>>(static_cast<const uint8_t*>(w) + r * ldw * (T == LC_F32 ? 4 : 2), ldw,
+            static_cast<uint8_t*>(q.codes) + r * q.pitch, q.pitch, q.scales + r, rows, (uint32_t)q.k);
+    }
+}
+template <int T>
+void quantize(const void* w, uint64_t ldw, const lc_i8& q, hipStream_t s) {
+    // A wavefront a row where there are rows enough to fill the chip with them.
+    if (q.n >= 2048 && q.k <= 512) quantize_of<T, 1, 1>(w, ldw, q, s);
+    else if (q.n >= 2048 && q.k <= 2048) quantize_of<T, 1, 4>(w, ldw, q, s);
+    else if (q.k <= 2048) quantize_of<T, 4, 1>(w, ldw, q, s);
+    else if (q.k <= 4096) quantize_of<T, 4, 2>(w, ldw, q, s);
+    else if (q.k <= 8192) quantize_of<T, 4, 4>(w, ldw, q, s);
+    else quantize_of<T, 4, 8>(w, ldw, q, s);
+}
+template <int T>
+void dequantize(const lc_i8& q, void* w, uint64_t ldw, hipStream_t s) {
+    const uint32_t lanes = (uint32_t)((q.k + kAtOnce<T> - 1) / kAtOnce<T>);
+    const uint64_t step = (1ull << 30) / lanes;
+    for (uint64_t r = 0; r < q.n; r += step) {
+        const uint32_t rows = (uint32_t)(q.n - r < step ? q.n - r : step);
+        k_i8_dequantize<T><<<(uint32_t)(((uint64_t)rows * lanes + 255) / 256), 256, 0, s>>>(static_cast<const uint8_t*>(q.codes) + r * q.pitch, q.pitch, q.scales + r,
+            static_cast<uint8_t*>(w) + r * ldw * (T == LC_F32 ? 4 : 2), ldw, rows * lanes, (uint32_t)q.k, FastDiv(lanes));
+    }
+}
+
+void multiply_piece(const Product& p, hipStream_t s) {
+    if (p.m <= 16) k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, 1), 512, 0, s>>>(p);
+    else if (p.m <= 64) k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p);
+    else k_i8_tiles<128, 128, 2, 2><<<(p.m + 127) / 128 * ((p.n + 127) / 128), 256, 0, s>>>(p);
+}
+// By pieces of w's rows of which each makes a launch of fewer than 2^32 threads.
+void multiply(const Product& p, hipStream_t s) {
+    const uint64_t step = p.m <= 64 ? 1ull << 26 : ((1ull << 23) / ((p.m + 127) / 128)) * 128;
+    for (uint64_t j = 0; j < p.n; j += step) {
+        Product q = p;
+        q.n = (uint32_t)(p.n - j < step ? p.n - j : step);
+        q.w += j * p.w_pitch;
+        q.sw += j;
+        if (q.bias) q.bias = static_cast<const uint8_t*>(p.bias) + j * size_of(p.dtype);
+        q.y = static_cast<uint8_t*>(p.y) + j * size_of(p.dtype);
+        multiply_piece(q, s);
+    }
+}
+
+bool bad_result(const lc_i8* w8, uint64_t m, const void* bias, const void* y, uint64_t ldy, int dtype) {
+    return !y || off(y, size_of(dtype)) || off(bias, size_of(dtype)) || ldy > (1ull << 40) || (m > 1 && ldy < w8->n);
+}
+constexpr uint64_t kMostRows = 1ull << 19;
+
+}  // namespace
+}  // namespace serve
+}  // namespace lc
+
+using namespace lc::serve;
+
+extern "C" {
+
+int lc_i8_quantize(const void* w, uint64_t ldw, int dtype, const lc_i8* w8, void* stream) {
+    if (!served_type(dtype) || bad(w8)) return LC_ERR_BADARG;
+    if (w8->n == 0) return LC_OK;
+    if ((w8->k && (!w || off(w, size_of(dtype)))) || (w8->n > 1 && ldw < w8->k) || ldw > (1ull << 40)) return LC_ERR_BADARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (dtype == LC_F32) quantize<LC_F32>(w, ldw, *w8, s);
+    else if (dtype == LC_BF16) quantize<LC_BF16>(w, ldw, *w8, s);
+    else quantize<LC_F16>(w, ldw, *w8, s);
+    return launched();
+}
+
+int lc_i8_dequantize(const lc_i8* w8, void* w, uint64_t ldw, int dtype, void* stream) {
+    if (!served_type(dtype) || bad(w8)) return LC_ERR_BADARG;
+    if (w8->n == 0 || w8->k == 0) return LC_OK;
+    if (!w || off(w, size_of(dtype)) || (w8->n > 1 && ldw < w8->k) || ldw > (1ull << 40)) return LC_ERR_BADARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (dtype == LC_F32) dequantize<LC_F32>(*w8, w, ldw, s);
+    else if (dtype == LC_BF16) dequantize<LC_BF16>(*w8, w, ldw, s);
+    else dequantize<LC_F16>(*w8, w, ldw, s);
+    return launched();
+}
+
+int lc_i8_matmul(const lc_i8* x8, const lc_i8* w8, const void* bias, void* y, uint64_t ldy, int dtype, void* stream) {
+    if (!served_type(dtype) || bad(x8) || bad(w8) || x8->k != w8->k || x8->n > kMostRows) return LC_ERR_BADARG;
+    if (x8->n == 0 || w8->n == 0) return LC_OK;
+    if (bad_result(w8, x8->n, bias, y, ldy, dtype)) return LC_ERR_BADARG;
+    const Product p = {static_cast<const uint8_t*>(x8->codes), static_cast<const uint8_t*>(w8->codes), x8->scales, w8->scales, bias, y, x8->pitch, w8->pitch, ldy,
+                       (uint32_t)x8->n, (uint32_t)w8->n, (uint32_t)((w8->k + 15) / 16 * 16), dtype};
+    multiply(p, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+size_t lc_i8_workspace_bytes(uint64_t m, uint64_t k) {
+    if (m > kMostRows || k > LC_I8_MAX_K) return 0;
+    return (size_t)((m * ((k + 15) / 16 * 16) + 255) / 256 * 256 + (m * 4 + 255) / 256 * 256 + 256);
+}
+
+int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const void* bias, void* y, uint64_t ldy, int dtype, void* ws, size_t ws_bytes,
+                 void* stream) {
+    if (!served_type(dtype) || bad(w8) || m > kMostRows) return LC_ERR_BADARG;
+    if (m == 0 || w8->n == 0) return LC_OK;
+    if (bad_result(w8, m, bias, y, ldy, dtype) || (w8->k && (!x || off(x, size_of(dtype)))) || (m > 1 && ldx < w8->k) || ldx > (1ull << 40)) return LC_ERR_BADARG;
+    if (!ws || off(ws, 256) || ws_bytes < lc_i8_workspace_bytes(m, w8->k)) return LC_ERR_WORKSPACE;
+    const uint64_t row = (w8->k + 15) / 16 * 16;
+    const lc_i8 x8 = {ws, reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (m * row + 255) / 256 * 256), m, w8->k, row};
+    const int st = lc_i8_quantize(x, ldx, dtype, &x8, stream);
+    return st != LC_OK ? st : lc_i8_matmul(&x8, w8, bias, y, ldy, dtype, stream);
+}
+
+}  // extern "C"

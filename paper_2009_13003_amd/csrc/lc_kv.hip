@@ -1,23 +1,11 @@
 // A paged cache of keys and values in 8 or 4 bits: writing, reading back, and the attention over it (include/lc_serve.h).
-#include "lc_serve.h"
+#include "lc_cache.h"
 
 #include <atomic>
 
 namespace lc {
 namespace serve {
 namespace {
-
-struct Cache {
-    uint8_t *k, *v;
-    float *k_scale, *v_scale;
-    uint64_t slots;             // pages * page_tokens
-    uint32_t page_shift, heads, dim, row_bytes;
-};
-
-// Where a head's token lies: the row of codes and the scale, counted in rows.
-__device__ __forceinline__ uint64_t row_of(const Cache& c, uint64_t page, uint32_t head, uint32_t token) {
-    return ((page * c.heads + head) << c.page_shift) + token;
-}
 
 // ---------------------------------------------------------------- writing and reading back
 // A lane takes eight elements of a token's head, a power of two of lanes (those behind the last element idle) the whole head; the
@@ -688,18 +676,6 @@ int tiles_of_rows(uint64_t rows, int dim, int dtype) { return rows > 16 && dtype
 // pays (one token of 16 sequences of up to 16384 of 8 heads of 128 47.0 us for 50.5, of 40 of up to 2000 of 2 heads of 96 16.1 for 15.6; one over 32000 of
 // 16 heads of 64 25.0 for 22.9).
 uint32_t workgroups_of(int bits, int dim, int dtype, int tiles) { return bits == 4 && dim > 64 && dim <= 128 && dtype != LC_F32 && tiles == 1 ? 768 : 512; }
-
-bool bad(const lc_kv_cache* c) {
-    if (!c || c->heads < 1 || c->heads > 1024 || c->dim < 32 || c->dim > 256 || c->dim % 32 || (c->bits != 8 && c->bits != 4)) return true;
-    if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) || c->pages > (1ull << 31) / c->page_tokens) return true;
-    if (c->pages == 0) return false;
-    return !c->k || !c->v || !c->k_scale || !c->v_scale || off(c->k, 16) || off(c->v, 16) || off(c->k_scale, 16) || off(c->v_scale, 16);
-}
-Cache described(const lc_kv_cache& c) {
-    return {static_cast<uint8_t*>(c.k), static_cast<uint8_t*>(c.v), c.k_scale, c.v_scale, c.pages * c.page_tokens,
-            (uint32_t)__builtin_ctz((unsigned)c.page_tokens), (uint32_t)c.heads, (uint32_t)c.dim, (uint32_t)(c.dim * c.bits / 8)};
-}
-int launched() { return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP; }
 
 bool bad_vectors(const lc_kv_cache* c, const void* k, const void* v, uint64_t ld_token, uint64_t ld_head, const int64_t* slots, uint64_t tokens, int dtype) {
     const uintptr_t size = size_of(dtype);

@@ -1,0 +1,498 @@
+// Attention of many new tokens a sequence over the paged cache in 8 or 4 bits (include/lc_serve.h).
+#include "lc_cache.h"
+
+namespace lc {
+namespace serve {
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+// The rows that share a head of the cache are a sequence's new tokens times the queries to a head.  A workgroup takes 128 of them, a wavefront 32, and walks over the
+// tokens 64 at a time.  Codes are converted once for all of its rows, on their way into LDS (K as it lies, V with tokens and elements changed about), and from there:
+//   S^T = K Q^T   32 tokens by 32 rows by 16 elements an instruction: lane l gets row l % 32, tokens 8 (i / 4) + 4 (l / 32) + i % 4
+//   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens of each 16 in the order 0-3, 8-11, 4-7, 12-15,
+//                    in which V^T is kept
+// so that the running maximum and the sum are one number a lane.  Scales of keys multiply the scores.
+//   bf16: scales of values multiply the probabilities, whose product is rounded to bf16; codes are whole numbers, exact
+//   fp16: values are rounded to fp16 as they are converted, probabilities to fp16
+//   fp32: as bf16 with queries and probabilities in three parts
+constexpr int kWaves = 4, kRows = 32 * kWaves, kTile = 64;
+constexpr float kFar = 8.0f;                                // by how much, in powers of two, a score may pass what probabilities are measured from
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr uint32_t kMostSplits = 32;
+
+struct Prompt {
+    Cache c;
+    const void* q; uint64_t ld_q;
+    const int32_t* starts;
+    const int32_t* table; uint64_t ld_table; uint64_t table_pages;
+    const int32_t* lens;
+    void* out; uint64_t ld_out;
+    float* stats;               // the maximum and the sum of each [split][token][head]
+    float* part;                // [split][token][head][dim]
+    float scale;                // times log2(e)
+    uint32_t tokens, batch, heads, group, splits;
+    int32_t pages;
+    FastDiv by_group;
+};
+
+template <int T> struct Kind;       // how many 16-bit parts an element of q, and a probability, are given
+template <> struct Kind<LC_F32> { static constexpr int kParts = 3; static constexpr bool kHalf = false; };
+template <> struct Kind<LC_BF16> { static constexpr int kParts = 1; static constexpr bool kHalf = false; };
+template <> struct Kind<LC_F16> { static constexpr int kParts = 1; static constexpr bool kHalf = true; };
+
+template <bool HALF> __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    if (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// a below b, rounded to nearest even.
+template <bool HALF> __device__ __forceinline__ uint32_t pair_of(float a, float b) {
+    if (!HALF) return rounded_halves(a, b);
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+}
+// The other half's number of the same column.
+__device__ __forceinline__ float other_half(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(bits_of(v), bits_of(v), false, false);
+    return threadIdx.x % 64 < 32 ? float_of(a[1]) : float_of(a[0]);
+}
+
+__device__ __forceinline__ int32_t held(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Which rows of which sequence a workgroup has: blocks of rows are counted over all sequences.
+struct Own { uint32_t b; int32_t first, count, block; };    // the sequence's first new token and how many it has; the block of rows within it
+__device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t lane) {
+    uint32_t before = 0;
+    for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
+        const uint32_t b = b0 + lane;
+        const int32_t s = held(b < a.batch ? a.starts[b] : 0, 0, (int32_t)a.tokens), e = held(b < a.batch ? a.starts[b + 1] : 0, 0, (int32_t)a.tokens);
+        const uint32_t own = e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + kRows - 1) / kRows) : 0;
+        uint32_t upto = own;
+        for (int x = 1; x < 64; x *= 2) { const uint32_t o = __shfl_up(upto, x); if (lane >= (uint32_t)x) upto += o; }
+        const unsigned long long mine = __ballot(before + upto > block && before + upto - own <= block);
+        if (mine) {
+            const int from = __builtin_ctzll(mine);
+            const uint32_t first_block = before + __builtin_amdgcn_readlane(upto, from) - __builtin_amdgcn_readlane(own, from);
+            return {b0 + from, __builtin_amdgcn_readlane(s, from), __builtin_amdgcn_readlane(e, from) - __builtin_amdgcn_readlane(s, from),
+                    (int32_t)(block - first_block)};
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {0, 0, 0, 0};
+}
+
+template <int T, int BITS, int DP> struct Shape {
+    static constexpr int kUnits = (DP / 8 + 7) / 8 * 8;     // 16-byte units a row of K has room for
+    static constexpr int kRowBytes = DP * BITS / 8;
+    static constexpr int kChunks = kRowBytes / 16;          // pieces of 16 bytes of codes a token has
+    static constexpr int kKeyLoads = (kTile * kChunks + kWaves * 64 - 1) / (kWaves * 64);
+    static constexpr int kWords = kRowBytes / 4;            // and of 4 bytes
+    static constexpr int kValueItems = kTile / 4 * kWords, kValueLoads = (kValueItems + kWaves * 64 - 1) / (kWaves * 64);
+};
+// Where a row of V^T keeps a unit: turned by the row, so that neither the lanes that read a column of units nor those that write, whose rows are 4 (8 bits) or 8 (4
+// bits) apart, meet in one bank.
+template <int BITS> __device__ __forceinline__ uint32_t turned_unit(uint32_t d, uint32_t u) { return u ^ ((BITS == 8 ? d ^ d >> 2 : d ^ d >> 2 ^ d >> 3) & 7); }
+
+// Eight codes as numbers: 8 bits from two words, 4 bits from one.
+template <int BITS> __device__ __forceinline__ float code_of(uint32_t w, int e) {
+    return BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : (float)((int)(w >> (4 * e) & 15u) - 8);
+}
+
+template <int T, int BITS, int DP, int PERSIMD>
+__global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
+    using S = Shape<T, BITS, DP>;
+    constexpr bool HALF = Kind<T>::kHalf;
+    constexpr int NP = Kind<T>::kParts, KS = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) uint16_t sk[2][kTile][S::kUnits * 8];
+    __shared__ __attribute__((aligned(16))) uint16_t sv[2][DP][kTile];
+    __shared__ __attribute__((aligned(16))) float sks[2][kTile], svs[2][kTile];
+    __shared__ uint32_t sbad[2][2];                         // the tile's tokens that are not there, or whose value is not finite (a half a wavefront)
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
+    const uint32_t head = blockIdx.x % a.c.heads;
+    const Own own = own_of(a, blockIdx.x / a.c.heads, lane);
+    if (own.count == 0) return;
+    const uint32_t b = own.b;
+    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    const int32_t len = held(a.lens[b], 0, room);
+    const int32_t rows = (int32_t)(own.count * a.group), blocks = (rows + kRows - 1) / kRows;
+    const int32_t row0 = (blocks - 1 - own.block) * kRows;  // (the rows that see most first)
+    const int32_t row_last = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
+    const int32_t base = len - own.count;                   // the place of the first new token
+    auto place_of = [&](int32_t row) { return base + (int32_t)a.by_group((uint32_t)row); };
+    const int32_t tiles_all = place_of(row_last) >= 0 ? place_of(row_last) / kTile + 1 : 0;
+    const int32_t per = (tiles_all + (int32_t)a.splits - 1) / (int32_t)a.splits;
+    const int32_t tile0 = (int32_t)blockIdx.y * per, tile1 = tile0 + per < tiles_all ? tile0 + per : tiles_all;
+
+    // this lane's row
+    const int32_t row = row0 + (int32_t)(32 * wave + c);
+    const bool has_row = row < rows;
+    const uint32_t rr = (uint32_t)(has_row ? row : rows - 1), qi = a.by_group(rr), qg = rr - qi * a.group;
+    const int32_t place = has_row ? base + (int32_t)qi : -1;
+    const int32_t wave_first = place_of(row0 + 32 * (int32_t)wave < rows ? row0 + 32 * (int32_t)wave : rows - 1);
+    const int32_t wave_end = row0 + 32 * (int32_t)wave < rows ? place_of(row0 + 32 * (int32_t)wave + 31 < rows ? row0 + 32 * (int32_t)wave + 31 : rows - 1) : -1;
+    u32x4 q[KS][NP];
+    {
+        const uint64_t at = (uint64_t)(own.first + qi) * a.ld_q + (uint64_t)(head * a.group + qg) * a.c.dim;
+#pragma unroll
+        for (int o = 0; o < KS; ++o) {
+            const uint32_t d = 16 * o + 8 * h;
+            float v[8];
+            load_eight<T>(a.q, at + d, has_row && d < a.c.dim ? 8 : 0, v);
+            // An infinity is taken as NaN: the score of whatever is seen is infinite or NaN, so the softmax of any set of them is NaN.
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += v[e] - v[e];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[o][p][j] = HALF ? f16_of(v[2 * j]) | f16_of(v[2 * j + 1]) << 16 : high_halves(bits_of(v[2 * j]), bits_of(v[2 * j + 1]));
+                if (NP > 1)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);
+            }
+        }
+    }
+
+    // A tile on its way: codes in registers, then converted into LDS.
+    const int32_t* table = a.table + b * a.ld_table;
+    u32x4 keys[S::kKeyLoads];
+    uint32_t values[S::kValueLoads][4];
+    float scale_raw = 0;
+    bool there_raw = true;
+    auto slot_row = [&](int32_t t, bool& there) -> uint64_t {       // the row of token t (held to the sequence) of this head
+        t = t < len ? t : len - 1;
+        const int32_t page = table[t >> a.c.page_shift];
+        there = (uint32_t)page < (uint32_t)a.pages;
+        return row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
+    };
+    auto ask = [&](int32_t tile) {
+        const int32_t t0 = tile * kTile;
+#pragma unroll
+        for (int l = 0; l < S::kKeyLoads; ++l) {
+            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
+            bool there;
+            keys[l] = u32x4{0, 0, 0, 0};
+            if (i < kTile * S::kChunks && ch * 16 < a.c.row_bytes)
+                keys[l] = *reinterpret_cast<const u32x4*>(a.c.k + slot_row(t0 + (int32_t)t, there) * a.c.row_bytes + ch * 16);
+        }
+#pragma unroll
+        for (int l = 0; l < S::kValueLoads; ++l) {
+            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, w = i % S::kWords;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) values[l][r] = 0;
+            if (i < (uint32_t)S::kValueItems && w * 4 < a.c.row_bytes) {
+                // (four tokens that begin at a multiple of four lie together)
+                bool there;
+                const uint32_t first = (uint32_t)(t0 + (int32_t)t) < (uint32_t)len ? t0 + t : (uint32_t)(len - 1) & ~3u;
+                const uint8_t* from = a.c.v + slot_row((int32_t)first, there) * a.c.row_bytes + w * 4;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) values[l][r] = *reinterpret_cast<const uint32_t*>(from + r * a.c.row_bytes);
+            }
+        }
+        if (threadIdx.x < 128) {
+            const int32_t t = t0 + (int32_t)(threadIdx.x % 64);
+            bool there;
+            const uint64_t at = slot_row(t, there);
+            there_raw = there && t < len;
+            scale_raw = threadIdx.x < 64 ? a.c.k_scale[at] : a.c.v_scale[at];
+        }
+    };
+    auto put = [&](uint32_t buffer) {
+        // scales first: values in fp16 are converted with theirs
+        if (threadIdx.x < 128) {
+            const uint32_t t = threadIdx.x % 64;
+            if (threadIdx.x < 64) sks[buffer][t] = scale_raw * a.scale;
+            else svs[buffer][t] = there_raw ? scale_raw : 0.0f;
+            const unsigned long long wrong = __ballot(!there_raw || (HALF && threadIdx.x >= 64 && !(scale_raw < __builtin_inff())));
+            if (threadIdx.x == 64) { sbad[buffer][0] = (uint32_t)wrong; sbad[buffer][1] = (uint32_t)(wrong >> 32); }
+        }
+        if (HALF) __syncthreads();
+#pragma unroll
+        for (int l = 0; l < S::kKeyLoads; ++l) {
+            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
+            if (i >= kTile * S::kChunks) continue;
+#pragma unroll
+            for (int u = 0; u < 16 / BITS; ++u) {           // units of eight codes
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float x, y;
+                    if (BITS == 8) { x = code_of<8>(keys[l][2 * u + j / 2], 2 * (j % 2)); y = code_of<8>(keys[l][2 * u + j / 2], 2 * (j % 2) + 1); }
+                    else { x = code_of<4>(keys[l][u], 2 * j); y = code_of<4>(keys[l][u], 2 * j + 1); }
+                    v[j] = pair_of<HALF>(x, y);
+                }
+                const uint32_t unit = ch * (16 / BITS) + u;
+                *reinterpret_cast<u32x4*>(&sk[buffer][t][(unit ^ (t & 7)) * 8]) = v;
+            }
+        }
+#pragma unroll
+        for (int l = 0; l < S::kValueLoads; ++l) {
+            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, w = i % S::kWords;
+            if (i >= (uint32_t)S::kValueItems) continue;
+            f32x4 by = {1, 1, 1, 1};
+            if (HALF) {
+                by = *reinterpret_cast<const f32x4*>(&svs[buffer][t]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) by[r] = by[r] < __builtin_inff() ? by[r] : 0.0f;      // (NaN: the tokens are marked)
+            }
+            const uint32_t group = t / 4 % 4, unit = t / 16 * 2 + group % 2, half = group / 2;      // tokens 0-3, 8-11, 4-7, 12-15
+#pragma unroll
+            for (int e = 0; e < 32 / BITS; ++e) {
+                const uint32_t d = w * (32 / BITS) + e;
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] = code_of<BITS>(values[l][r], e);
+                    if (HALF) x[r] = fminf(fmaxf(x[r] * by[r], -65504.0f), 65504.0f);
+                }
+                *reinterpret_cast<u32x2*>(&sv[buffer][d][turned_unit<BITS>(d, unit) * 8 + half * 4]) = u32x2{pair_of<HALF>(x[0], x[1]), pair_of<HALF>(x[2], x[3])};
+            }
+        }
+    };
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int j = 0; j < DB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[j][e] = 0;
+    float top = -__builtin_inff(), from = 0, sum = 0;       // the largest score so far (or about that), what probabilities are measured from, their sum
+
+    if (tile0 < tile1) {
+        ask(tile0);
+        put(0);
+    }
+    uint32_t buffer = 0;
+    for (int32_t tile = tile0; tile < tile1; ++tile, buffer ^= 1) {
+        __syncthreads();
+        if (tile + 1 < tile1) ask(tile + 1);
+        const int32_t tb = tile * kTile;
+        if (tb <= wave_end) {
+            f32x16 score[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) score[s][e] = 0;
+#pragma unroll
+                for (int o = 0; o < KS; ++o) {
+                    const uint32_t t = 32 * s + c;
+                    const u32x4 key = *reinterpret_cast<const u32x4*>(&sk[buffer][t][((2 * o + h) ^ (t & 7)) * 8]);
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) score[s] = mfma<HALF>(key, q[o][p], score[s]);
+                }
+            }
+            const bool whole = tb + kTile - 1 <= wave_first && (sbad[buffer][0] | sbad[buffer][1]) == 0;
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 ks = *reinterpret_cast<const f32x4*>(&sks[buffer][32 * s + 8 * g + 4 * h]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) score[s][4 * g + r] = fmaf(score[s][4 * g + r], ks[r], -from);
+                }
+            uint32_t hidden[2] = {0, 0};                    // of this lane's 16 tokens each
+            if (!whole) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int32_t t = 32 * s + 8 * (e / 4) + 4 * h + e % 4;
+                        const bool marked = sbad[buffer][s] >> (t & 31) & 1;
+                        const bool is_nan = HALF && marked && tb + t <= place && tb + t < len && !(svs[buffer][t] < __builtin_inff());
+                        if (tb + t > place || (marked && !is_nan)) { hidden[s] |= 1u << e; score[s][e] = -__builtin_inff(); }
+                        if (is_nan) score[s][e] = __builtin_nanf("");
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, score[s][e]);
+            if (__any(most > kFar || top == -__builtin_inff())) {
+                most = fmaxf(fmaxf(most, other_half(most)) + from, top);
+                const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - then);
+                sum *= shrink;
+#pragma unroll
+                for (int j = 0; j < DB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) score[s][e] -= then - from;
+                top = most;
+                from = then;
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) { score[s][e] = __builtin_amdgcn_exp2f(score[s][e]); sum += score[s][e]; }
+                if (!HALF) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 vs = *reinterpret_cast<const f32x4*>(&svs[buffer][32 * s + 8 * g + 4 * h]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) score[s][4 * g + r] *= !whole && (hidden[s] >> (4 * g + r) & 1) ? 0.0f : vs[r];
+                    }
+                }
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {               // 16 tokens at a time
+                    u32x4 pp[NP];
+                    float p[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = score[s][8 * o + e];
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            pp[k][j] = k == NP - 1 ? pair_of<HALF>(p[2 * j], p[2 * j + 1]) : high_halves(bits_of(p[2 * j]), bits_of(p[2 * j + 1]));
+                        if (k < NP - 1)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
+                    }
+#pragma unroll
+                    for (int j = 0; j < DB; ++j) {
+                        const uint32_t d = 32 * j + c;
+                        const u32x4 value = *reinterpret_cast<const u32x4*>(&sv[buffer][d][turned_unit<BITS>(d, 4 * s + 2 * o + h) * 8]);
+#pragma unroll
+                        for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value, pp[k], acc[j]);
+                    }
+                }
+            }
+        }
+        if (tile + 1 < tile1) put(buffer ^ 1);
+    }
+
+    const float total = sum + other_half(sum);
+    if (!has_row) return;
+    const uint64_t at = (uint64_t)(own.first + qi), hd = head * a.group + qg;
+    const float whole = a.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+    if (a.splits > 1) {
+        const uint64_t place_at = ((uint64_t)blockIdx.y * a.tokens + at) * a.heads + hd;
+        if (h == 0) { a.stats[2 * place_at] = top; a.stats[2 * place_at + 1] = total; }
+        if (total == 0.0f) return;
+        float* to = a.part + place_at * a.c.dim;
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t d = 32 * j + 8 * g + 4 * h;
+                if (d < a.c.dim) *reinterpret_cast<f32x4*>(to + d) = f32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+            }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < DB; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t d = 32 * j + 8 * g + 4 * h;
+            f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+            v *= whole;
+            if (d < a.c.dim) store_four<T>(a.out, at * a.ld_out + hd * a.c.dim + d, v);
+        }
+}
+
+// The parts of rows that several workgroups had, joined: a lane four elements of a row.
+template <int T>
+__global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t lanes, FastDiv by_quads, FastDiv by_heads) {
+    const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
+    if (lane >= lanes) return;
+    const uint32_t r = by_quads(lane), d = 4 * (lane - r * by_quads.d), token = by_heads(r), hd = r - token * a.heads;
+    if ((int32_t)token < a.starts[0] || (int32_t)token >= a.starts[a.batch]) return;      // (of no sequence)
+    float m = -__builtin_inff(), l = 0;
+    for (uint32_t s = 0; s < a.splits; ++s) m = fmaxf(m, a.stats[2 * (((uint64_t)s * a.tokens + token) * a.heads + hd)]);
+    f32x4 o = {0, 0, 0, 0};
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        const uint64_t at = ((uint64_t)s * a.tokens + token) * a.heads + hd;
+        const float sum = a.stats[2 * at + 1];
+        if (sum == 0.0f) continue;
+        const float f = __builtin_amdgcn_exp2f(a.stats[2 * at] - m);
+        l += f * sum;
+        const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + at * a.c.dim + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+    }
+    const float whole = l == 0.0f ? 1.0f : 1.0f / l;
+    o *= whole;
+    store_four<T>(a.out, (uint64_t)token * a.ld_out + (uint64_t)hd * a.c.dim + d, o);
+}
+
+// Row blocks at most, and into how many parts their tokens are split so that the chip is full.
+uint32_t blocks_of(uint64_t tokens, uint64_t batch, uint32_t group) {
+    const uint64_t most = tokens < batch ? tokens : batch;  // sequences with new tokens
+    return (uint32_t)((tokens * group + kRows - 1) / kRows + most);
+}
+uint32_t splits_of(uint64_t blocks, uint32_t kv_heads) {
+    const uint64_t have = blocks * kv_heads;
+    if (have >= 512) return 1;
+    const uint64_t s = 512 / have;
+    return (uint32_t)(s < kMostSplits ? s : kMostSplits);
+}
+
+template <int T, int BITS, int DP>
+void prompt_of(const Prompt& a, uint32_t blocks, hipStream_t s) {
+    constexpr int PERSIMD = T == LC_F32 || DP > 128 ? 1 : 2;
+    k_kv_prompt<T, BITS, DP, PERSIMD><<<dim3(blocks * a.c.heads, a.splits), kWaves * 64, 0, s>>>(a);
+    if (a.splits > 1) {
+        const uint32_t quads = a.c.dim / 4, lanes = a.tokens * a.heads * quads;
+        k_kv_prompt_join<T><<<(lanes + 255) / 256, 256, 0, s>>>(a, lanes, FastDiv(quads), FastDiv(a.heads));
+    }
+}
+template <int T, int BITS>
+void prompt(const Prompt& a, uint32_t blocks, hipStream_t s) {
+    if (a.c.dim <= 64) prompt_of<T, BITS, 64>(a, blocks, s);
+    else if (a.c.dim <= 128) prompt_of<T, BITS, 128>(a, blocks, s);
+    else prompt_of<T, BITS, 256>(a, blocks, s);
+}
+
+}  // namespace
+}  // namespace serve
+}  // namespace lc
+
+using namespace lc::serve;
+
+extern "C" {
+
+size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim) {
+    if (tokens > (1ull << 24) || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 || dim > 256 ||
+        dim % 32 || tokens * heads > (1ull << 30)) return 0;
+    if (tokens == 0 || batch == 0) return 256;
+    const uint32_t splits = splits_of(blocks_of(tokens, batch, (uint32_t)(heads / kv_heads)), (uint32_t)kv_heads);
+    if (splits == 1) return 256;
+    const uint64_t rows = splits * tokens * heads;
+    return (size_t)((rows * 8 + 255) / 256 * 256 + (rows * dim * 4 + 255) / 256 * 256);
+}
+
+int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,
+                        const int32_t* table, uint64_t ld_table, uint64_t table_pages, const int32_t* lens, float scale, void* out, uint64_t ld_out, int dtype,
+                        void* ws, size_t ws_bytes, void* stream) {
+    if (!served_type(dtype) || bad(cache)) return LC_ERR_BADARG;
+    const size_t need = lc_kv_prompt_workspace_bytes(tokens, batch, heads, cache->heads, cache->dim);
+    if (!need) return LC_ERR_BADARG;
+    if (tokens == 0 || batch == 0) return LC_OK;
+    const uint64_t width = (uint64_t)heads * cache->dim, step = dtype == LC_F32 ? 4 : 8;
+    if (!q || !out || !starts || !lens || off(q, 16) || off(out, 16) || off(starts, 4) || off(lens, 4) || (table_pages && (!table || off(table, 4))) ||
+        ld_table > (1ull << 31) || table_pages > (1ull << 30) / cache->page_tokens || (batch > 1 && ld_table < table_pages)) return LC_ERR_BADARG;
+    if (ld_q > (1ull << 40) || ld_out > (1ull << 40) || (tokens > 1 && (ld_q < width || ld_out < width || ld_q % step || ld_out % step))) return LC_ERR_BADARG;
+    if (!ws || off(ws, 256) || ws_bytes < need) return LC_ERR_WORKSPACE;
+    Prompt a = {};
+    a.c = described(*cache);
+    a.q = q; a.ld_q = ld_q; a.starts = starts; a.table = table; a.ld_table = ld_table; a.table_pages = cache->pages ? table_pages : 0; a.lens = lens;
+    a.out = out; a.ld_out = ld_out;
+    a.scale = scale * kLog2e;
+    a.tokens = (uint32_t)tokens; a.batch = (uint32_t)batch; a.heads = (uint32_t)heads; a.group = (uint32_t)(heads / cache->heads);
+    a.by_group = FastDiv(a.group);
+    a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
+    const uint32_t blocks = blocks_of(tokens, batch, a.group);
+    a.splits = splits_of(blocks, a.c.heads);
+    const uint64_t rows = (uint64_t)a.splits * tokens * heads;
+    a.stats = static_cast<float*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (rows * 8 + 255) / 256 * 256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, blocks, s); else prompt<T, 4>(a, blocks, s); } while (0)
+    if (dtype == LC_F32) CALL(LC_F32);
+    else if (dtype == LC_BF16) CALL(LC_BF16);
+    else CALL(LC_F16);
+#undef CALL
+    return launched();
+}
+
+}  // extern "C"

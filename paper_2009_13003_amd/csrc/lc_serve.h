@@ -1,4 +1,4 @@
-// Shared between the kernels of the serving operators (lc_w4.hip, lc_kv.hip): element types, packing, matrix instructions.  gfx950 only.
+// Shared between the kernels of the serving operators (lc_w4.hip, lc_i8.hip, lc_kv.hip, lc_prompt.hip, lc_pages.hip, lc_draft.hip): element types, packing, matrix instructions.  gfx950 only.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -20,6 +20,7 @@ constexpr float kSmallest = 1.17549435e-38f;      // 2^-126: scales below it are
 
 inline bool served_type(int dtype) { return dtype == LC_F32 || dtype == LC_BF16 || dtype == LC_F16; }
 inline bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+inline int launched() { return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP; }
 inline uintptr_t size_of(int dtype) { return dtype == LC_F32 ? 4 : 2; }
 
 // n / d for 32-bit n by a product with what the host worked out once (round-up method: exact for every n).

@@ -691,7 +691,6 @@ bool bad(const lc_w4* q) {
            q->scales_pitch < (q->k + q->group - 1) / q->group || q->codes_pitch > (1ull << 40) || q->scales_pitch > (1ull << 40);
 }
 
-int launched() { return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP; }
 
 }  // namespace
 }  // namespace serve

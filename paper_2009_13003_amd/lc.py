@@ -94,6 +94,15 @@ class _W4(ctypes.Structure):            # struct lc_w4
     _fields_ = [("codes", _vp), ("scales", _vp), ("n", _u64), ("k", _u64), ("codes_pitch", _u64), ("scales_pitch", _u64), ("group", _int)]
 
 
+class _I8(ctypes.Structure):            # struct lc_i8
+    _fields_ = [("codes", _vp), ("scales", _vp), ("n", _u64), ("k", _u64), ("pitch", _u64)]
+
+
+class _KvPages(ctypes.Structure):       # struct lc_kv_pages
+    _fields_ = [("table", _vp), ("lens", _vp), ("free_pages", _vp), ("free_count", _vp), ("batch", _u64), ("ld_table", _u64), ("table_pages", _u64),
+                ("free_room", _u64), ("page_tokens", _int)]
+
+
 class _KvCache(ctypes.Structure):       # struct lc_kv_cache
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _u64), ("page_tokens", _int), ("heads", _int),
                 ("dim", _int), ("bits", _int)]
@@ -114,6 +123,28 @@ _lib.lc_kv_read.restype = _int
 _lib.lc_kv_read.argtypes = [_vp, _vp, _u64, _vp, _vp, _u64, _u64, _int, _vp]
 _lib.lc_kv_workspace_bytes.restype = _sz
 _lib.lc_kv_workspace_bytes.argtypes = [_u64, _int, _int, _int, _int]
+_lib.lc_i8_quantize.restype = _int
+_lib.lc_i8_quantize.argtypes = [_vp, _u64, _int, _vp, _vp]
+_lib.lc_i8_dequantize.restype = _int
+_lib.lc_i8_dequantize.argtypes = [_vp, _vp, _u64, _int, _vp]
+_lib.lc_i8_matmul.restype = _int
+_lib.lc_i8_matmul.argtypes = [_vp, _vp, _vp, _vp, _u64, _int, _vp]
+_lib.lc_i8_workspace_bytes.restype = _sz
+_lib.lc_i8_workspace_bytes.argtypes = [_u64, _u64]
+_lib.lc_i8_linear.restype = _int
+_lib.lc_i8_linear.argtypes = [_vp, _u64, _u64, _vp, _vp, _vp, _u64, _int, _vp, _sz, _vp]
+_lib.lc_kv_prompt_workspace_bytes.restype = _sz
+_lib.lc_kv_prompt_workspace_bytes.argtypes = [_u64, _u64, _int, _int, _int]
+_lib.lc_kv_attend_prompt.restype = _int
+_lib.lc_kv_attend_prompt.argtypes = [_vp, _vp, _u64, _u64, _int, _vp, _u64, _vp, _u64, _u64, _vp, ctypes.c_float, _vp, _u64, _int, _vp, _sz, _vp]
+_lib.lc_kv_extend.restype = _int
+_lib.lc_kv_extend.argtypes = [_vp, _vp, _u64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.lc_kv_trim.restype = _int
+_lib.lc_kv_trim.argtypes = [_vp, _vp, _vp, _vp, _vp]
+_lib.lc_draft_workspace_bytes.restype = _sz
+_lib.lc_draft_workspace_bytes.argtypes = [_u64]
+_lib.lc_draft_verify.restype = _int
+_lib.lc_draft_verify.argtypes = [_vp, _u64, _u64, _u64, _int, _u64, _vp, _vp, _u64, _u64, _vp, _vp, _vp, _int, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.lc_kv_attend.restype = _int
 _lib.lc_kv_attend.argtypes = [_vp, _vp, _u64, _int, _int, _vp, _u64, _u64, _vp, _vp, ctypes.c_float, _vp, _int, _vp, _sz, _vp]
 
@@ -743,3 +774,273 @@ def lc_kv_attend(cache, q, table, lens, scale=None, mask=None, out=None, ws=None
     if st != OK:
         raise LcError(st)
     return out
+
+
+def lc_i8_workspace_bytes(m, k):
+    return int(_lib.lc_i8_workspace_bytes(m, k))
+
+
+class I8:
+    """A matrix [n][k] in 8 bits with a scale a row: codes int8 [n][at least k rounded up to 16], rows of any pitch that is a multiple of 16 bytes, scales float32 [n].
+    Keeps the two tensors and their marshalled description; they must stay in place.  Where it is the left side of a product, codes behind k have to be zeros."""
+
+    def __init__(self, codes, scales, k):
+        assert codes.is_cuda and codes.dtype == torch.int8 and codes.dim() == 2 and (codes.stride(1) == 1 or codes.shape[1] <= 1)
+        assert scales.is_cuda and scales.dtype == torch.float32 and scales.shape == (codes.shape[0],) and (scales.stride(0) == 1 or codes.shape[0] <= 1)
+        assert codes.shape[1] >= (k + 15) // 16 * 16
+        self._describe(codes, scales, codes.shape[0], k, (k + 15) // 16 * 16 if codes.shape[0] <= 1 else codes.stride(0))
+
+    def _describe(self, codes, scales, n, k, pitch):
+        self.codes, self.scales, self.n, self.k = codes, scales, n, k
+        self._c = _I8(codes.data_ptr() or None, scales.data_ptr() or None, n, k, pitch)
+        self._p = ctypes.addressof(self._c)
+
+
+def lc_i8_quantize(w, out=None, stream=None):
+    """w [n][k] (float32, bfloat16 or float16, contiguous rows) in 8 bits with a scale a row; returns an I8 (`out`, if one is given)."""
+    p, ld = _matrix(w)
+    n, k = w.shape
+    assert not w.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
+    if out is None:
+        row, device = (k + 15) // 16 * 16, w.device
+        make = lambda: (torch.empty(n, row, dtype=torch.int8, device=device), torch.empty(n, dtype=torch.float32, device=device))
+        codes, scales = make() if stream is None else _made_on(stream, make)
+        out = I8.__new__(I8)
+        out._describe(codes, scales, n, k, row)
+    else:
+        assert out.n == n and out.k == k
+    st = _lib.lc_i8_quantize(p, ld, SERVED[w.dtype], out._p, _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def lc_i8_dequantize(w8, dtype=None, out=None, stream=None):
+    """The values that w8 stands for, as a matrix of `dtype` (or in `out`)."""
+    if out is None:
+        dtype = torch.float32 if dtype is None else dtype
+        make = lambda: (torch.empty(w8.n, w8.k, dtype=dtype, device=w8.codes.device),)
+        out, = make() if stream is None else _made_on(stream, make)
+        p, ld = out.data_ptr(), w8.k
+    else:
+        p, ld = _matrix(out)
+        assert out.shape == (w8.n, w8.k) and (dtype is None or out.dtype == dtype)
+        dtype = out.dtype
+    st = _lib.lc_i8_dequantize(w8._p, p, ld, SERVED.get(dtype, -1), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def _bias(bias, n, dtype):
+    assert not bias.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
+    assert bias.is_cuda and bias.dtype == dtype and bias.shape == (n,) and (bias.stride(0) == 1 or n <= 1)
+    return bias.data_ptr()
+
+
+def lc_i8_matmul(x8, w8, bias=None, dtype=None, out=None, stream=None):
+    """x8 [m][k] times w8 [n][k] transposed, plus bias [n]: a matrix [m][n] of `dtype` (float32 if None), or in `out`."""
+    assert x8.k == w8.k
+    m, n = x8.n, w8.n
+    if out is None:
+        dtype = torch.float32 if dtype is None else dtype
+        make = lambda: (torch.empty(m, n, dtype=dtype, device=w8.codes.device),)
+        out, = make() if stream is None else _made_on(stream, make)
+        q, ldq = out.data_ptr(), n
+    else:
+        q, ldq = _matrix(out)
+        assert out.shape == (m, n) and (dtype is None or out.dtype == dtype)
+        dtype = out.dtype
+    st = _lib.lc_i8_matmul(x8._p, w8._p, None if bias is None else _bias(bias, n, dtype), q, ldq, SERVED.get(dtype, -1), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def new_i8_workspace(m, k, device="cuda", stream=None):
+    """Scratch for lc_i8_linear of up to m rows of up to k elements, to be used on `stream` (None: the current one); calls that may run at the same time
+    need one each."""
+    make = lambda: (torch.empty(lc_i8_workspace_bytes(m, k), dtype=torch.uint8, device=device),)
+    return (make() if stream is None else _made_on(stream, make))[0]
+
+
+def lc_i8_linear(x, w8, bias=None, out=None, ws=None, stream=None):
+    """x [m][k] (float32, bfloat16 or float16) times w8 [n][k] transposed, plus bias [n]: a matrix [m][n] of x's dtype (or in `out`), x's rows in 8 bits as by
+    lc_i8_quantize.  ws: a tensor from new_i8_workspace (None: allocated for this call).  No gradient flows through it."""
+    p, ld = _matrix(x)
+    m, k = x.shape
+    dtype, n = x.dtype, w8.n
+    assert k == w8.k
+    assert not x.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
+    if out is None:
+        out = x.new_empty(m, n) if stream is None else _made_on(stream, lambda: (x.new_empty(m, n),))[0]
+        q, ldq = out.data_ptr(), n
+    else:
+        q, ldq = _matrix(out)
+        assert out.shape == (m, n) and out.dtype == dtype
+    if ws is None:
+        ws = new_i8_workspace(m, k, x.device, stream)
+    assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
+    st = _lib.lc_i8_linear(p, ld, m, w8._p, None if bias is None else _bias(bias, n, dtype), q, ldq, SERVED[dtype], ws.data_ptr(), ws.numel(), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+def lc_kv_prompt_workspace_bytes(tokens, batch, heads, kv_heads, dim):
+    return int(_lib.lc_kv_prompt_workspace_bytes(tokens, batch, heads, kv_heads, dim))
+
+
+def new_prompt_workspace(cache, tokens, batch, heads, stream=None):
+    """Scratch for lc_kv_attend_prompt with these sizes, to be used on `stream` (None: the current one); calls that may run at the same time need one each."""
+    make = lambda: (torch.empty(lc_kv_prompt_workspace_bytes(tokens, batch, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device),)
+    return (make() if stream is None else _made_on(stream, make))[0]
+
+
+def _tokens_of(t):
+    """Pitch of a tensor [tokens][heads][dim] whose tokens are contiguous."""
+    assert t.is_cuda and t.dtype in SERVED and t.dim() == 3, "need a CUDA float32 / bfloat16 / float16 tensor [tokens][heads][dim]"
+    tokens, heads, dim = t.shape
+    (st, sh, s1) = t.stride()
+    assert tokens == 0 or (s1 == 1 and (sh == dim or heads == 1)), "need contiguous tokens"
+    return st if tokens > 1 else heads * dim
+
+
+def lc_kv_attend_prompt(cache, q, starts, table, lens, scale=None, out=None, ws=None, stream=None):
+    """Attention of the new tokens of several sequences over the cache: q [tokens][heads][dim], of sequence b those from starts[b] to before starts[b + 1] (int32
+    [batch + 1], not decreasing), which are the newest of its lens[b] cached ones and see what is cached up to themselves; table and lens as for lc_kv_attend.
+    scale: 1 / sqrt(dim) if None.  ws: a tensor from new_prompt_workspace (None: allocated for this call).  Rows of `out` (None: a new tensor) that no sequence
+    has are left as they are.  No gradient flows through it."""
+    ldq = _tokens_of(q)
+    tokens, heads, dim = q.shape
+    assert dim == cache.dim
+    assert not q.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
+    batch = lens.shape[0]
+    assert starts.is_cuda and starts.dtype == torch.int32 and starts.shape == (batch + 1,) and starts.is_contiguous()
+    assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == batch and (table.stride(1) == 1 or table.shape[1] <= 1)
+    assert lens.is_cuda and lens.dtype == torch.int32 and lens.dim() == 1 and lens.is_contiguous()
+    if out is None:
+        make = lambda: (torch.empty(tokens, heads, dim, dtype=q.dtype, device=q.device),)
+        out, = make() if stream is None else _made_on(stream, make)
+        ldo = heads * dim
+    else:
+        assert out.dtype == q.dtype and out.shape == q.shape
+        ldo = _tokens_of(out)
+    if ws is None:
+        ws = new_prompt_workspace(cache, tokens, batch, heads, stream)
+    assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
+    st = _lib.lc_kv_attend_prompt(cache._p, q.data_ptr(), ldq, tokens, heads, starts.data_ptr(), batch, table.data_ptr(),
+                                  table.stride(0) if batch > 1 else table.shape[1], table.shape[1], lens.data_ptr(), dim ** -0.5 if scale is None else scale,
+                                  out.data_ptr(), ldo, SERVED[q.dtype], ws.data_ptr(), ws.numel(), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return out
+
+
+class KvPages:
+    """The pages of sequences that share a cache: table int32 [batch][pages a sequence] and lens int32 [batch], which attention takes, free_pages int32 [room], a stack
+    of the pages that nobody has, and free_count int32 [1], how many there are.  Keeps the tensors and their marshalled description; they must stay in place."""
+
+    def __init__(self, table, lens, free_pages, free_count, page_tokens):
+        batch = lens.shape[0]
+        assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == batch and (table.stride(1) == 1 or table.shape[1] <= 1)
+        for t in (lens, free_pages, free_count):
+            assert t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+        assert free_count.shape == (1,)
+        self.table, self.lens, self.free_pages, self.free_count, self.page_tokens, self.batch = table, lens, free_pages, free_count, page_tokens, batch
+        self._c = _KvPages(table.data_ptr() or None, lens.data_ptr() or None, free_pages.data_ptr() or None, free_count.data_ptr(), batch,
+                           table.stride(0) if batch > 1 else table.shape[1], table.shape[1], free_pages.shape[0], page_tokens)
+        self._p = ctypes.addressof(self._c)
+
+
+def new_kv_pages(cache, batch, context):
+    """The pages of `batch` empty sequences of up to `context` tokens each that share all of the cache; page 0 is given out first."""
+    device = cache.k.device
+    table = torch.zeros(batch, -(-context // cache.page_tokens), dtype=torch.int32, device=device)
+    return KvPages(table, torch.zeros(batch, dtype=torch.int32, device=device), torch.arange(cache.pages - 1, -1, -1, dtype=torch.int32, device=device),
+                   torch.full((1,), cache.pages, dtype=torch.int32, device=device), cache.page_tokens)
+
+
+def _counts(t, n):
+    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def lc_kv_extend(pages, add, room, new_lens=None, new_count=None, out=None, stream=None):
+    """Room for add[b] (int32 [batch]) more tokens of each sequence, of all sequences together at most `room`; the leading sequences for which pages, their rows of the
+    table and `room` suffice get theirs.  Returns starts int32 [batch + 1], and of the new tokens slots int64 [room], places and owners int32 [room] (-1 behind the
+    last), in out = (starts, slots, places, owners) if given.  The lengths and the number of free pages go to new_lens and new_count (None: into `pages`)."""
+    batch = pages.batch
+    if out is None:
+        device = pages.lens.device
+
+        def make():
+            few = torch.empty(batch + 1 + 2 * room, dtype=torch.int32, device=device)      # (one allocation for the three of 32 bits)
+            return torch.empty(room, dtype=torch.int64, device=device), few
+        slots, few = make() if stream is None else _made_on(stream, make)
+        starts, places, owners = few[:batch + 1], few[batch + 1:batch + 1 + room], few[batch + 1 + room:]
+    else:
+        starts, slots, places, owners = out
+        assert slots.is_cuda and slots.dtype == torch.int64 and slots.shape == (room,) and slots.is_contiguous()
+    st = _lib.lc_kv_extend(pages._p, _counts(add, batch), room, pages.lens.data_ptr() if new_lens is None else _counts(new_lens, batch),
+                           pages.free_count.data_ptr() if new_count is None else _counts(new_count, 1), _counts(starts, batch + 1), slots.data_ptr(),
+                           _counts(places, room), _counts(owners, room), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return starts, slots, places, owners
+
+
+def lc_kv_trim(pages, keep, new_lens=None, new_count=None, stream=None):
+    """Of every sequence its first keep[b] tokens stay (int32 [batch]), and the pages behind them go back on the stack.  The lengths and the number of free pages go to
+    new_lens and new_count (None: into `pages`)."""
+    st = _lib.lc_kv_trim(pages._p, _counts(keep, pages.batch), pages.lens.data_ptr() if new_lens is None else _counts(new_lens, pages.batch),
+                         pages.free_count.data_ptr() if new_count is None else _counts(new_count, 1), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+
+
+def lc_draft_workspace_bytes(batch):
+    return int(_lib.lc_draft_workspace_bytes(batch))
+
+
+def new_draft_workspace(batch, device="cuda", stream=None):
+    """Scratch for lc_draft_verify of up to `batch` sequences, to be used on `stream` (None: the current one); calls that may run at the same time need one each."""
+    make = lambda: (torch.empty(lc_draft_workspace_bytes(batch), dtype=torch.uint8, device=device),)
+    return (make() if stream is None else _made_on(stream, make))[0]
+
+
+def _rows(t, batch, rows, vocab):
+    """Pitches of probabilities [batch][rows][vocab] whose rows are contiguous."""
+    assert t.is_cuda and t.dtype in SERVED and t.shape == (batch, rows, vocab) and (t.stride(2) == 1 or vocab == 1 or t.numel() == 0)
+    assert not t.requires_grad or not torch.is_grad_enabled(), _NO_GRADIENT
+    return t.data_ptr(), (t.stride(0) if batch > 1 else rows * vocab), (t.stride(1) if rows > 1 else vocab)
+
+
+def lc_draft_verify(target, tokens, uniform, draft=None, parent=None, count=None, out=None, ws=None, stream=None):
+    """Judges drafted tokens against the model's probabilities target [batch][nodes][vocab], those behind each node; tokens int32 [batch][nodes], of which node 0 is known.
+    draft [batch][nodes - 1][vocab]: what nodes 1, 2 ... were drawn from, one behind the other; without it they are guesses, below parent int32 [batch][nodes] (None:
+    below the one before).  count int32 [batch]: nodes that exist (None: all).  uniform float32 [batch][nodes] in [0, 1): for each node's judgement, and node 0's
+    for the token drawn behind the path.  Returns {"path": int32 [batch][nodes], node numbers and -1 behind them, "count": int32 [batch], how many, "next": int32
+    [batch], the token drawn}, in out = (path, count, next) if given.  ws: a tensor from new_draft_workspace (None: allocated for this call)."""
+    batch, nodes, vocab = target.shape
+    p, ldb, ldr = _rows(target, batch, nodes, vocab)
+    q, qldb, qldr = (None, 0, 0) if draft is None else _rows(draft, batch, nodes - 1, vocab)
+    assert draft is None or draft.dtype == target.dtype
+    for t, dtype in ((tokens, torch.int32), (uniform, torch.float32)) if parent is None else ((tokens, torch.int32), (uniform, torch.float32), (parent, torch.int32)):
+        assert t.is_cuda and t.dtype == dtype and t.shape == (batch, nodes) and t.is_contiguous()
+    if out is None:
+        make = lambda: (torch.empty(batch * (nodes + 2), dtype=torch.int32, device=target.device),)
+        few, = make() if stream is None else _made_on(stream, make)
+        path, length, following = few[:batch * nodes].view(batch, nodes), few[batch * nodes:batch * nodes + batch], few[batch * nodes + batch:]
+    else:
+        path, length, following = out
+        assert path.is_cuda and path.dtype == torch.int32 and path.shape == (batch, nodes) and path.is_contiguous()
+    if ws is None:
+        ws = new_draft_workspace(batch, target.device, stream)
+    assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
+    st = _lib.lc_draft_verify(p, ldb, ldr, batch, nodes, vocab, tokens.data_ptr(), q or None, qldb, qldr, None if parent is None else parent.data_ptr(),
+                              None if count is None else _counts(count, batch), uniform.data_ptr(), SERVED[target.dtype], path.data_ptr(), _counts(length, batch),
+                              _counts(following, batch), ws.data_ptr(), ws.numel(), _handle(stream))
+    if st != OK:
+        raise LcError(st)
+    return {"path": path, "count": length, "next": following}
