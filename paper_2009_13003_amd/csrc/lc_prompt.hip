@@ -12,12 +12,10 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 //   S^T = K Q^T   32 tokens by 32 rows by 16 elements an instruction: lane l gets row l % 32, tokens 8 (i / 4) + 4 (l / 32) + i % 4
 //   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens of each 16 in the order 0-3, 8-11, 4-7, 12-15,
 //                    in which V^T is kept
-// so that the running maximum and the sum are one number a lane.  Scales of keys multiply the scores.
-//   bf16: scales of values multiply the probabilities, whose product is rounded to bf16; codes are whole numbers, exact
-//   fp16: values are rounded to fp16 as they are converted, probabilities to fp16
-//   fp32: as bf16 with queries and probabilities in three parts
+// so that the running maximum and the sum are one number a lane.  Codes are whole numbers in 16 bits, exactly; scales of keys multiply the scores, scales of values the
+// probabilities, whose product is rounded: to bf16, in fp32 in three parts, and in fp16 measured from a power of two near the largest scale so far, so that products down to
+// 2^-24 of the largest have all of its 11 bits.
 constexpr int kWaves = 4, kRows = 32 * kWaves, kTile = 64;
-constexpr float kFar = 8.0f;                                // by how much, in powers of two, a score may pass what probabilities are measured from
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostSplits = 32;
 
@@ -36,10 +34,12 @@ struct Prompt {
     FastDiv by_group;
 };
 
-template <int T> struct Kind;       // how many 16-bit parts an element of q, and a probability, are given
-template <> struct Kind<LC_F32> { static constexpr int kParts = 3; static constexpr bool kHalf = false; };
-template <> struct Kind<LC_BF16> { static constexpr int kParts = 1; static constexpr bool kHalf = false; };
-template <> struct Kind<LC_F16> { static constexpr int kParts = 1; static constexpr bool kHalf = true; };
+// How many 16-bit parts an element of q, and a probability, are given, and by how much, in powers of two, a score may pass what probabilities are measured from (in fp16
+// they have room for 2^16, of which 2^11 are the scales').
+template <int T> struct Kind;
+template <> struct Kind<LC_F32> { static constexpr int kParts = 3; static constexpr bool kHalf = false; static constexpr float kFar = 8; };
+template <> struct Kind<LC_BF16> { static constexpr int kParts = 1; static constexpr bool kHalf = false; static constexpr float kFar = 8; };
+template <> struct Kind<LC_F16> { static constexpr int kParts = 1; static constexpr bool kHalf = true; static constexpr float kFar = 4; };
 
 template <bool HALF> __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     if (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -81,32 +81,33 @@ __device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t 
     return {0, 0, 0, 0};
 }
 
-template <int T, int BITS, int DP> struct Shape {
-    static constexpr int kUnits = (DP / 8 + 7) / 8 * 8;     // 16-byte units a row of K has room for
-    static constexpr int kRowBytes = DP * BITS / 8;
-    static constexpr int kChunks = kRowBytes / 16;          // pieces of 16 bytes of codes a token has
-    static constexpr int kKeyLoads = (kTile * kChunks + kWaves * 64 - 1) / (kWaves * 64);
-    static constexpr int kWords = kRowBytes / 4;            // and of 4 bytes
-    static constexpr int kValueItems = kTile / 4 * kWords, kValueLoads = (kValueItems + kWaves * 64 - 1) / (kWaves * 64);
+template <int BITS, int D> struct Shape {
+    static constexpr int kUnits = D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32;      // 16-byte units a row of K has room for
+    static constexpr int kRowBytes = D * BITS / 8;
+    static constexpr int kChunks = kRowBytes / 16, kKeyItems = kTile * kChunks;         // pieces of 16 bytes of codes
+    static constexpr int kWords = kRowBytes / 4, kValueItems = kTile / 4 * kWords;      // and of 4 bytes by 4 tokens
+    static constexpr int kKeyLoads = (kKeyItems + kWaves * 64 - 1) / (kWaves * 64), kValueLoads = (kValueItems + kWaves * 64 - 1) / (kWaves * 64);
 };
-// Where a row of V^T keeps a unit: turned by the row, so that neither the lanes that read a column of units nor those that write, whose rows are 4 (8 bits) or 8 (4
-// bits) apart, meet in one bank.
-template <int BITS> __device__ __forceinline__ uint32_t turned_unit(uint32_t d, uint32_t u) { return u ^ ((BITS == 8 ? d ^ d >> 2 : d ^ d >> 2 ^ d >> 3) & 7); }
+// Where in its row a unit is kept: sixteen lanes that read one column of units from rows that follow each other, and those that write it, have sixteen places in the 256
+// bytes that LDS gives at once.  Rows of V^T have eight units; lanes that write it are 4 (8 bits) or 8 (4 bits) rows apart.
+template <int UNITS> __device__ __forceinline__ uint32_t key_unit(uint32_t t, uint32_t u) { return u ^ (UNITS >= 16 ? t & 15 : UNITS == 8 ? t >> 1 & 7 : t >> 2 & 3); }
+__device__ __forceinline__ uint32_t value_unit(uint32_t d, uint32_t u) { return u ^ ((d >> 1 ^ (d >> 4 & 1)) & 7); }
 
-// Eight codes as numbers: 8 bits from two words, 4 bits from one.
 template <int BITS> __device__ __forceinline__ float code_of(uint32_t w, int e) {
     return BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : (float)((int)(w >> (4 * e) & 15u) - 8);
 }
 
-template <int T, int BITS, int DP, int PERSIMD>
+template <int T, int BITS, int D, int PERSIMD>
 __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
-    using S = Shape<T, BITS, DP>;
+    using S = Shape<BITS, D>;
     constexpr bool HALF = Kind<T>::kHalf;
-    constexpr int NP = Kind<T>::kParts, KS = DP / 16, DB = DP / 32;
+    constexpr int NP = Kind<T>::kParts, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(16))) uint16_t sk[2][kTile][S::kUnits * 8];
-    __shared__ __attribute__((aligned(16))) uint16_t sv[2][DP][kTile];
+    __shared__ __attribute__((aligned(16))) uint16_t sv[2][D][kTile];
     __shared__ __attribute__((aligned(16))) float sks[2][kTile], svs[2][kTile];
-    __shared__ uint32_t sbad[2][2];                         // the tile's tokens that are not there, or whose value is not finite (a half a wavefront)
+    __shared__ uint64_t srow[4][8];                         // where each eight tokens of a tile lie, counted in rows
+    __shared__ uint32_t snot[4];                            // which of them lie in pages that are not there
+    __shared__ int sunit[2];                                // fp16: probabilities times scales are counted in 2^sunit
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     const uint32_t head = blockIdx.x % a.c.heads;
     const Own own = own_of(a, blockIdx.x / a.c.heads, lane);
@@ -128,16 +129,16 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     const bool has_row = row < rows;
     const uint32_t rr = (uint32_t)(has_row ? row : rows - 1), qi = a.by_group(rr), qg = rr - qi * a.group;
     const int32_t place = has_row ? base + (int32_t)qi : -1;
-    const int32_t wave_first = place_of(row0 + 32 * (int32_t)wave < rows ? row0 + 32 * (int32_t)wave : rows - 1);
-    const int32_t wave_end = row0 + 32 * (int32_t)wave < rows ? place_of(row0 + 32 * (int32_t)wave + 31 < rows ? row0 + 32 * (int32_t)wave + 31 : rows - 1) : -1;
+    const int32_t wave_row = row0 + 32 * (int32_t)wave;     // the places of the wavefront's first and last rows
+    const int32_t wave_first = place_of(wave_row < rows ? wave_row : rows - 1);
+    const int32_t wave_end = wave_row < rows ? place_of(wave_row + 31 < rows ? wave_row + 31 : rows - 1) : -1;
     u32x4 q[KS][NP];
     {
-        const uint64_t at = (uint64_t)(own.first + qi) * a.ld_q + (uint64_t)(head * a.group + qg) * a.c.dim;
+        const uint64_t at = (uint64_t)(own.first + qi) * a.ld_q + (uint64_t)(head * a.group + qg) * D;
 #pragma unroll
         for (int o = 0; o < KS; ++o) {
-            const uint32_t d = 16 * o + 8 * h;
             float v[8];
-            load_eight<T>(a.q, at + d, has_row && d < a.c.dim ? 8 : 0, v);
+            load_eight<T>(a.q, at + 16 * o + 8 * h, has_row ? 8 : 0, v);
             // An infinity is taken as NaN: the score of whatever is seen is infinite or NaN, so the softmax of any set of them is NaN.
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += v[e] - v[e];
@@ -152,99 +153,96 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         }
     }
 
-    // A tile on its way: codes in registers, then converted into LDS.
+    // A tile on its way: the first eight lanes look up where it lies, a tile ahead; codes go to registers and, converted, into LDS.
     const int32_t* table = a.table + b * a.ld_table;
+    int32_t page_raw = 0;
+    auto look = [&](int32_t tile) {
+        if (threadIdx.x >= 8) return;
+        int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)threadIdx.x;
+        t = t < len ? t : (len - 1) & ~7;                   // (eight tokens that begin at a multiple of eight lie together)
+        page_raw = table[t >> a.c.page_shift];
+    };
+    auto place_eights = [&](int32_t tile) {
+        if (threadIdx.x >= 8) return;
+        int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)threadIdx.x;
+        t = t < len ? t : (len - 1) & ~7;
+        const bool there = (uint32_t)page_raw < (uint32_t)a.pages;
+        srow[tile % 4][threadIdx.x] = row_of(a.c, there ? page_raw : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
+        const unsigned long long missing = __ballot(!there);
+        if (threadIdx.x == 0) snot[tile % 4] = (uint32_t)missing;
+    };
     u32x4 keys[S::kKeyLoads];
     uint32_t values[S::kValueLoads][4];
-    float scale_raw = 0;
-    bool there_raw = true;
-    auto slot_row = [&](int32_t t, bool& there) -> uint64_t {       // the row of token t (held to the sequence) of this head
-        t = t < len ? t : len - 1;
-        const int32_t page = table[t >> a.c.page_shift];
-        there = (uint32_t)page < (uint32_t)a.pages;
-        return row_of(a.c, there ? page : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
-    };
+    float key_scale = 0, value_scale = 0;
     auto ask = [&](int32_t tile) {
-        const int32_t t0 = tile * kTile;
+        const uint64_t* eights = srow[tile % 4];
 #pragma unroll
         for (int l = 0; l < S::kKeyLoads; ++l) {
             const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
-            bool there;
-            keys[l] = u32x4{0, 0, 0, 0};
-            if (i < kTile * S::kChunks && ch * 16 < a.c.row_bytes)
-                keys[l] = *reinterpret_cast<const u32x4*>(a.c.k + slot_row(t0 + (int32_t)t, there) * a.c.row_bytes + ch * 16);
+            if (S::kKeyItems % (kWaves * 64) == 0 || i < (uint32_t)S::kKeyItems)
+                keys[l] = *reinterpret_cast<const u32x4*>(a.c.k + eights[t / 8] * S::kRowBytes + (t % 8 * S::kRowBytes + ch * 16));
         }
 #pragma unroll
         for (int l = 0; l < S::kValueLoads; ++l) {
             const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, w = i % S::kWords;
+            if (S::kValueItems % (kWaves * 64) == 0 || i < (uint32_t)S::kValueItems) {
+                const uint8_t* from = a.c.v + eights[t / 8] * S::kRowBytes + (t % 8 * S::kRowBytes + w * 4);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) values[l][r] = 0;
-            if (i < (uint32_t)S::kValueItems && w * 4 < a.c.row_bytes) {
-                // (four tokens that begin at a multiple of four lie together)
-                bool there;
-                const uint32_t first = (uint32_t)(t0 + (int32_t)t) < (uint32_t)len ? t0 + t : (uint32_t)(len - 1) & ~3u;
-                const uint8_t* from = a.c.v + slot_row((int32_t)first, there) * a.c.row_bytes + w * 4;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) values[l][r] = *reinterpret_cast<const uint32_t*>(from + r * a.c.row_bytes);
+                for (int r = 0; r < 4; ++r) values[l][r] = *reinterpret_cast<const uint32_t*>(from + r * S::kRowBytes);
             }
         }
-        if (threadIdx.x < 128) {
-            const int32_t t = t0 + (int32_t)(threadIdx.x % 64);
-            bool there;
-            const uint64_t at = slot_row(t, there);
-            there_raw = there && t < len;
-            scale_raw = threadIdx.x < 64 ? a.c.k_scale[at] : a.c.v_scale[at];
+        if (wave == 0) {
+            key_scale = a.c.k_scale[eights[lane / 8] + lane % 8];
+            value_scale = a.c.v_scale[eights[lane / 8] + lane % 8];
         }
     };
+    int unit = -1000;                                       // fp16: what this wavefront's sums are counted in; and for the first one the tiles so far
+    int unit_next = -1000;
     auto put = [&](uint32_t buffer) {
-        // scales first: values in fp16 are converted with theirs
-        if (threadIdx.x < 128) {
-            const uint32_t t = threadIdx.x % 64;
-            if (threadIdx.x < 64) sks[buffer][t] = scale_raw * a.scale;
-            else svs[buffer][t] = there_raw ? scale_raw : 0.0f;
-            const unsigned long long wrong = __ballot(!there_raw || (HALF && threadIdx.x >= 64 && !(scale_raw < __builtin_inff())));
-            if (threadIdx.x == 64) { sbad[buffer][0] = (uint32_t)wrong; sbad[buffer][1] = (uint32_t)(wrong >> 32); }
+        if (wave == 0) {
+            // A value that is not finite makes all of a result NaN: as well a key that is not does, and products with the values are left without it.
+            const uint32_t size = bits_of(value_scale) & 0x7fffffffu;
+            const bool finite = size < 0x7f800000u;
+            sks[buffer][lane] = finite ? key_scale * a.scale : __builtin_nanf("");
+            if (!finite) value_scale = 0;
+            if (HALF) {
+                uint32_t most = max_of_lanes<32>(finite ? size : 0);
+                { const uint32_t o = (uint32_t)__shfl_xor((int)most, 32); most = o > most ? o : most; }
+                int e = (int)(most >> 23) - 127 - 10;
+                e = e < -100 ? -100 : e;
+                unit_next = e > unit_next ? e : unit_next;
+                value_scale = ldexpf(value_scale, -unit_next);
+                if (lane == 0) sunit[buffer] = unit_next;
+            }
+            svs[buffer][lane] = value_scale;
         }
-        if (HALF) __syncthreads();
 #pragma unroll
         for (int l = 0; l < S::kKeyLoads; ++l) {
             const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
-            if (i >= kTile * S::kChunks) continue;
+            if (S::kKeyItems % (kWaves * 64) && i >= (uint32_t)S::kKeyItems) continue;
 #pragma unroll
             for (int u = 0; u < 16 / BITS; ++u) {           // units of eight codes
                 u32x4 v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float x, y;
-                    if (BITS == 8) { x = code_of<8>(keys[l][2 * u + j / 2], 2 * (j % 2)); y = code_of<8>(keys[l][2 * u + j / 2], 2 * (j % 2) + 1); }
-                    else { x = code_of<4>(keys[l][u], 2 * j); y = code_of<4>(keys[l][u], 2 * j + 1); }
-                    v[j] = pair_of<HALF>(x, y);
+                    uint32_t w = BITS == 8 ? keys[l][2 * u + j / 2] : keys[l][u];
+                    asm("" : "+v"(w));                      // (else codes are cut out one by one before they are converted)
+                    const int e = BITS == 8 ? 2 * (j % 2) : 2 * j;
+                    v[j] = pair_of<HALF>(code_of<BITS>(w, e), code_of<BITS>(w, e + 1));
                 }
-                const uint32_t unit = ch * (16 / BITS) + u;
-                *reinterpret_cast<u32x4*>(&sk[buffer][t][(unit ^ (t & 7)) * 8]) = v;
+                *reinterpret_cast<u32x4*>(&sk[buffer][t][key_unit<S::kUnits>(t, ch * (16 / BITS) + u) * 8]) = v;
             }
         }
 #pragma unroll
         for (int l = 0; l < S::kValueLoads; ++l) {
             const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, w = i % S::kWords;
-            if (i >= (uint32_t)S::kValueItems) continue;
-            f32x4 by = {1, 1, 1, 1};
-            if (HALF) {
-                by = *reinterpret_cast<const f32x4*>(&svs[buffer][t]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) by[r] = by[r] < __builtin_inff() ? by[r] : 0.0f;      // (NaN: the tokens are marked)
-            }
+            if (S::kValueItems % (kWaves * 64) && i >= (uint32_t)S::kValueItems) continue;
             const uint32_t group = t / 4 % 4, unit = t / 16 * 2 + group % 2, half = group / 2;      // tokens 0-3, 8-11, 4-7, 12-15
 #pragma unroll
             for (int e = 0; e < 32 / BITS; ++e) {
                 const uint32_t d = w * (32 / BITS) + e;
-                float x[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] = code_of<BITS>(values[l][r], e);
-                    if (HALF) x[r] = fminf(fmaxf(x[r] * by[r], -65504.0f), 65504.0f);
-                }
-                *reinterpret_cast<u32x2*>(&sv[buffer][d][turned_unit<BITS>(d, unit) * 8 + half * 4]) = u32x2{pair_of<HALF>(x[0], x[1]), pair_of<HALF>(x[2], x[3])};
+                *reinterpret_cast<u32x2*>(&sv[buffer][d][value_unit(d, unit) * 8 + half * 4]) =
+                    u32x2{pair_of<HALF>(code_of<BITS>(values[l][0], e), code_of<BITS>(values[l][1], e)), pair_of<HALF>(code_of<BITS>(values[l][2], e), code_of<BITS>(values[l][3], e))};
             }
         }
     };
@@ -256,126 +254,148 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         for (int e = 0; e < 16; ++e) acc[j][e] = 0;
     float top = -__builtin_inff(), from = 0, sum = 0;       // the largest score so far (or about that), what probabilities are measured from, their sum
 
+    // A tile: scores, what probabilities are measured from, probabilities, products with the values.
+    auto use = [&](int32_t tile, uint32_t buffer) {
+        const int32_t tb = tile * kTile;
+        uint32_t c = lane % 32;
+        asm("" : "+v"(c));                                  // (else the places in LDS are worked out once for all tiles, for which there are no registers)
+        f32x16 score[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) score[s][e] = 0;
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                const uint32_t t = 32 * s + c;
+                const u32x4 key = *reinterpret_cast<const u32x4*>(&sk[buffer][t][key_unit<S::kUnits>(t, 2 * o + h) * 8]);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) score[s] = mfma<HALF>(key, q[o][p], score[s]);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 ks = *reinterpret_cast<const f32x4*>(&sks[buffer][32 * s + 8 * g + 4 * h]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) score[s][4 * g + r] = fmaf(score[s][4 * g + r], ks[r], -from);
+            }
+        const uint32_t missing = __builtin_amdgcn_readfirstlane(snot[tile % 4]);
+        if (tb + kTile - 1 > wave_first || missing) {       // (else every row sees all of it)
+            asm volatile("");                               // (a branch, not 64 selections for every tile)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool hidden = tb + 32 * s + 8 * (e / 4) + (int32_t)(4 * h) + e % 4 > place || (missing >> (4 * s + e / 4) & 1);
+                    score[s][e] = hidden ? -__builtin_inff() : score[s][e];
+                }
+        }
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, score[s][e]);
+        if (HALF) {
+            const int next = __builtin_amdgcn_readfirstlane(sunit[buffer]);
+            if (next != unit) {
+                const float shrink = ldexpf(1.0f, unit - next);
+#pragma unroll
+                for (int j = 0; j < DB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
+                unit = next;
+            }
+        }
+        if (__any(most > Kind<T>::kFar || top == -__builtin_inff())) {
+            most = fmaxf(fmaxf(most, other_half(most)) + from, top);
+            const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - then);
+            sum *= shrink;
+#pragma unroll
+            for (int j = 0; j < DB; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) score[s][e] -= then - from;
+            top = most;
+            from = then;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {                   // 16 tokens at a time
+                u32x4 pp[NP];
+                float p[8];
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&svs[buffer][32 * s + 16 * o + 8 * g + 4 * h]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = __builtin_amdgcn_exp2f(score[s][8 * o + 4 * g + r]);
+                        sum += e;
+                        p[4 * g + r] = e * vs[r];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        pp[k][j] = k == NP - 1 ? pair_of<HALF>(p[2 * j], p[2 * j + 1]) : high_halves(bits_of(p[2 * j]), bits_of(p[2 * j + 1]));
+                    if (k < NP - 1)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
+                }
+#pragma unroll
+                for (int j = 0; j < DB; ++j) {
+                    const uint32_t d = 32 * j + c;
+                    const u32x4 value = *reinterpret_cast<const u32x4*>(&sv[buffer][d][value_unit(d, 4 * s + 2 * o + h) * 8]);
+#pragma unroll
+                    for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value, pp[k], acc[j]);
+                }
+            }
+    };
+
     if (tile0 < tile1) {
+        look(tile0);
+        place_eights(tile0);
+        look(tile0 + 1);
+        __syncthreads();
         ask(tile0);
+        place_eights(tile0 + 1);
         put(0);
     }
     uint32_t buffer = 0;
     for (int32_t tile = tile0; tile < tile1; ++tile, buffer ^= 1) {
         __syncthreads();
-        if (tile + 1 < tile1) ask(tile + 1);
-        const int32_t tb = tile * kTile;
-        if (tb <= wave_end) {
-            f32x16 score[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) score[s][e] = 0;
-#pragma unroll
-                for (int o = 0; o < KS; ++o) {
-                    const uint32_t t = 32 * s + c;
-                    const u32x4 key = *reinterpret_cast<const u32x4*>(&sk[buffer][t][((2 * o + h) ^ (t & 7)) * 8]);
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) score[s] = mfma<HALF>(key, q[o][p], score[s]);
-                }
-            }
-            const bool whole = tb + kTile - 1 <= wave_first && (sbad[buffer][0] | sbad[buffer][1]) == 0;
-            float most = -__builtin_inff();
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 ks = *reinterpret_cast<const f32x4*>(&sks[buffer][32 * s + 8 * g + 4 * h]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) score[s][4 * g + r] = fmaf(score[s][4 * g + r], ks[r], -from);
-                }
-            uint32_t hidden[2] = {0, 0};                    // of this lane's 16 tokens each
-            if (!whole) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int32_t t = 32 * s + 8 * (e / 4) + 4 * h + e % 4;
-                        const bool marked = sbad[buffer][s] >> (t & 31) & 1;
-                        const bool is_nan = HALF && marked && tb + t <= place && tb + t < len && !(svs[buffer][t] < __builtin_inff());
-                        if (tb + t > place || (marked && !is_nan)) { hidden[s] |= 1u << e; score[s][e] = -__builtin_inff(); }
-                        if (is_nan) score[s][e] = __builtin_nanf("");
-                    }
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) most = fmaxf(most, score[s][e]);
-            if (__any(most > kFar || top == -__builtin_inff())) {
-                most = fmaxf(fmaxf(most, other_half(most)) + from, top);
-                const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - then);
-                sum *= shrink;
-#pragma unroll
-                for (int j = 0; j < DB; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) score[s][e] -= then - from;
-                top = most;
-                from = then;
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) { score[s][e] = __builtin_amdgcn_exp2f(score[s][e]); sum += score[s][e]; }
-                if (!HALF) {
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 vs = *reinterpret_cast<const f32x4*>(&svs[buffer][32 * s + 8 * g + 4 * h]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) score[s][4 * g + r] *= !whole && (hidden[s] >> (4 * g + r) & 1) ? 0.0f : vs[r];
-                    }
-                }
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {               // 16 tokens at a time
-                    u32x4 pp[NP];
-                    float p[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = score[s][8 * o + e];
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            pp[k][j] = k == NP - 1 ? pair_of<HALF>(p[2 * j], p[2 * j + 1]) : high_halves(bits_of(p[2 * j]), bits_of(p[2 * j + 1]));
-                        if (k < NP - 1)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
-                    }
-#pragma unroll
-                    for (int j = 0; j < DB; ++j) {
-                        const uint32_t d = 32 * j + c;
-                        const u32x4 value = *reinterpret_cast<const u32x4*>(&sv[buffer][d][turned_unit<BITS>(d, 4 * s + 2 * o + h) * 8]);
-#pragma unroll
-                        for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value, pp[k], acc[j]);
-                    }
-                }
-            }
+        if (tile + 1 < tile1) {
+            ask(tile + 1);
+            look(tile + 2);
         }
-        if (tile + 1 < tile1) put(buffer ^ 1);
+        if (tile * kTile <= wave_end) use(tile, buffer);
+        if (tile + 1 < tile1) {
+            put(buffer ^ 1);
+            place_eights(tile + 2);
+        }
     }
 
     const float total = sum + other_half(sum);
     if (!has_row) return;
     const uint64_t at = (uint64_t)(own.first + qi), hd = head * a.group + qg;
-    const float whole = a.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+    float whole = a.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+    if (HALF) whole = total == 0.0f ? 0.0f : ldexpf(whole, unit);
     if (a.splits > 1) {
         const uint64_t place_at = ((uint64_t)blockIdx.y * a.tokens + at) * a.heads + hd;
         if (h == 0) { a.stats[2 * place_at] = top; a.stats[2 * place_at + 1] = total; }
         if (total == 0.0f) return;
-        float* to = a.part + place_at * a.c.dim;
+        float* to = a.part + place_at * D;
 #pragma unroll
         for (int j = 0; j < DB; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const uint32_t d = 32 * j + 8 * g + 4 * h;
-                if (d < a.c.dim) *reinterpret_cast<f32x4*>(to + d) = f32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+                f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+                *reinterpret_cast<f32x4*>(to + 32 * j + 8 * g + 4 * h) = v * whole;
             }
         return;
     }
@@ -383,10 +403,10 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     for (int j = 0; j < DB; ++j)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const uint32_t d = 32 * j + 8 * g + 4 * h;
-            f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
-            v *= whole;
-            if (d < a.c.dim) store_four<T>(a.out, at * a.ld_out + hd * a.c.dim + d, v);
+            const f32x4 v = f32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]} * whole;
+            const uint64_t to = at * a.ld_out + hd * D + 32 * j + 8 * g + 4 * h;
+            if (T == LC_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to) = v;
+            else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to) = u32x2{pair_of<HALF>(v[0], v[1]), pair_of<HALF>(v[2], v[3])};
         }
 }
 
@@ -427,20 +447,27 @@ uint32_t splits_of(uint64_t blocks, uint32_t kv_heads) {
     return (uint32_t)(s < kMostSplits ? s : kMostSplits);
 }
 
-template <int T, int BITS, int DP>
+template <int T, int BITS, int D>
 void prompt_of(const Prompt& a, uint32_t blocks, hipStream_t s) {
-    constexpr int PERSIMD = T == LC_F32 || DP > 128 ? 1 : 2;
-    k_kv_prompt<T, BITS, DP, PERSIMD><<<dim3(blocks * a.c.heads, a.splits), kWaves * 64, 0, s>>>(a);
+    constexpr int PERSIMD = T == LC_F32 || D > 128 ? 1 : 2;
+    k_kv_prompt<T, BITS, D, PERSIMD><<<dim3(blocks * a.c.heads, a.splits), kWaves * 64, 0, s>>>(a);
+}
+template <int T, int BITS>
+void prompt(const Prompt& a, uint32_t blocks, hipStream_t s) {
+    switch (a.c.dim) {
+        case 32: prompt_of<T, BITS, 32>(a, blocks, s); break;
+        case 64: prompt_of<T, BITS, 64>(a, blocks, s); break;
+        case 96: prompt_of<T, BITS, 96>(a, blocks, s); break;
+        case 128: prompt_of<T, BITS, 128>(a, blocks, s); break;
+        case 160: prompt_of<T, BITS, 160>(a, blocks, s); break;
+        case 192: prompt_of<T, BITS, 192>(a, blocks, s); break;
+        case 224: prompt_of<T, BITS, 224>(a, blocks, s); break;
+        default: prompt_of<T, BITS, 256>(a, blocks, s); break;
+    }
     if (a.splits > 1) {
         const uint32_t quads = a.c.dim / 4, lanes = a.tokens * a.heads * quads;
         k_kv_prompt_join<T><<<(lanes + 255) / 256, 256, 0, s>>>(a, lanes, FastDiv(quads), FastDiv(a.heads));
     }
-}
-template <int T, int BITS>
-void prompt(const Prompt& a, uint32_t blocks, hipStream_t s) {
-    if (a.c.dim <= 64) prompt_of<T, BITS, 64>(a, blocks, s);
-    else if (a.c.dim <= 128) prompt_of<T, BITS, 128>(a, blocks, s);
-    else prompt_of<T, BITS, 256>(a, blocks, s);
 }
 
 }  // namespace

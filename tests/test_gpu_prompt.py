@@ -47,7 +47,7 @@ def want_of(lc, cache, q, starts, table, lens, scale=None):
       scores      q . k of dim terms added up in 32 bits in steps of 16, then scale and key's scale: (dim / 16 + 16 + 4) half steps of |q| . |k| times both at most;
                   exp2 and what scores are measured from: 4 half steps of the score and 4 more; both the numerator's and the sum's
       products    sums over n tokens in steps of 16, joined: n / 16 + 64 half steps of the sum of p |v|
-      roundings   of p times the value's scale to bf16 (2^-8), of p and v to fp16 (2^-11 each, and 2^-25 of every |v| for p and 2^-25 for v), of three parts 2^-24
+      roundings   of p times the value's scale to bf16 (2^-8), to fp16 (2^-11, and 2^-35 of the largest so far), in three parts 2^-23
       the result  half a step of its type, and of its smallest numbers"""
     dtype, (_, heads, dim), g = q.dtype, q.shape, q.shape[1] // cache.heads
     out, room = torch.zeros(q.shape, dtype=torch.float64, device=DEV), torch.zeros(q.shape, dtype=torch.float64, device=DEV)
@@ -74,10 +74,10 @@ def want_of(lc, cache, q, starts, table, lens, scale=None):
             size = ((x.abs() @ kk.abs().T) * abs(scale)).masked_fill(~seen, 0.0)
             far = 2 * ((dim / 16 + 20) * size.amax(1) + 4 * score.abs().nan_to_num(0.0, 0.0, 0.0).amax(1) + 4) * eps
             carried = p.nan_to_num(0.0) @ vv.abs().nan_to_num(0.0)
-            each = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -10}[dtype]
+            each = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[dtype]
             r = carried * (far[:, None] + (n / 16 + 64) * eps + each) * 1.01
-            if dtype == torch.float16:
-                r = r + 2.0 ** -25 * (seen.double() @ vv.abs().nan_to_num(0.0)) + 2.0 ** -25
+            if dtype == torch.float16:                       # (codes of 127 at most; a row's tiles reach 63 tokens beyond it)
+                r = r + seen.sum(1, keepdim=True) * 2.0 ** -35 * 16 * vv.abs().nan_to_num(0.0).max() + 2.0 ** -25
             out[first:first + count, h] = o
             room[first:first + count, h] = r + HALF[dtype] * 1.01 * o.abs().nan_to_num(0.0) + (2.0 ** -25 if dtype == torch.float16 else 2.0 ** -133)
     return out, room
@@ -190,14 +190,43 @@ def test_values_of_unlike_sizes(lc, dtype):
 
 
 def test_values_beyond_fp16(lc):
-    """In fp16 values count as 65504 at most."""
+    """In fp16 only results have to fit."""
     cache = lc.new_kv_cache(1, 1, 8, 32, 8)
     v = torch.full((2, 1, 32), 1e5, device=DEV)
     v[1] = -3e4
     lc.lc_kv_write(cache, torch.zeros_like(v), v, torch.tensor([0, 1], device=DEV))
     q = torch.zeros(2, 1, 32, dtype=torch.float16, device=DEV)
     got = lc.lc_kv_attend_prompt(cache, q, ints([0, 2]), ints([[0]]), ints([2])).float()
-    assert (got[0] == 65504).all() and ((got[1] - (65504 - 3e4) / 2).abs() <= 16).all()
+    assert (got[0] == float("inf")).all() and ((got[1] - 3.5e4).abs() <= 16 + (1e5 + 3e4) / 2 * 2.0 ** -11).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("step", [-3, 3])
+def test_values_that_grow_and_shrink(lc, dtype, step):
+    """Scales of values by 2^3 a tile up or down, to 2^45; with an even probability over all, and one that follows the small ones: each row's result within its
+    type's roundings of the values that carry it."""
+    n = 960
+    cache, table = filled(lc, 14, [n], 1, 64, 8, 16)
+    g = torch.Generator(DEV).manual_seed(3)
+    slots = torch.tensor([int(table[0, t // 16]) * 16 + t % 16 for t in range(n)], device=DEV)
+    k, v = (torch.randn(n, 1, 64, device=DEV, generator=g) for _ in range(2))
+    power = torch.arange(n, device=DEV) // 64 * step
+    lc.lc_kv_write(cache, 0.1 * k, v * torch.exp2(power.float() - (0 if step < 0 else 45))[:, None, None], slots)
+    q = torch.randn(n, 2, 64, device=DEV, generator=g).to(dtype)
+    check(lc.lc_kv_attend_prompt(cache, q, ints([0, n]), table, ints([n])), *want_of(lc, cache, q, [0, n], table, [n]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_of_zero(lc, dtype):
+    """Vectors of zeros, whose scale is zero, count in the sum of probabilities: first alone, then among others."""
+    cache, table = filled(lc, 15, [200], 1, 64, 8, 16)
+    slots = torch.tensor([int(table[0, t // 16]) * 16 + t % 16 for t in range(200)], device=DEV)
+    k, v = (torch.randn(200, 1, 64, device=DEV) for _ in range(2))
+    v[:100], k[30:60] = 0, 0
+    v[::3] = 0
+    lc.lc_kv_write(cache, k, v, slots)
+    q = torch.randn(200, 1, 64, device=DEV).to(dtype)
+    check(lc.lc_kv_attend_prompt(cache, q, ints([0, 200]), table, ints([200])), *want_of(lc, cache, q, [0, 200], table, [200]))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
