@@ -15,7 +15,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // so that the running maximum and the sum are one number a lane.  Codes are whole numbers in 16 bits, exactly; scales of keys multiply the scores, scales of values the
 // probabilities, whose product is rounded: to bf16, in fp32 in three parts, and in fp16 measured from a power of two near the largest scale so far, so that products down to
 // 2^-24 of the largest have all of its 11 bits.
-constexpr int kWaves = 4, kRows = 32 * kWaves, kTile = 64;
+constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostSplits = 32;
 
@@ -61,12 +61,12 @@ __device__ __forceinline__ int32_t held(int32_t v, int32_t lo, int32_t hi) { ret
 
 // Which rows of which sequence a workgroup has: blocks of rows are counted over all sequences.
 struct Own { uint32_t b; int32_t first, count, block; };    // the sequence's first new token and how many it has; the block of rows within it
-__device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t lane) {
+__device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t lane, uint32_t rows) {
     uint32_t before = 0;
     for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
         const uint32_t b = b0 + lane;
         const int32_t s = held(b < a.batch ? a.starts[b] : 0, 0, (int32_t)a.tokens), e = held(b < a.batch ? a.starts[b + 1] : 0, 0, (int32_t)a.tokens);
-        const uint32_t own = e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + kRows - 1) / kRows) : 0;
+        const uint32_t own = e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + rows - 1) / rows) : 0;
         uint32_t upto = own;
         for (int x = 1; x < 64; x *= 2) { const uint32_t o = __shfl_up(upto, x); if (lane >= (uint32_t)x) upto += o; }
         const unsigned long long mine = __ballot(before + upto > block && before + upto - own <= block);
@@ -81,7 +81,7 @@ __device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t 
     return {0, 0, 0, 0};
 }
 
-template <int BITS, int D> struct Shape {
+template <int BITS, int D, int kWaves> struct Shape {
     static constexpr int kUnits = D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32;      // 16-byte units a row of K has room for
     static constexpr int kRowBytes = D * BITS / 8;
     static constexpr int kChunks = kRowBytes / 16, kKeyItems = kTile * kChunks;         // pieces of 16 bytes of codes
@@ -97,9 +97,16 @@ template <int BITS> __device__ __forceinline__ float code_of(uint32_t w, int e) 
     return BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : (float)((int)(w >> (4 * e) & 15u) - 8);
 }
 
-template <int T, int BITS, int D, int PERSIMD>
+// f(Number<0>), f(Number<1>) ... of N.
+template <int I> struct Number { static constexpr int value = I; };
+template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F&& f) {
+    if constexpr (I < N) { f(Number<I>{}); each<N, I + 1>(f); }
+}
+
+template <int T, int BITS, int D, int kWaves, int PERSIMD>
 __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
-    using S = Shape<BITS, D>;
+    using S = Shape<BITS, D, kWaves>;
+    constexpr int kRows = 32 * kWaves;
     constexpr bool HALF = Kind<T>::kHalf;
     constexpr int NP = Kind<T>::kParts, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(16))) uint16_t sk[2][kTile][S::kUnits * 8];
@@ -110,7 +117,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     __shared__ int sunit[2];                                // fp16: probabilities times scales are counted in 2^sunit
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     const uint32_t head = blockIdx.x % a.c.heads;
-    const Own own = own_of(a, blockIdx.x / a.c.heads, lane);
+    const Own own = own_of(a, blockIdx.x / a.c.heads, lane, kRows);
     if (own.count == 0) return;
     const uint32_t b = own.b;
     const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
@@ -132,24 +139,37 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     const int32_t wave_row = row0 + 32 * (int32_t)wave;     // the places of the wavefront's first and last rows
     const int32_t wave_first = place_of(wave_row < rows ? wave_row : rows - 1);
     const int32_t wave_end = wave_row < rows ? place_of(wave_row + 31 < rows ? wave_row + 31 : rows - 1) : -1;
+    const int32_t wave_tiles = __builtin_amdgcn_readfirstlane(wave_end < 0 ? 0 : wave_end / kTile + 1 < tile1 ? wave_end / kTile + 1 : tile1);     // those that any of them sees
     u32x4 q[KS][NP];
     {
         const uint64_t at = (uint64_t)(own.first + qi) * a.ld_q + (uint64_t)(head * a.group + qg) * D;
+        // An infinity is taken as NaN: the score of whatever is seen is infinite or NaN, so the softmax of any set of them is NaN.
+        if constexpr (T == LC_F32) {
 #pragma unroll
-        for (int o = 0; o < KS; ++o) {
-            float v[8];
-            load_eight<T>(a.q, at + 16 * o + 8 * h, has_row ? 8 : 0, v);
-            // An infinity is taken as NaN: the score of whatever is seen is infinite or NaN, so the softmax of any set of them is NaN.
+            for (int o = 0; o < KS; ++o) {
+                float v[8];
+                load_eight<T>(a.q, at + 16 * o + 8 * h, has_row ? 8 : 0, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += v[e] - v[e];
+                for (int e = 0; e < 8; ++e) v[e] += v[e] - v[e];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
+                for (int p = 0; p < NP; ++p) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q[o][p][j] = HALF ? f16_of(v[2 * j]) | f16_of(v[2 * j + 1]) << 16 : high_halves(bits_of(v[2 * j]), bits_of(v[2 * j + 1]));
-                if (NP > 1)
+                    for (int j = 0; j < 4; ++j) q[o][p][j] = high_halves(bits_of(v[2 * j]), bits_of(v[2 * j + 1]));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] -= float_of(bits_of(v[e]) & 0xffff0000u);
+                }
+                __builtin_amdgcn_sched_barrier(0);          // (else all of q is there three times over)
             }
+        } else {
+            constexpr uint32_t kTop = HALF ? 0x7c00u : 0x7f80u;     // the exponent of what is not finite
+            bool wrong = false;
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                q[o][0] = has_row ? load_once<u32x4>(static_cast<const uint16_t*>(a.q) + at + 16 * o + 8 * h) : u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) wrong |= (q[o][0][j] & kTop) == kTop || (q[o][0][j] & kTop << 16) == kTop << 16;
+            }
+            if (wrong) q[0][0][0] = 0x7fff7fffu;
         }
     }
 
@@ -198,7 +218,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     };
     int unit = -1000;                                       // fp16: what this wavefront's sums are counted in; and for the first one the tiles so far
     int unit_next = -1000;
-    auto put = [&](uint32_t buffer) {
+    auto put_scales = [&](uint32_t buffer) {
         if (wave == 0) {
             // A value that is not finite makes all of a result NaN: as well a key that is not does, and products with the values are left without it.
             const uint32_t size = bits_of(value_scale) & 0x7fffffffu;
@@ -216,36 +236,48 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             }
             svs[buffer][lane] = value_scale;
         }
+    };
+    // The conversions of a lane, by pieces: eight codes of a key, or one element of four tokens' values.  Where they go in LDS: a place a load, turned by the piece (units of
+    // a row and rows of V^T follow each other in powers of two, so turning and counting do not meet).
+    constexpr int kKeyPieces = S::kKeyLoads * (16 / BITS), kPieces = kKeyPieces + S::kValueLoads * (32 / BITS);
+    uint32_t key_to[S::kKeyLoads], value_to[S::kValueLoads];
 #pragma unroll
-        for (int l = 0; l < S::kKeyLoads; ++l) {
-            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
-            if (S::kKeyItems % (kWaves * 64) && i >= (uint32_t)S::kKeyItems) continue;
+    for (int l = 0; l < S::kKeyLoads; ++l) {
+        const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kChunks, ch = i % S::kChunks;
+        key_to[l] = t * S::kUnits * 16 + key_unit<S::kUnits>(t, ch * (16 / BITS)) * 16;
+    }
 #pragma unroll
-            for (int u = 0; u < 16 / BITS; ++u) {           // units of eight codes
-                u32x4 v;
+    for (int l = 0; l < S::kValueLoads; ++l) {
+        const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, d = i % S::kWords * (32 / BITS);
+        const uint32_t group = t / 4 % 4, unit = t / 16 * 2 + group % 2, half = group / 2;      // tokens 0-3, 8-11, 4-7, 12-15
+        value_to[l] = d * kTile * 2 + value_unit(d, unit) * 16 + half * 8;
+    }
+    auto put = [&](uint32_t buffer, auto piece_of) {
+        constexpr int piece = decltype(piece_of)::value;
+        if constexpr (piece < kKeyPieces) {
+            constexpr int l = piece / (16 / BITS), u = piece % (16 / BITS);
+            if (S::kKeyItems % (kWaves * 64) && l * kWaves * 64 + threadIdx.x >= (uint32_t)S::kKeyItems) return;
+            u32x4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t w = BITS == 8 ? keys[l][2 * u + j / 2] : keys[l][u];
-                    asm("" : "+v"(w));                      // (else codes are cut out one by one before they are converted)
-                    const int e = BITS == 8 ? 2 * (j % 2) : 2 * j;
-                    v[j] = pair_of<HALF>(code_of<BITS>(w, e), code_of<BITS>(w, e + 1));
-                }
-                *reinterpret_cast<u32x4*>(&sk[buffer][t][key_unit<S::kUnits>(t, ch * (16 / BITS) + u) * 8]) = v;
+            for (int j = 0; j < 4; ++j) {
+                uint32_t w = BITS == 8 ? keys[l][2 * u + j / 2] : keys[l][u];
+                asm("" : "+v"(w));                          // (else codes are cut out one by one before they are converted)
+                const int e = BITS == 8 ? 2 * (j % 2) : 2 * j;
+                v[j] = pair_of<HALF>(code_of<BITS>(w, e), code_of<BITS>(w, e + 1));
             }
-        }
-#pragma unroll
-        for (int l = 0; l < S::kValueLoads; ++l) {
-            const uint32_t i = l * kWaves * 64 + threadIdx.x, t = i / S::kWords * 4, w = i % S::kWords;
-            if (S::kValueItems % (kWaves * 64) && i >= (uint32_t)S::kValueItems) continue;
-            const uint32_t group = t / 4 % 4, unit = t / 16 * 2 + group % 2, half = group / 2;      // tokens 0-3, 8-11, 4-7, 12-15
-#pragma unroll
-            for (int e = 0; e < 32 / BITS; ++e) {
-                const uint32_t d = w * (32 / BITS) + e;
-                *reinterpret_cast<u32x2*>(&sv[buffer][d][value_unit(d, unit) * 8 + half * 4]) =
-                    u32x2{pair_of<HALF>(code_of<BITS>(values[l][0], e), code_of<BITS>(values[l][1], e)), pair_of<HALF>(code_of<BITS>(values[l][2], e), code_of<BITS>(values[l][3], e))};
-            }
+            uint32_t to = key_to[l];
+            asm("" : "+v"(to));                             // (... and places worked out for every piece before the first tile, for which there are no registers)
+            *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(sk[buffer]) + (to ^ (u * 16))) = v;
+        } else {
+            constexpr int l = (piece - kKeyPieces) / (32 / BITS), e = (piece - kKeyPieces) % (32 / BITS);
+            if (S::kValueItems % (kWaves * 64) && l * kWaves * 64 + threadIdx.x >= (uint32_t)S::kValueItems) return;
+            uint32_t to = value_to[l];
+            asm("" : "+v"(to));
+            *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) =
+                u32x2{pair_of<HALF>(code_of<BITS>(values[l][0], e), code_of<BITS>(values[l][1], e)), pair_of<HALF>(code_of<BITS>(values[l][2], e), code_of<BITS>(values[l][3], e))};
         }
     };
+    auto put_all = [&](uint32_t buffer) { each<kPieces>([&](auto piece) { put(buffer, piece); }); };
 
     f32x16 acc[DB];
 #pragma unroll
@@ -255,23 +287,32 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     float top = -__builtin_inff(), from = 0, sum = 0;       // the largest score so far (or about that), what probabilities are measured from, their sum
 
     // A tile: scores, what probabilities are measured from, probabilities, products with the values.
-    auto use = [&](int32_t tile, uint32_t buffer) {
+    auto use = [&](int32_t tile, uint32_t buffer) {         // (and, beside the scores, puts the next one in its place)
         const int32_t tb = tile * kTile;
-        uint32_t c = lane % 32;
-        asm("" : "+v"(c));                                  // (else the places in LDS are worked out once for all tiles, for which there are no registers)
+        // Scores: keys are read four products ahead, and between those the next tile is converted.  (What is written here one after the other stays so: left to
+        // itself the compiler reads each key right before its product, and the matrix unit waits.)
         f32x16 score[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 16; ++e) score[s][e] = 0;
+        uint32_t key_from = c * S::kUnits * 16 + key_unit<S::kUnits>(c, h) * 16 + buffer * (uint32_t)sizeof(sk[0]);
+        asm("" : "+v"(key_from));
+        auto key_at = [&](int i) {
+            return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sk) + (key_from ^ (i % KS * 32)) + i / KS * 32 * S::kUnits * 16);
+        };
+        u32x4 key[4];
 #pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                const uint32_t t = 32 * s + c;
-                const u32x4 key = *reinterpret_cast<const u32x4*>(&sk[buffer][t][key_unit<S::kUnits>(t, 2 * o + h) * 8]);
+        for (int i = 0; i < 4; ++i) key[i] = key_at(i);
+        each<2 * KS>([&](auto step) {
+            constexpr int i = decltype(step)::value;
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p) score[s] = mfma<HALF>(key, q[o][p], score[s]);
-            }
-        }
+            for (int p = NP - 1; p >= 0; --p) score[i / KS] = mfma<HALF>(key[i % 4], q[i % KS][p], score[i / KS]);
+            if constexpr (i + 4 < 2 * KS) key[i % 4] = key_at(i + 4);
+            each<(i + 1) * kPieces / (2 * KS) - i * kPieces / (2 * KS)>([&](auto n) { put(buffer ^ 1, Number<i * kPieces / (2 * KS) + decltype(n)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        ask(tile + 2);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -322,62 +363,82 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             top = most;
             from = then;
         }
+        // Products with the values, 16 tokens at a time: those of the next 16 are read, and their probabilities worked out, between them.
+        uint32_t value_from = c * kTile * 2 + value_unit(c, h) * 16 + buffer * (uint32_t)sizeof(sv[0]);
+        asm("" : "+v"(value_from));
+        auto value_at = [&](int g, int j) { return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sv) + (value_from ^ (g * 32)) + j * 32 * kTile * 2); };
+        u32x4 value[DB], pp[2][NP];
+        f32x4 vs[2][2];
+        auto scales_at = [&](int g) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+            for (int x = 0; x < 2; ++x) vs[g % 2][x] = *reinterpret_cast<const f32x4*>(&svs[buffer][16 * g + 8 * x + 4 * h]);
+        };
+        auto probability = [&](int g, int pair) {           // two of the lane's eight
+            float p[2];
 #pragma unroll
-            for (int o = 0; o < 2; ++o) {                   // 16 tokens at a time
-                u32x4 pp[NP];
-                float p[8];
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&svs[buffer][32 * s + 16 * o + 8 * g + 4 * h]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float e = __builtin_amdgcn_exp2f(score[s][8 * o + 4 * g + r]);
-                        sum += e;
-                        p[4 * g + r] = e * vs[r];
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        pp[k][j] = k == NP - 1 ? pair_of<HALF>(p[2 * j], p[2 * j + 1]) : high_halves(bits_of(p[2 * j]), bits_of(p[2 * j + 1]));
-                    if (k < NP - 1)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] -= float_of(bits_of(p[e]) & 0xffff0000u);
-                }
-#pragma unroll
-                for (int j = 0; j < DB; ++j) {
-                    const uint32_t d = 32 * j + c;
-                    const u32x4 value = *reinterpret_cast<const u32x4*>(&sv[buffer][d][value_unit(d, 4 * s + 2 * o + h) * 8]);
-#pragma unroll
-                    for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value, pp[k], acc[j]);
-                }
+            for (int x = 0; x < 2; ++x) {
+                const int e = 2 * pair + x;
+                p[x] = __builtin_amdgcn_exp2f(score[g / 2][8 * (g % 2) + e]);
+                sum += p[x];
+                p[x] *= vs[g % 2][e / 4][e % 4];
             }
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                pp[g % 2][k][pair] = k == NP - 1 ? pair_of<HALF>(p[0], p[1]) : high_halves(bits_of(p[0]), bits_of(p[1]));
+                if (k < NP - 1)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) p[x] -= float_of(bits_of(p[x]) & 0xffff0000u);
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < DB; ++j) value[j] = value_at(0, j);
+        scales_at(0);
+#pragma unroll
+        for (int pair = 0; pair < 4; ++pair) probability(0, pair);
+        each<4>([&](auto group) {
+            constexpr int g = decltype(group)::value;
+            if constexpr (g < 3) scales_at(g + 1);
+            each<DB>([&](auto block) {
+                constexpr int j = decltype(block)::value;
+#pragma unroll
+                for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value[j], pp[g % 2][k], acc[j]);
+                if constexpr (g < 3) {
+                    value[j] = value_at(g + 1, j);
+                    each<(j + 1) * 4 / DB - j * 4 / DB>([&](auto n) { probability(g + 1, j * 4 / DB + decltype(n)::value); });
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
     };
 
+    // (Behind the last tile it is asked for once more, into a buffer that nothing reads.)
     if (tile0 < tile1) {
-        look(tile0);
-        place_eights(tile0);
-        look(tile0 + 1);
+        for (int i = 0; i < 3; ++i) {
+            look(tile0 + i);
+            place_eights(tile0 + i);
+        }
         __syncthreads();
         ask(tile0);
-        place_eights(tile0 + 1);
-        put(0);
+        put_scales(0);
+        put_all(0);
+        ask(tile0 + 1);
     }
     uint32_t buffer = 0;
-    for (int32_t tile = tile0; tile < tile1; ++tile, buffer ^= 1) {
+    int32_t tile = tile0;
+    for (; tile < wave_tiles; ++tile, buffer ^= 1) {
         __syncthreads();
-        if (tile + 1 < tile1) {
-            ask(tile + 1);
-            look(tile + 2);
-        }
-        if (tile * kTile <= wave_end) use(tile, buffer);
-        if (tile + 1 < tile1) {
-            put(buffer ^ 1);
-            place_eights(tile + 2);
-        }
+        look(tile + 3);
+        put_scales(buffer ^ 1);
+        use(tile, buffer);
+        place_eights(tile + 3);
+    }
+    for (; tile < tile1; ++tile, buffer ^= 1) {             // (what only other wavefronts' rows see; they meet as often in this loop as in the one above)
+        __syncthreads();
+        look(tile + 3);
+        put_scales(buffer ^ 1);
+        put_all(buffer ^ 1);
+        ask(tile + 2);
+        place_eights(tile + 3);
     }
 
     const float total = sum + other_half(sum);
@@ -436,33 +497,36 @@ __global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t lanes
 }
 
 // Row blocks at most, and into how many parts their tokens are split so that the chip is full.
-uint32_t blocks_of(uint64_t tokens, uint64_t batch, uint32_t group) {
-    const uint64_t most = tokens < batch ? tokens : batch;  // sequences with new tokens
-    return (uint32_t)((tokens * group + kRows - 1) / kRows + most);
-}
-uint32_t splits_of(uint64_t blocks, uint32_t kv_heads) {
-    const uint64_t have = blocks * kv_heads;
-    if (have >= 512) return 1;
-    const uint64_t s = 512 / have;
-    return (uint32_t)(s < kMostSplits ? s : kMostSplits);
+struct Split { uint32_t waves, blocks, splits; };
+bool eight_fit(int dtype, uint32_t dim) { return dtype != LC_F32 && dim <= 128; }        // two wavefronts a SIMD have the registers
+Split split_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads, bool eight) {
+    const uint64_t sequences = tokens < batch ? tokens : batch;      // those with new tokens
+    Split s;
+    s.waves = eight && tokens * group / 256 * kv_heads >= 256 ? 8 : 4;
+    s.blocks = (uint32_t)((tokens * group + 32 * s.waves - 1) / (32 * s.waves) + sequences);
+    const uint64_t have = (uint64_t)s.blocks * kv_heads, want = have >= 512 ? 1 : 512 / have;
+    s.splits = (uint32_t)(want < kMostSplits ? want : kMostSplits);
+    return s;
 }
 
 template <int T, int BITS, int D>
-void prompt_of(const Prompt& a, uint32_t blocks, hipStream_t s) {
+void prompt_of(const Prompt& a, const Split& to, hipStream_t s) {
     constexpr int PERSIMD = T == LC_F32 || D > 128 ? 1 : 2;
-    k_kv_prompt<T, BITS, D, PERSIMD><<<dim3(blocks * a.c.heads, a.splits), kWaves * 64, 0, s>>>(a);
+    if constexpr (T != LC_F32 && D <= 128)
+        if (to.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<dim3(to.blocks * a.c.heads, a.splits), 512, 0, s>>>(a); return; }
+    k_kv_prompt<T, BITS, D, 4, PERSIMD><<<dim3(to.blocks * a.c.heads, a.splits), 256, 0, s>>>(a);
 }
 template <int T, int BITS>
-void prompt(const Prompt& a, uint32_t blocks, hipStream_t s) {
+void prompt(const Prompt& a, const Split& to, hipStream_t s) {
     switch (a.c.dim) {
-        case 32: prompt_of<T, BITS, 32>(a, blocks, s); break;
-        case 64: prompt_of<T, BITS, 64>(a, blocks, s); break;
-        case 96: prompt_of<T, BITS, 96>(a, blocks, s); break;
-        case 128: prompt_of<T, BITS, 128>(a, blocks, s); break;
-        case 160: prompt_of<T, BITS, 160>(a, blocks, s); break;
-        case 192: prompt_of<T, BITS, 192>(a, blocks, s); break;
-        case 224: prompt_of<T, BITS, 224>(a, blocks, s); break;
-        default: prompt_of<T, BITS, 256>(a, blocks, s); break;
+        case 32: prompt_of<T, BITS, 32>(a, to, s); break;
+        case 64: prompt_of<T, BITS, 64>(a, to, s); break;
+        case 96: prompt_of<T, BITS, 96>(a, to, s); break;
+        case 128: prompt_of<T, BITS, 128>(a, to, s); break;
+        case 160: prompt_of<T, BITS, 160>(a, to, s); break;
+        case 192: prompt_of<T, BITS, 192>(a, to, s); break;
+        case 224: prompt_of<T, BITS, 224>(a, to, s); break;
+        default: prompt_of<T, BITS, 256>(a, to, s); break;
     }
     if (a.splits > 1) {
         const uint32_t quads = a.c.dim / 4, lanes = a.tokens * a.heads * quads;
@@ -482,9 +546,12 @@ size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, 
     if (tokens > (1ull << 24) || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 || dim > 256 ||
         dim % 32 || tokens * heads > (1ull << 30)) return 0;
     if (tokens == 0 || batch == 0) return 256;
-    const uint32_t splits = splits_of(blocks_of(tokens, batch, (uint32_t)(heads / kv_heads)), (uint32_t)kv_heads);
-    if (splits == 1) return 256;
-    const uint64_t rows = splits * tokens * heads;
+    uint64_t rows = 0;                                      // (of both ways there are, whatever the type)
+    for (int eight = 0; eight < 2; ++eight) {
+        const uint32_t splits = split_of(tokens, batch, (uint32_t)(heads / kv_heads), (uint32_t)kv_heads, eight != 0).splits;
+        if (splits > 1 && splits * tokens * heads > rows) rows = splits * tokens * heads;
+    }
+    if (rows == 0) return 256;
     return (size_t)((rows * 8 + 255) / 256 * 256 + (rows * dim * 4 + 255) / 256 * 256);
 }
 
@@ -508,13 +575,13 @@ int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, 
     a.tokens = (uint32_t)tokens; a.batch = (uint32_t)batch; a.heads = (uint32_t)heads; a.group = (uint32_t)(heads / cache->heads);
     a.by_group = FastDiv(a.group);
     a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
-    const uint32_t blocks = blocks_of(tokens, batch, a.group);
-    a.splits = splits_of(blocks, a.c.heads);
+    const Split to = split_of(tokens, batch, a.group, a.c.heads, eight_fit(dtype, a.c.dim));
+    a.splits = to.splits;
     const uint64_t rows = (uint64_t)a.splits * tokens * heads;
     a.stats = static_cast<float*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (rows * 8 + 255) / 256 * 256);
     hipStream_t s = static_cast<hipStream_t>(stream);
-#define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, blocks, s); else prompt<T, 4>(a, blocks, s); } while (0)
+#define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, to, s); else prompt<T, 4>(a, to, s); } while (0)
     if (dtype == LC_F32) CALL(LC_F32);
     else if (dtype == LC_BF16) CALL(LC_BF16);
     else CALL(LC_F16);
