@@ -17,7 +17,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // 2^-24 of the largest have all of its 11 bits.
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr uint32_t kMostSplits = 32;
+constexpr uint32_t kMostParts = 32, kLeastTiles = 4;       // of a sequence's tokens, and tiles that a part has at least
 
 struct Prompt {
     Cache c;
@@ -26,10 +26,11 @@ struct Prompt {
     const int32_t* table; uint64_t ld_table; uint64_t table_pages;
     const int32_t* lens;
     void* out; uint64_t ld_out;
-    float* stats;               // the maximum and the sum of each [split][token][head]
-    float* part;                // [split][token][head][dim]
+    float* stats;               // the maximum and the sum of each [place of a part][row]
+    float* part;                // [place of a part][row][dim]
     float scale;                // times log2(e)
-    uint32_t tokens, batch, heads, group, splits;
+    uint32_t tokens, batch, heads, group;
+    uint32_t most_parts, share; // parts of a sequence at most; workgroups that are on the chip at once, for one head
     int32_t pages;
     FastDiv by_group;
 };
@@ -59,26 +60,73 @@ __device__ __forceinline__ float other_half(float v) {
 
 __device__ __forceinline__ int32_t held(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-// Which rows of which sequence a workgroup has: blocks of rows are counted over all sequences.
-struct Own { uint32_t b; int32_t first, count, block; };    // the sequence's first new token and how many it has; the block of rows within it
-__device__ __forceinline__ Own own_of(const Prompt& a, uint32_t block, uint32_t lane, uint32_t rows) {
-    uint32_t before = 0;
+// Which rows of which sequence a workgroup has, and which part of the tokens.  Where a sequence's tokens are more than an even share of all the work, or rows alone leave the
+// chip idle, its blocks of rows are split along the tokens; lengths are known on the device only, so every wavefront works it out for itself: with T the tiles that each
+// workgroup on the chip would have if all had the same, a sequence of more than 5/4 T is dealt in parts of about T.  (So units are at most the blocks of rows and as
+// many as fit the chip, and parts at most twice the latter.)
+struct Own {
+    uint32_t b, block, part, parts, place;      // place: of the part, among those of all sequences that are split
+    int32_t first, count;                       // the sequence's first new token and how many it has
+};
+// JOIN: of blocks of rows that are split, counted by themselves.
+template <bool JOIN>
+__device__ __forceinline__ Own own_of(const Prompt& a, uint32_t unit, uint32_t lane, uint32_t rows) {
+    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    int32_t s = 0, e = 0;
+    auto blocks_of = [&](uint32_t b, uint32_t& tiles) {
+        s = held(b < a.batch ? a.starts[b] : 0, 0, (int32_t)a.tokens);
+        e = held(b < a.batch ? a.starts[b + 1] : 0, 0, (int32_t)a.tokens);
+        tiles = b < a.batch ? (uint32_t)(held(a.lens[b], 0, room) + kTile - 1) / kTile : 0;
+        return e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + rows - 1) / rows) : 0;
+    };
+    auto over_lanes = [](uint64_t v) { for (int x = 32; x; x /= 2) v += __shfl_xor(v, x); return v; };
+    uint32_t even = 0xffffffffu;
+    if (a.most_parts > 1) {
+        uint64_t work = 0;
+        for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
+            uint32_t tiles;
+            const uint32_t blocks = blocks_of(b0 + lane, tiles);
+            work += over_lanes((uint64_t)blocks * tiles);
+        }
+        const uint64_t t = (work + a.share - 1) / a.share;
+        even = t < kLeastTiles ? kLeastTiles : (uint32_t)t;
+    }
+    uint32_t before = 0, places = 0;
     for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
-        const uint32_t b = b0 + lane;
-        const int32_t s = held(b < a.batch ? a.starts[b] : 0, 0, (int32_t)a.tokens), e = held(b < a.batch ? a.starts[b + 1] : 0, 0, (int32_t)a.tokens);
-        const uint32_t own = e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + rows - 1) / rows) : 0;
-        uint32_t upto = own;
-        for (int x = 1; x < 64; x *= 2) { const uint32_t o = __shfl_up(upto, x); if (lane >= (uint32_t)x) upto += o; }
-        const unsigned long long mine = __ballot(before + upto > block && before + upto - own <= block);
+        uint32_t tiles;
+        const uint32_t blocks = blocks_of(b0 + lane, tiles);
+        uint32_t parts = tiles > even + even / 4 ? (tiles + even - 1) / even : 1;
+        parts = parts < a.most_parts ? parts : a.most_parts;
+        const uint32_t own = JOIN ? (parts > 1 ? blocks : 0) : blocks * parts, held_places = parts > 1 ? blocks * parts : 0;
+        // of each 64 the longest sequences first, so that no long one begins when the others end
+        uint32_t upto = own, places_upto = held_places, all = 0, all_places = 0;
+        const int there = (int)(a.batch - b0 < 64 ? a.batch - b0 : 64);
+        for (int j = 0; j < there; ++j) {
+            const uint32_t t = __builtin_amdgcn_readlane(tiles, j), o = __builtin_amdgcn_readlane(own, j), p = __builtin_amdgcn_readlane(held_places, j);
+            const bool ahead = t > tiles || (t == tiles && j < (int)lane);
+            upto += ahead ? o : 0;
+            places_upto += ahead ? p : 0;
+            all += o;
+            all_places += p;
+        }
+        const unsigned long long mine = __ballot(before + upto > unit && before + upto - own <= unit);
         if (mine) {
             const int from = __builtin_ctzll(mine);
-            const uint32_t first_block = before + __builtin_amdgcn_readlane(upto, from) - __builtin_amdgcn_readlane(own, from);
-            return {b0 + from, __builtin_amdgcn_readlane(s, from), __builtin_amdgcn_readlane(e, from) - __builtin_amdgcn_readlane(s, from),
-                    (int32_t)(block - first_block)};
+            Own r;
+            r.b = b0 + from;
+            r.parts = __builtin_amdgcn_readlane(parts, from);
+            r.first = __builtin_amdgcn_readlane(s, from);
+            r.count = __builtin_amdgcn_readlane(e, from) - r.first;
+            const uint32_t at = unit - (before + __builtin_amdgcn_readlane(upto, from) - __builtin_amdgcn_readlane(own, from));
+            r.block = JOIN ? at : at / r.parts;
+            r.part = JOIN ? 0 : at - r.block * r.parts;
+            r.place = places + __builtin_amdgcn_readlane(places_upto, from) - __builtin_amdgcn_readlane(held_places, from) + r.block * r.parts + r.part;
+            return r;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
+        before += all;
+        places += all_places;
     }
-    return {0, 0, 0, 0};
+    return {0, 0, 0, 0, 0, 0, 0};
 }
 
 template <int BITS, int D, int kWaves> struct Shape {
@@ -93,9 +141,17 @@ template <int BITS, int D, int kWaves> struct Shape {
 template <int UNITS> __device__ __forceinline__ uint32_t key_unit(uint32_t t, uint32_t u) { return u ^ (UNITS >= 16 ? t & 15 : UNITS == 8 ? t >> 1 & 7 : t >> 2 & 3); }
 __device__ __forceinline__ uint32_t value_unit(uint32_t d, uint32_t u) { return u ^ ((d >> 1 ^ (d >> 4 & 1)) & 7); }
 
-template <int BITS> __device__ __forceinline__ float code_of(uint32_t w, int e) {
-    return BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : (float)((int)(w >> (4 * e) & 15u) - 8);
-}
+// Code e of a word of keys; of 4 bits in sixteenths (from a turned word, whose upper nibbles have one of their own).
+template <int BITS> struct Word {
+    uint32_t w, up;
+    __device__ __forceinline__ explicit Word(uint32_t x) : w(x), up(0) {
+        if (BITS == 4) w = turned(x);
+        asm("" : "+v"(w));                                  // (else codes are cut out one by one before they are converted)
+        if (BITS == 4) up = upper_nibbles(w);
+    }
+    __device__ __forceinline__ float code(int e) const { return BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : low_nibble_of(e % 2 ? up : w, e / 2); }
+};
+constexpr float unit_of(int bits) { return bits == 4 ? 16.0f : 1.0f; }
 
 // f(Number<0>), f(Number<1>) ... of N.
 template <int I> struct Number { static constexpr int value = I; };
@@ -117,19 +173,19 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     __shared__ int sunit[2];                                // fp16: probabilities times scales are counted in 2^sunit
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     const uint32_t head = blockIdx.x % a.c.heads;
-    const Own own = own_of(a, blockIdx.x / a.c.heads, lane, kRows);
+    const Own own = own_of<false>(a, blockIdx.x / a.c.heads, lane, kRows);
     if (own.count == 0) return;
     const uint32_t b = own.b;
     const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
     const int32_t len = held(a.lens[b], 0, room);
     const int32_t rows = (int32_t)(own.count * a.group), blocks = (rows + kRows - 1) / kRows;
-    const int32_t row0 = (blocks - 1 - own.block) * kRows;  // (the rows that see most first)
+    const int32_t row0 = (blocks - 1 - (int32_t)own.block) * kRows;  // (the rows that see most first)
     const int32_t row_last = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
     const int32_t base = len - own.count;                   // the place of the first new token
     auto place_of = [&](int32_t row) { return base + (int32_t)a.by_group((uint32_t)row); };
     const int32_t tiles_all = place_of(row_last) >= 0 ? place_of(row_last) / kTile + 1 : 0;
-    const int32_t per = (tiles_all + (int32_t)a.splits - 1) / (int32_t)a.splits;
-    const int32_t tile0 = (int32_t)blockIdx.y * per, tile1 = tile0 + per < tiles_all ? tile0 + per : tiles_all;
+    const int32_t per = (tiles_all + (int32_t)own.parts - 1) / (int32_t)own.parts;
+    const int32_t tile0 = (int32_t)own.part * per, tile1 = tile0 + per < tiles_all ? tile0 + per : tiles_all;
 
     // this lane's row
     const int32_t row = row0 + (int32_t)(32 * wave + c);
@@ -176,20 +232,20 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     // A tile on its way: the first eight lanes look up where it lies, a tile ahead; codes go to registers and, converted, into LDS.
     const int32_t* table = a.table + b * a.ld_table;
     int32_t page_raw = 0;
-    auto look = [&](int32_t tile) {
-        if (threadIdx.x >= 8) return;
-        int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)threadIdx.x;
-        t = t < len ? t : (len - 1) & ~7;                   // (eight tokens that begin at a multiple of eight lie together)
-        page_raw = table[t >> a.c.page_shift];
+    auto token_of = [&](int32_t tile) {                     // the lane's eight tokens (that begin at a multiple of eight, and so lie together)
+        const int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)(threadIdx.x % 8);
+        return t < len ? t : (len - 1) & ~7;
     };
-    auto place_eights = [&](int32_t tile) {
-        if (threadIdx.x >= 8) return;
-        int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)threadIdx.x;
-        t = t < len ? t : (len - 1) & ~7;
+    auto look = [&](int32_t tile, uint32_t lanes) {         // (of several tiles that follow each other, eight lanes each)
+        if (threadIdx.x < lanes) page_raw = table[token_of(tile + (int32_t)threadIdx.x / 8) >> a.c.page_shift];
+    };
+    auto place_eights = [&](int32_t tile, uint32_t lanes) {
+        if (threadIdx.x >= lanes) return;
+        tile += (int32_t)threadIdx.x / 8;
         const bool there = (uint32_t)page_raw < (uint32_t)a.pages;
-        srow[tile % 4][threadIdx.x] = row_of(a.c, there ? page_raw : 0, head, (uint32_t)t & ((1u << a.c.page_shift) - 1));
+        srow[tile % 4][threadIdx.x % 8] = row_of(a.c, there ? page_raw : 0, head, (uint32_t)token_of(tile) & ((1u << a.c.page_shift) - 1));
         const unsigned long long missing = __ballot(!there);
-        if (threadIdx.x == 0) snot[tile % 4] = (uint32_t)missing;
+        if (threadIdx.x % 8 == 0) snot[tile % 4] = (uint32_t)(missing >> threadIdx.x) & 255u;
     };
     u32x4 keys[S::kKeyLoads];
     uint32_t values[S::kValueLoads][4];
@@ -259,22 +315,29 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             if (S::kKeyItems % (kWaves * 64) && l * kWaves * 64 + threadIdx.x >= (uint32_t)S::kKeyItems) return;
             u32x4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t w = BITS == 8 ? keys[l][2 * u + j / 2] : keys[l][u];
-                asm("" : "+v"(w));                          // (else codes are cut out one by one before they are converted)
-                const int e = BITS == 8 ? 2 * (j % 2) : 2 * j;
-                v[j] = pair_of<HALF>(code_of<BITS>(w, e), code_of<BITS>(w, e + 1));
+            for (int n = 0; n < BITS / 4; ++n) {
+                const Word<BITS> w(keys[l][u * BITS / 4 + n]);
+#pragma unroll
+                for (int j = 0; j < 16 / BITS; ++j) v[n * 2 + j] = pair_of<HALF>(w.code(2 * j), w.code(2 * j + 1));
             }
             uint32_t to = key_to[l];
-            asm("" : "+v"(to));                             // (... and places worked out for every piece before the first tile, for which there are no registers)
+            asm("" : "+v"(to));                             // (else places are worked out for every piece before the first tile, for which there are no registers)
             *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(sk[buffer]) + (to ^ (u * 16))) = v;
         } else {
-            constexpr int l = (piece - kKeyPieces) / (32 / BITS), e = (piece - kKeyPieces) % (32 / BITS);
+            // (4 bits: the lower nibbles of all bytes first, then the upper ones, for which words are moved on)
+            constexpr int l = (piece - kKeyPieces) / (32 / BITS), n = (piece - kKeyPieces) % (32 / BITS), e = BITS == 8 ? n : n % 4 * 2 + n / 4;
             if (S::kValueItems % (kWaves * 64) && l * kWaves * 64 + threadIdx.x >= (uint32_t)S::kValueItems) return;
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t& w = values[l][r];
+                if (BITS == 4 && n == 0) w = turned(w);
+                if (BITS == 4 && n == 4) w = upper_nibbles(w);
+                x[r] = BITS == 8 ? (float)(int8_t)(w >> (8 * e)) : low_nibble_of(w, n % 4);
+            }
             uint32_t to = value_to[l];
             asm("" : "+v"(to));
-            *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) =
-                u32x2{pair_of<HALF>(code_of<BITS>(values[l][0], e), code_of<BITS>(values[l][1], e)), pair_of<HALF>(code_of<BITS>(values[l][2], e), code_of<BITS>(values[l][3], e))};
+            *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) = u32x2{pair_of<HALF>(x[0], x[1]), pair_of<HALF>(x[2], x[3])};
         }
     };
     auto put_all = [&](uint32_t buffer) { each<kPieces>([&](auto piece) { put(buffer, piece); }); };
@@ -413,10 +476,8 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
 
     // (Behind the last tile it is asked for once more, into a buffer that nothing reads.)
     if (tile0 < tile1) {
-        for (int i = 0; i < 3; ++i) {
-            look(tile0 + i);
-            place_eights(tile0 + i);
-        }
+        look(tile0, 24);
+        place_eights(tile0, 24);
         __syncthreads();
         ask(tile0);
         put_scales(0);
@@ -427,28 +488,29 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     int32_t tile = tile0;
     for (; tile < wave_tiles; ++tile, buffer ^= 1) {
         __syncthreads();
-        look(tile + 3);
+        look(tile + 3, 8);
         put_scales(buffer ^ 1);
         use(tile, buffer);
-        place_eights(tile + 3);
+        place_eights(tile + 3, 8);
     }
     for (; tile < tile1; ++tile, buffer ^= 1) {             // (what only other wavefronts' rows see; they meet as often in this loop as in the one above)
         __syncthreads();
-        look(tile + 3);
+        look(tile + 3, 8);
         put_scales(buffer ^ 1);
         put_all(buffer ^ 1);
         ask(tile + 2);
-        place_eights(tile + 3);
+        place_eights(tile + 3, 8);
     }
 
     const float total = sum + other_half(sum);
     if (!has_row) return;
     const uint64_t at = (uint64_t)(own.first + qi), hd = head * a.group + qg;
-    float whole = a.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+    float whole = own.parts > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+    whole *= unit_of(BITS);
     if (HALF) whole = total == 0.0f ? 0.0f : ldexpf(whole, unit);
-    if (a.splits > 1) {
-        const uint64_t place_at = ((uint64_t)blockIdx.y * a.tokens + at) * a.heads + hd;
-        if (h == 0) { a.stats[2 * place_at] = top; a.stats[2 * place_at + 1] = total; }
+    if (own.parts > 1) {
+        const uint64_t place_at = ((uint64_t)own.place * a.c.heads + head) * kRows + 32 * wave + c;
+        if (h == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * place_at) = f32x2{top, total};
         if (total == 0.0f) return;
         float* to = a.part + place_at * D;
 #pragma unroll
@@ -471,66 +533,98 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         }
 }
 
-// The parts of rows that several workgroups had, joined: a lane four elements of a row.
+// The parts of a block of rows, joined, 32 rows a workgroup: first each row's factors, then a lane four elements, eight parts' at once.
+constexpr uint32_t kJoined = 32;
 template <int T>
-__global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t lanes, FastDiv by_quads, FastDiv by_heads) {
-    const uint32_t lane = blockIdx.x * 256u + threadIdx.x;
-    if (lane >= lanes) return;
-    const uint32_t r = by_quads(lane), d = 4 * (lane - r * by_quads.d), token = by_heads(r), hd = r - token * a.heads;
-    if ((int32_t)token < a.starts[0] || (int32_t)token >= a.starts[a.batch]) return;      // (of no sequence)
-    float m = -__builtin_inff(), l = 0;
-    for (uint32_t s = 0; s < a.splits; ++s) m = fmaxf(m, a.stats[2 * (((uint64_t)s * a.tokens + token) * a.heads + hd)]);
-    f32x4 o = {0, 0, 0, 0};
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        const uint64_t at = ((uint64_t)s * a.tokens + token) * a.heads + hd;
-        const float sum = a.stats[2 * at + 1];
-        if (sum == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(a.stats[2 * at] - m);
-        l += f * sum;
-        const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + at * a.c.dim + d);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+__global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t rows) {
+    __shared__ float factor[kJoined][kMostParts + 1];
+    const uint32_t head = blockIdx.x % a.c.heads, lane = threadIdx.x % 64;
+    __shared__ Own shared_own;
+    if (threadIdx.x < 64) {                                 // (most workgroups find that there is nothing for them)
+        const Own found = own_of<true>(a, blockIdx.x / a.c.heads, lane, rows);
+        if (lane == 0) shared_own = found;
     }
-    const float whole = l == 0.0f ? 1.0f : 1.0f / l;
-    o *= whole;
-    store_four<T>(a.out, (uint64_t)token * a.ld_out + (uint64_t)hd * a.c.dim + d, o);
+    __syncthreads();
+    const Own own = shared_own;
+    if (own.count == 0) return;
+    const uint32_t all = (uint32_t)own.count * a.group, blocks = (all + rows - 1) / rows, row0 = (blocks - 1 - own.block) * rows + blockIdx.y * kJoined;
+    if (row0 >= all) return;
+    const uint32_t here = all - row0 < kJoined ? all - row0 : kJoined;
+    const uint64_t step = (uint64_t)a.c.heads * rows, first = ((uint64_t)own.place * a.c.heads + head) * rows + blockIdx.y * kJoined;      // from part to part; the first
+    for (uint32_t r = threadIdx.x / 32; r < here; r += 8) {             // half a wavefront a row, a lane a part
+        const uint32_t p = threadIdx.x % 32;
+        f32x2 stat = {-__builtin_inff(), 0};
+        if (p < own.parts) stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * (first + r + p * step));
+        float m = stat[0];
+        for (int x = 16; x; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
+        const float f = stat[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(stat[0] - m);
+        float l = stat[1] == 0.0f ? 0.0f : f * stat[1];
+        for (int x = 16; x; x /= 2) l += __shfl_xor(l, x);
+        factor[r][p] = l == 0.0f ? 0.0f : f * (1.0f / l);
+    }
+    static_assert(kMostParts == 32, "a lane a part");
+    __syncthreads();
+    const uint32_t quads = a.c.dim / 4;
+    for (uint32_t i = threadIdx.x; i < here * quads; i += 256) {
+        const uint32_t r = i / quads, d = 4 * (i - r * quads), qi = a.by_group(row0 + r), qg = row0 + r - qi * a.group;
+        const float* from = a.part + (first + r) * a.c.dim + d;
+        f32x4 o = {0, 0, 0, 0};
+        for (uint32_t p0 = 0; p0 < own.parts; p0 += 8) {    // (the last again beyond the last)
+            f32x4 v[8];
+#pragma unroll
+            for (uint32_t p = 0; p < 8; ++p) v[p] = *reinterpret_cast<const f32x4*>(from + (p0 + p < own.parts ? p0 + p : own.parts - 1) * step * a.c.dim);
+#pragma unroll
+            for (uint32_t p = 0; p < 8; ++p) {
+                const float f = p0 + p < own.parts ? factor[r][p0 + p] : 0.0f;
+                if (f != 0.0f)                              // (else nothing was written there)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[p][e], o[e]);
+            }
+        }
+        store_four<T>(a.out, (uint64_t)(own.first + qi) * a.ld_out + (uint64_t)(head * a.group + qg) * a.c.dim + d, o);
+    }
 }
 
-// Row blocks at most, and into how many parts their tokens are split so that the chip is full.
-struct Split { uint32_t waves, blocks, splits; };
-bool eight_fit(int dtype, uint32_t dim) { return dtype != LC_F32 && dim <= 128; }        // two wavefronts a SIMD have the registers
-Split split_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads, bool eight) {
+// How rows are dealt to workgroups.  Eight wavefronts a workgroup share conversions (2048 of 10000 tokens of 32 / 8 heads 323 us for 355 with four) where two a SIMD have the
+// registers and rows are many; sequences of few rows leave much of 256 unused (9 of 57 to 517 tokens 155 for 141).  Splitting is left out where rows fill the chip: once if
+// all is one sequence, else four times.
+struct Deal { uint32_t waves, blocks, share, most_parts; };
+Deal deal_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads, bool two) {
     const uint64_t sequences = tokens < batch ? tokens : batch;      // those with new tokens
-    Split s;
-    s.waves = eight && tokens * group / 256 * kv_heads >= 256 ? 8 : 4;
-    s.blocks = (uint32_t)((tokens * group + 32 * s.waves - 1) / (32 * s.waves) + sequences);
-    const uint64_t have = (uint64_t)s.blocks * kv_heads, want = have >= 512 ? 1 : 512 / have;
-    s.splits = (uint32_t)(want < kMostSplits ? want : kMostSplits);
-    return s;
+    Deal d;
+    d.waves = two && tokens * group / 256 * kv_heads >= 256 && tokens * group >= 1024 * sequences ? 8 : 4;
+    const uint64_t rows = 32 * d.waves, chip = two && d.waves == 4 ? 512 : 256;      // workgroups that are on the chip at once
+    d.blocks = (uint32_t)((tokens * group + rows - 1) / rows + sequences);
+    d.share = (uint32_t)(chip > kv_heads ? chip / kv_heads : 1);
+    d.most_parts = tokens * group / rows * kv_heads >= chip * (batch == 1 ? 1 : 4) ? 1 : kMostParts;
+    return d;
 }
+bool two_fit(int dtype, uint32_t dim) { return dtype != LC_F32 && dim <= 128; }        // two wavefronts a SIMD have the registers
+uint64_t places_of(const Deal& d, uint32_t kv_heads) { return d.most_parts == 1 ? 0 : 2ull * d.share * kv_heads; }
 
 template <int T, int BITS, int D>
-void prompt_of(const Prompt& a, const Split& to, hipStream_t s) {
+void prompt_of(const Prompt& a, const Deal& d, hipStream_t s) {
     constexpr int PERSIMD = T == LC_F32 || D > 128 ? 1 : 2;
-    if constexpr (T != LC_F32 && D <= 128)
-        if (to.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<dim3(to.blocks * a.c.heads, a.splits), 512, 0, s>>>(a); return; }
-    k_kv_prompt<T, BITS, D, 4, PERSIMD><<<dim3(to.blocks * a.c.heads, a.splits), 256, 0, s>>>(a);
+    const uint32_t units = (d.blocks + (a.most_parts > 1 ? d.share : 0)) * a.c.heads;
+    if constexpr (PERSIMD == 2)
+        if (d.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<units, 512, 0, s>>>(a); return; }
+    k_kv_prompt<T, BITS, D, 4, PERSIMD><<<units, 256, 0, s>>>(a);
 }
 template <int T, int BITS>
-void prompt(const Prompt& a, const Split& to, hipStream_t s) {
+void prompt(const Prompt& a, const Deal& d, hipStream_t s) {
     switch (a.c.dim) {
-        case 32: prompt_of<T, BITS, 32>(a, to, s); break;
-        case 64: prompt_of<T, BITS, 64>(a, to, s); break;
-        case 96: prompt_of<T, BITS, 96>(a, to, s); break;
-        case 128: prompt_of<T, BITS, 128>(a, to, s); break;
-        case 160: prompt_of<T, BITS, 160>(a, to, s); break;
-        case 192: prompt_of<T, BITS, 192>(a, to, s); break;
-        case 224: prompt_of<T, BITS, 224>(a, to, s); break;
-        default: prompt_of<T, BITS, 256>(a, to, s); break;
+        case 32: prompt_of<T, BITS, 32>(a, d, s); break;
+        case 64: prompt_of<T, BITS, 64>(a, d, s); break;
+        case 96: prompt_of<T, BITS, 96>(a, d, s); break;
+        case 128: prompt_of<T, BITS, 128>(a, d, s); break;
+        case 160: prompt_of<T, BITS, 160>(a, d, s); break;
+        case 192: prompt_of<T, BITS, 192>(a, d, s); break;
+        case 224: prompt_of<T, BITS, 224>(a, d, s); break;
+        default: prompt_of<T, BITS, 256>(a, d, s); break;
     }
-    if (a.splits > 1) {
-        const uint32_t quads = a.c.dim / 4, lanes = a.tokens * a.heads * quads;
-        k_kv_prompt_join<T><<<(lanes + 255) / 256, 256, 0, s>>>(a, lanes, FastDiv(quads), FastDiv(a.heads));
+    if (a.most_parts > 1) {
+        const uint32_t blocks = (d.blocks < d.share ? d.blocks : d.share) * a.c.heads;      // (a block that is split has the work of more than one of the chip's)
+        k_kv_prompt_join<T><<<dim3(blocks, 32 * d.waves / kJoined), 256, 0, s>>>(a, 32 * d.waves);
     }
 }
 
@@ -546,13 +640,13 @@ size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, 
     if (tokens > (1ull << 24) || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 || dim > 256 ||
         dim % 32 || tokens * heads > (1ull << 30)) return 0;
     if (tokens == 0 || batch == 0) return 256;
-    uint64_t rows = 0;                                      // (of both ways there are, whatever the type)
-    for (int eight = 0; eight < 2; ++eight) {
-        const uint32_t splits = split_of(tokens, batch, (uint32_t)(heads / kv_heads), (uint32_t)kv_heads, eight != 0).splits;
-        if (splits > 1 && splits * tokens * heads > rows) rows = splits * tokens * heads;
+    uint64_t most = 0;                                      // (of both ways there are, whatever the type)
+    for (int two = 0; two < 2; ++two) {
+        const Deal d = deal_of(tokens, batch, (uint32_t)(heads / kv_heads), (uint32_t)kv_heads, two != 0);
+        const uint64_t rows = places_of(d, (uint32_t)kv_heads) * 32 * d.waves;
+        most = rows > most ? rows : most;
     }
-    if (rows == 0) return 256;
-    return (size_t)((rows * 8 + 255) / 256 * 256 + (rows * dim * 4 + 255) / 256 * 256);
+    return (size_t)((most * 8 + 255) / 256 * 256 + most * dim * 4 + 256);
 }
 
 int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,
@@ -571,17 +665,17 @@ int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, 
     a.c = described(*cache);
     a.q = q; a.ld_q = ld_q; a.starts = starts; a.table = table; a.ld_table = ld_table; a.table_pages = cache->pages ? table_pages : 0; a.lens = lens;
     a.out = out; a.ld_out = ld_out;
-    a.scale = scale * kLog2e;
+    a.scale = scale * kLog2e * unit_of(cache->bits);
     a.tokens = (uint32_t)tokens; a.batch = (uint32_t)batch; a.heads = (uint32_t)heads; a.group = (uint32_t)(heads / cache->heads);
     a.by_group = FastDiv(a.group);
     a.pages = (int32_t)(cache->pages > 0x7fffffffull ? 0x7fffffff : cache->pages);
-    const Split to = split_of(tokens, batch, a.group, a.c.heads, eight_fit(dtype, a.c.dim));
-    a.splits = to.splits;
-    const uint64_t rows = (uint64_t)a.splits * tokens * heads;
+    const Deal d = deal_of(tokens, batch, a.group, a.c.heads, two_fit(dtype, a.c.dim));
+    a.share = d.share;
+    a.most_parts = a.table_pages << a.c.page_shift <= (kLeastTiles + kLeastTiles / 4) * kTile ? 1 : d.most_parts;
     a.stats = static_cast<float*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (rows * 8 + 255) / 256 * 256);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (places_of(d, a.c.heads) * 32 * d.waves * 8 + 255) / 256 * 256);
     hipStream_t s = static_cast<hipStream_t>(stream);
-#define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, to, s); else prompt<T, 4>(a, to, s); } while (0)
+#define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, d, s); else prompt<T, 4>(a, d, s); } while (0)
     if (dtype == LC_F32) CALL(LC_F32);
     else if (dtype == LC_BF16) CALL(LC_BF16);
     else CALL(LC_F16);
