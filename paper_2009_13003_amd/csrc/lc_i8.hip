@@ -172,26 +172,59 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// Many rows: TM rows of x by TN rows of w a workgroup, WM x WN wavefronts, 128 bytes of the width at a time in LDS, twice buffered.  A row is eight units
-// of 16 bytes, stored at unit ^ row % 8, so that the lanes that read a column of units from eight rows have eight places; loads that go to LDS write it lane by lane, so
-// it is where each lane loads from that is turned.
-template <int TM, int TN, int WM, int WN>
+// Four results of a row that follow each other, the first `valid` of them.
+__device__ __forceinline__ void put_four(const Product& p, uint64_t at, f32x4 v, uint32_t valid) {
+    if (valid >= 4) {
+        typedef f32x4 __attribute__((aligned(2))) Four;
+        typedef u32x2 __attribute__((aligned(2))) Halves;
+        typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+        if (p.dtype == LC_F32) *reinterpret_cast<Four*>(static_cast<float*>(p.y) + at) = v;
+        else if (p.dtype == LC_BF16) *reinterpret_cast<Halves*>(static_cast<uint16_t*>(p.y) + at) = u32x2{rounded_halves(v[0], v[1]), rounded_halves(v[2], v[3])};
+        else *reinterpret_cast<Halves*>(static_cast<uint16_t*>(p.y) + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(v, f16x4));
+    } else
+        for (uint32_t e = 0; e < valid; ++e) put(p, at + e, v[e]);
+}
+
+// N of the loads that go to LDS may still be under way.
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Many rows: TM rows of x by TN rows of w a workgroup, WM x WN wavefronts, 128 bytes of the width at a time in LDS, in BUFFERS places that are filled in turn.  A row is
+// eight units of 16 bytes, stored at unit ^ row / 2 % 8, so that the sixteen lanes that LDS serves at once, which read one column of units from sixteen rows, have
+// all of its 256 bytes; loads that go to LDS write it lane by lane, so it is where each lane loads from that is turned.  Operands are read a step of 32 bytes ahead
+// of their products.  The workgroup meets once a tile, ahead of its last step, whose operands have been read by then: behind the meeting the tile's place is filled again.
+// Rows of the matrix instruction's result are rows of w, so a lane has four results of a row of y that follow each other.
+template <int TM, int TN, int WM, int WN, int BUFFERS>
 __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
     constexpr int WAVES = WM * WN, MT = TM / WM / 32, NT = TN / WN / 32, BYTES = (TM + TN) * 128, LOADS = (TM + TN) / 8 / WAVES;
     static_assert((TM + TN) % (8 * WAVES) == 0, "whole loads");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[BUFFERS][BYTES];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
-    const uint32_t tiles_m = (p.m + TM - 1) / TM;
-    const uint32_t m0 = blockIdx.x % tiles_m * TM, n0 = blockIdx.x / tiles_m * TN;
+    // Workgroups go round the eight dies, each with an L2 of its own: those of one die get tiles that lie together, by bands of eight tiles of x.
+    const uint32_t tiles_m = (p.m + TM - 1) / TM, tiles_n = (p.n + TN - 1) / TN, all = tiles_m * tiles_n, whole = all / 8;
+    const uint32_t id = blockIdx.x < whole * 8 ? blockIdx.x % 8 * whole + blockIdx.x / 8 : blockIdx.x;
+    const uint32_t band = id / (8 * tiles_n), high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8, in_band = id - band * 8 * tiles_n;
+    const uint32_t m0 = (band * 8 + in_band % high) * TM, n0 = in_band / high * TN;
     const uint8_t* from[LOADS];
-    uint32_t unit = (lane % 8) ^ (lane / 8);
+    uint32_t unit[LOADS];
 #pragma unroll
     for (int l = 0; l < LOADS; ++l) {
         const uint32_t row = (wave * LOADS + l) * 8 + lane / 8;     // of x, and behind them of w
-        if (row < TM) { const uint32_t i = m0 + row < p.m ? m0 + row : p.m - 1; from[l] = p.x + i * p.x_pitch; }
-        else { const uint32_t i = n0 + row - TM < p.n ? n0 + row - TM : p.n - 1; from[l] = p.w + i * p.w_pitch; }
+        unit[l] = ((lane % 8) ^ (row / 2 % 8)) * 16;
+        if (row < TM) { const uint32_t i = m0 + row < p.m ? m0 + row : p.m - 1; from[l] = p.x + i * p.x_pitch + unit[l]; }
+        else { const uint32_t i = n0 + row - TM < p.n ? n0 + row - TM : p.n - 1; from[l] = p.w + i * p.w_pitch + unit[l]; }
     }
-    const uint32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
+    const uint32_t tiles = (p.k16 + 127) / 128;
+    auto ask = [&](uint32_t tile, int l, uint32_t buffer) { // (beyond the width: zeros; beyond the last tile: nothing that is read)
+        const uint32_t k0 = tile * 128;
+        load_to_lds(k0 + unit[l] < p.k16 ? (const void*)(from[l] + k0) : (const void*)&zeros16, &lds[buffer][(wave * LOADS + l) * 1024]);
+    };
+    const uint32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN), turn = c / 2 % 8;
+    u32x4 a[2][NT], b[2][MT];                               // of w and of x
+    auto read = [&](uint32_t buffer, int s, int i) {        // the i-th operand of step s
+        const uint32_t u = ((2 * s + h) ^ turn) * 16;
+        const uint32_t row = i < NT ? TM + wn + 32 * i + c : wm + 32 * (i - NT) + c;
+        (i < NT ? a[s % 2][i < NT ? i : 0] : b[s % 2][i < NT ? 0 : i - NT]) = *reinterpret_cast<const u32x4*>(&lds[buffer][row * 128 + u]);
+    };
     i32x16 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -199,41 +232,58 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    auto ask = [&](uint32_t k0, uint32_t buffer) {
-        const uint32_t at = k0 + unit * 16;
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) load_to_lds(at < p.k16 ? (const void*)(from[l] + at) : (const void*)&zeros16, &lds[buffer][(wave * LOADS + l) * 1024]);
-    };
-    ask(0, 0);
-    uint32_t buffer = 0;
-    for (uint32_t k0 = 0; k0 < p.k16; k0 += 128, buffer ^= 1) {
-        __syncthreads();                                    // (what was asked for is there, and the other buffer is free)
-        if (k0 + 128 < p.k16) ask(k0 + 128, buffer ^ 1);
+    for (int t = 0; t < BUFFERS; ++t)
+#pragma unroll
+        for (int l = 0; l < (t == BUFFERS - 1 ? LOADS / 4 : LOADS); ++l) ask(t, l, t);
+    wait_loads<(BUFFERS - 2) * LOADS + LOADS / 4>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int i = 0; i < NT + MT; ++i) read(0, 0, i);
+    uint32_t buffer = 0, last = BUFFERS - 1;                // the tile's place, and that of the one before
+    for (uint32_t t = 0; t < tiles; ++t) {
+        const uint32_t next = buffer + 1 == BUFFERS ? 0 : buffer + 1;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            u32x4 a[MT], b[NT];
-            const uint32_t u = ((2 * s + h) ^ (c % 8)) * 16;
+            if (s == 3) {
+                // the next tile is there, and everyone has read this one
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFFERS - 2) * LOADS) : "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = *reinterpret_cast<const u32x4*>(&lds[buffer][(wm + 32 * i + c) * 128 + u]);
+            for (int x = 0; x < MT * NT; ++x) {
+                const int i = x / NT, j = x % NT;
+                acc[i][j] = mfma_32(a[s % 2][j], b[s % 2][i], acc[i][j]);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = *reinterpret_cast<const u32x4*>(&lds[buffer][(TM + wn + 32 * j + c) * 128 + u]);
+                for (int y = x * (NT + MT) / (MT * NT); y < (x + 1) * (NT + MT) / (MT * NT); ++y) read(s == 3 ? next : buffer, (s + 1) % 4, y);
+                // a quarter of what is asked for beside each step
+                const int first = (s + 1) % 4 * LOADS / 4, loads = ((s + 1) % 4 + 1) * LOADS / 4 - first;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_32(a[i], b[j], acc[i][j]);
+                for (int y = x * loads / (MT * NT); y < (x + 1) * loads / (MT * NT); ++y) ask(s == 3 ? t + BUFFERS : t - 1 + BUFFERS, first + y, s == 3 ? buffer : last);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+        last = buffer;
+        buffer = next;
     }
+    wait_loads<0>();                                        // (LDS is the next workgroup's then)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const uint32_t col = n0 + wn + 32 * j + c;
-        if (col >= p.n) continue;
-        const float sw = p.sw[col];
+    for (int i = 0; i < MT; ++i) {
+        const uint32_t row = m0 + wm + 32 * i + c;
+        if (row >= p.m) continue;
+        const float sx = p.sx[row];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t row = m0 + wm + 32 * i + 8 * (e / 4) + 4 * h + e % 4;
-                if (row < p.m) put(p, row * p.ldy + col, result_of(p, acc[i][j][e], p.sx[row], sw, col));
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t col = n0 + wn + 32 * j + 8 * g + 4 * h;
+                if (col >= p.n) continue;
+                const uint32_t valid = p.n - col < 4 ? p.n - col : 4;
+                f32x4 v;
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) v[e] = e < valid ? result_of(p, acc[i][j][4 * g + e], sx, p.sw[col + e], col + e) : 0.0f;
+                put_four(p, row * p.ldy + col, v, valid);
             }
     }
 }
@@ -277,7 +327,7 @@ void dequantize(const lc_i8& q, void* w, uint64_t ldw, hipStream_t s) {
 void multiply_piece(const Product& p, hipStream_t s) {
     if (p.m <= 16) k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, 1), 512, 0, s>>>(p);
     else if (p.m <= 64) k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p);
-    else k_i8_tiles<128, 128, 2, 2><<<(p.m + 127) / 128 * ((p.n + 127) / 128), 256, 0, s>>>(p);
+    else k_i8_tiles<128, 256, 2, 2, 3><<<(p.m + 127) / 128 * ((p.n + 255) / 256), 256, 0, s>>>(p);
 }
 // By pieces of w's rows of which each makes a launch of fewer than 2^32 threads.
 void multiply(const Product& p, hipStream_t s) {
