@@ -165,8 +165,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_i8_rows(Product p) {
     }
 }
 
-__device__ const u32x4 zeros16 = {0, 0, 0, 0};
-
 // 16 bytes of each lane's own place into LDS at `to` + 16 lane, without passing through registers.
 __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
@@ -188,15 +186,16 @@ __device__ __forceinline__ void put_four(const Product& p, uint64_t at, f32x4 v,
 // N of the loads that go to LDS may still be under way.
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// Many rows: TM rows of x by TN rows of w a workgroup, WM x WN wavefronts, 128 bytes of the width at a time in LDS, in BUFFERS places that are filled in turn.  A row is
-// eight units of 16 bytes, stored at unit ^ row / 2 % 8, so that the sixteen lanes that LDS serves at once, which read one column of units from sixteen rows, have
-// all of its 256 bytes; loads that go to LDS write it lane by lane, so it is where each lane loads from that is turned.  Operands are read a step of 32 bytes ahead
-// of their products.  The workgroup meets once a tile, ahead of its last step, whose operands have been read by then: behind the meeting the tile's place is filled again.
+// Many rows: TM rows of x by TN rows of w a workgroup, WM x WN wavefronts, 128 bytes of the width at a time in LDS, in BUFFERS places that are filled in turn.  A load that
+// goes to LDS brings eight rows of 128 bytes, each by eight lanes in its own order (turned about within a row, so that LDS has no bank conflicts, such loads cost: 2048x4096x11008
+// 105 us for 96), and eight rows apart, so that the sixteen rows that LDS serves at once lie in eight such pieces, 16 bytes more than 1024 apart, and have all of
+// its 256 bytes.  Operands are read a step of 32 bytes ahead of their products.  The workgroup meets once a tile, ahead of its last step, whose operands have been read by
+// then: behind the meeting the tile's place is filled again.
 // Rows of the matrix instruction's result are rows of w, so a lane has four results of a row of y that follow each other.
 template <int TM, int TN, int WM, int WN, int BUFFERS>
 __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
-    constexpr int WAVES = WM * WN, MT = TM / WM / 32, NT = TN / WN / 32, BYTES = (TM + TN) * 128, LOADS = (TM + TN) / 8 / WAVES;
-    static_assert((TM + TN) % (8 * WAVES) == 0, "whole loads");
+    constexpr int WAVES = WM * WN, MT = TM / WM / 32, NT = TN / WN / 32, PIECE = 1024 + 16, BYTES = (TM + TN) / 8 * PIECE, LOADS = (TM + TN) / 8 / WAVES;
+    static_assert((TM + TN) % (8 * WAVES) == 0 && TM % 64 == 0 && TN % 64 == 0, "whole loads");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[BUFFERS][BYTES];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     // Workgroups go round the eight dies, each with an L2 of its own: those of one die get tiles that lie together, by bands of eight tiles of x.
@@ -204,26 +203,27 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
     const uint32_t id = blockIdx.x < whole * 8 ? blockIdx.x % 8 * whole + blockIdx.x / 8 : blockIdx.x;
     const uint32_t band = id / (8 * tiles_n), high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8, in_band = id - band * 8 * tiles_n;
     const uint32_t m0 = (band * 8 + in_band % high) * TM, n0 = in_band / high * TN;
-    const uint8_t* from[LOADS];
-    uint32_t unit[LOADS];
+    // Where each lane loads from: a scalar place and 32 bits behind it, held to the row's end (what lies behind the width is left out of the products).
+    const uint8_t *x0 = p.x + m0 * p.x_pitch, *w0 = p.w + n0 * p.w_pitch;
+    uint32_t from[LOADS];
+    const uint32_t end = p.k16 - 16;
 #pragma unroll
     for (int l = 0; l < LOADS; ++l) {
-        const uint32_t row = (wave * LOADS + l) * 8 + lane / 8;     // of x, and behind them of w
-        unit[l] = ((lane % 8) ^ (row / 2 % 8)) * 16;
-        if (row < TM) { const uint32_t i = m0 + row < p.m ? m0 + row : p.m - 1; from[l] = p.x + i * p.x_pitch + unit[l]; }
-        else { const uint32_t i = n0 + row - TM < p.n ? n0 + row - TM : p.n - 1; from[l] = p.w + i * p.w_pitch + unit[l]; }
+        const uint32_t piece = wave * LOADS + l, row = piece / 8 * 64 + lane / 8 * 8 + piece % 8;      // of x, and behind them of w
+        const uint32_t i = row < TM ? (m0 + row < p.m ? row : p.m - 1 - m0) : (n0 + row - TM < p.n ? row - TM : p.n - 1 - n0);
+        from[l] = i * (uint32_t)(row < TM ? p.x_pitch : p.w_pitch);
     }
-    const uint32_t tiles = (p.k16 + 127) / 128;
-    auto ask = [&](uint32_t tile, int l, uint32_t buffer) { // (beyond the width: zeros; beyond the last tile: nothing that is read)
-        const uint32_t k0 = tile * 128;
-        load_to_lds(k0 + unit[l] < p.k16 ? (const void*)(from[l] + k0) : (const void*)&zeros16, &lds[buffer][(wave * LOADS + l) * 1024]);
+    auto ask = [&](uint32_t tile, int l, uint32_t buffer) {
+        const uint32_t piece = wave * LOADS + l, at = tile * 128 + lane % 8 * 16;
+        load_to_lds((piece < TM / 8 ? x0 : w0) + (uint64_t)(from[l] + (at < end ? at : end)), &lds[buffer][piece * PIECE]);
     };
-    const uint32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN), turn = c / 2 % 8;
+    const uint32_t wm = wave % WM * (TM / WM), wn = TM + wave / WM * (TN / WN);
     u32x4 a[2][NT], b[2][MT];                               // of w and of x
+    auto operand_at = [&](uint32_t buffer, uint32_t u, uint32_t row) {      // unit u of this lane's of the 32 rows from `row` on
+        return *reinterpret_cast<const u32x4*>(&lds[buffer][c % 8 * PIECE + c / 8 * 128 + row / 64 * 8 * PIECE + row % 64 / 8 * 128 + u * 16]);
+    };
     auto read = [&](uint32_t buffer, int s, int i) {        // the i-th operand of step s
-        const uint32_t u = ((2 * s + h) ^ turn) * 16;
-        const uint32_t row = i < NT ? TM + wn + 32 * i + c : wm + 32 * (i - NT) + c;
-        (i < NT ? a[s % 2][i < NT ? i : 0] : b[s % 2][i < NT ? 0 : i - NT]) = *reinterpret_cast<const u32x4*>(&lds[buffer][row * 128 + u]);
+        (i < NT ? a[s % 2][i < NT ? i : 0] : b[s % 2][i < NT ? 0 : i - NT]) = operand_at(buffer, 2 * s + h, i < NT ? wn + 32 * i : wm + 32 * (i - NT));
     };
     i32x16 acc[MT][NT];
 #pragma unroll
@@ -241,6 +241,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
 #pragma unroll
     for (int i = 0; i < NT + MT; ++i) read(0, 0, i);
     uint32_t buffer = 0, last = BUFFERS - 1;                // the tile's place, and that of the one before
+    const uint32_t tiles = p.k16 / 128, rest = p.k16 % 128 / 16;       // whole ones, and 16 bytes behind them
     for (uint32_t t = 0; t < tiles; ++t) {
         const uint32_t next = buffer + 1 == BUFFERS ? 0 : buffer + 1;
 #pragma unroll
@@ -267,7 +268,23 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         last = buffer;
         buffer = next;
     }
-    wait_loads<0>();                                        // (LDS is the next workgroup's then)
+    wait_loads<0>();
+    if (rest) {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        for (uint32_t s = 0; 2 * s < rest; ++s) {
+            const bool in = 2 * s + h < rest;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) a[0][j] = operand_at(buffer, 2 * s + h, wn + 32 * j);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                b[0][i] = operand_at(buffer, 2 * s + h, wm + 32 * i);
+                if (!in) b[0][i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_32(a[0][j], b[0][i], acc[i][j]);
+            }
+        }
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const uint32_t row = m0 + wm + 32 * i + c;
@@ -277,7 +294,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const uint32_t col = n0 + wn + 32 * j + 8 * g + 4 * h;
+                const uint32_t col = n0 + wn - TM + 32 * j + 8 * g + 4 * h;
                 if (col >= p.n) continue;
                 const uint32_t valid = p.n - col < 4 ? p.n - col : 4;
                 f32x4 v;
@@ -324,14 +341,16 @@ void dequantize(const lc_i8& q, void* w, uint64_t ldw, hipStream_t s) {
     }
 }
 
-void multiply_piece(const Product& p, hipStream_t s) {
-    if (p.m <= 16) k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, 1), 512, 0, s>>>(p);
+void multiply_piece(const Product& p, bool few, hipStream_t s) {
+    if (p.m <= 16 || few) k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, (p.m + 15) / 16), 512, 0, s>>>(p);
     else if (p.m <= 64) k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p);
     else k_i8_tiles<128, 256, 2, 2, 3><<<(p.m + 127) / 128 * ((p.n + 255) / 256), 256, 0, s>>>(p);
 }
 // By pieces of w's rows of which each makes a launch of fewer than 2^32 threads.
 void multiply(const Product& p, hipStream_t s) {
-    const uint64_t step = p.m <= 64 ? 1ull << 26 : ((1ull << 23) / ((p.m + 127) / 128)) * 128;
+    // (no width, or rows so far apart that 32 bits do not count the bytes of a tile: what is right for any)
+    const bool few = p.k16 == 0 || p.x_pitch > (1u << 23) || p.w_pitch > (1u << 23);
+    const uint64_t step = p.m <= 64 ? 1ull << 26 : few ? (1ull << 23) / ((p.m + 15) / 16) * 16 : ((1ull << 23) / ((p.m + 127) / 128)) * 128;
     for (uint64_t j = 0; j < p.n; j += step) {
         Product q = p;
         q.n = (uint32_t)(p.n - j < step ? p.n - j : step);
@@ -339,7 +358,7 @@ void multiply(const Product& p, hipStream_t s) {
         q.sw += j;
         if (q.bias) q.bias = static_cast<const uint8_t*>(p.bias) + j * size_of(p.dtype);
         q.y = static_cast<uint8_t*>(p.y) + j * size_of(p.dtype);
-        multiply_piece(q, s);
+        multiply_piece(q, few, s);
     }
 }
 
