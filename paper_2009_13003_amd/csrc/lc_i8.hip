@@ -11,6 +11,32 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) int i32x16;
 
 // ---------------------------------------------------------------- quantising and reading back
+// A row's scale and its reciprocal by its largest magnitude, as the bits of a number: NaN above infinity above the rest.
+__device__ __forceinline__ float scale_of(uint32_t most, float& inv) {
+    const float s = float_of(most) * (1.0f / 127.0f);
+    inv = 0.0f;
+    if (most >= 0x7f800000u) return __builtin_nanf("");
+    if (s < kSmallest) return 0.0f;
+    inv = 1.0f / s;
+    return s;
+}
+__device__ __forceinline__ uint32_t largest_of(const float x[8], uint32_t most) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { const uint32_t a = bits_of(x[e]) & 0x7fffffffu; most = a > most ? a : most; }
+    return most;
+}
+__device__ __forceinline__ uint32_t largest_of_wave(uint32_t most) {
+    most = max_of_lanes<32>(most);
+    const uint32_t o = (uint32_t)__shfl_xor((int)most, 32);
+    return o > most ? o : most;
+}
+__device__ __forceinline__ u32x2 codes_of(const float x[8], float inv) {
+    u32x2 q = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e / 4] |= (rounded(fminf(fmaxf(inv == 0.0f ? 0.0f : x[e] * inv, -127.0f), 127.0f), 0.0f) & 255u) << (8 * (e % 4));
+    return q;
+}
+
 // A row to a workgroup, or of short rows to a wavefront: 8 elements a lane at a time, kept in registers between the search for the largest and the rounding
 // (rows too long for that are read again).  s = max |w| / 127, q = rint(w (1 / s)).
 template <int T, int WAVES, int R>
@@ -22,38 +48,27 @@ __global__ __launch_bounds__(256) void k_i8_quantize(const void* w, uint64_t ldw
     float v[R][8];
     uint32_t most = 0;
     auto load = [&](uint32_t at, float x[8]) { load_eight<T>(w, row * ldw + at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, x); };
-    auto look = [&](const float x[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { const uint32_t a = bits_of(x[e]) & 0x7fffffffu; most = a > most ? a : most; }
-    };
 #pragma unroll
     for (int r = 0; r < R; ++r) load((r * LANES + lane) * 8, v[r]);
 #pragma unroll
-    for (int r = 0; r < R; ++r) look(v[r]);
+    for (int r = 0; r < R; ++r) most = largest_of(v[r], most);
     for (uint32_t at = (R * LANES + lane) * 8; at < k; at += LANES * 8) {
         float x[8];
         load(at, x);
-        look(x);
+        most = largest_of(x, most);
     }
-    most = max_of_lanes<32>(most);
-    { const uint32_t o = (uint32_t)__shfl_xor((int)most, 32); most = o > most ? o : most; }
+    most = largest_of_wave(most);
     if (WAVES == 4) {
         if (lane % 64 == 0) tops[lane / 64] = most;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = tops[i] > most ? tops[i] : most;
     }
-    float s = float_of(most) * (1.0f / 127.0f), inv = 0.0f;
-    if (most >= 0x7f800000u) s = __builtin_nanf("");
-    else if (s < kSmallest) s = 0.0f;
-    else inv = 1.0f / s;
+    float inv;
+    const float s = scale_of(most, inv);
     const uint32_t end = (k + 15) & ~15u;
     auto store = [&](uint32_t at, const float x[8]) {
-        if (at >= end) return;
-        u32x2 q = {0, 0};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q[e / 4] |= (rounded(fminf(fmaxf(inv == 0.0f ? 0.0f : x[e] * inv, -127.0f), 127.0f), 0.0f) & 255u) << (8 * (e % 4));
-        *reinterpret_cast<u32x2*>(codes + row * pitch + at) = q;
+        if (at < end) *reinterpret_cast<u32x2*>(codes + row * pitch + at) = codes_of(x, inv);
     };
 #pragma unroll
     for (int r = 0; r < R; ++r) store((r * LANES + lane) * 8, v[r]);
@@ -163,6 +178,69 @@ __global__ __launch_bounds__(WAVES * 64) void k_i8_rows(Product p) {
         for (int v = 0; v < WAVES; ++v) sum += sums[v][r][e % 16];
         put(p, i * p.ldy + col, result_of(p, sum, p.sx[i], p.sw[col], col));
     }
+}
+
+// One row of x as it comes: every workgroup works out its codes for itself, into LDS, while its first loads of w are under way.
+constexpr uint32_t kFused = 32768;                          // codes of x at most
+template <int T>
+__global__ __launch_bounds__(512, 6) void k_i8_one_row(Product p, const void* x, uint32_t k) {
+    constexpr uint32_t WAVES = 8, S = 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t codes[];      // of x
+    __shared__ uint32_t tops[WAVES];
+    __shared__ int sums[WAVES][16];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16;
+    const uint32_t n0 = blockIdx.x * 16, j = n0 + c < p.n ? n0 + c : p.n - 1;
+    const uint8_t* w = p.w + j * p.w_pitch;
+    u32x4 a[S][2];
+    auto load = [&](uint32_t k0) {
+#pragma unroll
+        for (uint32_t s = 0; s < S; ++s)
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t at = k0 + s * WAVES * 128 + 32 * h + 16 * i;
+                a[s][i] = load_once<u32x4>(w + (at < p.k16 ? at : 0));
+            }
+    };
+    load(wave * 128);
+    float v[8] = {};                                        // (kept where a lane has no more)
+    uint32_t most = 0;
+    for (uint32_t at = threadIdx.x * 8; at < k; at += WAVES * 512) {
+        load_eight<T>(x, at, (int)(k - at < 8 ? k - at : 8), v);
+        most = largest_of(v, most);
+    }
+    most = largest_of_wave(most);
+    if (lane == 0) tops[wave] = most;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < WAVES; ++i) most = tops[i] > most ? tops[i] : most;
+    float inv;
+    const float sx = scale_of(most, inv);
+    for (uint32_t at = threadIdx.x * 8; at < p.k16; at += WAVES * 512) {
+        if (k > WAVES * 512) load_eight<T>(x, at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, v);
+        *reinterpret_cast<u32x2*>(codes + at) = codes_of(v, inv);
+    }
+    __syncthreads();
+    i32x4 acc = {0, 0, 0, 0};                               // (of sixteen rows of x that are all this one)
+    for (uint32_t k0 = wave * 128; k0 < p.k16; k0 += S * WAVES * 128) {
+        if (k0 != wave * 128) load(k0);
+#pragma unroll
+        for (uint32_t s = 0; s < S; ++s)
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t at = k0 + s * WAVES * 128 + 32 * h + 16 * i;
+                u32x4 b = *reinterpret_cast<const u32x4*>(codes + (at < p.k16 ? at : 0));
+                if (at >= p.k16) b = u32x4{0, 0, 0, 0};
+                acc = mfma_16(b, a[s][i], acc);
+            }
+    }
+    if (h == 0) sums[wave][c] = acc[0];
+    __syncthreads();
+    const uint32_t col = n0 + threadIdx.x;
+    if (threadIdx.x >= 16 || col >= p.n) return;
+    int sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < WAVES; ++i) sum += sums[i][threadIdx.x];
+    put(p, col, result_of(p, sum, sx, p.sw[col], col));
 }
 
 // 16 bytes of each lane's own place into LDS at `to` + 16 lane, without passing through registers.
@@ -328,6 +406,7 @@ void quantize(const void* w, uint64_t ldw, const lc_i8& q, hipStream_t s) {
     else if (q.k <= 2048) quantize_of<T, 4, 1>(w, ldw, q, s);
     else if (q.k <= 4096) quantize_of<T, 4, 2>(w, ldw, q, s);
     else if (q.k <= 8192) quantize_of<T, 4, 4>(w, ldw, q, s);
+    else if (q.k <= 12288) quantize_of<T, 4, 6>(w, ldw, q, s);
     else quantize_of<T, 4, 8>(w, ldw, q, s);
 }
 template <int T>
@@ -341,16 +420,29 @@ void dequantize(const lc_i8& q, void* w, uint64_t ldw, hipStream_t s) {
     }
 }
 
+template <int TM, int TN, int BUFFERS>
+void tiles(const Product& p, hipStream_t s) {
+    k_i8_tiles<TM, TN, 2, 2, BUFFERS><<<(p.m + TM - 1) / TM * ((p.n + TN - 1) / TN), 256, 0, s>>>(p);
+}
 void multiply_piece(const Product& p, bool few, hipStream_t s) {
-    if (p.m <= 16 || few) k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, (p.m + 15) / 16), 512, 0, s>>>(p);
-    else if (p.m <= 64) k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p);
-    else k_i8_tiles<128, 256, 2, 2, 3><<<(p.m + 127) / 128 * ((p.n + 255) / 256), 256, 0, s>>>(p);
+    if (p.m <= 16 || few) { k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, (p.m + 15) / 16), 512, 0, s>>>(p); return; }
+    // Two tiles of rows for as many of w's rows as leave 64 x 64 tiles half of the chip (24 rows by 4096x4096 7.7 us for 9.6; 48 by 11008x4096 34 for 11.1).
+    if (p.m <= 32 && p.n <= 8192) { k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p); return; }
+    // The tiles that take the least time, by how many of them the chip has at once and what such a round takes at a width of 4096, in us:
+    // 64 x 64 up to 256 of them 10, 512 18; 128 x 64 256 18, 512 29; 128 x 128 256 28; 128 x 256 256 49.  (1000 rows by 4096: 28.6 with 128 x 128, 32 with 64 x 64, 41 with
+    // 128 x 256; 2048 rows: 57, 64, 50; 256 rows: 22.6, 11.3, 37.)
+    auto rounds = [&](uint64_t tm, uint64_t tn, uint64_t chip) { return (((p.m + tm - 1) / tm) * ((p.n + tn - 1) / tn) + chip - 1) / chip; };
+    const uint64_t a = rounds(64, 64, 256) == 1 ? 10 : 18 * rounds(64, 64, 512), b = rounds(128, 64, 256) == 1 ? 18 : 29 * rounds(128, 64, 512);
+    const uint64_t c = 28 * rounds(128, 128, 256), d = 49 * rounds(128, 256, 256), least = a < b ? a : b, most = c < d ? c : d;
+    if (most <= least) { if (d <= c) tiles<128, 256, 3>(p, s); else tiles<128, 128, 4>(p, s); }
+    else if (b <= a) tiles<128, 64, 3>(p, s);
+    else tiles<64, 64, 4>(p, s);
 }
 // By pieces of w's rows of which each makes a launch of fewer than 2^32 threads.
 void multiply(const Product& p, hipStream_t s) {
     // (no width, or rows so far apart that 32 bits do not count the bytes of a tile: what is right for any)
     const bool few = p.k16 == 0 || p.x_pitch > (1u << 23) || p.w_pitch > (1u << 23);
-    const uint64_t step = p.m <= 64 ? 1ull << 26 : few ? (1ull << 23) / ((p.m + 15) / 16) * 16 : ((1ull << 23) / ((p.m + 127) / 128)) * 128;
+    const uint64_t step = p.m <= 64 || few ? (1ull << 22) / ((p.m + 15) / 16) * 16 : (1ull << 22) / ((p.m + 63) / 64) * 64;
     for (uint64_t j = 0; j < p.n; j += step) {
         Product q = p;
         q.n = (uint32_t)(p.n - j < step ? p.n - j : step);
@@ -419,6 +511,16 @@ int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const
     if (bad_result(w8, m, bias, y, ldy, dtype) || (w8->k && (!x || off(x, size_of(dtype)))) || (m > 1 && ldx < w8->k) || ldx > (1ull << 40)) return LC_ERR_BADARG;
     if (!ws || off(ws, 256) || ws_bytes < lc_i8_workspace_bytes(m, w8->k)) return LC_ERR_WORKSPACE;
     const uint64_t row = (w8->k + 15) / 16 * 16;
+    // (Each row is a load and a meeting more: two rows and more by 4096 and more take as long in two launches, 7 rows by 1000x2043 10.6 us for 11.5.)
+    if (w8->k && m == 1 && row <= kFused && w8->n <= (1u << 26)) {
+        const Product p = {nullptr, static_cast<const uint8_t*>(w8->codes), nullptr, w8->scales, bias, y, 0, w8->pitch, ldy, (uint32_t)m, (uint32_t)w8->n, (uint32_t)row, dtype};
+        const uint32_t blocks = (p.n + 15) / 16, lds = (uint32_t)row, k = (uint32_t)w8->k;
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        if (dtype == LC_F32) k_i8_one_row<LC_F32><<<blocks, 512, lds, s>>>(p, x, k);
+        else if (dtype == LC_BF16) k_i8_one_row<LC_BF16><<<blocks, 512, lds, s>>>(p, x, k);
+        else k_i8_one_row<LC_F16><<<blocks, 512, lds, s>>>(p, x, k);
+        return launched();
+    }
     const lc_i8 x8 = {ws, reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (m * row + 255) / 256 * 256), m, w8->k, row};
     const int st = lc_i8_quantize(x, ldx, dtype, &x8, stream);
     return st != LC_OK ? st : lc_i8_matmul(&x8, w8, bias, y, ldy, dtype, stream);

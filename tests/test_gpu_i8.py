@@ -89,7 +89,9 @@ def product(q, s, r, t, bias):
 
 
 SIZES = [(1, 1, 1), (1, 17, 16), (3, 16, 129), (16, 33, 512), (7, 1000, 2043), (17, 40, 300), (33, 100, 4099), (64, 65, 1000), (65, 1, 64), (100, 129, 127), (128, 128, 128),
-         (129, 257, 1024), (300, 513, 2051), (1, 3000, 11008), (13, 130, 40000), (5, 3, 0), (1030, 300, 200), (260, 1100, 513)]
+         (129, 257, 1024), (300, 513, 2051), (1, 3000, 11008), (13, 130, 40000), (5, 3, 0), (1030, 300, 200), (260, 1100, 513),
+         # each way of dealing tiles, with what is left over at every edge; one row too wide for its codes to be kept
+         (300, 3001, 200), (641, 2501, 333), (1031, 2003, 130), (1901, 4099, 300), (25, 8200, 270), (1, 40, 33000), (2, 100, 6000), (70, 100, 4112)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
