@@ -9,7 +9,7 @@ namespace {
 
 // The path hangs on a few probabilities, which every workgroup of a sequence looks up for itself, a lane a node; what is read at length is the row behind its
 // end, once for the sums and, the slice in which the drawn token lies, once more.  A sequence's row is dealt to up to 64 workgroups in slices; each leaves its slice's
-// sums and a mark, and the one that finds all marks there finds the slice and, in it, the token.  Sums are held in 64 bits: products of two 32-bit
+// sum and a mark, and the one that finds all marks there finds the slice and, in it, the token.  Sums are held in 64 bits: products of two 32-bit
 // numbers and differences of probabilities are exact in them or nearly, and which token is drawn must not hang on the order of a sum.
 constexpr uint32_t kMostSlices = 64, kThreads = 256, kEach = 8, kStep = kThreads * kEach;      // elements a lane takes, and a workgroup at once
 
@@ -20,35 +20,45 @@ struct Draft {
     const float* uniform;
     int32_t *path, *length, *next;
     unsigned long long* marks;  // [batch][slices]
-    double* sums;               // [batch][slices][2]: of what is left, and of p
+    double* sums;               // [batch][slices], of what is left
     unsigned long long call;
     uint32_t nodes, vocab, slices, slice;       // slice: elements of each, a multiple of kStep
 };
 
 __device__ __forceinline__ double weight(float p) { return p > 0.0f && p < __builtin_inff() ? (double)p : 0.0; }
 
-struct Pair { double a, b; };
 __device__ __forceinline__ double get_shared(const double* p) {
     return __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 __device__ __forceinline__ void put_shared(double* p, double v) {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ double lane_value(double v, int lane) { return __shfl(v, lane); }
+// Lane i's number, the same i in all lanes, without a way through LDS.
+__device__ __forceinline__ double lane_value(double v, uint32_t i) {
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, i), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), i);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+// The sum over a wavefront, in every lane.
+__device__ __forceinline__ double sum_of_wave(double v) {
+#define LC_DPP(ctrl) { \
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v); \
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, ctrl, 0xf, 0xf, false), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), ctrl, 0xf, 0xf, false); \
+    v += __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo); }
+    LC_DPP(0xB1) LC_DPP(0x4E) LC_DPP(0x141) LC_DPP(0x140)     // of sixteen lanes
+#undef LC_DPP
+    return lane_value(v, 0) + lane_value(v, 16) + (lane_value(v, 32) + lane_value(v, 48));
+}
 
-// A lane's eight weights of what is left, and of p, from element `at` on.
+// A lane's eight weights of what is left, from element `at` on: p less q, if there is one, and without what was refused.
 template <int T>
-__device__ __forceinline__ void left_of(const Draft& d, const void* target, uint64_t p_row, const void* draft, uint64_t q_row, const int32_t* gone, uint32_t n_gone,
-                                        uint32_t at, double rest[kEach], double all[kEach]) {
+__device__ __forceinline__ void left_of(const Draft& d, uint64_t p_row, const void* draft, uint64_t q_row, const int32_t* gone, uint32_t n_gone, uint32_t at, double rest[kEach]) {
     const int valid = at < d.vocab ? (int)(d.vocab - at < kEach ? d.vocab - at : kEach) : 0;
     float p[kEach], q[kEach];
-    load_eight<T>(target, p_row + at, valid, p);
+    load_eight<T>(d.target, p_row + at, valid, p);
     if (draft) load_eight<T>(draft, q_row + at, valid, q);
 #pragma unroll
-    for (uint32_t e = 0; e < kEach; ++e) {
-        all[e] = weight(p[e]);
-        rest[e] = draft ? fmax(all[e] - weight(q[e]), 0.0) : all[e];
-    }
+    for (uint32_t e = 0; e < kEach; ++e) rest[e] = draft ? fmax(weight(p[e]) - weight(q[e]), 0.0) : weight(p[e]);
     for (uint32_t g = 0; g < n_gone; ++g) {
         const uint32_t o = (uint32_t)gone[g] - at;
         if (o < kEach)
@@ -61,7 +71,7 @@ template <int T>
 __global__ __launch_bounds__(kThreads) void k_draft_verify(Draft d) {
     __shared__ int32_t gone[64];
     __shared__ uint32_t s_cur, s_gone, s_refused, is_last, s_slice, found, any;
-    __shared__ double s_sum[kThreads / 64][2], s_target, s_before;
+    __shared__ double s_sum[kThreads / 64], s_target, s_before;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, b = blockIdx.y, slice = blockIdx.x;
     if (wave == 0) {                                        // the path
         const uint64_t at = (uint64_t)b * d.nodes;
@@ -112,30 +122,33 @@ __global__ __launch_bounds__(kThreads) void k_draft_verify(Draft d) {
         }
     }
     __syncthreads();
-    const uint32_t n_gone = s_gone;
+    uint32_t n_gone = s_gone;
     const uint64_t p_row = b * d.ld_batch + s_cur * d.ld_row, q_row = b * d.ld_draft_batch + s_cur * d.ld_draft_row;
     const void* draft = s_refused ? d.draft : nullptr;      // (that of node s_cur + 1, which was refused)
-    double rest[kEach], all[kEach];
-    double sum = 0, sum_p = 0;
-    const uint32_t first = slice * d.slice;
-    for (uint32_t at = first; at < first + d.slice && at < d.vocab; at += kStep) {
-        left_of<T>(d, d.target, p_row, draft, q_row, gone, n_gone, at + threadIdx.x * kEach, rest, all);
+    double rest[kEach];
+    // The sum of the elements from `first` to before `end`, in every lane.
+    auto sum_of = [&](uint32_t first, uint32_t end) {
+        double sum = 0;
+        for (uint32_t at = first; at < end && at < d.vocab; at += kStep) {
+            left_of<T>(d, p_row, draft, q_row, gone, n_gone, at + threadIdx.x * kEach, rest);
 #pragma unroll
-        for (uint32_t e = 0; e < kEach; ++e) { sum += rest[e]; sum_p += all[e]; }
-    }
-    for (int x = 32; x; x /= 2) { sum += __shfl_xor(sum, x); sum_p += __shfl_xor(sum_p, x); }
-    if (lane == 0) { s_sum[wave][0] = sum; s_sum[wave][1] = sum_p; }
-    __syncthreads();
-    const uint64_t row = (uint64_t)b * d.slices;
-    if (wave == 0) {
-        if (lane == 0) {
-            sum = sum_p = 0;
-            for (uint32_t w = 0; w < kThreads / 64; ++w) { sum += s_sum[w][0]; sum_p += s_sum[w][1]; }
-            put_shared(d.sums + 2 * (row + slice), sum);
-            put_shared(d.sums + 2 * (row + slice) + 1, sum_p);
+            for (uint32_t e = 0; e < kEach; ++e) sum += rest[e];
         }
-        // The last one to get here goes on: each marks its slice done with the call's number, once its sums have arrived, and looks at the marks of all;
+        sum = sum_of_wave(sum);
+        __syncthreads();
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        sum = 0;
+        for (uint32_t w = 0; w < kThreads / 64; ++w) sum += s_sum[w];
+        return sum;
+    };
+    const double sum = sum_of(slice * d.slice, (slice + 1) * d.slice);
+    const uint64_t row = (uint64_t)b * d.slices;
+    const double u = (double)d.uniform[(uint64_t)b * d.nodes];
+    if (wave == 0) {
+        // The last one to get here goes on: each marks its slice done with the call's number, once its sum has arrived, and looks at the marks of all;
         // whoever marks last finds them all there (should two find that, both write the same).  Marks are taken back, so that a replayed call begins without them.
+        if (lane == 0) put_shared(d.sums + row + slice, sum);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         unsigned long long* marks = d.marks + row;
         if (lane == 0) __hip_atomic_store(marks + slice, d.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -145,62 +158,64 @@ __global__ __launch_bounds__(kThreads) void k_draft_verify(Draft d) {
         if (lane == 0) is_last = done;
         if (done) {
             if (lane < d.slices) __hip_atomic_store(marks + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const double mine = lane < d.slices ? get_shared(d.sums + 2 * (row + lane)) : 0.0, mine_p = lane < d.slices ? get_shared(d.sums + 2 * (row + lane) + 1) : 0.0;
+            const double own = lane < d.slices ? get_shared(d.sums + row + lane) : 0.0;
             // one after the other, so that the sums before a slice and behind the one before it are the same number
-            double total = 0, total_p = 0, before = 0, before_p = 0;
+            double total = 0, before = 0;
             for (uint32_t i = 0; i < d.slices; ++i) {
-                if (i == lane) { before = total; before_p = total_p; }
-                total += lane_value(mine, i);
-                total_p += lane_value(mine_p, i);
+                if (i == lane) before = total;
+                total += lane_value(own, i);
             }
-            const bool from_p = !(total > 0);
-            const double want = (double)d.uniform[(uint64_t)b * d.nodes] * (from_p ? total_p : total);
-            const double own = from_p ? mine_p : mine, ahead = from_p ? before_p : before;
-            const unsigned long long holds = __ballot(own > 0), past = __ballot(own > 0 && ahead + own > want);
+            const double want = u * total;
+            const unsigned long long holds = __ballot(own > 0), past = __ballot(own > 0 && before + own > want);
             // (where rounding leaves no sum above what is wanted: the last slice that holds anything)
             const int at = past ? __builtin_ctzll(past) : holds ? 63 - __builtin_clzll(holds) : 0;
             if (lane == 0) {
                 s_slice = holds ? (uint32_t)at : 0xffffffffu;
-                s_refused = from_p;
                 s_target = want;
             }
-            if ((int)lane == at) s_before = ahead;
+            if ((int)lane == at) s_before = before;
         }
     }
     __syncthreads();
     if (!is_last) return;
-    if (s_slice == 0xffffffffu) {
-        if (threadIdx.x == 0) d.next[b] = -1;
-        return;
+    double want = s_target, before = s_before;
+    uint32_t begin = s_slice * d.slice, end = begin + d.slice;
+    if (s_slice == 0xffffffffu) {                           // nothing is left: of p, all of it
+        draft = nullptr;
+        n_gone = 0;
+        begin = 0;
+        end = d.vocab;
+        const double total = sum_of(begin, end);
+        if (!(total > 0)) {
+            if (threadIdx.x == 0) d.next[b] = -1;
+            return;
+        }
+        want = u * total;
+        before = 0;
     }
-    // The slice again, up to the element at which the running sum passes what is wanted.
-    const bool from_p = s_refused;
-    const double want = s_target;
-    double before = s_before;
-    const uint32_t begin = s_slice * d.slice;
-    for (uint32_t at = begin; at < begin + d.slice && at < d.vocab; at += kStep) {
-        left_of<T>(d, d.target, p_row, draft, q_row, gone, n_gone, at + threadIdx.x * kEach, rest, all);
+    // Once more, up to the element at which the running sum passes what is wanted.
+    for (uint32_t at = begin; at < end && at < d.vocab; at += kStep) {
+        left_of<T>(d, p_row, draft, q_row, gone, n_gone, at + threadIdx.x * kEach, rest);
         double own = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < kEach; ++e) own += from_p ? all[e] : rest[e];
+        for (uint32_t e = 0; e < kEach; ++e) own += rest[e];
         double upto = own;
         for (int x = 1; x < 64; x *= 2) { const double o = __shfl_up(upto, x); if (lane >= (uint32_t)x) upto += o; }
         __syncthreads();
-        if (lane == 63) s_sum[wave][0] = upto;
+        if (lane == 63) s_sum[wave] = upto;
         __syncthreads();
         double run = before;
         for (uint32_t w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) run += s_sum[w][0];
-            before += s_sum[w][0];
+            if (w < wave) run += s_sum[w];
+            before += s_sum[w];
         }
         run += upto - own;
         uint32_t hit = 0xffffffffu, last = 0;
 #pragma unroll
         for (uint32_t e = 0; e < kEach; ++e) {
-            const double w = from_p ? all[e] : rest[e];
-            run += w;
-            if (w > 0 && run > want && hit == 0xffffffffu) hit = at + threadIdx.x * kEach + e;
-            if (w > 0) last = at + threadIdx.x * kEach + e + 1;
+            run += rest[e];
+            if (rest[e] > 0 && run > want && hit == 0xffffffffu) hit = at + threadIdx.x * kEach + e;
+            if (rest[e] > 0) last = at + threadIdx.x * kEach + e + 1;
         }
         if (hit != 0xffffffffu) atomicMin(&found, hit);
         if (last) atomicMax(&any, last);
@@ -210,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_verify(Draft d) {
     if (threadIdx.x == 0) d.next[b] = (int32_t)(found != 0xffffffffu ? found : any - 1);
 }
 
-constexpr uint64_t kMarks = kMostSlices * 8, kSums = kMostSlices * 16;
+constexpr uint64_t kMarks = kMostSlices * 8, kSums = kMostSlices * 8;
 
 }  // namespace
 }  // namespace serve
@@ -237,8 +252,8 @@ int lc_draft_verify(const void* target, uint64_t ld_batch, uint64_t ld_row, uint
     d.draft = nodes > 1 ? draft : nullptr; d.ld_draft_batch = ld_draft_batch; d.ld_draft_row = ld_draft_row;
     d.tokens = tokens; d.parent = parent; d.count = count; d.uniform = uniform; d.path = path; d.length = length; d.next = next;
     d.nodes = (uint32_t)nodes; d.vocab = (uint32_t)vocab;
-    // Slices of at least a step of a workgroup, as many as give the chip three workgroups a compute unit.
-    const uint32_t steps = (d.vocab + kStep - 1) / kStep, want = batch >= 768 ? 1 : (uint32_t)(768 / batch);
+    // Slices of a step of a workgroup each, or of as many as leave eight workgroups a compute unit, which is what fits.
+    const uint32_t steps = (d.vocab + kStep - 1) / kStep, want = batch >= 2048 ? 1 : (uint32_t)(2048 / batch);
     uint32_t slices = want < kMostSlices ? want : kMostSlices;
     slices = slices < steps ? slices : steps;
     d.slice = (steps + slices - 1) / slices * kStep;

@@ -970,21 +970,19 @@ def lc_kv_extend(pages, add, room, new_lens=None, new_count=None, out=None, stre
     """Room for add[b] (int32 [batch]) more tokens of each sequence, of all sequences together at most `room`; the leading sequences for which pages, their rows of the
     table and `room` suffice get theirs.  Returns starts int32 [batch + 1], and of the new tokens slots int64 [room], places and owners int32 [room] (-1 behind the
     last), in out = (starts, slots, places, owners) if given.  The lengths and the number of free pages go to new_lens and new_count (None: into `pages`)."""
-    batch = pages.batch
+    batch, device = pages.batch, pages.lens.device
     if out is None:
-        device = pages.lens.device
-
-        def make():
-            few = torch.empty(batch + 1 + 2 * room, dtype=torch.int32, device=device)      # (one allocation for the three of 32 bits)
-            return torch.empty(room, dtype=torch.int64, device=device), few
-        slots, few = make() if stream is None else _made_on(stream, make)
-        starts, places, owners = few[:batch + 1], few[batch + 1:batch + 1 + room], few[batch + 1 + room:]
+        make = lambda: (torch.empty(room, dtype=torch.int64, device=device), torch.empty(batch + 1, dtype=torch.int32, device=device),
+                        torch.empty(2, room, dtype=torch.int32, device=device))
+        slots, starts, both = make() if stream is None else _made_on(stream, make)
+        places, owners = both.unbind(0)
     else:
         starts, slots, places, owners = out
         assert slots.is_cuda and slots.dtype == torch.int64 and slots.shape == (room,) and slots.is_contiguous()
+        _counts(starts, batch + 1), _counts(places, room), _counts(owners, room)
     st = _lib.lc_kv_extend(pages._p, _counts(add, batch), room, pages.lens.data_ptr() if new_lens is None else _counts(new_lens, batch),
-                           pages.free_count.data_ptr() if new_count is None else _counts(new_count, 1), _counts(starts, batch + 1), slots.data_ptr(),
-                           _counts(places, room), _counts(owners, room), _handle(stream))
+                           pages.free_count.data_ptr() if new_count is None else _counts(new_count, 1), starts.data_ptr(), slots.data_ptr(), places.data_ptr() or None,
+                           owners.data_ptr() or None, _handle(stream))
     if st != OK:
         raise LcError(st)
     return starts, slots, places, owners
@@ -1029,9 +1027,9 @@ def lc_draft_verify(target, tokens, uniform, draft=None, parent=None, count=None
     for t, dtype in ((tokens, torch.int32), (uniform, torch.float32)) if parent is None else ((tokens, torch.int32), (uniform, torch.float32), (parent, torch.int32)):
         assert t.is_cuda and t.dtype == dtype and t.shape == (batch, nodes) and t.is_contiguous()
     if out is None:
-        make = lambda: (torch.empty(batch * (nodes + 2), dtype=torch.int32, device=target.device),)
-        few, = make() if stream is None else _made_on(stream, make)
-        path, length, following = few[:batch * nodes].view(batch, nodes), few[batch * nodes:batch * nodes + batch], few[batch * nodes + batch:]
+        make = lambda: (torch.empty(batch, nodes, dtype=torch.int32, device=target.device), torch.empty(2, batch, dtype=torch.int32, device=target.device))
+        path, few = make() if stream is None else _made_on(stream, make)
+        length, following = few.unbind(0)
     else:
         path, length, following = out
         assert path.is_cuda and path.dtype == torch.int32 and path.shape == (batch, nodes) and path.is_contiguous()
