@@ -13,8 +13,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 //   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens of each 16 in the order 0-3, 8-11, 4-7, 12-15,
 //                    in which V^T is kept
 // so that the running maximum and the sum are one number a lane.  Codes are whole numbers in 16 bits, exactly; scales of keys multiply the scores, scales of values the
-// probabilities, whose product is rounded: to bf16, in fp32 in three parts, and in fp16 measured from a power of two near the largest scale so far, so that products down to
-// 2^-24 of the largest have all of its 11 bits.
+// probabilities, whose product is rounded: in fp32 to three bf16 parts, else to fp16, measured from a power of two near the largest scale so far, so that products down to
+// 2^-24 of the largest have all of its 11 bits (in bf16 their rounding would be as large as the result's own: errors 1.4 times as large).
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostParts = 32, kLeastTiles = 4;       // of a sequence's tokens, and tiles that a part has at least
@@ -35,12 +35,12 @@ struct Prompt {
     FastDiv by_group;
 };
 
-// How many 16-bit parts an element of q, and a probability, are given, and by how much, in powers of two, a score may pass what probabilities are measured from (in fp16
-// they have room for 2^16, of which 2^11 are the scales').
+// How many 16-bit parts an element of q, and a probability, are given; whether keys and queries, and probabilities and values, are fp16 (else bf16); and by how much, in powers
+// of two, a score may pass what probabilities are measured from (in fp16 they have room for 2^16, of which 2^11 are the scales').
 template <int T> struct Kind;
-template <> struct Kind<LC_F32> { static constexpr int kParts = 3; static constexpr bool kHalf = false; static constexpr float kFar = 8; };
-template <> struct Kind<LC_BF16> { static constexpr int kParts = 1; static constexpr bool kHalf = false; static constexpr float kFar = 8; };
-template <> struct Kind<LC_F16> { static constexpr int kParts = 1; static constexpr bool kHalf = true; static constexpr float kFar = 4; };
+template <> struct Kind<LC_F32> { static constexpr int kParts = 3; static constexpr bool kHalf = false, kHalfValues = false; static constexpr float kFar = 8; };
+template <> struct Kind<LC_BF16> { static constexpr int kParts = 1; static constexpr bool kHalf = false, kHalfValues = true; static constexpr float kFar = 4; };
+template <> struct Kind<LC_F16> { static constexpr int kParts = 1; static constexpr bool kHalf = true, kHalfValues = true; static constexpr float kFar = 4; };
 
 template <bool HALF> __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     if (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -56,6 +56,14 @@ template <bool HALF> __device__ __forceinline__ uint32_t pair_of(float a, float 
 __device__ __forceinline__ float other_half(float v) {
     const auto a = __builtin_amdgcn_permlane32_swap(bits_of(v), bits_of(v), false, false);
     return threadIdx.x % 64 < 32 ? float_of(a[1]) : float_of(a[0]);
+}
+
+__device__ __forceinline__ uint32_t largest_of_wave(uint32_t v) {
+    v = max_of_lanes<16>(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = a[0] > a[1] ? a[0] : a[1];
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return b[0] > b[1] ? b[0] : b[1];
 }
 
 __device__ __forceinline__ int32_t held(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -163,14 +171,14 @@ template <int T, int BITS, int D, int kWaves, int PERSIMD>
 __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     using S = Shape<BITS, D, kWaves>;
     constexpr int kRows = 32 * kWaves;
-    constexpr bool HALF = Kind<T>::kHalf;
+    constexpr bool HALF = Kind<T>::kHalf, PHALF = Kind<T>::kHalfValues;
     constexpr int NP = Kind<T>::kParts, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(16))) uint16_t sk[2][kTile][S::kUnits * 8];
     __shared__ __attribute__((aligned(16))) uint16_t sv[2][D][kTile];
     __shared__ __attribute__((aligned(16))) float sks[2][kTile], svs[2][kTile];
     __shared__ uint64_t srow[4][8];                         // where each eight tokens of a tile lie, counted in rows
     __shared__ uint32_t snot[4];                            // which of them lie in pages that are not there
-    __shared__ int sunit[2];                                // fp16: probabilities times scales are counted in 2^sunit
+    __shared__ int sunit[2];                                // 16-bit types: probabilities times scales are counted in 2^sunit
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     const uint32_t head = blockIdx.x % a.c.heads;
     const Own own = own_of<false>(a, blockIdx.x / a.c.heads, lane, kRows);
@@ -272,7 +280,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             value_scale = a.c.v_scale[eights[lane / 8] + lane % 8];
         }
     };
-    int unit = -1000;                                       // fp16: what this wavefront's sums are counted in; and for the first one the tiles so far
+    int unit = -1000;                                       // 16-bit types: what this wavefront's sums are counted in; and for the first one the tiles so far
     int unit_next = -1000;
     auto put_scales = [&](uint32_t buffer) {
         if (wave == 0) {
@@ -281,9 +289,8 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             const bool finite = size < 0x7f800000u;
             sks[buffer][lane] = finite ? key_scale * a.scale : __builtin_nanf("");
             if (!finite) value_scale = 0;
-            if (HALF) {
-                uint32_t most = max_of_lanes<32>(finite ? size : 0);
-                { const uint32_t o = (uint32_t)__shfl_xor((int)most, 32); most = o > most ? o : most; }
+            if (PHALF) {
+                const uint32_t most = largest_of_wave(finite ? size : 0);
                 int e = (int)(most >> 23) - 127 - 10;
                 e = e < -100 ? -100 : e;
                 unit_next = e > unit_next ? e : unit_next;
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             }
             uint32_t to = value_to[l];
             asm("" : "+v"(to));
-            *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) = u32x2{pair_of<HALF>(x[0], x[1]), pair_of<HALF>(x[2], x[3])};
+            *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) = u32x2{pair_of<PHALF>(x[0], x[1]), pair_of<PHALF>(x[2], x[3])};
         }
     };
     auto put_all = [&](uint32_t buffer) { each<kPieces>([&](auto piece) { put(buffer, piece); }); };
@@ -352,6 +359,8 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     // A tile: scores, what probabilities are measured from, probabilities, products with the values.
     auto use = [&](int32_t tile, uint32_t buffer) {         // (and, beside the scores, puts the next one in its place)
         const int32_t tb = tile * kTile;
+        const uint32_t missing = __builtin_amdgcn_readfirstlane(snot[tile % 4]);
+        const int unit_now = PHALF ? __builtin_amdgcn_readfirstlane(sunit[buffer]) : unit;
         // Scores: keys are read four products ahead, and between those the next tile is converted.  (What is written here one after the other stays so: left to
         // itself the compiler reads each key right before its product, and the matrix unit waits.)
         f32x16 score[2];
@@ -384,7 +393,6 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) score[s][4 * g + r] = fmaf(score[s][4 * g + r], ks[r], -from);
             }
-        const uint32_t missing = __builtin_amdgcn_readfirstlane(snot[tile % 4]);
         if (tb + kTile - 1 > wave_first || missing) {       // (else every row sees all of it)
             asm volatile("");                               // (a branch, not 64 selections for every tile)
 #pragma unroll
@@ -400,31 +408,23 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, score[s][e]);
-        if (HALF) {
-            const int next = __builtin_amdgcn_readfirstlane(sunit[buffer]);
-            if (next != unit) {
-                const float shrink = ldexpf(1.0f, unit - next);
-#pragma unroll
-                for (int j = 0; j < DB; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
-                unit = next;
-            }
-        }
-        if (__any(most > Kind<T>::kFar || top == -__builtin_inff())) {
+        // What probabilities are measured from moves only when one would pass 2^kFar, what sums are counted in when a larger scale comes, so sums are seldom rescaled.
+        if (__any(most > Kind<T>::kFar || top == -__builtin_inff()) || unit_now != unit) {
             most = fmaxf(fmaxf(most, other_half(most)) + from, top);
             const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - then);
             sum *= shrink;
+            const float by = PHALF ? ldexpf(shrink, unit - unit_now) : shrink;
 #pragma unroll
             for (int j = 0; j < DB; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[j][e] *= shrink;
+                for (int e = 0; e < 16; ++e) acc[j][e] *= by;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) score[s][e] -= then - from;
             top = most;
             from = then;
+            unit = unit_now;
         }
         // Products with the values, 16 tokens at a time: those of the next 16 are read, and their probabilities worked out, between them.
         uint32_t value_from = c * kTile * 2 + value_unit(c, h) * 16 + buffer * (uint32_t)sizeof(sv[0]);
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             }
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                pp[g % 2][k][pair] = k == NP - 1 ? pair_of<HALF>(p[0], p[1]) : high_halves(bits_of(p[0]), bits_of(p[1]));
+                pp[g % 2][k][pair] = k == NP - 1 ? pair_of<PHALF>(p[0], p[1]) : high_halves(bits_of(p[0]), bits_of(p[1]));
                 if (k < NP - 1)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) p[x] -= float_of(bits_of(p[x]) & 0xffff0000u);
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             each<DB>([&](auto block) {
                 constexpr int j = decltype(block)::value;
 #pragma unroll
-                for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<HALF>(value[j], pp[g % 2][k], acc[j]);
+                for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<PHALF>(value[j], pp[g % 2][k], acc[j]);
                 if constexpr (g < 3) {
                     value[j] = value_at(g + 1, j);
                     each<(j + 1) * 4 / DB - j * 4 / DB>([&](auto n) { probability(g + 1, j * 4 / DB + decltype(n)::value); });
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     const uint64_t at = (uint64_t)(own.first + qi), hd = head * a.group + qg;
     float whole = own.parts > 1 || total == 0.0f ? 1.0f : 1.0f / total;
     whole *= unit_of(BITS);
-    if (HALF) whole = total == 0.0f ? 0.0f : ldexpf(whole, unit);
+    if (PHALF) whole = total == 0.0f ? 0.0f : ldexpf(whole, unit);
     if (own.parts > 1) {
         const uint64_t place_at = ((uint64_t)own.place * a.c.heads + head) * kRows + 32 * wave + c;
         if (h == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * place_at) = f32x2{top, total};

@@ -47,7 +47,7 @@ def want_of(lc, cache, q, starts, table, lens, scale=None):
       scores      q . k of dim terms added up in 32 bits in steps of 16, then scale and key's scale: (dim / 16 + 16 + 4) half steps of |q| . |k| times both at most;
                   exp2 and what scores are measured from: 4 half steps of the score and 4 more; both the numerator's and the sum's
       products    sums over n tokens in steps of 16, joined: n / 16 + 64 half steps of the sum of p |v|
-      roundings   of p times the value's scale to bf16 (2^-8), to fp16 (2^-11, and 2^-35 of the largest so far), in three parts 2^-23
+      roundings   of p times the value's scale to fp16 (2^-11, and 2^-35 of the largest so far), in fp32 in three parts 2^-23
       the result  half a step of its type, and of its smallest numbers"""
     dtype, (_, heads, dim), g = q.dtype, q.shape, q.shape[1] // cache.heads
     out, room = torch.zeros(q.shape, dtype=torch.float64, device=DEV), torch.zeros(q.shape, dtype=torch.float64, device=DEV)
@@ -74,10 +74,10 @@ def want_of(lc, cache, q, starts, table, lens, scale=None):
             size = ((x.abs() @ kk.abs().T) * abs(scale)).masked_fill(~seen, 0.0)
             far = 2 * ((dim / 16 + 20) * size.amax(1) + 4 * score.abs().nan_to_num(0.0, 0.0, 0.0).amax(1) + 4) * eps
             carried = p.nan_to_num(0.0) @ vv.abs().nan_to_num(0.0)
-            each = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[dtype]
+            each = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -11, torch.float16: 2.0 ** -11}[dtype]
             r = carried * (far[:, None] + (n / 16 + 64) * eps + each) * 1.01
-            if dtype == torch.float16:                       # (codes of 127 at most; a row's tiles reach 63 tokens beyond it)
-                r = r + seen.sum(1, keepdim=True) * 2.0 ** -35 * 16 * vv.abs().nan_to_num(0.0).max() + 2.0 ** -25
+            if dtype != torch.float32:                       # (codes of 127 at most; a row's tiles reach 63 tokens beyond it)
+                r = r + seen.sum(1, keepdim=True) * 2.0 ** -35 * 16 * vv.abs().nan_to_num(0.0).max()
             out[first:first + count, h] = o
             room[first:first + count, h] = r + HALF[dtype] * 1.01 * o.abs().nan_to_num(0.0) + (2.0 ** -25 if dtype == torch.float16 else 2.0 ** -133)
     return out, room
