@@ -173,6 +173,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     constexpr int kRows = 32 * kWaves;
     constexpr bool HALF = Kind<T>::kHalf, PHALF = Kind<T>::kHalfValues;
     constexpr int NP = Kind<T>::kParts, KS = D / 16, DB = D / 32;
+    constexpr int kScaler = kWaves - 3, kPlacer = kWaves - 1;      // the wavefronts that see to scales and to places
     __shared__ __attribute__((aligned(16))) uint16_t sk[2][kTile][S::kUnits * 8];
     __shared__ __attribute__((aligned(16))) uint16_t sv[2][D][kTile];
     __shared__ __attribute__((aligned(16))) float sks[2][kTile], svs[2][kTile];
@@ -237,23 +238,23 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         }
     }
 
-    // A tile on its way: the first eight lanes look up where it lies, a tile ahead; codes go to registers and, converted, into LDS.
+    // A tile on its way: eight lanes look up where it lies, a tile ahead; codes go to registers and, converted, into LDS.
     const int32_t* table = a.table + b * a.ld_table;
     int32_t page_raw = 0;
     auto token_of = [&](int32_t tile) {                     // the lane's eight tokens (that begin at a multiple of eight, and so lie together)
-        const int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)(threadIdx.x % 8);
+        const int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)(lane % 8);
         return t < len ? t : (len - 1) & ~7;
     };
     auto look = [&](int32_t tile, uint32_t lanes) {         // (of several tiles that follow each other, eight lanes each)
-        if (threadIdx.x < lanes) page_raw = table[token_of(tile + (int32_t)threadIdx.x / 8) >> a.c.page_shift];
+        if (wave == kPlacer && lane < lanes) page_raw = table[token_of(tile + (int32_t)lane / 8) >> a.c.page_shift];
     };
     auto place_eights = [&](int32_t tile, uint32_t lanes) {
-        if (threadIdx.x >= lanes) return;
-        tile += (int32_t)threadIdx.x / 8;
+        if (wave != kPlacer || lane >= lanes) return;
+        tile += (int32_t)lane / 8;
         const bool there = (uint32_t)page_raw < (uint32_t)a.pages;
-        srow[tile % 4][threadIdx.x % 8] = row_of(a.c, there ? page_raw : 0, head, (uint32_t)token_of(tile) & ((1u << a.c.page_shift) - 1));
+        srow[tile % 4][lane % 8] = row_of(a.c, there ? page_raw : 0, head, (uint32_t)token_of(tile) & ((1u << a.c.page_shift) - 1));
         const unsigned long long missing = __ballot(!there);
-        if (threadIdx.x % 8 == 0) snot[tile % 4] = (uint32_t)(missing >> threadIdx.x) & 255u;
+        if (lane % 8 == 0) snot[tile % 4] = (uint32_t)(missing >> lane) & 255u;
     };
     u32x4 keys[S::kKeyLoads];
     uint32_t values[S::kValueLoads][4];
@@ -275,15 +276,15 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
                 for (int r = 0; r < 4; ++r) values[l][r] = *reinterpret_cast<const uint32_t*>(from + r * S::kRowBytes);
             }
         }
-        if (wave == 0) {
+        if (wave == kScaler) {
             key_scale = a.c.k_scale[eights[lane / 8] + lane % 8];
             value_scale = a.c.v_scale[eights[lane / 8] + lane % 8];
         }
     };
-    int unit = -1000;                                       // 16-bit types: what this wavefront's sums are counted in; and for the first one the tiles so far
+    int unit = -1000;                                       // 16-bit types: what this wavefront's sums are counted in; and for the one that sees to scales the tiles so far
     int unit_next = -1000;
     auto put_scales = [&](uint32_t buffer) {
-        if (wave == 0) {
+        if (wave == kScaler) {
             // A value that is not finite makes all of a result NaN: as well a key that is not does, and products with the values are left without it.
             const uint32_t size = bits_of(value_scale) & 0x7fffffffu;
             const bool finite = size < 0x7f800000u;
