@@ -161,6 +161,8 @@ template <int BITS> struct Word {
 };
 constexpr float unit_of(int bits) { return bits == 4 ? 16.0f : 1.0f; }
 
+// What is left to the compiler's own judgement becomes calls, with registers put away around them, in some of the kernels (heads of 160 in 4 bits twice the time).
+#define LC_INLINE __attribute__((always_inline))
 // f(Number<0>), f(Number<1>) ... of N.
 template <int I> struct Number { static constexpr int value = I; };
 template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F&& f) {
@@ -191,7 +193,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     const int32_t row0 = (blocks - 1 - (int32_t)own.block) * kRows;  // (the rows that see most first)
     const int32_t row_last = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
     const int32_t base = len - own.count;                   // the place of the first new token
-    auto place_of = [&](int32_t row) { return base + (int32_t)a.by_group((uint32_t)row); };
+    auto place_of = [&](int32_t row) LC_INLINE { return base + (int32_t)a.by_group((uint32_t)row); };
     const int32_t tiles_all = place_of(row_last) >= 0 ? place_of(row_last) / kTile + 1 : 0;
     const int32_t per = (tiles_all + (int32_t)own.parts - 1) / (int32_t)own.parts;
     const int32_t tile0 = (int32_t)own.part * per, tile1 = tile0 + per < tiles_all ? tile0 + per : tiles_all;
@@ -241,14 +243,14 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     // A tile on its way: eight lanes look up where it lies, a tile ahead; codes go to registers and, converted, into LDS.
     const int32_t* table = a.table + b * a.ld_table;
     int32_t page_raw = 0;
-    auto token_of = [&](int32_t tile) {                     // the lane's eight tokens (that begin at a multiple of eight, and so lie together)
+    auto token_of = [&](int32_t tile) LC_INLINE {                     // the lane's eight tokens (that begin at a multiple of eight, and so lie together)
         const int32_t t = (tile < tiles_all ? tile : tiles_all - 1) * kTile + 8 * (int32_t)(lane % 8);
         return t < len ? t : (len - 1) & ~7;
     };
-    auto look = [&](int32_t tile, uint32_t lanes) {         // (of several tiles that follow each other, eight lanes each)
+    auto look = [&](int32_t tile, uint32_t lanes) LC_INLINE {         // (of several tiles that follow each other, eight lanes each)
         if (wave == kPlacer && lane < lanes) page_raw = table[token_of(tile + (int32_t)lane / 8) >> a.c.page_shift];
     };
-    auto place_eights = [&](int32_t tile, uint32_t lanes) {
+    auto place_eights = [&](int32_t tile, uint32_t lanes) LC_INLINE {
         if (wave != kPlacer || lane >= lanes) return;
         tile += (int32_t)lane / 8;
         const bool there = (uint32_t)page_raw < (uint32_t)a.pages;
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     u32x4 keys[S::kKeyLoads];
     uint32_t values[S::kValueLoads][4];
     float key_scale = 0, value_scale = 0;
-    auto ask = [&](int32_t tile) {
+    auto ask = [&](int32_t tile) LC_INLINE {
         const uint64_t* eights = srow[tile % 4];
 #pragma unroll
         for (int l = 0; l < S::kKeyLoads; ++l) {
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     };
     int unit = -1000;                                       // 16-bit types: what this wavefront's sums are counted in; and for the one that sees to scales the tiles so far
     int unit_next = -1000;
-    auto put_scales = [&](uint32_t buffer) {
+    auto put_scales = [&](uint32_t buffer) LC_INLINE {
         if (wave == kScaler) {
             // A value that is not finite makes all of a result NaN: as well a key that is not does, and products with the values are left without it.
             const uint32_t size = bits_of(value_scale) & 0x7fffffffu;
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         const uint32_t group = t / 4 % 4, unit = t / 16 * 2 + group % 2, half = group / 2;      // tokens 0-3, 8-11, 4-7, 12-15
         value_to[l] = d * kTile * 2 + value_unit(d, unit) * 16 + half * 8;
     }
-    auto put = [&](uint32_t buffer, auto piece_of) {
+    auto put = [&](uint32_t buffer, auto piece_of) LC_INLINE {
         constexpr int piece = decltype(piece_of)::value;
         if constexpr (piece < kKeyPieces) {
             constexpr int l = piece / (16 / BITS), u = piece % (16 / BITS);
@@ -348,7 +350,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             *reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv[buffer]) + (to ^ (e / 2 * 16)) + e * kTile * 2) = u32x2{pair_of<PHALF>(x[0], x[1]), pair_of<PHALF>(x[2], x[3])};
         }
     };
-    auto put_all = [&](uint32_t buffer) { each<kPieces>([&](auto piece) { put(buffer, piece); }); };
+    auto put_all = [&](uint32_t buffer) LC_INLINE { each<kPieces>([&](auto piece) LC_INLINE { put(buffer, piece); }); };
 
     f32x16 acc[DB];
 #pragma unroll
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     float top = -__builtin_inff(), from = 0, sum = 0;       // the largest score so far (or about that), what probabilities are measured from, their sum
 
     // A tile: scores, what probabilities are measured from, probabilities, products with the values.
-    auto use = [&](int32_t tile, uint32_t buffer) {         // (and, beside the scores, puts the next one in its place)
+    auto use = [&](int32_t tile, uint32_t buffer) LC_INLINE {         // (and, beside the scores, puts the next one in its place)
         const int32_t tb = tile * kTile;
         const uint32_t missing = __builtin_amdgcn_readfirstlane(snot[tile % 4]);
         const int unit_now = PHALF ? __builtin_amdgcn_readfirstlane(sunit[buffer]) : unit;
@@ -371,18 +373,18 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             for (int e = 0; e < 16; ++e) score[s][e] = 0;
         uint32_t key_from = c * S::kUnits * 16 + key_unit<S::kUnits>(c, h) * 16 + buffer * (uint32_t)sizeof(sk[0]);
         asm("" : "+v"(key_from));
-        auto key_at = [&](int i) {
+        auto key_at = [&](int i) LC_INLINE {
             return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sk) + (key_from ^ (i % KS * 32)) + i / KS * 32 * S::kUnits * 16);
         };
         u32x4 key[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) key[i] = key_at(i);
-        each<2 * KS>([&](auto step) {
+        each<2 * KS>([&](auto step) LC_INLINE {
             constexpr int i = decltype(step)::value;
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p) score[i / KS] = mfma<HALF>(key[i % 4], q[i % KS][p], score[i / KS]);
             if constexpr (i + 4 < 2 * KS) key[i % 4] = key_at(i + 4);
-            each<(i + 1) * kPieces / (2 * KS) - i * kPieces / (2 * KS)>([&](auto n) { put(buffer ^ 1, Number<i * kPieces / (2 * KS) + decltype(n)::value>{}); });
+            each<(i + 1) * kPieces / (2 * KS) - i * kPieces / (2 * KS)>([&](auto n) LC_INLINE { put(buffer ^ 1, Number<i * kPieces / (2 * KS) + decltype(n)::value>{}); });
             __builtin_amdgcn_sched_barrier(0);
         });
         ask(tile + 2);
@@ -430,14 +432,14 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         // Products with the values, 16 tokens at a time: those of the next 16 are read, and their probabilities worked out, between them.
         uint32_t value_from = c * kTile * 2 + value_unit(c, h) * 16 + buffer * (uint32_t)sizeof(sv[0]);
         asm("" : "+v"(value_from));
-        auto value_at = [&](int g, int j) { return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sv) + (value_from ^ (g * 32)) + j * 32 * kTile * 2); };
+        auto value_at = [&](int g, int j) LC_INLINE { return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sv) + (value_from ^ (g * 32)) + j * 32 * kTile * 2); };
         u32x4 value[DB], pp[2][NP];
         f32x4 vs[2][2];
-        auto scales_at = [&](int g) {
+        auto scales_at = [&](int g) LC_INLINE {
 #pragma unroll
             for (int x = 0; x < 2; ++x) vs[g % 2][x] = *reinterpret_cast<const f32x4*>(&svs[buffer][16 * g + 8 * x + 4 * h]);
         };
-        auto probability = [&](int g, int pair) {           // two of the lane's eight
+        auto probability = [&](int g, int pair) LC_INLINE {           // two of the lane's eight
             float p[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -459,16 +461,16 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         scales_at(0);
 #pragma unroll
         for (int pair = 0; pair < 4; ++pair) probability(0, pair);
-        each<4>([&](auto group) {
+        each<4>([&](auto group) LC_INLINE {
             constexpr int g = decltype(group)::value;
             if constexpr (g < 3) scales_at(g + 1);
-            each<DB>([&](auto block) {
+            each<DB>([&](auto block) LC_INLINE {
                 constexpr int j = decltype(block)::value;
 #pragma unroll
                 for (int k = NP - 1; k >= 0; --k) acc[j] = mfma<PHALF>(value[j], pp[g % 2][k], acc[j]);
                 if constexpr (g < 3) {
                     value[j] = value_at(g + 1, j);
-                    each<(j + 1) * 4 / DB - j * 4 / DB>([&](auto n) { probability(g + 1, j * 4 / DB + decltype(n)::value); });
+                    each<(j + 1) * 4 / DB - j * 4 / DB>([&](auto n) LC_INLINE { probability(g + 1, j * 4 / DB + decltype(n)::value); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });

@@ -197,3 +197,23 @@ def test_refused(lc):
         lc.lc_i8_linear(x.detach(), w, ws=torch.empty(0, dtype=torch.uint8, device=DEV))
     with pytest.raises(lc.LcError):
         lc.lc_i8_matmul(w, w, dtype=torch.float64)
+
+
+@pytest.mark.parametrize("m", [1, 3, 100])
+def test_a_matrix_beyond_4_gib(lc, m):
+    """The last of w's rows, and of y's columns, whose codes lie beyond 2^32 bytes."""
+    n, k = 70000, 65536
+    w = lc.I8(torch.empty(n, k, dtype=torch.int8, device=DEV), torch.ones(n, device=DEV), k)
+    g = torch.Generator(DEV).manual_seed(m)
+    for at in (0, n - 200):
+        w.codes[at:at + 200] = torch.randint(-127, 128, (200, k), device=DEV, generator=g).to(torch.int8)
+    w.codes[200:n - 200] = 1
+    x = lc.lc_i8_quantize(torch.randn(m, k, device=DEV, generator=g))
+    y = lc.lc_i8_matmul(x, w)
+    for at in (0, n - 200):
+        want, room = product(x.codes, x.scales, w.codes[at:at + 200], w.scales[at:at + 200], None)
+        assert ((y[:, at:at + 200].double() - want).abs() <= room).all()
+    back = lc.lc_i8_dequantize(w, torch.bfloat16)
+    assert torch.equal(back[n - 1], w.codes[n - 1].to(torch.bfloat16))
+    again = lc.lc_i8_quantize(back[n - 3:])
+    assert torch.equal(again.codes, coded(back[n - 3:])[0])
