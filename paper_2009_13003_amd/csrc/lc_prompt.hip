@@ -15,6 +15,11 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // so that the running maximum and the sum are one number a lane.  Codes are whole numbers in 16 bits, exactly; scales of keys multiply the scores, scales of values the
 // probabilities, whose product is rounded: in fp32 to three bf16 parts, else to fp16, measured from a power of two near the largest scale so far, so that products down to
 // 2^-24 of the largest have all of its 11 bits (in bf16 their rounding would be as large as the result's own: errors 1.4 times as large).
+// 2048 of 10000 tokens of 32 / 8 heads of 128 in 8 bits, bf16: 335 us (340 to 350 on some cards), 900 TFLOP/s, where a large library product's rate would give 211.  Per 32 rows by 64
+// tokens 32 matrix instructions stand beside 280 of the vector unit: 63 for conversions, 32 exponentials, 128 for scores, sums, scales and roundings.  The matrix unit
+// has 44% of the cycles, vector instructions 56%, LDS 46%, and the clock stands at 1.9 GHz: fewer vector instructions (scales in the values, 48 fewer, sums by the
+// matrix unit) and wavefronts that take turns on a SIMD changed nothing or cost 2%.  9 sequences of 57 to 517 new tokens of up to 3001, 32 heads, 4 bits, fp16: 100 us, of which the
+// join 11; 25 blocks of rows a head of which a third are partly filled, and codes converted for 128 rows at most.  fp32, three parts each: 2 of 333 of 1500 tokens 23 and 9 us.
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostParts = 32, kLeastTiles = 4;       // of a sequence's tokens, and tiles that a part has at least
@@ -588,14 +593,14 @@ __global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t rows)
     }
 }
 
-// How rows are dealt to workgroups.  Eight wavefronts a workgroup share conversions (2048 of 10000 tokens of 32 / 8 heads 323 us for 355 with four) where two a SIMD have the
-// registers and rows are many; sequences of few rows leave much of 256 unused (9 of 57 to 517 tokens 155 for 141).  Splitting is left out where rows fill the chip: once if
-// all is one sequence, else four times.
+// How rows are dealt to workgroups.  Eight wavefronts a workgroup share conversions (2048 of 10000 tokens of 32 / 8 heads 323 us for 355 with four, 512 of 8192 97 for 107) where two
+// a SIMD have the registers and rows are many; sequences of few rows leave much of 256 unused (9 of 57 to 517 tokens 155 for 141).  Splitting is left out where rows fill the
+// chip: once if all is one sequence, else four times.
 struct Deal { uint32_t waves, blocks, share, most_parts; };
 Deal deal_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads, bool two) {
     const uint64_t sequences = tokens < batch ? tokens : batch;      // those with new tokens
     Deal d;
-    d.waves = two && tokens * group / 256 * kv_heads >= 256 && tokens * group >= 1024 * sequences ? 8 : 4;
+    d.waves = two && tokens * group / 256 * kv_heads >= 64 && tokens * group >= 1024 * sequences ? 8 : 4;
     const uint64_t rows = 32 * d.waves, chip = two && d.waves == 4 ? 512 : 256;      // workgroups that are on the chip at once
     d.blocks = (uint32_t)((tokens * group + rows - 1) / rows + sequences);
     d.share = (uint32_t)(chip > kv_heads ? chip / kv_heads : 1);
