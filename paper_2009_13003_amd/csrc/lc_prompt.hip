@@ -31,6 +31,7 @@ struct Prompt {
     const int32_t* table; uint64_t ld_table; uint64_t table_pages;
     const int32_t* lens;
     void* out; uint64_t ld_out;
+    uint32_t* deal;             // of more than 64 sequences: how they are dealt (k_kv_prompt_deal); else NULL
     float* stats;               // the maximum and the sum of each [place of a part][row]
     float* part;                // [place of a part][row][dim]
     float scale;                // times log2(e)
@@ -81,65 +82,111 @@ struct Own {
     uint32_t b, block, part, parts, place;      // place: of the part, among those of all sequences that are split
     int32_t first, count;                       // the sequence's first new token and how many it has
 };
-// JOIN: of blocks of rows that are split, counted by themselves.
+struct Work { int32_t first, end; uint32_t blocks, tiles; };
+__device__ __forceinline__ Work work_of(const Prompt& a, uint32_t b, uint32_t rows) {
+    if (b >= a.batch) return {0, 0, 0, 0};
+    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
+    const int32_t s = held(a.starts[b], 0, (int32_t)a.tokens), e = held(a.starts[b + 1], 0, (int32_t)a.tokens);
+    return {s, e, e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + rows - 1) / rows) : 0, (uint32_t)(held(a.lens[b], 0, room) + kTile - 1) / kTile};
+}
+__device__ __forceinline__ uint32_t even_of(const Prompt& a, uint64_t work) {
+    const uint64_t t = (work + a.share - 1) / a.share;
+    return a.most_parts == 1 ? 0x7fffffffu : t < kLeastTiles ? kLeastTiles : t < 0x7fffffffu ? (uint32_t)t : 0x7fffffffu;
+}
+__device__ __forceinline__ uint32_t parts_of(const Prompt& a, uint32_t tiles, uint32_t even) {
+    const uint32_t parts = tiles > even + even / 4 ? (tiles + even - 1) / even : 1;
+    return parts < a.most_parts ? parts : a.most_parts;
+}
+// JOIN: of blocks of rows that are split, counted by themselves.  Of up to 64 sequences the longest first, so that no long one begins when the others end.
 template <bool JOIN>
 __device__ __forceinline__ Own own_of(const Prompt& a, uint32_t unit, uint32_t lane, uint32_t rows) {
-    const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
-    int32_t s = 0, e = 0;
-    auto blocks_of = [&](uint32_t b, uint32_t& tiles) {
-        s = held(b < a.batch ? a.starts[b] : 0, 0, (int32_t)a.tokens);
-        e = held(b < a.batch ? a.starts[b + 1] : 0, 0, (int32_t)a.tokens);
-        tiles = b < a.batch ? (uint32_t)(held(a.lens[b], 0, room) + kTile - 1) / kTile : 0;
-        return e > s ? (uint32_t)(((uint64_t)(e - s) * a.group + rows - 1) / rows) : 0;
-    };
-    auto over_lanes = [](uint64_t v) { for (int x = 32; x; x /= 2) v += __shfl_xor(v, x); return v; };
-    uint32_t even = 0xffffffffu;
-    if (a.most_parts > 1) {
-        uint64_t work = 0;
-        for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
-            uint32_t tiles;
-            const uint32_t blocks = blocks_of(b0 + lane, tiles);
-            work += over_lanes((uint64_t)blocks * tiles);
+    if (a.deal) {
+        const uint32_t step = a.batch + 1, *before = a.deal + (JOIN ? step : 0), *places = a.deal + 2 * step;
+        if (unit >= before[a.batch]) return {0, 0, 0, 0, 0, 0, 0};
+        uint32_t lo = 0, hi = a.batch;                      // the last sequence that begins at `unit` or before
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (before[mid] <= unit) lo = mid; else hi = mid;
         }
-        const uint64_t t = (work + a.share - 1) / a.share;
-        even = t < kLeastTiles ? kLeastTiles : (uint32_t)t;
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        const Work w = work_of(a, lo, rows);
+        const uint32_t parts = parts_of(a, w.tiles, a.deal[3 * step]), at = unit - before[lo], block = JOIN ? at : at / parts, part = JOIN ? 0 : at - block * parts;
+        return {lo, block, part, parts, places[lo] + block * parts + part, w.first, w.end - w.first};
     }
-    uint32_t before = 0, places = 0;
-    for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
-        uint32_t tiles;
-        const uint32_t blocks = blocks_of(b0 + lane, tiles);
-        uint32_t parts = tiles > even + even / 4 ? (tiles + even - 1) / even : 1;
-        parts = parts < a.most_parts ? parts : a.most_parts;
-        const uint32_t own = JOIN ? (parts > 1 ? blocks : 0) : blocks * parts, held_places = parts > 1 ? blocks * parts : 0;
-        // of each 64 the longest sequences first, so that no long one begins when the others end
-        uint32_t upto = own, places_upto = held_places, all = 0, all_places = 0;
-        const int there = (int)(a.batch - b0 < 64 ? a.batch - b0 : 64);
-        for (int j = 0; j < there; ++j) {
-            const uint32_t t = __builtin_amdgcn_readlane(tiles, j), o = __builtin_amdgcn_readlane(own, j), p = __builtin_amdgcn_readlane(held_places, j);
-            const bool ahead = t > tiles || (t == tiles && j < (int)lane);
-            upto += ahead ? o : 0;
-            places_upto += ahead ? p : 0;
-            all += o;
-            all_places += p;
-        }
-        const unsigned long long mine = __ballot(before + upto > unit && before + upto - own <= unit);
-        if (mine) {
-            const int from = __builtin_ctzll(mine);
-            Own r;
-            r.b = b0 + from;
-            r.parts = __builtin_amdgcn_readlane(parts, from);
-            r.first = __builtin_amdgcn_readlane(s, from);
-            r.count = __builtin_amdgcn_readlane(e, from) - r.first;
-            const uint32_t at = unit - (before + __builtin_amdgcn_readlane(upto, from) - __builtin_amdgcn_readlane(own, from));
-            r.block = JOIN ? at : at / r.parts;
-            r.part = JOIN ? 0 : at - r.block * r.parts;
-            r.place = places + __builtin_amdgcn_readlane(places_upto, from) - __builtin_amdgcn_readlane(held_places, from) + r.block * r.parts + r.part;
-            return r;
-        }
-        before += all;
-        places += all_places;
+    const Work w = work_of(a, lane, rows);
+    uint64_t work = (uint64_t)w.blocks * w.tiles;
+    if (a.most_parts > 1)
+        for (int x = 32; x; x /= 2) work += __shfl_xor(work, x);
+    const uint32_t parts = parts_of(a, w.tiles, even_of(a, work));
+    const uint32_t own = JOIN ? (parts > 1 ? w.blocks : 0) : w.blocks * parts, held_places = parts > 1 ? w.blocks * parts : 0;
+    uint32_t upto = own, places_upto = held_places;
+    for (int j = 0; j < (int)a.batch; ++j) {
+        const uint32_t t = __builtin_amdgcn_readlane(w.tiles, j), o = __builtin_amdgcn_readlane(own, j), p = __builtin_amdgcn_readlane(held_places, j);
+        const bool ahead = t > w.tiles || (t == w.tiles && j < (int)lane);
+        upto += ahead ? o : 0;
+        places_upto += ahead ? p : 0;
     }
-    return {0, 0, 0, 0, 0, 0, 0};
+    const unsigned long long mine = __ballot(lane < a.batch && upto > unit && upto - own <= unit);
+    if (!mine) return {0, 0, 0, 0, 0, 0, 0};
+    const int from = __builtin_ctzll(mine);
+    Own r;
+    r.b = from;
+    r.parts = __builtin_amdgcn_readlane(parts, from);
+    r.first = __builtin_amdgcn_readlane(w.first, from);
+    r.count = __builtin_amdgcn_readlane(w.end, from) - r.first;
+    const uint32_t at = unit - (__builtin_amdgcn_readlane(upto, from) - __builtin_amdgcn_readlane(own, from));
+    r.block = JOIN ? at : at / r.parts;
+    r.part = JOIN ? 0 : at - r.block * r.parts;
+    r.place = __builtin_amdgcn_readlane(places_upto, from) - __builtin_amdgcn_readlane(held_places, from) + r.block * r.parts + r.part;
+    return r;
+}
+
+// How more than 64 sequences are dealt, once for all workgroups: of each the units before it, the blocks that are split and the places of their parts, and what is even.
+// One workgroup, a run of sequences a lane.
+__global__ __launch_bounds__(1024) void k_kv_prompt_deal(Prompt a, uint32_t rows) {
+    __shared__ uint64_t works[1024];
+    __shared__ uint32_t sums[3][1024];
+    const uint32_t each = (a.batch + 1023) / 1024, first = threadIdx.x * each, end = first + each < a.batch ? first + each : a.batch, step = a.batch + 1;
+    uint64_t work = 0;
+    for (uint32_t b = first; b < end; ++b) { const Work w = work_of(a, b, rows); work += (uint64_t)w.blocks * w.tiles; }
+    works[threadIdx.x] = work;
+    __syncthreads();
+    for (uint32_t x = 512; x; x /= 2) {
+        if (threadIdx.x < x) works[threadIdx.x] += works[threadIdx.x + x];
+        __syncthreads();
+    }
+    const uint32_t even = even_of(a, works[0]);
+    uint32_t mine[3] = {0, 0, 0};
+    for (uint32_t b = first; b < end; ++b) {
+        const Work w = work_of(a, b, rows);
+        const uint32_t parts = parts_of(a, w.tiles, even);
+        mine[0] += w.blocks * parts;
+        mine[1] += parts > 1 ? w.blocks : 0;
+        mine[2] += parts > 1 ? w.blocks * parts : 0;
+    }
+    for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = mine[k];
+    __syncthreads();
+    for (uint32_t x = 1; x < 1024; x *= 2) {
+        uint32_t before[3];
+        for (int k = 0; k < 3; ++k) before[k] = threadIdx.x >= x ? sums[k][threadIdx.x - x] : 0;
+        __syncthreads();
+        for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] += before[k];
+        __syncthreads();
+    }
+    uint32_t run[3];
+    for (int k = 0; k < 3; ++k) run[k] = sums[k][threadIdx.x] - mine[k];
+    for (uint32_t b = first; b < end; ++b) {
+        const Work w = work_of(a, b, rows);
+        const uint32_t parts = parts_of(a, w.tiles, even);
+        for (int k = 0; k < 3; ++k) a.deal[k * step + b] = run[k];
+        run[0] += w.blocks * parts;
+        run[1] += parts > 1 ? w.blocks : 0;
+        run[2] += parts > 1 ? w.blocks * parts : 0;
+    }
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < 3; ++k) a.deal[k * step + a.batch] = sums[k][1023];
+        a.deal[3 * step] = even;
+    }
 }
 
 template <int BITS, int D, int kWaves> struct Shape {
@@ -608,12 +655,14 @@ Deal deal_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads,
     return d;
 }
 bool two_fit(int dtype, uint32_t dim) { return dtype != LC_F32 && dim <= 128; }        // two wavefronts a SIMD have the registers
+uint64_t deal_bytes(uint64_t batch) { return batch > 64 ? ((3 * (batch + 1) + 1) * 4 + 255) / 256 * 256 : 0; }
 uint64_t places_of(const Deal& d, uint32_t kv_heads) { return d.most_parts == 1 ? 0 : 2ull * d.share * kv_heads; }
 
 template <int T, int BITS, int D>
 void prompt_of(const Prompt& a, const Deal& d, hipStream_t s) {
     constexpr int PERSIMD = T == LC_F32 || D > 128 ? 1 : 2;
     const uint32_t units = (d.blocks + (a.most_parts > 1 ? d.share : 0)) * a.c.heads;
+    if (a.deal) k_kv_prompt_deal<<<1, 1024, 0, s>>>(a, 32 * (PERSIMD == 2 ? d.waves : 4));
     if constexpr (PERSIMD == 2)
         if (d.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<units, 512, 0, s>>>(a); return; }
     k_kv_prompt<T, BITS, D, 4, PERSIMD><<<units, 256, 0, s>>>(a);
@@ -654,7 +703,7 @@ size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, 
         const uint64_t rows = places_of(d, (uint32_t)kv_heads) * 32 * d.waves;
         most = rows > most ? rows : most;
     }
-    return (size_t)((most * 8 + 255) / 256 * 256 + most * dim * 4 + 256);
+    return (size_t)((most * 8 + 255) / 256 * 256 + most * dim * 4 + 256 + deal_bytes(batch));
 }
 
 int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,
@@ -680,8 +729,9 @@ int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, 
     const Deal d = deal_of(tokens, batch, a.group, a.c.heads, two_fit(dtype, a.c.dim));
     a.share = d.share;
     a.most_parts = a.table_pages << a.c.page_shift <= (kLeastTiles + kLeastTiles / 4) * kTile ? 1 : d.most_parts;
-    a.stats = static_cast<float*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (places_of(d, a.c.heads) * 32 * d.waves * 8 + 255) / 256 * 256);
+    a.deal = batch > 64 ? static_cast<uint32_t*>(ws) : nullptr;
+    a.stats = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + deal_bytes(batch));
+    a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.stats) + (places_of(d, a.c.heads) * 32 * d.waves * 8 + 255) / 256 * 256);
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define CALL(T) do { if (cache->bits == 8) prompt<T, 8>(a, d, s); else prompt<T, 4>(a, d, s); } while (0)
     if (dtype == LC_F32) CALL(LC_F32);

@@ -264,6 +264,31 @@ def test_many_sequences(lc):
     run(lc, 11, new, lens, 4, 2, 64, 8, torch.bfloat16, 8)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_than_64_sequences_some_of_them_split(lc, dtype):
+    """One long one among many short ones, empty ones among them, in any order; and 64 and 65 of them."""
+    for batch, heads, kv in ((70, 4, 2), (64, 2, 2), (65, 2, 2), (1100, 2, 1)):
+        new = [(b * 7) % 5 for b in range(batch)]
+        lens = [max(1, n + (b * 11) % 40) for b, n in enumerate(new)]
+        new[batch // 2], lens[batch // 2] = 100, 1500
+        new[3], lens[3] = 40, 900
+        run(lc, batch, new, lens, heads, kv, 32, 8, dtype, 8)
+
+
+def test_as_many_sequences_as_there_may_be(lc):
+    """65535 of a token each, all over one page, and of none: the same as one alone."""
+    cache, table = filled(lc, 16, [8], 1, 32, 8, 8)
+    q = torch.randn(1, 2, 32, device=DEV).to(torch.bfloat16)
+    want = lc.lc_kv_attend_prompt(cache, q, ints([0, 1]), table, ints([5]))
+    n = 65535
+    got = lc.lc_kv_attend_prompt(cache, q.expand(n, 2, 32).contiguous(), torch.arange(n + 1, dtype=torch.int32, device=DEV), table.expand(n, 1).contiguous(),
+                                 torch.full((n,), 5, dtype=torch.int32, device=DEV))
+    assert torch.equal(got, want.expand(n, 2, 32))
+    starts = torch.ones(n + 1, dtype=torch.int32, device=DEV)
+    starts[:30000] = 0
+    assert torch.equal(lc.lc_kv_attend_prompt(cache, q, starts, table.expand(n, 1).contiguous(), torch.full((n,), 5, dtype=torch.int32, device=DEV)), want)
+
+
 def test_a_long_cache(lc):
     """Codes beyond 4 GiB from where they begin."""
     pages, kv, page, dim = 9000, 8, 512, 128
