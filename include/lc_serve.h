@@ -167,7 +167,8 @@ int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, 
 
 /*
  * The pages of sequences that share a cache.  table and lens are those that attention takes; free_pages is a stack of the pages that nobody has, with
- * *free_count of them (both on the device), the next one to be given out last.
+ * *free_count of them (both on the device), the next one to be given out last.  No page is on the stack twice, and none has two owners: a page that two rows of the
+ * table name would go back twice.
  */
 typedef struct lc_kv_pages {
     int32_t* table;         /* [batch][ld_table]; entries behind a sequence's pages may hold anything */

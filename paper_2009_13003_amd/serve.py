@@ -130,6 +130,10 @@ class Decoder:
     def read_prompts(self, prompts):
         """Puts prompts of unlike lengths (a list of tokens a sequence, none of them empty) into the cache in one pass; the logits [batch][vocab] behind their last
         tokens.  The sequences share their pages."""
+        if self.pages is None:
+            raise ValueError("prompts of unlike lengths need a cache whose pages are shared")
+        if len(prompts) != self.batch or not all(len(p) for p in prompts):
+            raise ValueError("one prompt a sequence, of a token or more")
         s, device = self.shape, self.lens.device
         add = [len(p) for p in prompts]
         self.room_for(add)
@@ -184,6 +188,8 @@ def write_on(model, prompt, count, drafts=2, guess=seen_before, sample=None, tem
     """The `count` tokens a sequence that model writes behind prompt ([batch][n], or a list of tokens a sequence), each the likeliest, or drawn with the random numbers of
     `sample`; and the number of passes it took.  With drafts, a pass judges the known next token and, below it, a tree: `drafts` of the tokens that guess(b, tokens of
     sequence b) lists to follow, and one below each, as long as the model's context has room for the tree."""
+    if sample is not None and not temperature >= 1e-30:     # (logits divided by less might not be finite)
+        raise ValueError("a temperature above zero")
     batch, device = model.batch, model.lens.device
     if torch.is_tensor(prompt):
         known, logits = [p.tolist() for p in prompt], model.read_in(prompt)

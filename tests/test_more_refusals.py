@@ -147,3 +147,20 @@ def test_draft_arguments(lib):
         a = dict(ok)
         a[name] = value
         assert lib.lc_draft_verify(*(a[n] for n in names), None) == want, (name, value)
+
+
+def test_prompts_and_temperatures_of_the_decoder():
+    """Refused before anything is counted or enqueued."""
+    from paper_2009_13003_amd import serve
+    model = serve.Decoder.__new__(serve.Decoder)
+    model.batch, model.count, model.pages = 2, [0, 0], None
+    with pytest.raises(ValueError, match="shared"):
+        model.read_prompts([[1], [2]])
+    model.pages = object()
+    for prompts in ([[1]], [[1], [2], [3]], [[1], []], [[], []]):
+        with pytest.raises(ValueError, match="a token or more"):
+            model.read_prompts(prompts)
+    for temperature in (0.0, -1.0, 1e-40, float("nan")):
+        with pytest.raises(ValueError, match="temperature"):
+            serve.write_on(model, [[1], [2]], 3, sample=object(), temperature=temperature)
+    assert model.count == [0, 0]
