@@ -246,6 +246,84 @@ __global__ __launch_bounds__(512, 6) void k_i8_one_row(Product p, const void* x,
     put(p, col, result_of(p, sum, sx, p.sw[col], col));
 }
 
+// The same for 2 to 16 rows that are short: eights of their elements a lane, at most R of them, so that x is read once, and its largest by atomics in LDS.  2 rows by 4096x4096 6.5 us (in
+// two launches 7.3), 8 by 1024x1024 5.8 (7.3), 16 by 4096x512 5.9 (6.5).  Beyond two eights a lane every workgroup has too much of x to do: 4 rows by 4096x4096 8.9 (7.9), 7 by 1000x2043 8.1 (7.4).
+constexpr uint32_t kShort = 8192;                           // elements of all rows at most
+template <int T, int R>
+__global__ __launch_bounds__(512, 6) void k_i8_short_rows(Product p, const void* x, uint64_t ldx, uint32_t k, FastDiv by_row) {
+    constexpr uint32_t WAVES = 8, S = 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t codes[];      // of x, a row every k16 + 16 bytes
+    __shared__ uint32_t tops[16];
+    __shared__ int sums[WAVES][16][17];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, h = lane / 16, pitch = p.k16 + 16;
+    const uint32_t n0 = blockIdx.x * 16, j = n0 + c < p.n ? n0 + c : p.n - 1;
+    const uint8_t* w = p.w + j * p.w_pitch;
+    u32x4 a[S][2];
+    auto load = [&](uint32_t k0) {
+#pragma unroll
+        for (uint32_t s = 0; s < S; ++s)
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t at = k0 + s * WAVES * 128 + 32 * h + 16 * i;
+                a[s][i] = load_once<u32x4>(w + (at < p.k16 ? at : 0));
+            }
+    };
+    load(wave * 128);
+    if (threadIdx.x < 16) tops[threadIdx.x] = 0;
+    float v[R][8];
+    uint32_t row[R], at[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t i = r * 512 + threadIdx.x;
+        row[r] = by_row(i);
+        at[r] = (i - row[r] * by_row.d) * 8;
+        load_eight<T>(x, row[r] * ldx + at[r], row[r] < p.m && at[r] < k ? (int)(k - at[r] < 8 ? k - at[r] : 8) : 0, v[r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t most = largest_of(v[r], 0), first = __builtin_amdgcn_readfirstlane(row[r]);
+        if (__all(row[r] == first)) {
+            const uint32_t all = largest_of_wave(most);
+            if (lane == 0 && first < p.m) atomicMax(&tops[first], all);
+        } else if (row[r] < p.m) atomicMax(&tops[row[r]], most);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (row[r] < p.m) {
+            float inv;
+            scale_of(tops[row[r]], inv);
+            *reinterpret_cast<u32x2*>(codes + row[r] * pitch + at[r]) = codes_of(v[r], inv);
+        }
+    __syncthreads();
+    i32x4 acc = {0, 0, 0, 0};
+    const uint8_t* own = codes + (c < p.m ? c : 0) * pitch; // (rows that are not there give results that nothing takes)
+    for (uint32_t k0 = wave * 128; k0 < p.k16; k0 += S * WAVES * 128) {
+        if (k0 != wave * 128) load(k0);
+#pragma unroll
+        for (uint32_t s = 0; s < S; ++s)
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t place = k0 + s * WAVES * 128 + 32 * h + 16 * i;
+                u32x4 b = *reinterpret_cast<const u32x4*>(own + (place < p.k16 ? place : 0));
+                if (place >= p.k16) b = u32x4{0, 0, 0, 0};
+                acc = mfma_16(b, a[s][i], acc);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sums[wave][4 * h + r][c] = acc[r];
+    __syncthreads();
+    const uint32_t i = threadIdx.x / 16, col = n0 + threadIdx.x % 16;
+    if (i >= p.m || col >= p.n) return;
+    int sum = 0;
+#pragma unroll
+    for (uint32_t v = 0; v < WAVES; ++v) sum += sums[v][i][threadIdx.x % 16];
+    float inv;
+    const float sx = scale_of(tops[i], inv);
+    put(p, i * p.ldy + col, result_of(p, sum, sx, p.sw[col], col));
+}
+
 // 16 bytes of each lane's own place into LDS at `to` + 16 lane, without passing through registers.
 __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
@@ -459,6 +537,14 @@ void multiply(const Product& p, hipStream_t s) {
     }
 }
 
+template <int T>
+void short_rows(const Product& p, const void* x, uint64_t ldx, uint32_t k, hipStream_t s) {
+    const uint32_t blocks = (p.n + 15) / 16, lds = p.m * (p.k16 + 16);
+    const FastDiv by_row(p.k16 / 8);
+    if (p.m * p.k16 <= kShort / 2) k_i8_short_rows<T, 1><<<blocks, 512, lds, s>>>(p, x, ldx, k, by_row);
+    else k_i8_short_rows<T, 2><<<blocks, 512, lds, s>>>(p, x, ldx, k, by_row);
+}
+
 bool bad_result(const lc_i8* w8, uint64_t m, const void* bias, const void* y, uint64_t ldy, int dtype) {
     return !y || off(y, size_of(dtype)) || off(bias, size_of(dtype)) || ldy > (1ull << 40) || (m > 1 && ldy < w8->n);
 }
@@ -516,7 +602,6 @@ int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const
     if (bad_result(w8, m, bias, y, ldy, dtype) || (w8->k && (!x || off(x, size_of(dtype)))) || (m > 1 && ldx < w8->k) || ldx > (1ull << 40)) return LC_ERR_BADARG;
     if (!ws || off(ws, 256) || ws_bytes < lc_i8_workspace_bytes(m, w8->k)) return LC_ERR_WORKSPACE;
     const uint64_t row = (w8->k + 15) / 16 * 16;
-    // (Each row is a load and a meeting more: two rows and more by 4096 and more take as long in two launches, 7 rows by 1000x2043 10.6 us for 11.5.)
     if (w8->k && m == 1 && row <= kFused && w8->n <= (1u << 26)) {
         const Product p = {nullptr, static_cast<const uint8_t*>(w8->codes), nullptr, w8->scales, bias, y, 0, w8->pitch, ldy, (uint32_t)m, (uint32_t)w8->n, (uint32_t)row, dtype};
         const uint32_t blocks = (p.n + 15) / 16, lds = (uint32_t)row, k = (uint32_t)w8->k;
@@ -524,6 +609,14 @@ int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const
         if (dtype == LC_F32) k_i8_one_row<LC_F32><<<blocks, 512, lds, s>>>(p, x, k);
         else if (dtype == LC_BF16) k_i8_one_row<LC_BF16><<<blocks, 512, lds, s>>>(p, x, k);
         else k_i8_one_row<LC_F16><<<blocks, 512, lds, s>>>(p, x, k);
+        return launched();
+    }
+    if (w8->k && m > 1 && m <= 16 && m * row <= kShort && w8->n <= (1u << 26)) {
+        const Product p = {nullptr, static_cast<const uint8_t*>(w8->codes), nullptr, w8->scales, bias, y, 0, w8->pitch, ldy, (uint32_t)m, (uint32_t)w8->n, (uint32_t)row, dtype};
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        if (dtype == LC_F32) short_rows<LC_F32>(p, x, ldx, (uint32_t)w8->k, s);
+        else if (dtype == LC_BF16) short_rows<LC_BF16>(p, x, ldx, (uint32_t)w8->k, s);
+        else short_rows<LC_F16>(p, x, ldx, (uint32_t)w8->k, s);
         return launched();
     }
     const lc_i8 x8 = {ws, reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + (m * row + 255) / 256 * 256), m, w8->k, row};

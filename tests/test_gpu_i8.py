@@ -108,6 +108,25 @@ def test_products(lc, m, n, k, dtype):
     assert torch.equal(got, lc.lc_i8_matmul(lc.lc_i8_quantize(x), w, bias, dtype))
 
 
+# few rows that one launch works out the codes of: one and two eights a lane, rows that share a wavefront, the last sizes that fit and the first that do not
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(2, 33, 1), (16, 1, 17), (9, 15, 100), (2, 200, 2048), (4, 31, 1030), (16, 100, 256), (2, 300, 4096), (2, 40, 4081), (2, 40, 4097), (4, 17, 2043),
+                                   (8, 1024, 1024), (15, 50, 544), (15, 50, 545), (16, 2000, 511), (3, 2500, 2720), (3, 16, 2721), (17, 30, 300)])
+def test_short_rows(lc, m, n, k, dtype):
+    g = torch.Generator(DEV).manual_seed(m + n + k)
+    x, w = torch.randn(m, k + 5, device=DEV, generator=g).to(dtype)[:, :k], lc.lc_i8_quantize(0.05 * torch.randn(n, k, device=DEV, generator=g))
+    x[m // 2] = 0
+    bias = torch.randn(n, device=DEV, generator=g).to(dtype)
+    out = torch.full((m + 1, n + 3), 9.0, dtype=dtype, device=DEV)
+    lc.lc_i8_linear(x, w, bias, out=out[:m, :n])
+    assert torch.equal(out[:m, :n], lc.lc_i8_matmul(lc.lc_i8_quantize(x), w, bias, dtype)) and (out[m] == 9).all() and (out[:, n:] == 9).all()
+    want, room = product(*coded(x), w.codes[:, :k], w.scales, bias)
+    room = room + (1.01 * HALF[dtype] * want.abs() + LEAST[dtype] if dtype != torch.float32 else 0)
+    assert ((out[:m, :n].double() - want).abs() <= room).all()
+    for i in range(m):
+        assert torch.equal(lc.lc_i8_linear(x[i:i + 1], w, bias)[0], out[i, :n])
+
+
 @pytest.mark.parametrize("m", [1, 20, 200])
 def test_extreme_codes(lc, m):
     """The largest sums there are, at the largest width; bytes behind a row of w that are not zeros; a code of -128."""
