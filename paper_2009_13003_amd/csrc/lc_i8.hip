@@ -111,9 +111,12 @@ struct Product {
     int dtype;
 };
 
+__device__ __forceinline__ float bias_of(const Product& p, uint32_t j) {
+    return !p.bias ? 0.0f : p.dtype == LC_F32 ? load_one<LC_F32>(p.bias, j) : p.dtype == LC_BF16 ? load_one<LC_BF16>(p.bias, j) : load_one<LC_F16>(p.bias, j);
+}
 __device__ __forceinline__ float result_of(const Product& p, int sum, float sx, float sw, uint32_t j) {
     float v = (float)sum * sx * sw;
-    if (p.bias) v += p.dtype == LC_F32 ? load_one<LC_F32>(p.bias, j) : p.dtype == LC_BF16 ? load_one<LC_BF16>(p.bias, j) : load_one<LC_F16>(p.bias, j);
+    if (p.bias) v += bias_of(p, j);
     return v;
 }
 __device__ __forceinline__ void put(const Product& p, uint64_t at, float v) {
@@ -379,6 +382,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         load_to_lds((piece < TM / 8 ? x0 : w0) + (uint64_t)(from[l] + (at < end ? at : end)), &lds[buffer][piece * PIECE]);
     };
     const uint32_t wm = wave % WM * (TM / WM), wn = TM + wave / WM * (TN / WN);
+    static_assert(TN <= WAVES * 64, "a lane a column");
     u32x4 a[2][NT], b[2][MT];                               // of w and of x
     auto operand_at = [&](uint32_t buffer, uint32_t u, uint32_t row) {      // unit u of this lane's of the 32 rows from `row` on
         return *reinterpret_cast<const u32x4*>(&lds[buffer][c % 8 * PIECE + c / 8 * 128 + row / 64 * 8 * PIECE + row % 64 / 8 * 128 + u * 16]);
@@ -429,6 +433,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         last = buffer;
         buffer = next;
     }
+    const uint32_t own = n0 + threadIdx.x < p.n ? n0 + threadIdx.x : p.n - 1;
+    const float column = p.sw[own], shift = bias_of(p, own);
+    float sx[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) { const uint32_t row = m0 + wm + 32 * i + c; sx[i] = p.sx[row < p.m ? row : p.m - 1]; }
     wait_loads<0>();
     if (rest) {
         __builtin_amdgcn_s_barrier();
@@ -446,21 +455,32 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
             }
         }
     }
+    // Scales of w's rows and the bias by way of LDS (303 rows by 28891x40 23 us for 40 with loads beside the stores), in an array that there is: a second one has the
+    // compiler wait for all loads in every tile (330 us for 113).
+    float* columns = reinterpret_cast<float*>(&lds[0][0]);
+    __syncthreads();
+    if (threadIdx.x < TN) { columns[threadIdx.x] = column; columns[TN + threadIdx.x] = shift; }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const uint32_t row = m0 + wm + 32 * i + c;
         if (row >= p.m) continue;
-        const float sx = p.sx[row];
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const uint32_t col = n0 + wn - TM + 32 * j + 8 * g + 4 * h;
+                const uint32_t at = wn - TM + 32 * j + 8 * g + 4 * h, col = n0 + at;
                 if (col >= p.n) continue;
                 const uint32_t valid = p.n - col < 4 ? p.n - col : 4;
+                const f32x4 sw = *reinterpret_cast<const f32x4*>(columns + at);
                 f32x4 v;
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) v[e] = e < valid ? result_of(p, acc[i][j][4 * g + e], sx, p.sw[col + e], col + e) : 0.0f;
+                for (uint32_t e = 0; e < 4; ++e) v[e] = (float)acc[i][j][4 * g + e] * sx[i] * sw[e];
+                if (p.bias) {
+                    const f32x4 more = *reinterpret_cast<const f32x4*>(columns + TN + at);
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e) v[e] += more[e];
+                }
                 put_four(p, row * p.ldy + col, v, valid);
             }
     }
