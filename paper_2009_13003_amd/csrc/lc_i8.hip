@@ -1,6 +1,7 @@
 // Matrices in 8 bits with a scale a row: quantising, reading back, and the products of two of them (include/lc_serve.h).
 #include "lc_serve.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lc {
@@ -529,17 +530,22 @@ void tiles(const Product& p, hipStream_t s) {
 }
 void multiply_piece(const Product& p, bool few, hipStream_t s) {
     if (p.m <= 16 || few) { k_i8_rows<1, 8><<<dim3((p.n + 15) / 16, (p.m + 15) / 16), 512, 0, s>>>(p); return; }
-    // Two tiles of rows for as many of w's rows as leave 64 x 64 tiles half of the chip (24 rows by 4096x4096 7.7 us for 9.6; 48 by 11008x4096 34 for 11.1).
-    if (p.m <= 32 && p.n <= 8192) { k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p); return; }
-    // The tiles that take the least time, by how many of them the chip has at once and what such a round takes at a width of 4096, in us:
-    // 64 x 64 up to 256 of them 10, 512 18; 128 x 64 256 18, 512 29; 128 x 128 256 28; 128 x 256 256 49.  (1000 rows by 4096: 28.6 with 128 x 128, 32 with 64 x 64, 41 with
-    // 128 x 256; 2048 rows: 57, 64, 50; 256 rows: 22.6, 11.3, 37.)
-    auto rounds = [&](uint64_t tm, uint64_t tn, uint64_t chip) { return (((p.m + tm - 1) / tm) * ((p.n + tn - 1) / tn) + chip - 1) / chip; };
-    const uint64_t a = rounds(64, 64, 256) == 1 ? 10 : 18 * rounds(64, 64, 512), b = rounds(128, 64, 256) == 1 ? 18 : 29 * rounds(128, 64, 512);
-    const uint64_t c = 28 * rounds(128, 128, 256), d = 49 * rounds(128, 256, 256), least = a < b ? a : b, most = c < d ? c : d;
-    if (most <= least) { if (d <= c) tiles<128, 256, 3>(p, s); else tiles<128, 128, 4>(p, s); }
-    else if (b <= a) tiles<128, 64, 3>(p, s);
-    else tiles<64, 64, 4>(p, s);
+    // What takes the least time, by how many workgroups the chip has at once and what such a round takes: some time for its start and its results, and some for 4096 of the width, in
+    // tenths of a us as measured (2048 rows by 4096, with the launch's 2.3 us, at widths of 64 / 1024 / 4096: 64 x 64 14.3 / 23.5 / 58, 128 x 64 13.4 / 20.4 / 49, 128 x 128 15.5 / 22.2 / 47,
+    // 128 x 256 13.6 / 19.7 / 39; 256 rows 3.9 / 5.3 / 9.9, 4.9 / 6.7 / 13.2, 6.9 / 9.2 / 17.2, 10.4 / 14 / 26.9; 24 rows by 4096x4096 with
+    // two tiles of rows 7.4, by 8192x4096 13 and 64 x 64 9.8; widths above 4096 are more than one step of those, 100 rows by 797x9538 22.5 and 64 x 64 16.5).
+    auto takes = [&](uint64_t tm, uint64_t tn, uint64_t chip, uint64_t start, uint64_t width) {
+        return (((p.m + tm - 1) / tm) * ((p.n + tn - 1) / tn) + chip - 1) / chip * (start * 4096 + width * p.k16);
+    };
+    const bool a_few = (uint64_t)((p.m + 63) / 64) * ((p.n + 63) / 64) <= 256, b_few = (uint64_t)((p.m + 127) / 128) * ((p.n + 63) / 64) <= 256;
+    const uint64_t rows = p.k16 <= 4096 ? takes(32, 16, 256, 15, 39) : ~0ull, a = a_few ? takes(64, 64, 256, 15, 60) : takes(64, 64, 512, 29, 113),
+                   b = b_few ? takes(128, 64, 256, 30, 106) : takes(128, 64, 512, 46, 190), c = takes(128, 128, 256, 53, 174), d = takes(128, 256, 256, 110, 260);
+    const uint64_t least = std::min({rows, a, b, c, d});
+    if (d == least) tiles<128, 256, 3>(p, s);
+    else if (c == least) tiles<128, 128, 4>(p, s);
+    else if (b == least) tiles<128, 64, 3>(p, s);
+    else if (a == least) tiles<64, 64, 4>(p, s);
+    else k_i8_rows<2, 8><<<dim3((p.n + 15) / 16, (p.m + 31) / 32), 512, 0, s>>>(p);
 }
 // By pieces of w's rows of which each makes a launch of fewer than 2^32 threads.
 void multiply(const Product& p, hipStream_t s) {
