@@ -38,6 +38,39 @@ __device__ __forceinline__ u32x2 codes_of(const float x[8], float inv) {
     return q;
 }
 
+// Eights of a row's elements from `first` on, `step` apart, zeros behind its end at k: all whole ones are under way before the first is looked at (in a branch each, every one would be
+// waited for), the one that the row ends in by itself.
+template <int T, int R>
+__device__ __forceinline__ void load_eights(const void* x, uint64_t row, uint32_t first, uint32_t step, uint32_t k, float v[R][8]) {
+    const uint32_t whole = k & ~7u;
+    f32x4 raw[R][T == LC_F32 ? 2 : 1];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < (T == LC_F32 ? 2 : 1); ++i) raw[r][i] = f32x4{0, 0, 0, 0};
+    if (whole)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint64_t at = row + (first + r * step < whole ? first + r * step : 0);
+            if (T == LC_F32) {
+                raw[r][0] = load_once<f32x4>(static_cast<const float*>(x) + at);
+                raw[r][T == LC_F32 ? 1 : 0] = load_once<f32x4>(static_cast<const float*>(x) + at + 4);
+            } else raw[r][0] = load_once<f32x4>(static_cast<const uint16_t*>(x) + at);
+        }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t at = first + r * step;
+        const bool in = at < whole;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t u = bits_of(raw[r][0][e / 2 % 4]);
+            const float f = T == LC_F32 ? raw[r][T == LC_F32 ? e / 4 : 0][e % 4] : T == LC_BF16 ? float_of(e % 2 ? u & 0xffff0000u : u << 16) : of_f16(e % 2 ? u >> 16 : u & 0xffffu);
+            v[r][e] = in ? f : 0.0f;
+        }
+        if (!in && at < k) load_eight<T>(x, row + at, (int)(k - at), v[r]);
+    }
+}
+
 // A row to a workgroup, or of short rows to a wavefront: 8 elements a lane at a time, kept in registers between the search for the largest and the rounding
 // (rows too long for that are read again).  s = max |w| / 127, q = rint(w (1 / s)).  Bound by memory: 2048 rows of 11008 in bf16 17.6 us, 3.8 TB/s of what is read and
 // written, at a copy's rate 13; vector instructions fill half of its cycles.
@@ -50,8 +83,7 @@ __global__ __launch_bounds__(256) void k_i8_quantize(const void* w, uint64_t ldw
     float v[R][8];
     uint32_t most = 0;
     auto load = [&](uint32_t at, float x[8]) { load_eight<T>(w, row * ldw + at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, x); };
-#pragma unroll
-    for (int r = 0; r < R; ++r) load((r * LANES + lane) * 8, v[r]);
+    load_eights<T, R>(w, row * ldw, lane * 8, LANES * 8, k, v);
 #pragma unroll
     for (int r = 0; r < R; ++r) most = largest_of(v[r], most);
     for (uint32_t at = (R * LANES + lane) * 8; at < k; at += LANES * 8) {
@@ -189,8 +221,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_i8_rows(Product p) {
 // One row of x as it comes: every workgroup works out its codes for itself, into LDS, while its first loads of w are under way.  By 11008x4096 10 us (in two launches 12.4), by
 // 4096x4096 5.5; at the rate of a bare read w takes 6.4 and 2.4, a launch 2.3.  (Sixteen wavefronts for widths above 4096: no faster.)
 constexpr uint32_t kFused = 32768;                          // codes of x at most
-template <int T>
-__global__ __launch_bounds__(512, 6) void k_i8_one_row(Product p, const void* x, uint32_t k) {
+template <int T, int R>
+__global__ __launch_bounds__(512, R == 1 ? 6 : 4) void k_i8_one_row(Product p, const void* x, uint32_t k) {
     constexpr uint32_t WAVES = 8, S = 4;
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];      // of x
     __shared__ uint32_t tops[WAVES];
@@ -209,11 +241,15 @@ __global__ __launch_bounds__(512, 6) void k_i8_one_row(Product p, const void* x,
             }
     };
     load(wave * 128);
-    float v[8] = {};                                        // (kept where a lane has no more)
+    float v[R][8];
     uint32_t most = 0;
-    for (uint32_t at = threadIdx.x * 8; at < k; at += WAVES * 512) {
-        load_eight<T>(x, at, (int)(k - at < 8 ? k - at : 8), v);
-        most = largest_of(v, most);
+    load_eights<T, R>(x, 0, threadIdx.x * 8, WAVES * 512, k, v);
+#pragma unroll
+    for (int r = 0; r < R; ++r) most = largest_of(v[r], most);
+    for (uint32_t at = (R * WAVES * 64 + threadIdx.x) * 8; at < k; at += WAVES * 512) {
+        float more[8];
+        load_eight<T>(x, at, (int)(k - at < 8 ? k - at : 8), more);
+        most = largest_of(more, most);
     }
     most = largest_of_wave(most);
     if (lane == 0) tops[wave] = most;
@@ -222,9 +258,15 @@ __global__ __launch_bounds__(512, 6) void k_i8_one_row(Product p, const void* x,
     for (uint32_t i = 0; i < WAVES; ++i) most = tops[i] > most ? tops[i] : most;
     float inv;
     const float sx = scale_of(most, inv);
-    for (uint32_t at = threadIdx.x * 8; at < p.k16; at += WAVES * 512) {
-        if (k > WAVES * 512) load_eight<T>(x, at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, v);
-        *reinterpret_cast<u32x2*>(codes + at) = codes_of(v, inv);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t at = (r * WAVES * 64 + threadIdx.x) * 8;
+        if (at < p.k16) *reinterpret_cast<u32x2*>(codes + at) = codes_of(v[r], inv);
+    }
+    for (uint32_t at = (R * WAVES * 64 + threadIdx.x) * 8; at < p.k16; at += WAVES * 512) {
+        float more[8];
+        load_eight<T>(x, at, at < k ? (int)(k - at < 8 ? k - at : 8) : 0, more);
+        *reinterpret_cast<u32x2*>(codes + at) = codes_of(more, inv);
     }
     __syncthreads();
     i32x4 acc = {0, 0, 0, 0};                               // (of sixteen rows of x that are all this one)
@@ -564,6 +606,12 @@ void multiply(const Product& p, hipStream_t s) {
 }
 
 template <int T>
+void one_row(const Product& p, const void* x, uint32_t k, hipStream_t s) {
+    const uint32_t blocks = (p.n + 15) / 16;
+    if (k <= 4096) k_i8_one_row<T, 1><<<blocks, 512, p.k16, s>>>(p, x, k);
+    else k_i8_one_row<T, 3><<<blocks, 512, p.k16, s>>>(p, x, k);
+}
+template <int T>
 void short_rows(const Product& p, const void* x, uint64_t ldx, uint32_t k, hipStream_t s) {
     const uint32_t blocks = (p.n + 15) / 16, lds = p.m * (p.k16 + 16);
     const FastDiv by_row(p.k16 / 8);
@@ -630,11 +678,10 @@ int lc_i8_linear(const void* x, uint64_t ldx, uint64_t m, const lc_i8* w8, const
     const uint64_t row = (w8->k + 15) / 16 * 16;
     if (w8->k && m == 1 && row <= kFused && w8->n <= (1u << 26)) {
         const Product p = {nullptr, static_cast<const uint8_t*>(w8->codes), nullptr, w8->scales, bias, y, 0, w8->pitch, ldy, (uint32_t)m, (uint32_t)w8->n, (uint32_t)row, dtype};
-        const uint32_t blocks = (p.n + 15) / 16, lds = (uint32_t)row, k = (uint32_t)w8->k;
         hipStream_t s = static_cast<hipStream_t>(stream);
-        if (dtype == LC_F32) k_i8_one_row<LC_F32><<<blocks, 512, lds, s>>>(p, x, k);
-        else if (dtype == LC_BF16) k_i8_one_row<LC_BF16><<<blocks, 512, lds, s>>>(p, x, k);
-        else k_i8_one_row<LC_F16><<<blocks, 512, lds, s>>>(p, x, k);
+        if (dtype == LC_F32) one_row<LC_F32>(p, x, (uint32_t)w8->k, s);
+        else if (dtype == LC_BF16) one_row<LC_BF16>(p, x, (uint32_t)w8->k, s);
+        else one_row<LC_F16>(p, x, (uint32_t)w8->k, s);
         return launched();
     }
     if (w8->k && m > 1 && m <= 16 && m * row <= kShort && w8->n <= (1u << 26)) {

@@ -10,7 +10,7 @@ from .test_kernel_resources import ROCM, registers_of
 LIMITS = {"11k_kv_promptILi%dELi%dELi%dELi%dELi2E" % (t, bits, dim, waves): (256, 0) for t in (1, 2) for bits in (8, 4) for dim in (32, 64, 96, 128) for waves in (4, 8)}
 LIMITS.update({"10k_i8_tilesILi128ELi256E": (512, 0), "10k_i8_tilesILi128ELi128E": (512, 0), "10k_i8_tilesILi128ELi64E": (256, 0), "10k_i8_tilesILi64ELi64E": (256, 0),
                "9k_i8_rowsILi1E": (64, 0), "9k_i8_rowsILi2E": (72, 0)})
-LIMITS.update({"12k_i8_one_rowILi%dE" % t: (84, 0) for t in range(3)})
+LIMITS.update({"12k_i8_one_rowILi%dELi%dE" % (t, r): (84 if r == 1 else 128, 0) for t in range(3) for r in (1, 3)})
 LIMITS.update({"15k_i8_short_rowsILi%dELi%dE" % (t, r): (84, 0) for t in range(3) for r in (1, 2)})
 
 
