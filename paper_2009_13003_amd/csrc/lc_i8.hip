@@ -72,8 +72,8 @@ __device__ __forceinline__ void load_eights(const void* x, uint64_t row, uint32_
 }
 
 // A row to a workgroup, or of short rows to a wavefront: 8 elements a lane at a time, kept in registers between the search for the largest and the rounding
-// (rows too long for that are read again).  s = max |w| / 127, q = rint(w (1 / s)).  Bound by memory: 2048 rows of 11008 in bf16 17.6 us, 3.8 TB/s of what is read and
-// written, at a copy's rate 13; vector instructions fill half of its cycles.
+// (rows too long for that are read again).  s = max |w| / 127, q = rint(w (1 / s)).  Bound by memory: 2048 rows of 11008 in bf16 12.5 us, 5.4 TB/s of what is read and
+// written, a copy's rate.
 template <int T, int WAVES, int R>
 __global__ __launch_bounds__(256) void k_i8_quantize(const void* w, uint64_t ldw, uint8_t* codes, uint64_t pitch, float* scales, uint32_t rows, uint32_t k) {
     __shared__ uint32_t tops[4];
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_i8_rows(Product p) {
 }
 
 // One row of x as it comes: every workgroup works out its codes for itself, into LDS, while its first loads of w are under way.  By 11008x4096 10 us (in two launches 12.4), by
-// 4096x4096 5.5; at the rate of a bare read w takes 6.4 and 2.4, a launch 2.3.  (Sixteen wavefronts for widths above 4096: no faster.)
+// 4096x4096 5.5, by 4096x11008 with three eights a lane 12.6 (read one after the other 14.4); at the rate of a bare read w takes 6.4 and 2.4, a launch 2.3.  (Sixteen wavefronts for widths above 4096: no faster.)
 constexpr uint32_t kFused = 32768;                          // codes of x at most
 template <int T, int R>
 __global__ __launch_bounds__(512, R == 1 ? 6 : 4) void k_i8_one_row(Product p, const void* x, uint32_t k) {
@@ -397,8 +397,8 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 // its 256 bytes.  Operands are read a step of 32 bytes ahead of their products.  The workgroup meets once a tile, ahead of its last step, whose operands have been read by
 // then: behind the meeting the tile's place is filled again.
 // Rows of the matrix instruction's result are rows of w, so a lane has four results of a row of y that follow each other.
-// 2048 rows by 4096x11008: 97 to 101 us, 1.83 to 1.9 PFLOP/s, the matrix unit 54% of its cycles.  Copies of the kernel without loads and reads take 71 us, with reads alone 80, with loads
-// alone 106 when the kernel took 116: it is the way of 48 KB a tile into LDS that products wait for, at a clock that goes down as they do not (1.7 GHz then).
+// 2048 rows by 4096x11008: 86 us, 2.15 PFLOP/s, the matrix unit 66% of its cycles.  Copies of the kernel without loads and reads take 71 us, with reads alone 80, with loads
+// alone 106 when the kernel, with 20 us of waits behind its loop, took 116: it is the way of 48 KB a tile into LDS that products wait for, at a clock that goes down as they do not (1.7 GHz then).
 template <int TM, int TN, int WM, int WN, int BUFFERS>
 __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
     constexpr int WAVES = WM * WN, MT = TM / WM / 32, NT = TN / WN / 32, PIECE = 1024 + 16, BYTES = (TM + TN) / 8 * PIECE, LOADS = (TM + TN) / 8 / WAVES;
