@@ -337,8 +337,11 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     };
     int unit = -1000;                                       // 16-bit types: what this wavefront's sums are counted in; and for the one that sees to scales the tiles so far
     int unit_next = -1000;
-    auto put_scales = [&](uint32_t buffer) LC_INLINE {
+    const int32_t place_last = place_of(row_last);          // the last place that any row here sees
+    auto put_scales = [&](int32_t tile, uint32_t buffer) LC_INLINE {
         if (wave == kScaler) {
+            // What no row here sees, behind that place or in a page that is not there, may have any scale, which must not set what products are counted in.
+            if (PHALF && (tile * kTile + (int32_t)lane > place_last || (snot[tile % 4] >> lane / 8 & 1))) value_scale = 0;
             // A value that is not finite makes all of a result NaN: as well a key that is not does, and products with the values are left without it.
             const uint32_t size = bits_of(value_scale) & 0x7fffffffu;
             const bool finite = size < 0x7f800000u;
@@ -535,7 +538,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         place_eights(tile0, 24);
         __syncthreads();
         ask(tile0);
-        put_scales(0);
+        put_scales(tile0, 0);
         put_all(0);
         ask(tile0 + 1);
     }
@@ -544,14 +547,14 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     for (; tile < wave_tiles; ++tile, buffer ^= 1) {
         __syncthreads();
         look(tile + 3, 8);
-        put_scales(buffer ^ 1);
+        put_scales(tile + 1, buffer ^ 1);
         use(tile, buffer);
         place_eights(tile + 3, 8);
     }
     for (; tile < tile1; ++tile, buffer ^= 1) {             // (what only other wavefronts' rows see; they meet as often in this loop as in the one above)
         __syncthreads();
         look(tile + 3, 8);
-        put_scales(buffer ^ 1);
+        put_scales(tile + 1, buffer ^ 1);
         put_all(buffer ^ 1);
         ask(tile + 2);
         place_eights(tile + 3, 8);
