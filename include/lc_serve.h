@@ -157,8 +157,10 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
  *           belong to no sequence are left as they were.
  *   table, lens, scale: as above; the newest cached tokens of a sequence are the new ones, and each sees what is cached up to itself.  A new token
  *           that would lie before the first cached one gets zeros.
- * Roundings: probabilities times the values' scales are rounded once, in bf16 and fp16 to 11 bits (or to 2^-35 of the largest scale times probability so far, if that is
- * more), in fp32 to 24.  Sums, maxima and scores are held in 32 bits, with the ranges of lc_kv_attend.
+ * Keys and values that a token does not see do not matter, whatever they hold (in bf16 and fp16 as long as no scale of a later token's value, among the 64 that begin at a multiple of 64, is
+ * above 2^90 times the largest that it sees).
+ * Roundings: probabilities times the values' scales are rounded once, in bf16 and fp16 to 11 bits, or to 2^-35 of the largest scale that the token sees times its largest probability, if that is
+ * more; in fp32 to 24.  Sums, maxima and scores are held in 32 bits, with the ranges of lc_kv_attend.
  */
 size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim);
 int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,

@@ -22,6 +22,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // join 11; 25 blocks of rows a head of which a third are partly filled, and codes converted for 128 rows at most.  fp32, three parts each: 2 of 333 of 1500 tokens 23 and 9 us.
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kLowest = 90;                                // 16-bit types: how far below its largest score, in powers of two, a row measures at most (2^30 of them have a sum)
 constexpr uint32_t kMostParts = 32, kLeastTiles = 4;       // of a sequence's tokens, and tiles that a part has at least
 
 struct Prompt {
@@ -469,6 +470,22 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         // What probabilities are measured from moves only when one would pass 2^kFar, what sums are counted in when a larger scale comes, so sums are seldom rescaled.
         if (__any(most > Kind<T>::kFar || top == -__builtin_inff()) || unit_now != unit) {
             most = fmaxf(fmaxf(most, other_half(most)) + from, top);
+            // Products are counted in a unit for all rows, by the largest scale that any of them sees.  A row that does not see it, because its token is later, measures its probabilities from
+            // as much lower: its products do not pass 2^11 so, and keep their bits.  (This is the last tile that such a row sees anything of.)
+            if (PHALF && tb + kTile - 1 > wave_first && unit_now != unit) {
+                float large = 0;
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 vs = *reinterpret_cast<const f32x4*>(&svs[buffer][32 * s + 8 * g + 4 * h]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) large = fmaxf(large, score[s][4 * g + r] == -__builtin_inff() ? 0.0f : fabsf(vs[r]));
+                    }
+                large = fmaxf(large, other_half(large));
+                const int own_unit = (int)(bits_of(large) >> 23) - 127 - 10, below = -(own_unit > unit - unit_now ? own_unit : unit - unit_now);
+                most -= large > 0.0f ? (float)(below < kLowest ? below : kLowest) : 0.0f;
+            }
             const float then = most == -__builtin_inff() ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - then);
             sum *= shrink;
             const float by = PHALF ? ldexpf(shrink, unit - unit_now) : shrink;
@@ -560,13 +577,20 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
         place_eights(tile + 3, 8);
     }
 
-    const float total = sum + other_half(sum);
+    float total = sum + other_half(sum);
     if (!has_row) return;
     const uint64_t at = (uint64_t)(own.first + qi), hd = head * a.group + qg;
     float whole = own.parts > 1 || total == 0.0f ? 1.0f : 1.0f / total;
     whole *= unit_of(BITS);
     if (PHALF) whole = total == 0.0f ? 0.0f : ldexpf(whole, unit);
     if (own.parts > 1) {
+        // (A sum of probabilities measured from far below the largest is brought near 1, so that products with large values fit.)
+        if (PHALF && total > 0x1p40f) {
+            const int e = (int)(bits_of(total) >> 23) - 127;
+            top += (float)e;
+            total = ldexpf(total, -e);
+            whole = ldexpf(whole, -e);
+        }
         const uint64_t place_at = ((uint64_t)own.place * a.c.heads + head) * kRows + 32 * wave + c;
         if (h == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * place_at) = f32x2{top, total};
         if (total == 0.0f) return;

@@ -66,3 +66,43 @@ def test_pages_that_are_not_there(lc, new, lens, page, bits, dtype):
     unseen[0] = True
     table[0, 0], table[-1, -(-lens[-1] // page) - 1] = cache.pages, 2 ** 31 - 1
     same_whatever_is_not_seen(lc, cache, unseen, queries(sum(new), 4, 64, dtype), starts_of(new), table, lens)
+
+
+def later_ones_larger(lc, seed, n, kv, dim, bits, page, power):
+    """A cache of one sequence of n tokens, of which number t has values of a size of 2^power[t]."""
+    cache, table = filled(lc, seed, [n], kv, dim, bits, page)
+    g = torch.Generator(DEV).manual_seed(seed)
+    k, v = (torch.randn(n, kv, dim, device=DEV, generator=g) for _ in range(2))
+    slots = torch.tensor([int(table[0, t // page]) * page + t % page for t in range(n)], device=DEV)
+    lc.lc_kv_write(cache, k, v * torch.exp2(torch.as_tensor(power, dtype=torch.float32, device=DEV))[:, None, None], slots)
+    return cache, table
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("power", [24, 40, 80])
+@pytest.mark.parametrize("new,n,heads,kv,first", [(300, 300, 1, 1, 200), (300, 300, 2, 2, 128), (64, 64, 1, 1, 20), (40, 2000, 2, 1, 1985), (600, 1000, 8, 2, 770)])
+def test_later_blocks_of_rows(lc, new, n, heads, kv, first, power, dtype):
+    """Tokens from `first` on have values 2^power times as large.  Those before are within the room that what they see gives them."""
+    cache, table = later_ones_larger(lc, 40 + new, n, kv, 64, 8, 16, [power * (t >= first) for t in range(n)])
+    q = queries(new, heads, 64, dtype)
+    got = lc.lc_kv_attend_prompt(cache, q, ints([0, new]), table, ints([n]))
+    few = first - (n - new)
+    want, room = want_of(lc, cache, q[:few], [0, few], table, [first])
+    # (a score measured from up to 2^7 away is rounded to 2^-18 at most, in the products and in their sum: 2^-17 ln 2 of the result's products, whose own
+    # rounding to 2^-11 is in the room; fp32 does not measure so)
+    check(got[:few], want, room * (1 if dtype == torch.float32 else 1 + 2.0 ** -6))
+    if dtype != torch.float16:
+        check(got[few:], *(t[few:] for t in want_of(lc, cache, q, [0, new], table, [n])))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,cached", [(64, 64), (90, 90), (70, 1000)])
+def test_every_token_larger_than_the_one_before(lc, n, cached, dtype):
+    """Values that double from token to token over the new ones: each one's room is that of what it sees."""
+    base = cached - n
+    cache, table = later_ones_larger(lc, 50 + n, cached, 1, 64, 8, 16, [max(0, t - base) - 40 for t in range(cached)])
+    q = queries(n, 2, 64, dtype)
+    got = lc.lc_kv_attend_prompt(cache, q, ints([0, n]), table, ints([cached]))
+    for i in list(range(0, n, 5)) + [n - 1]:
+        want, room = want_of(lc, cache, q[i:i + 1], [0, 1], table, [base + i + 1])
+        check(got[i:i + 1], want, room * (1 if dtype == torch.float32 else 1 + 2.0 ** -6))
