@@ -37,6 +37,7 @@ struct Prompt {
     float* part;                // [place of a part][row][dim]
     float scale;                // times log2(e)
     uint32_t tokens, batch, heads, group;
+    uint32_t first_unit;        // of this launch
     uint32_t most_parts, share; // parts of a sequence at most; workgroups that are on the chip at once, for one head
     int32_t pages;
     FastDiv by_group;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
     __shared__ int sunit[2];                                // 16-bit types: probabilities times scales are counted in 2^sunit
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane % 32, h = lane / 32;
     const uint32_t head = blockIdx.x % a.c.heads;
-    const Own own = own_of<false>(a, blockIdx.x / a.c.heads, lane, kRows);
+    const Own own = own_of<false>(a, a.first_unit + blockIdx.x / a.c.heads, lane, kRows);
     if (own.count == 0) return;
     const uint32_t b = own.b;
     const int32_t room = (int32_t)(a.table_pages << a.c.page_shift);
@@ -688,11 +689,17 @@ uint64_t places_of(const Deal& d, uint32_t kv_heads) { return d.most_parts == 1 
 template <int T, int BITS, int D>
 void prompt_of(const Prompt& a, const Deal& d, hipStream_t s) {
     constexpr int PERSIMD = T == LC_F32 || D > 128 ? 1 : 2;
-    const uint32_t units = (d.blocks + (a.most_parts > 1 ? d.share : 0)) * a.c.heads;
     if (a.deal) k_kv_prompt_deal<<<1, 1024, 0, s>>>(a, 32 * (PERSIMD == 2 ? d.waves : 4));
-    if constexpr (PERSIMD == 2)
-        if (d.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<units, 512, 0, s>>>(a); return; }
-    k_kv_prompt<T, BITS, D, 4, PERSIMD><<<units, 256, 0, s>>>(a);
+    // (by launches of fewer than 2^32 threads)
+    const uint32_t units = d.blocks + (a.most_parts > 1 ? d.share : 0), step = (1u << 31) / 512 / a.c.heads;
+    Prompt p = a;
+    for (uint32_t u = 0; u < units; u += step) {
+        const uint32_t grid = (units - u < step ? units - u : step) * a.c.heads;
+        p.first_unit = u;
+        if constexpr (PERSIMD == 2)
+            if (d.waves == 8) { k_kv_prompt<T, BITS, D, 8, 2><<<grid, 512, 0, s>>>(p); continue; }
+        k_kv_prompt<T, BITS, D, 4, PERSIMD><<<grid, 256, 0, s>>>(p);
+    }
 }
 template <int T, int BITS>
 void prompt(const Prompt& a, const Deal& d, hipStream_t s) {
