@@ -161,8 +161,11 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
  * above 2^90 times the largest that it sees).
  * Roundings: probabilities times the values' scales are rounded once, in bf16 and fp16 to 11 bits, or to 2^-35 of the largest scale that the token sees times its largest probability, if that is
  * more; in fp32 to 24.  Sums, maxima and scores are held in 32 bits, with the ranges of lc_kv_attend.
+ * ws: scratch, 256-byte aligned, lc_kv_prompt_workspace_bytes of these very sizes: fewer tokens may need more (rows enough to fill the chip are not split).  An area for calls of
+ * several sizes has lc_kv_prompt_workspace_most, which is enough for every call of up to that many tokens and sequences.
  */
 size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim);
+size_t lc_kv_prompt_workspace_most(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim);
 int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,
                         const int32_t* table, uint64_t ld_table, uint64_t table_pages, const int32_t* lens, float scale, void* out, uint64_t ld_out, int dtype,
                         void* ws, size_t ws_bytes, void* stream);

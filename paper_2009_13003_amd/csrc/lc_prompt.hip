@@ -672,19 +672,25 @@ __global__ __launch_bounds__(256) void k_kv_prompt_join(Prompt a, uint32_t rows)
 // a SIMD have the registers and rows are many; sequences of few rows leave much of 256 unused (9 of 57 to 517 tokens 155 for 141).  Splitting is left out where rows fill the
 // chip: once if all is one sequence, else four times.
 struct Deal { uint32_t waves, blocks, share, most_parts; };
+uint32_t share_of(uint64_t chip, uint32_t kv_heads) { return (uint32_t)(chip > kv_heads ? chip / kv_heads : 1); }
 Deal deal_of(uint64_t tokens, uint64_t batch, uint32_t group, uint32_t kv_heads, bool two) {
     const uint64_t sequences = tokens < batch ? tokens : batch;      // those with new tokens
     Deal d;
     d.waves = two && tokens * group / 256 * kv_heads >= 64 && tokens * group >= 1024 * sequences ? 8 : 4;
     const uint64_t rows = 32 * d.waves, chip = two && d.waves == 4 ? 512 : 256;      // workgroups that are on the chip at once
     d.blocks = (uint32_t)((tokens * group + rows - 1) / rows + sequences);
-    d.share = (uint32_t)(chip > kv_heads ? chip / kv_heads : 1);
+    d.share = share_of(chip, kv_heads);
     d.most_parts = tokens * group / rows * kv_heads >= chip * (batch == 1 ? 1 : 4) ? 1 : kMostParts;
     return d;
 }
 bool two_fit(int dtype, uint32_t dim) { return dtype != LC_F32 && dim <= 128; }        // two wavefronts a SIMD have the registers
 uint64_t deal_bytes(uint64_t batch) { return batch > 64 ? ((3 * (batch + 1) + 1) * 4 + 255) / 256 * 256 : 0; }
 uint64_t places_of(const Deal& d, uint32_t kv_heads) { return d.most_parts == 1 ? 0 : 2ull * d.share * kv_heads; }
+uint64_t rows_bytes(uint64_t rows, int dim) { return (rows * 8 + 255) / 256 * 256 + rows * dim * 4; }      // of parts: a maximum and a sum, and dim elements
+bool bad_sizes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim) {
+    return tokens > (1ull << 24) || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 || dim > 256 ||
+           dim % 32 || tokens * heads > (1ull << 30);
+}
 
 template <int T, int BITS, int D>
 void prompt_of(const Prompt& a, const Deal& d, hipStream_t s) {
@@ -728,8 +734,7 @@ using namespace lc::serve;
 extern "C" {
 
 size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim) {
-    if (tokens > (1ull << 24) || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads || heads % kv_heads || heads > 4096 || dim < 32 || dim > 256 ||
-        dim % 32 || tokens * heads > (1ull << 30)) return 0;
+    if (bad_sizes(tokens, batch, heads, kv_heads, dim)) return 0;
     if (tokens == 0 || batch == 0) return 256;
     uint64_t most = 0;                                      // (of both ways there are, whatever the type)
     for (int two = 0; two < 2; ++two) {
@@ -737,7 +742,20 @@ size_t lc_kv_prompt_workspace_bytes(uint64_t tokens, uint64_t batch, int heads, 
         const uint64_t rows = places_of(d, (uint32_t)kv_heads) * 32 * d.waves;
         most = rows > most ? rows : most;
     }
-    return (size_t)((most * 8 + 255) / 256 * 256 + most * dim * 4 + 256 + deal_bytes(batch));
+    return (size_t)(rows_bytes(most, dim) + 256 + deal_bytes(batch));
+}
+
+size_t lc_kv_prompt_workspace_most(uint64_t tokens, uint64_t batch, int heads, int kv_heads, int dim) {
+    if (bad_sizes(tokens, batch, heads, kv_heads, dim)) return 0;
+    if (tokens == 0 || batch == 0) return 256;
+    uint64_t most = 0;                                      // (of every way there is to deal rows)
+    for (const uint32_t waves : {4u, 8u})
+        for (const uint64_t chip : {256u, 512u}) {
+            if (waves == 8 && chip > 256) continue;        // (eight are given where one workgroup a compute unit is)
+            const uint64_t rows = places_of({waves, 0, share_of(chip, (uint32_t)kv_heads), kMostParts}, (uint32_t)kv_heads) * 32 * waves;
+            most = rows > most ? rows : most;
+        }
+    return (size_t)(rows_bytes(most, dim) + 256 + deal_bytes(batch));
 }
 
 int lc_kv_attend_prompt(const lc_kv_cache* cache, const void* q, uint64_t ld_q, uint64_t tokens, int heads, const int32_t* starts, uint64_t batch,

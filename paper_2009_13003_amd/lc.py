@@ -135,6 +135,8 @@ _lib.lc_i8_linear.restype = _int
 _lib.lc_i8_linear.argtypes = [_vp, _u64, _u64, _vp, _vp, _vp, _u64, _int, _vp, _sz, _vp]
 _lib.lc_kv_prompt_workspace_bytes.restype = _sz
 _lib.lc_kv_prompt_workspace_bytes.argtypes = [_u64, _u64, _int, _int, _int]
+_lib.lc_kv_prompt_workspace_most.restype = _sz
+_lib.lc_kv_prompt_workspace_most.argtypes = [_u64, _u64, _int, _int, _int]
 _lib.lc_kv_attend_prompt.restype = _int
 _lib.lc_kv_attend_prompt.argtypes = [_vp, _vp, _u64, _u64, _int, _vp, _u64, _vp, _u64, _u64, _vp, ctypes.c_float, _vp, _u64, _int, _vp, _sz, _vp]
 _lib.lc_kv_extend.restype = _int
@@ -891,9 +893,14 @@ def lc_kv_prompt_workspace_bytes(tokens, batch, heads, kv_heads, dim):
     return int(_lib.lc_kv_prompt_workspace_bytes(tokens, batch, heads, kv_heads, dim))
 
 
+def lc_kv_prompt_workspace_most(tokens, batch, heads, kv_heads, dim):
+    return int(_lib.lc_kv_prompt_workspace_most(tokens, batch, heads, kv_heads, dim))
+
+
 def new_prompt_workspace(cache, tokens, batch, heads, stream=None):
-    """Scratch for lc_kv_attend_prompt with these sizes, to be used on `stream` (None: the current one); calls that may run at the same time need one each."""
-    make = lambda: (torch.empty(lc_kv_prompt_workspace_bytes(tokens, batch, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device),)
+    """Scratch for lc_kv_attend_prompt of up to `tokens` new tokens of up to `batch` sequences, to be used on `stream` (None: the current one); calls that may run at the
+    same time need one each."""
+    make = lambda: (torch.empty(lc_kv_prompt_workspace_most(tokens, batch, heads, cache.heads, cache.dim), dtype=torch.uint8, device=cache.k.device),)
     return (make() if stream is None else _made_on(stream, make))[0]
 
 
@@ -927,7 +934,8 @@ def lc_kv_attend_prompt(cache, q, starts, table, lens, scale=None, out=None, ws=
         assert out.dtype == q.dtype and out.shape == q.shape
         ldo = _tokens_of(out)
     if ws is None:
-        ws = new_prompt_workspace(cache, tokens, batch, heads, stream)
+        make = lambda: (torch.empty(lc_kv_prompt_workspace_bytes(tokens, batch, heads, cache.heads, dim), dtype=torch.uint8, device=q.device),)
+        ws, = make() if stream is None else _made_on(stream, make)
     assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
     st = _lib.lc_kv_attend_prompt(cache._p, q.data_ptr(), ldq, tokens, heads, starts.data_ptr(), batch, table.data_ptr(),
                                   table.stride(0) if batch > 1 else table.shape[1], table.shape[1], lens.data_ptr(), dim ** -0.5 if scale is None else scale,
