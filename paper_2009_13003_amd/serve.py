@@ -75,14 +75,21 @@ class Decoder:
     def times(self, x, name):
         return lc.lc_w4_matmul(x, self.w[name]) if self.weights == 4 else lc.lc_i8_linear(x, self.w[name])
 
-    def room_for(self, add):
-        """Counts add[b] more tokens of each sequence, if there is room for them."""
+    def lacking(self, add):
+        """What has no room for add[b] more tokens of each sequence, or None."""
         count = [c + n for c, n in zip(self.count, add)]
         if max(count) > self.shape.context:
-            raise ValueError("more tokens than the model's context")
+            return "the model's context"
         if self.pages is not None and sum(-(-c // self.page_tokens) for c in count) > self.total:
-            raise ValueError("more tokens than the shared pages hold")
-        self.count = count
+            return "the shared pages hold"
+        return None
+
+    def room_for(self, add):
+        """Counts add[b] more tokens of each sequence, if there is room for them."""
+        lacking = self.lacking(add)
+        if lacking:
+            raise ValueError("more tokens than " + lacking)
+        self.count = [c + n for c, n in zip(self.count, add)]
 
     def slots(self, at):
         """Where the tokens at positions `at` [batch][n] lie in the cache."""
@@ -187,7 +194,7 @@ def drawn(logits, tokens, sample, temperature, parent=None):
 def write_on(model, prompt, count, drafts=2, guess=seen_before, sample=None, temperature=1.0):
     """The `count` tokens a sequence that model writes behind prompt ([batch][n], or a list of tokens a sequence), each the likeliest, or drawn with the random numbers of
     `sample`; and the number of passes it took.  With drafts, a pass judges the known next token and, below it, a tree: `drafts` of the tokens that guess(b, tokens of
-    sequence b) lists to follow, and one below each, as long as the model's context has room for the tree."""
+    sequence b) lists to follow, and one below each, as long as the model's context and the shared pages have room for the tree."""
     if sample is not None and not temperature >= 1e-30:     # (logits divided by less might not be finite)
         raise ValueError("a temperature above zero")
     batch, device = model.batch, model.lens.device
@@ -211,7 +218,7 @@ def write_on(model, prompt, count, drafts=2, guess=seen_before, sample=None, tem
         sees.append((sees[a] if a >= 0 else 0) | 1 << i)
     mask = torch.tensor([sees] * batch, dtype=torch.int64, device=device)
     while any(len(k) < g for k, g in zip(known, goal)):
-        if max(model.count) + len(above) > model.shape.context:              # no room for the tree any more: the known token alone
+        if model.lacking([len(above)] * batch):              # no room for the tree any more: the known token alone
             drafts, above, depth, mask = 0, above[:1], depth[:1], mask[:, :1].contiguous()
         rows = []
         for b, k in enumerate(known):
