@@ -446,6 +446,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_i8_tiles(Product p) {
         for (int l = 0; l < (t == BUFFERS - 1 ? LOADS / 4 : LOADS); ++l) ask(t, l, t);
     wait_loads<(BUFFERS - 2) * LOADS + LOADS / 4>();
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");                          // (the meeting by itself lets the compiler read before it)
 #pragma unroll
     for (int i = 0; i < NT + MT; ++i) read(0, 0, i);
     uint32_t buffer = 0, last = BUFFERS - 1;                // the tile's place, and that of the one before
