@@ -159,7 +159,7 @@ int lc_kv_attend(const lc_kv_cache* cache, const void* q, uint64_t batch, int nq
  *           that would lie before the first cached one gets zeros.
  * Keys and values that a token does not see do not matter, whatever they hold (in bf16 and fp16 as long as no scale of a later token's value, among the 64 that begin at a multiple of 64, is
  * above 2^90 times the largest that it sees).
- * Roundings: probabilities times the values' scales are rounded once, in bf16 and fp16 to 11 bits, or to 2^-35 of the largest scale that the token sees times its largest probability, if that is
+ * Roundings: probabilities times the values' scales are rounded once, in bf16 and fp16 to 11 bits, or to 2^-31 of the largest scale that the token sees times its largest probability, if that is
  * more; in fp32 to 24.  Sums, maxima and scores are held in 32 bits, with the ranges of lc_kv_attend.
  * ws: scratch, 256-byte aligned, lc_kv_prompt_workspace_bytes of these very sizes: fewer tokens may need more (rows enough to fill the chip are not split).  An area for calls of
  * several sizes has lc_kv_prompt_workspace_most, which is enough for every call of up to that many tokens and sequences.

@@ -22,6 +22,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // join 11; 25 blocks of rows a head of which a third are partly filled, and codes converted for 128 rows at most.  fp32, three parts each: 2 of 333 of 1500 tokens 23 and 9 us.
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNear = 64;                                // of the unit that has 2^10 of the largest: while no scale in a tile is below that, rows need not look for their own (100 of 100 tokens 8.7 us, 9.0 if all do)
 constexpr int kLowest = 90;                                // 16-bit types: how far below its largest score, in powers of two, a row measures at most (2^30 of them have a sum)
 constexpr uint32_t kMostParts = 32, kLeastTiles = 4;       // of a sequence's tokens, and tiles that a part has at least
 
@@ -473,7 +474,8 @@ __global__ __launch_bounds__(kWaves * 64, PERSIMD) void k_kv_prompt(Prompt a) {
             most = fmaxf(fmaxf(most, other_half(most)) + from, top);
             // Products are counted in a unit for all rows, by the largest scale that any of them sees.  A row that does not see it, because its token is later, measures its probabilities from
             // as much lower: its products do not pass 2^11 so, and keep their bits.  (This is the last tile that such a row sees anything of.)
-            if (PHALF && tb + kTile - 1 > wave_first && unit_now != unit) {
+            const bool unlike = PHALF && tb + kTile - 1 > wave_first && unit_now != unit;       // (else all rows see all that set the unit)
+            if (unlike && __any(svs[buffer][lane] != 0.0f && fabsf(svs[buffer][lane]) < kNear)) {
                 float large = 0;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
