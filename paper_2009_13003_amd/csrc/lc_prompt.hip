@@ -13,9 +13,9 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 //   O^T += V^T P^T   the same lane's probabilities are its part of the second operand as they stand, with the tokens of each 16 in the order 0-3, 8-11, 4-7, 12-15,
 //                    in which V^T is kept
 // so that the running maximum and the sum are one number a lane.  Codes are whole numbers in 16 bits, exactly; scales of keys multiply the scores, scales of values the
-// probabilities, whose product is rounded: in fp32 to three bf16 parts, else to fp16, measured from a power of two near the largest scale so far, so that products down to
-// 2^-24 of the largest have all of its 11 bits (in bf16 their rounding would be as large as the result's own: errors 1.4 times as large).
-// 2048 of 10000 tokens of 32 / 8 heads of 128 in 8 bits, bf16: 335 us (340 to 350 on some cards), 900 TFLOP/s, where a large library product's rate would give 211.  Per 32 rows by 64
+// probabilities, whose product is rounded: in fp32 to three bf16 parts, else to fp16, measured from a power of two near the largest scale that a row of the workgroup has seen so far, so that products
+// down to 2^-24 of the largest have all of its 11 bits (in bf16 their rounding would be as large as the result's own: errors 1.4 times as large).
+// 2048 of 10000 tokens of 32 / 8 heads of 128 in 8 bits, bf16: 340 us (345 to 355 on some cards), 850 to 885 TFLOP/s, where a large library product's rate would give 211.  Per 32 rows by 64
 // tokens 32 matrix instructions stand beside 280 of the vector unit: 63 for conversions, 32 exponentials, 128 for scores, sums, scales and roundings.  The matrix unit
 // has 44% of the cycles, vector instructions 56%, LDS 46%, and the clock stands at 1.9 GHz: fewer vector instructions (scales in the values, 48 fewer, sums by the
 // matrix unit) and wavefronts that take turns on a SIMD changed nothing or cost 2%.  9 sequences of 57 to 517 new tokens of up to 3001, 32 heads, 4 bits, fp16: 100 us, of which the
